@@ -44,6 +44,11 @@ typedef enum {
 #define SQAP_FP16 0
 #define SQAP_BF16 1
 #define SQAP_I32 2 /* raw int32 accumulators (checking only; SwiGLU not allowed) */
+#define SQAP_FP32 3 /* sqap_mx4_* only */
+
+/* Formats of the microscaled 4-bit operators (sqap_mx4_*). */
+#define SQAP_MX_NVFP4 0 /* blocks of 16 elements, one e4m3 scale each, one fp32 scale for the tensor */
+#define SQAP_MX_MXFP4 1 /* blocks of 32 elements, one power-of-two (e8m0) scale each, no scale of the tensor */
 
 /* Flags of sqap_quantize_act. */
 #define SQAP_Q_ROTATE 1u /* apply the orthonormal Hadamard rotation to each row first (Eq. 6) */
@@ -212,6 +217,62 @@ sqap_status sqap_quantize_linear(const void* x, int M, int64_t ldx, const int32_
 sqap_status sqap_w4a4_linear_static(const uint8_t* q_packed, const float* act_scales, int M, const sqap_weights* w,
                                     const sqap_weights* w_up, void* out, int64_t ldo, int out_dtype, uint32_t flags,
                                     void* stream);
+
+/*
+ * Microscaled 4-bit floating point: the W4A4 linear with floating codes and a scale for each short run of elements of a
+ * row instead of one for the row, which the tensor cores of sm_100 multiply without unpacking. A matrix [rows][K] is
+ *   codes   device [rows][K/2] bytes, element 2j in the low and 2j+1 in the high nibble of byte j of its row;
+ *           e2m1: sign, two exponent bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ *   scales  device, sqap_mx4_scale_bytes(rows, K, format) bytes, one for each block of 16 (NVFP4) or 32 (MXFP4) elements.
+ *           They are stored in tiles of 128 rows x 4 blocks, row tiles outermost: the scale of (row r, block b) is byte
+ *           ((r / 128) * ceil(blocks / 4) + b / 4) * 512 + (r % 32) * 16 + (r % 128) / 32 * 4 + b % 4.
+ *           The bytes behind the last block of a row must be zero; those behind the last row are never used.
+ *           NVFP4: e4m3 numbers, >= 0. MXFP4: the byte b stands for 2^(b - 127); 255 is not a number.
+ *   tensor_scale  NVFP4: device, one fp32, normal and > 0, or NULL for 1. MXFP4: not looked at.
+ * and element k of row r stands for  code * scale(block) * tensor_scale. Activations and weights have the same form
+ * and come from the same quantizer.
+ */
+size_t sqap_mx4_scale_bytes(int rows, int K, int format);
+
+/*
+ * Quantizer. Row i is row (row_index ? row_index[i] : i) of x, rows ldx elements apart, x_dtype FP16, BF16 or FP32.
+ *   NVFP4: scale = e4m3( (amax / 6) / tensor_scale )   round to nearest even, at most 448; fp32 divisions
+ *          code  = e2m1( x * (1 / (scale * tensor_scale)) ), the product rounded to a multiple of 2^-19 first
+ *   MXFP4: scale = 2^(floor(log2 amax) - 2), at least 2^-127;   code = e2m1( x / scale )
+ *   e2m1 rounds to nearest, ties to even, and stops at +-6. A block whose scale is 0 has zero codes.
+ * Writes every scale byte of the M rows, the zero bytes behind the last block among them. K % 32 == 0; x, codes and
+ * scales 16-byte aligned, the rows of x a multiple of 16 bytes apart. M = 0 is a no-op. Non-finite values give
+ * unspecified codes in their block only.
+ */
+sqap_status sqap_mx4_quantize(const void* x, int x_dtype, int M, int K, int64_t ldx, const int32_t* row_index, int format,
+                              const float* tensor_scale, uint8_t* codes, uint8_t* scales, void* stream);
+
+/* The numbers that codes and scales stand for, rounded once to out_dtype (FP16, BF16, FP32), rows ldo elements apart (a
+ * multiple of 16 bytes). */
+sqap_status sqap_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int M, int K, int format,
+                                const float* tensor_scale, void* out, int64_t ldo, int out_dtype, void* stream);
+
+/*
+ * Product: out[m][n] = round( (sum_k x[m][k] w[n][k]) * (x_tensor_scale * w_tensor_scale) ), sums of code * scale products in
+ * fp32, rounded once. Both matrices in the same format, K % 32 == 0. out: rows ldo elements apart, 16-byte aligned and a multiple of 16
+ * bytes apart, FP16, BF16 or FP32. The sums are added in an order that depends on the sizes alone: equal calls give equal
+ * bits. No workspace. Errors: INVALID, ALIGN, UNSUPPORTED (not an sm_100 device), CUDA.
+ */
+sqap_status sqap_mx4_linear(const uint8_t* x_codes, const uint8_t* x_scales, const float* x_tensor_scale, int M,
+                            const uint8_t* w_codes, const uint8_t* w_scales, const float* w_tensor_scale, int N, int K,
+                            int format, void* out, int64_t ldo, int out_dtype, void* stream);
+
+/*
+ * Quantizer and product as one call; the same bits as the two. workspace: device scratch of at least
+ * sqap_mx4_workspace_bytes(M, N, K, format) bytes, 16-byte aligned; calls in flight at once (two streams, two captured
+ * graphs that may run at the same time) need one each. The weights must not be written by work that is still to come
+ * before the call in other streams; the order within `stream` suffices.
+ */
+size_t sqap_mx4_workspace_bytes(int M, int N, int K, int format);
+sqap_status sqap_mx4_quantize_linear(const void* x, int x_dtype, int M, int64_t ldx, const int32_t* row_index,
+                                     const float* x_tensor_scale, const uint8_t* w_codes, const uint8_t* w_scales,
+                                     const float* w_tensor_scale, int N, int K, int format, void* out, int64_t ldo,
+                                     int out_dtype, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Parameters of the pruning criterion (Section "Quantization-aware Pruning Strategies").

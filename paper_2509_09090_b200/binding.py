@@ -14,7 +14,8 @@ LIB_PATH = os.path.join(_HERE, "libsqap.so")
 SQAP_OK, SQAP_ERR_INVALID, SQAP_ERR_RANGE, SQAP_ERR_ALIGN, SQAP_ERR_UNSUPPORTED, SQAP_ERR_NOMEM, \
     SQAP_ERR_CUDA, SQAP_ERR_TIMEOUT, SQAP_ERR_TOO_LARGE = range(9)
 SQAP_STATIC_WORKSPACE_BYTES = 4 * 1024 * 1024 + 8192
-SQAP_FP16, SQAP_BF16, SQAP_I32 = 0, 1, 2
+SQAP_FP16, SQAP_BF16, SQAP_I32, SQAP_FP32 = 0, 1, 2, 3
+SQAP_MX_NVFP4, SQAP_MX_MXFP4 = 0, 1
 SQAP_Q_ROTATE = 1
 SQAP_Q_PER_TENSOR = 2
 SQAP_W_ROTATED = 1
@@ -29,6 +30,8 @@ def SQAP_L_KSPLIT(n: int) -> int:
 EXPORTS = ("sqap_pack_weights", "sqap_quantize_weights", "sqap_free_weights", "sqap_weights_info", "sqap_unpack_weights",
            "sqap_quantize_act", "sqap_quantize_act_ex", "sqap_workspace_bytes", "sqap_w4a4_linear", "sqap_w4a4_linear_static",
            "sqap_quantize_linear", "sqap_quantize_linear_workspace_bytes",
+           "sqap_mx4_scale_bytes", "sqap_mx4_quantize", "sqap_mx4_dequantize", "sqap_mx4_linear", "sqap_mx4_workspace_bytes",
+           "sqap_mx4_quantize_linear",
            "sqap_prune_tokens", "sqap_prune_select", "sqap_attention_scores",
            "sqap_project_center", "sqap_device_status", "sqap_last_cuda_error", "sqap_status_string",
            "sqap_kernel_launch_count", "sqap_selftest_bounded_wait")
@@ -75,6 +78,14 @@ def lib() -> ctypes.CDLL:
     L.sqap_quantize_linear_workspace_bytes.argtypes = [i32, i32, i32]
     L.sqap_quantize_linear_workspace_bytes.restype = sz
     L.sqap_quantize_linear.argtypes = [vp, i32, i64, vp, u32, vp, vp, vp, i64, i32, u32, vp, sz, vp]
+    L.sqap_mx4_scale_bytes.argtypes = [i32, i32, i32]
+    L.sqap_mx4_scale_bytes.restype = sz
+    L.sqap_mx4_quantize.argtypes = [vp, i32, i32, i32, i64, vp, i32, vp, vp, vp, vp]
+    L.sqap_mx4_dequantize.argtypes = [vp, vp, i32, i32, i32, vp, vp, i64, i32, vp]
+    L.sqap_mx4_linear.argtypes = [vp, vp, vp, i32, vp, vp, vp, i32, i32, i32, vp, i64, i32, vp]
+    L.sqap_mx4_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    L.sqap_mx4_workspace_bytes.restype = sz
+    L.sqap_mx4_quantize_linear.argtypes = [vp, i32, i32, i64, vp, vp, vp, vp, vp, i32, i32, i32, vp, i64, i32, vp, sz, vp]
     L.sqap_prune_tokens.argtypes = [ctypes.POINTER(PruneParams), vp, vp, vp, i64, i32, vp, i64, i32, vp, vp, vp]
     L.sqap_prune_select.argtypes = [ctypes.POINTER(PruneParams), vp, vp, i32, vp, vp, vp, vp]
     L.sqap_attention_scores.argtypes = [vp, i64, i32, i32, i32, i32, i32, i32, i32, i32, i32, vp, vp]
@@ -211,6 +222,41 @@ def sqap_w4a4_linear_static(q_packed, act_scales, M: int, w: Weights, w_up, out,
     _check(lib().sqap_w4a4_linear_static(_ptr(q_packed), _ptr(act_scales), M, w.handle,
                                          w_up.handle if w_up else None, _ptr(out), ldo, out_dtype, flags,
                                          _stream(stream)), "sqap_w4a4_linear_static")
+
+
+def sqap_mx4_scale_bytes(rows: int, K: int, format: int) -> int:
+    return int(lib().sqap_mx4_scale_bytes(rows, K, format))
+
+
+def sqap_mx4_quantize(x, x_dtype: int, M: int, K: int, ldx: int, row_index, format: int, tensor_scale, codes, scales, stream=None):
+    """Rows of fp16 / bf16 / fp32 -> microscaled 4-bit codes [M, K/2] and the scale tiles, see include/sqap.h."""
+    _check(lib().sqap_mx4_quantize(_ptr(x), x_dtype, M, K, ldx, _ptr(row_index), format, _ptr(tensor_scale), _ptr(codes),
+                                   _ptr(scales), _stream(stream)), "sqap_mx4_quantize")
+
+
+def sqap_mx4_dequantize(codes, scales, M: int, K: int, format: int, tensor_scale, out, ldo: int, out_dtype: int, stream=None):
+    _check(lib().sqap_mx4_dequantize(_ptr(codes), _ptr(scales), M, K, format, _ptr(tensor_scale), _ptr(out), ldo, out_dtype,
+                                     _stream(stream)), "sqap_mx4_dequantize")
+
+
+def sqap_mx4_linear(x_codes, x_scales, x_tensor_scale, M: int, w_codes, w_scales, w_tensor_scale, N: int, K: int, format: int,
+                    out, ldo: int, out_dtype: int, stream=None):
+    _check(lib().sqap_mx4_linear(_ptr(x_codes), _ptr(x_scales), _ptr(x_tensor_scale), M, _ptr(w_codes), _ptr(w_scales),
+                                 _ptr(w_tensor_scale), N, K, format, _ptr(out), ldo, out_dtype, _stream(stream)),
+           "sqap_mx4_linear")
+
+
+def sqap_mx4_workspace_bytes(M: int, N: int, K: int, format: int) -> int:
+    return int(lib().sqap_mx4_workspace_bytes(M, N, K, format))
+
+
+def sqap_mx4_quantize_linear(x, x_dtype: int, M: int, ldx: int, row_index, x_tensor_scale, w_codes, w_scales, w_tensor_scale,
+                             N: int, K: int, format: int, out, ldo: int, out_dtype: int, workspace, workspace_bytes: int,
+                             stream=None):
+    """Quantizer and product as one call, see include/sqap.h."""
+    _check(lib().sqap_mx4_quantize_linear(_ptr(x), x_dtype, M, ldx, _ptr(row_index), _ptr(x_tensor_scale), _ptr(w_codes),
+                                          _ptr(w_scales), _ptr(w_tensor_scale), N, K, format, _ptr(out), ldo, out_dtype,
+                                          _ptr(workspace), workspace_bytes, _stream(stream)), "sqap_mx4_quantize_linear")
 
 
 def sqap_prune_tokens(params: dict, scores, ring_center, x, ldx: int, K: int, x_out, ldo: int, out_rows: int,

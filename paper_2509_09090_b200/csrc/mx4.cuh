@@ -1,0 +1,21 @@
+// Internal interface of the microscaled 4-bit operators (mx4.cu: quantizer and its inverse; mx4_linear.cu: product).
+#pragma once
+
+#include "common.cuh"
+
+namespace sqap {
+
+// Elements that share a scale.
+inline __host__ __device__ int mx4_block(int format) { return format == SQAP_MX_NVFP4 ? 16 : 32; }
+// 512-byte scale tiles (128 rows x 4 blocks) along K.
+inline __host__ __device__ int mx4_k_tiles(int K, int format) { return (K / mx4_block(format) + 3) / 4; }
+
+// Rows of any of the accepted input types -> codes and scales (arguments checked by the caller).
+sqap_status launch_mx4_quantize(const void* x, int x_dtype, int M, int K, int64_t ldx, const int32_t* row_index, int format,
+                                const float* tensor_scale, uint8_t* codes, uint8_t* scales, cudaStream_t s);
+sqap_status check_mx4_quantize(const void* x, int x_dtype, int M, int K, int64_t ldx, int format, const void* codes,
+                               const void* scales);
+
+inline int type_bytes(int dtype) { return dtype == SQAP_FP32 ? 4 : 2; }
+
+}  // namespace sqap
