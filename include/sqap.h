@@ -346,6 +346,115 @@ sqap_status sqap_attention_scores(const void* qkv, int64_t ldq, int batch, int r
                                   void* stream);
 
 /*
+ * Paged key/value cache in 8 bits. One layer's cache is
+ *   k, v              device codes [pages][kv_heads][page_tokens][head_dim], int8 or e4m3, 16-byte aligned
+ *   k_scale, v_scale  device fp32 [pages][kv_heads]: the scale of that page's codes of that head
+ * so the block of tokens that shares a scale is a page (of one head). An element stands for code * scale. Sequence b has
+ * lens[b] tokens; token p of it is token p % page_tokens of page table[b*ldt + p / page_tokens]. All index arrays are
+ * device int32. A table entry that is not a page (negative, or >= pages) holds no tokens: what is appended there is
+ * dropped, what is read there is zero, attention does not see it. Table, lengths and pages' use counts serve all layers of a
+ * model; each layer has a cache of its own with the same page numbers.
+ * page_tokens: 16, 32, 64 or 128. head_dim: 64, 128 or 256.
+ */
+#define SQAP_KV_INT8 0 /* codes -127 .. 127; scale = amax / 127 (0 if that is below 2^-100) */
+#define SQAP_KV_E4M3 1 /* e4m3 codes; scale = the smallest power of two (2^-100 at least) with amax / scale <= 448; 0 if amax is 0 */
+typedef struct {
+    void* k;
+    void* v;
+    float* k_scale;
+    float* v_scale;
+    int pages, kv_heads, page_tokens, head_dim;
+    int type; /* SQAP_KV_INT8 or SQAP_KV_E4M3 */
+} sqap_kv_cache;
+
+/*
+ * Appends: rows cu_new[b] .. cu_new[b+1]-1 of k and v (dtype FP16 or BF16, rows ldk / ldv elements apart, head h in columns
+ * h*head_dim ...: column slices of a fused QKV output are taken in place) become the LAST tokens of sequence b, whose
+ * lens[b] counts them already; tokens that would lie before position 0 are dropped. max_new: no sequence brings more (rows
+ * beyond that are not read). For each page and head that receives tokens:
+ *   scale' = max(scale if the page holds earlier tokens of the sequence, else 0; scale of the new tokens' amax)
+ *   earlier tokens, if the scale grew:  code' = round(code * (scale / scale'));  new tokens:  code = round(x * (1 / scale'))
+ * in fp32, round to nearest even, int8 clamped to +-127, e4m3 to +-448. Powers of two make the first rule exact for e4m3
+ * but for its subnormal codes. A page that receives tokens must belong to one sequence. Other places of the page
+ * keep their codes. cu_new: batch + 1 entries, not decreasing. Non-finite values give unspecified codes in their page.
+ */
+sqap_status sqap_kv_append(const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int batch, const int32_t* lens,
+                           const int32_t* cu_new, int max_new, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                           int dtype, void* stream);
+
+/*
+ * Attention of new query rows over the cache: rows cu_q[b] .. cu_q[b+1]-1 of q are the queries of the last n_q tokens of
+ * sequence b, heads x head_dim elements each; query head h reads key/value head h / (heads / kv_heads).
+ *   out[row][h] = sum_t p_t v_t,   p = softmax over the visible t of (q . k_t) * scale
+ * With SQAP_KV_CAUSAL query i of n_q sees tokens 0 .. lens[b] - n_q + i, without it all lens[b]. A row that sees nothing is 0
+ * (lse -inf). lse (may be NULL): fp32 [rows][heads], log sum_t exp((q . k_t) scale).
+ * dtype (of q and out): FP16 or BF16; rows ldq / ldo elements apart, 16-byte aligned, ldq, ldo % 8 == 0. Rows that belong to no
+ * sequence are left as they are. max_q, max_len: no sequence has more queries or tokens (more are not computed / not
+ * seen); they size the launch. Scores, maxima, denominators and sums are fp32; the queries enter the matrix
+ * instructions in fp16 after an exact scaling of each row by a power of two, the softmax's weights rounded to fp16
+ * (relative 2^-11). workspace: device scratch of at least sqap_kv_attention_workspace_bytes bytes (may be 0), 16-byte
+ * aligned, one per call in flight. Equal calls give equal bits.
+ */
+#define SQAP_KV_CAUSAL 1u
+size_t sqap_kv_attention_workspace_bytes(const sqap_kv_cache* cache, int batch, int max_q, int max_len, int heads);
+sqap_status sqap_kv_attention(const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int batch, const int32_t* lens,
+                              const int32_t* cu_q, int max_q, int max_len, const void* q, int64_t ldq, int heads, float scale,
+                              uint32_t flags, void* out, int64_t ldo, float* lse, int dtype, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* Reads back: tokens first[b] + i (first NULL: i) of sequence b, i < cu_rows[b+1] - cu_rows[b] (at most max_rows), become rows
+ * cu_rows[b] + i of k and v (either may be NULL), rounded once to dtype (FP16, BF16). Token positions are not compared
+ * with lens: a position whose page does not exist reads as zero. */
+sqap_status sqap_kv_read(const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int batch, const int32_t* first,
+                         const int32_t* cu_rows, int max_rows, void* k, int64_t ldk, void* v, int64_t ldv, int dtype,
+                         void* stream);
+
+/*
+ * Pages. refs: device int32 [pages], how many table rows use a page; 0 = free. table: [rows][ldt]; lens: [rows]. At most 16384
+ * rows, and as many entries in a list. These calls change refs, table and lens only, in one step of `stream`; the codes
+ * follow with sqap_kv_copy_pages / sqap_kv_compact for each layer. Free pages are given out lowest number first, in the
+ * order of the list: the outcome does not depend on timing. Calls on the same pool are for one stream at a time.
+ *
+ * sqap_kv_alloc: row row_list[i] grows by add[i] >= 0 tokens: its table row gets the pages it lacks, lens[row] += add[i].
+ * A request that cannot be met as a whole changes nothing: too few free pages for it after those before it, a table row too
+ * narrow, a row that does not exist, that is named earlier in the list already or whose length would pass 2^31 - 1. granted
+ * (may be NULL): int32 [n], 1 where the request was met, else 0.
+ */
+sqap_status sqap_kv_alloc(int32_t* refs, int pages, int page_tokens, int32_t* table, int64_t ldt, int rows, int32_t* lens,
+                          const int32_t* row_list, const int32_t* add, int n, int32_t* granted, void* stream);
+
+/*
+ * sqap_kv_fork: row dst_rows[i], which must be empty (lens 0), becomes a copy of src_rows[i]: the full pages are shared (refs + 1),
+ * an unfinished last page is copied into a fresh one. pairs: device int32 [n][2], 8-byte aligned, gets (page to copy, fresh
+ * page), (-1, -1) where there is none to copy, (-2, -2) where the request was not met: no such row, a destination that is
+ * not empty, is named earlier or is also a source, no free page. Such a request changes nothing. The same source may
+ * be forked many times.
+ */
+sqap_status sqap_kv_fork(int32_t* refs, int pages, int page_tokens, int32_t* table, int64_t ldt, int rows, int32_t* lens,
+                         const int32_t* src_rows, const int32_t* dst_rows, int n, int32_t* pairs, int32_t* granted, void* stream);
+
+/* sqap_kv_free: gives up the rows of the list: refs - 1 for each of their pages, table entries -1, lens 0. Rows that are empty, do
+ * not exist or were named before count for nothing. */
+sqap_status sqap_kv_free(int32_t* refs, int pages, int page_tokens, int32_t* table, int64_t ldt, int rows, int32_t* lens,
+                         const int32_t* row_list, int n, void* stream);
+
+/* Copies pages (codes and scales, keys and values) of one layer: pairs[i] = (from, to); a pair with a number that is no page is
+ * skipped. No page may be the `to` of two pairs, or of one pair and the `from` of another. */
+sqap_status sqap_kv_copy_pages(const sqap_kv_cache* cache, const int32_t* pairs, int n, void* stream);
+
+/*
+ * Brings the tokens that are kept together (the cache of a layer in front of the pruning, after sqap_prune_tokens): token t of row
+ * dst_rows[i] becomes token kept[i*ldkept + t] of row src_rows[i], t < n_kept[i] (at most max_kept). The pages of the destination
+ * (reserved with sqap_kv_alloc) get new scales from the largest magnitude that they receive; codes are round(value *
+ * (1 / scale)), values being code * scale of the source in fp32. Places behind the last token of a page become 0. A position
+ * outside the source reads as 0; positions may repeat and need no order. No destination page may be a source page of the
+ * call. Lengths and tables are only read; `rows` of them exist.
+ */
+sqap_status sqap_kv_compact(const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int rows, const int32_t* lens,
+                            const int32_t* src_rows, const int32_t* dst_rows, int n, const int32_t* kept, int64_t ldkept,
+                            const int32_t* n_kept, int max_kept, void* stream);
+
+/*
  * Host helper (no GPU): robot-aware protection, Eq. 2-3. Projects the world point xyz through the
  * intrinsics Kmat (3x3 row-major) and extrinsics Rt = [R|t] (3x4 row-major) and maps the pixel to
  * token coordinates with the patch size (patch_w, patch_h), in double precision:

@@ -16,6 +16,8 @@ SQAP_OK, SQAP_ERR_INVALID, SQAP_ERR_RANGE, SQAP_ERR_ALIGN, SQAP_ERR_UNSUPPORTED,
 SQAP_STATIC_WORKSPACE_BYTES = 4 * 1024 * 1024 + 8192
 SQAP_FP16, SQAP_BF16, SQAP_I32, SQAP_FP32 = 0, 1, 2, 3
 SQAP_MX_NVFP4, SQAP_MX_MXFP4 = 0, 1
+SQAP_KV_INT8, SQAP_KV_E4M3 = 0, 1
+SQAP_KV_CAUSAL = 1
 SQAP_Q_ROTATE = 1
 SQAP_Q_PER_TENSOR = 2
 SQAP_W_ROTATED = 1
@@ -32,6 +34,8 @@ EXPORTS = ("sqap_pack_weights", "sqap_quantize_weights", "sqap_free_weights", "s
            "sqap_quantize_linear", "sqap_quantize_linear_workspace_bytes",
            "sqap_mx4_scale_bytes", "sqap_mx4_quantize", "sqap_mx4_dequantize", "sqap_mx4_linear", "sqap_mx4_workspace_bytes",
            "sqap_mx4_quantize_linear",
+           "sqap_kv_append", "sqap_kv_attention", "sqap_kv_attention_workspace_bytes", "sqap_kv_read", "sqap_kv_alloc",
+           "sqap_kv_fork", "sqap_kv_free", "sqap_kv_copy_pages", "sqap_kv_compact",
            "sqap_prune_tokens", "sqap_prune_select", "sqap_attention_scores",
            "sqap_project_center", "sqap_device_status", "sqap_last_cuda_error", "sqap_status_string",
            "sqap_kernel_launch_count", "sqap_selftest_bounded_wait")
@@ -49,6 +53,11 @@ class PruneParams(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int) for n in ("batch", "rows", "visual_start", "n_visual", "grid_w", "grid_h",
                                             "score_rows", "k_attn", "keep_total", "ring_radius")] + \
                [("flags", ctypes.c_uint32)]
+
+
+class _KvCacheStruct(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + \
+               [(n, ctypes.c_int) for n in ("pages", "kv_heads", "page_tokens", "head_dim", "type")]
 
 
 _lib = None
@@ -86,6 +95,17 @@ def lib() -> ctypes.CDLL:
     L.sqap_mx4_workspace_bytes.argtypes = [i32, i32, i32, i32]
     L.sqap_mx4_workspace_bytes.restype = sz
     L.sqap_mx4_quantize_linear.argtypes = [vp, i32, i32, i64, vp, vp, vp, vp, vp, i32, i32, i32, vp, i64, i32, vp, sz, vp]
+    cache = ctypes.POINTER(_KvCacheStruct)
+    L.sqap_kv_append.argtypes = [cache, vp, i64, i32, vp, vp, i32, vp, i64, vp, i64, i32, vp]
+    L.sqap_kv_attention_workspace_bytes.argtypes = [cache, i32, i32, i32, i32]
+    L.sqap_kv_attention_workspace_bytes.restype = sz
+    L.sqap_kv_attention.argtypes = [cache, vp, i64, i32, vp, vp, i32, i32, vp, i64, i32, ctypes.c_float, u32, vp, i64, vp, i32, vp, sz, vp]
+    L.sqap_kv_read.argtypes = [cache, vp, i64, i32, vp, vp, i32, vp, i64, vp, i64, i32, vp]
+    L.sqap_kv_alloc.argtypes = [vp, i32, i32, vp, i64, i32, vp, vp, vp, i32, vp, vp]
+    L.sqap_kv_fork.argtypes = [vp, i32, i32, vp, i64, i32, vp, vp, vp, i32, vp, vp, vp]
+    L.sqap_kv_free.argtypes = [vp, i32, i32, vp, i64, i32, vp, vp, i32, vp]
+    L.sqap_kv_copy_pages.argtypes = [cache, vp, i32, vp]
+    L.sqap_kv_compact.argtypes = [cache, vp, i64, i32, vp, vp, vp, i32, vp, i64, vp, i32, vp]
     L.sqap_prune_tokens.argtypes = [ctypes.POINTER(PruneParams), vp, vp, vp, i64, i32, vp, i64, i32, vp, vp, vp]
     L.sqap_prune_select.argtypes = [ctypes.POINTER(PruneParams), vp, vp, i32, vp, vp, vp, vp]
     L.sqap_attention_scores.argtypes = [vp, i64, i32, i32, i32, i32, i32, i32, i32, i32, i32, vp, vp]
@@ -257,6 +277,76 @@ def sqap_mx4_quantize_linear(x, x_dtype: int, M: int, ldx: int, row_index, x_ten
     _check(lib().sqap_mx4_quantize_linear(_ptr(x), x_dtype, M, ldx, _ptr(row_index), _ptr(x_tensor_scale), _ptr(w_codes),
                                           _ptr(w_scales), _ptr(w_tensor_scale), N, K, format, _ptr(out), ldo, out_dtype,
                                           _ptr(workspace), workspace_bytes, _stream(stream)), "sqap_mx4_quantize_linear")
+
+
+class KvCache:
+    """A layer's 8-bit key/value cache over tensors that the caller owns: k, v codes [pages, kv_heads, page_tokens, head_dim]
+    (int8, or float8_e4m3fn / uint8), k_scale, v_scale fp32 [pages, kv_heads]; all contiguous."""
+
+    def __init__(self, k, v, k_scale, v_scale, type: int):
+        pages, heads, tokens, dim = k.shape
+        if tuple(v.shape) != (pages, heads, tokens, dim) or tuple(k_scale.shape) != (pages, heads) or tuple(v_scale.shape) != (pages, heads):
+            raise ValueError("KvCache: k, v are [pages, kv_heads, page_tokens, head_dim], the scales [pages, kv_heads]")
+        if any(x.element_size() != 1 for x in (k, v)) or any(x.element_size() != 4 or not x.is_floating_point() for x in (k_scale, v_scale)):
+            raise ValueError("KvCache: codes have 8 bits, scales are fp32")
+        if not all(x.is_contiguous() for x in (k, v, k_scale, v_scale)):
+            raise ValueError("KvCache: tensors must be contiguous")
+        self.tensors = (k, v, k_scale, v_scale)
+        self.struct = _KvCacheStruct(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), pages, heads, tokens, dim, type)
+        self.ref = ctypes.byref(self.struct)
+
+
+def sqap_kv_append(cache: KvCache, table, ldt: int, batch: int, lens, cu_new, max_new: int, k, ldk: int, v, ldv: int, dtype: int,
+                   stream=None):
+    """New tokens into the cache, see include/sqap.h."""
+    _check(lib().sqap_kv_append(cache.ref, _ptr(table), ldt, batch, _ptr(lens), _ptr(cu_new), max_new, _ptr(k), ldk, _ptr(v), ldv,
+                                dtype, _stream(stream)), "sqap_kv_append")
+
+
+def sqap_kv_attention_workspace_bytes(cache: KvCache, batch: int, max_q: int, max_len: int, heads: int) -> int:
+    return int(lib().sqap_kv_attention_workspace_bytes(cache.ref, batch, max_q, max_len, heads))
+
+
+def sqap_kv_attention(cache: KvCache, table, ldt: int, batch: int, lens, cu_q, max_q: int, max_len: int, q, ldq: int, heads: int,
+                      scale: float, flags: int, out, ldo: int, lse, dtype: int, workspace, workspace_bytes: int, stream=None):
+    """Attention of new query rows over the cache, see include/sqap.h."""
+    _check(lib().sqap_kv_attention(cache.ref, _ptr(table), ldt, batch, _ptr(lens), _ptr(cu_q), max_q, max_len, _ptr(q), ldq, heads,
+                                   scale, flags, _ptr(out), ldo, _ptr(lse), dtype, _ptr(workspace), workspace_bytes,
+                                   _stream(stream)), "sqap_kv_attention")
+
+
+def sqap_kv_read(cache: KvCache, table, ldt: int, batch: int, first, cu_rows, max_rows: int, k, ldk: int, v, ldv: int, dtype: int,
+                 stream=None):
+    _check(lib().sqap_kv_read(cache.ref, _ptr(table), ldt, batch, _ptr(first), _ptr(cu_rows), max_rows, _ptr(k), ldk, _ptr(v), ldv,
+                              dtype, _stream(stream)), "sqap_kv_read")
+
+
+def sqap_kv_alloc(refs, pages: int, page_tokens: int, table, ldt: int, rows: int, lens, row_list, add, n: int, granted=None, stream=None):
+    """Rows of the page table grow, see include/sqap.h."""
+    _check(lib().sqap_kv_alloc(_ptr(refs), pages, page_tokens, _ptr(table), ldt, rows, _ptr(lens), _ptr(row_list), _ptr(add), n,
+                               _ptr(granted), _stream(stream)), "sqap_kv_alloc")
+
+
+def sqap_kv_fork(refs, pages: int, page_tokens: int, table, ldt: int, rows: int, lens, src_rows, dst_rows, n: int, pairs, granted=None,
+                 stream=None):
+    _check(lib().sqap_kv_fork(_ptr(refs), pages, page_tokens, _ptr(table), ldt, rows, _ptr(lens), _ptr(src_rows), _ptr(dst_rows), n,
+                              _ptr(pairs), _ptr(granted), _stream(stream)), "sqap_kv_fork")
+
+
+def sqap_kv_free(refs, pages: int, page_tokens: int, table, ldt: int, rows: int, lens, row_list, n: int, stream=None):
+    _check(lib().sqap_kv_free(_ptr(refs), pages, page_tokens, _ptr(table), ldt, rows, _ptr(lens), _ptr(row_list), n,
+                              _stream(stream)), "sqap_kv_free")
+
+
+def sqap_kv_copy_pages(cache: KvCache, pairs, n: int, stream=None):
+    _check(lib().sqap_kv_copy_pages(cache.ref, _ptr(pairs), n, _stream(stream)), "sqap_kv_copy_pages")
+
+
+def sqap_kv_compact(cache: KvCache, table, ldt: int, rows: int, lens, src_rows, dst_rows, n: int, kept, ldkept: int, n_kept,
+                    max_kept: int, stream=None):
+    """The kept tokens of rows of the table, brought together in other rows, see include/sqap.h."""
+    _check(lib().sqap_kv_compact(cache.ref, _ptr(table), ldt, rows, _ptr(lens), _ptr(src_rows), _ptr(dst_rows), n, _ptr(kept), ldkept,
+                                 _ptr(n_kept), max_kept, _stream(stream)), "sqap_kv_compact")
 
 
 def sqap_prune_tokens(params: dict, scores, ring_center, x, ldx: int, K: int, x_out, ldo: int, out_rows: int,

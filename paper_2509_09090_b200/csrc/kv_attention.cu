@@ -1,0 +1,157 @@
+// Attention over the paged 8-bit cache: checks, the choice of kernel and of the pieces a history is cut into, and the kernel
+// that joins the pieces.
+#include "kv_attention.cuh"
+
+namespace sqap {
+namespace kv {
+namespace {
+
+// One warp per row: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
+template <typename T, int D>
+__global__ void __launch_bounds__(128) kv_combine_kernel(AttnArgs a) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    const int i = static_cast<int>(id % a.max_q);
+    const int64_t bh = id / a.max_q;
+    const int head = static_cast<int>(bh % a.heads);
+    const int64_t b = bh / a.heads;
+    if (b >= a.batch) return;
+    const int row0 = a.cu[b];
+    if (i >= a.cu[b + 1] - row0) return;
+    const int64_t at = part_index(a, static_cast<int>(b), head, i, 0);
+    float m = -INFINITY;
+    for (int s = lane; s < a.splits; s += 32) m = fmaxf(m, a.part_ml[at + s].x);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f, y[D / 32] = {};
+    for (int s = 0; s < a.splits; ++s) {
+        const float2 ml = a.part_ml[at + s];
+        if (!(ml.y > 0.0f)) continue;
+        const float f = fast_exp2(ml.x - ref);
+        l = fmaf(ml.y, f, l);
+        const float2* p = reinterpret_cast<const float2*>(a.part_o + (at + s) * D) + lane;
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) {
+            const float2 x = p[32 * e];
+            y[2 * e] = fmaf(x.x, f, y[2 * e]);
+            y[2 * e + 1] = fmaf(x.y, f, y[2 * e + 1]);
+        }
+    }
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    const int64_t row = static_cast<int64_t>(row0) + i;
+    uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + row * a.ldo + static_cast<int64_t>(head) * D) + lane;
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) out[32 * e] = pack2<T>(y[2 * e] * inv, y[2 * e + 1] * inv);
+    if (lane == 0 && a.lse) a.lse[row * a.heads + head] = l > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+}
+
+template <typename T>
+cudaError_t combine_as(const AttnArgs& a, cudaStream_t s) {
+    const int64_t rows = static_cast<int64_t>(a.batch) * a.heads * a.max_q;
+    const dim3 grid(static_cast<unsigned>((rows + 3) / 4));
+    if (a.c.head_dim == 64) return launch_dependent(kv_combine_kernel<T, 64>, grid, dim3(128), 0, s, a);
+    if (a.c.head_dim == 128) return launch_dependent(kv_combine_kernel<T, 128>, grid, dim3(128), 0, s, a);
+    return launch_dependent(kv_combine_kernel<T, 256>, grid, dim3(128), 0, s, a);
+}
+
+struct Plan {
+    bool decode;
+    int tiles, splits, chunk;
+};
+// From the sizes alone, so that the workspace can be asked for ahead: enough CTAs to fill the device a few times over
+// (uneven histories then even out), pieces of 256 keys at least.
+Plan plan_for(int64_t batch, int kv_heads, int group, int head_dim, int64_t max_q, int64_t max_len) {
+    Plan p;
+    const int64_t rows = max_q * group;
+    p.decode = rows <= decode_max_rows(head_dim);
+    p.tiles = p.decode ? 1 : static_cast<int>((rows + PREFILL_ROWS - 1) / PREFILL_ROWS);
+    const int64_t ctas = batch * kv_heads * p.tiles;
+    int64_t want;
+    if (p.decode) want = max_len > 1024 ? 148 * 16 : 148 * 3;
+    else want = ctas < 148 ? 148 * 2 : 0;
+    int64_t splits = ctas > 0 ? (want + ctas - 1) / ctas : 1;
+    const int64_t most = (max_len + 255) / 256;
+    if (splits > most) splits = most;
+    if (splits < 1) splits = 1;
+    const int64_t chunk = ((max_len + splits - 1) / splits + 127) / 128 * 128;
+    p.chunk = static_cast<int>(chunk < 128 ? 128 : chunk);
+    p.splits = static_cast<int>((max_len + p.chunk - 1) / p.chunk);
+    if (p.splits < 1) p.splits = 1;
+    return p;
+}
+size_t part_bytes(int64_t batch, int heads, int64_t max_q, int head_dim, const Plan& p) {
+    if (p.splits <= 1) return 0;
+    const size_t parts = static_cast<size_t>(batch) * heads * max_q * p.splits;
+    return parts * (static_cast<size_t>(head_dim) * 4 + 8);
+}
+
+}  // namespace
+}  // namespace kv
+}  // namespace sqap
+
+extern "C" size_t sqap_kv_attention_workspace_bytes(const sqap_kv_cache* cache, int batch, int max_q, int max_len, int heads) {
+    using namespace sqap::kv;
+    if (check_cache(cache) != SQAP_OK || batch <= 0 || max_q <= 0 || max_len < 0 || heads <= 0 || heads % cache->kv_heads != 0) return 0;
+    return part_bytes(batch, heads, max_q, cache->head_dim,
+                      plan_for(batch, cache->kv_heads, heads / cache->kv_heads, cache->head_dim, max_q, max_len));
+}
+
+extern "C" sqap_status sqap_kv_attention(const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int batch, const int32_t* lens,
+                                         const int32_t* cu_q, int max_q, int max_len, const void* q, int64_t ldq, int heads, float scale,
+                                         uint32_t flags, void* out, int64_t ldo, float* lse, int dtype, void* workspace,
+                                         size_t workspace_bytes, void* stream) {
+    using namespace sqap;
+    using namespace sqap::kv;
+    sqap_status st = check_cache(cache);
+    if (st != SQAP_OK) return st;
+    if (batch < 0 || max_q < 0 || max_len < 0 || ldt < 0 || ldt > 0x7FFFFFFF || heads <= 0 || !row_type(dtype)) return SQAP_ERR_INVALID;
+    if (flags & ~SQAP_KV_CAUSAL) return SQAP_ERR_INVALID;
+    if (heads % cache->kv_heads != 0 || !(scale == scale) || scale - scale != 0.0f) return SQAP_ERR_INVALID;
+    const int64_t width = static_cast<int64_t>(heads) * cache->head_dim;
+    if (ldq < width || ldo < width) return SQAP_ERR_INVALID;
+    if (ldq % 8 != 0 || ldo % 8 != 0) return SQAP_ERR_ALIGN;
+    if (batch == 0 || max_q == 0) return SQAP_OK;
+    if (!lens || !cu_q || !q || !out || (ldt > 0 && !table)) return SQAP_ERR_INVALID;
+    if (!aligned16(q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return SQAP_ERR_ALIGN;
+    AttnArgs a;
+    a.c = device_view(cache);
+    a.group = heads / cache->kv_heads;
+    if (static_cast<int64_t>(max_q) * a.group > (1 << 30) || max_len > (1 << 30)) return SQAP_ERR_UNSUPPORTED;
+    const Plan p = plan_for(batch, cache->kv_heads, a.group, cache->head_dim, max_q, max_len);
+    const int64_t grid = static_cast<int64_t>(batch) * cache->kv_heads * p.splits * p.tiles;
+    if (grid > 0x7FFFFFFF || static_cast<int64_t>(batch) * heads * max_q > 4ll * 0x7FFFFFFF) return SQAP_ERR_UNSUPPORTED;
+    const size_t need = part_bytes(batch, heads, max_q, cache->head_dim, p);
+    if (need > 0) {
+        if (!workspace) return SQAP_ERR_INVALID;
+        if (!aligned16(workspace)) return SQAP_ERR_ALIGN;
+        if (workspace_bytes < need) return SQAP_ERR_NOMEM;
+    }
+    a.table = table;
+    a.ldt = ldt;
+    a.batch = batch;
+    a.lens = lens;
+    a.cu = cu_q;
+    a.max_q = max_q;
+    a.max_len = max_len;
+    a.q = q;
+    a.ldq = ldq;
+    a.heads = heads;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.causal = (flags & SQAP_KV_CAUSAL) ? 1 : 0;
+    a.out = out;
+    a.ldo = ldo;
+    a.lse = lse;
+    a.splits = p.splits;
+    a.chunk = p.chunk;
+    a.tiles = p.tiles;
+    const int64_t parts = static_cast<int64_t>(batch) * heads * max_q * p.splits;
+    a.part_o = static_cast<float*>(workspace);
+    a.part_ml = p.splits > 1 ? reinterpret_cast<float2*>(a.part_o + parts * cache->head_dim) : nullptr;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    st = p.decode ? launch_kv_decode(a, cache->type, dtype, s) : launch_kv_prefill(a, cache->type, dtype, s);
+    if (st != SQAP_OK || p.splits <= 1) return st;
+    return finish_launch(dtype == SQAP_FP16 ? combine_as<__half>(a, s) : combine_as<__nv_bfloat16>(a, s));
+}

@@ -1,0 +1,107 @@
+// Internal: what the attention kernels over the 8-bit cache share.
+#pragma once
+
+#include "kv.cuh"
+
+namespace sqap {
+namespace kv {
+
+// For one query row and its keys t:   s_t = (q . k_t) * scale,   out = sum_t 2^(s_t log2 e) v_t / sum_t 2^(s_t log2 e).
+// The codes enter the matrix instructions as they are (exact in fp16); the scale of a page's keys multiplies its scores, and
+// the scale of its values goes into the exponent:  w_t = 2^(s_t log2 e + log2 vs - m) is the weight of the value CODES, with m
+// the running maximum of the whole exponent, so w_t <= 1 whatever the scales are and fp16 holds it to 11 bits; the
+// denominator adds w_t / vs. A page of zero values has no say in m worth keeping: any scale does, and gets this one.
+constexpr float ZERO_PAGE_SCALE = 0.015625f;
+
+struct AttnArgs {
+    Cache c;
+    const int32_t* table;
+    int64_t ldt;
+    int batch;
+    const int32_t* lens;
+    const int32_t* cu;
+    int max_q, max_len;
+    const void* q;
+    int64_t ldq;
+    int heads, group;      // query heads, and how many of them share a key/value head
+    float scale_log2;      // scale * log2 e
+    int causal;
+    void* out;
+    int64_t ldo;
+    float* lse;            // [rows][heads] or null
+    int splits, chunk;     // a history is cut into `splits` pieces of `chunk` keys, or one
+    float* part_o;         // [batch][heads][max_q][splits][D]
+    float2* part_ml;       // the same without D: maximum and denominator
+    int tiles;             // row tiles per (sequence, key/value head)
+};
+
+// Work of a CTA, from its index.
+struct Where {
+    int b, h, split, tile;
+    int row0, n_q, len;    // first row of the sequence, its query rows, its keys
+};
+__device__ __forceinline__ Where locate(const AttnArgs& a, unsigned id) {
+    Where w;
+    w.tile = static_cast<int>(id % a.tiles);
+    id /= a.tiles;
+    w.split = static_cast<int>(id % a.splits);
+    id /= a.splits;
+    w.h = static_cast<int>(id % a.c.kv_heads);
+    w.b = static_cast<int>(id / a.c.kv_heads);
+    w.row0 = a.cu[w.b];
+    const int n = a.cu[w.b + 1] - w.row0;
+    w.n_q = n < 0 ? 0 : n;
+    const int len = a.lens[w.b];
+    w.len = len < 0 ? 0 : (len > a.max_len ? a.max_len : len);
+    return w;
+}
+// Keys that query i of the sequence may look at (the first so many).
+__device__ __forceinline__ int visible(const AttnArgs& a, const Where& w, int i) {
+    if (!a.causal) return w.len;
+    const int64_t n = static_cast<int64_t>(w.len) - w.n_q + i + 1;
+    return n < 0 ? 0 : static_cast<int>(n);
+}
+__device__ __forceinline__ int64_t part_index(const AttnArgs& a, int b, int head, int i, int split) {
+    return ((static_cast<int64_t>(b) * a.heads + head) * a.max_q + i) * a.splits + split;
+}
+// Largest power of two not above 2^9 / amax, so that amax lands in [2^8, 2^9): rows of bf16 then fit fp16 with 22 binary
+// orders below their largest element, more than an fp32 sum resolves.
+__device__ __forceinline__ float fit_exponent(float amax, float* back) {
+    int e = static_cast<int>(__float_as_uint(amax) >> 23) - 127;
+    if (!(amax > 0.0f) || e > 127) e = 8;
+    e = max(e, -110);
+    *back = __uint_as_float(static_cast<uint32_t>(127 + e - 8) << 23);
+    return __uint_as_float(static_cast<uint32_t>(127 - e + 8) << 23);
+}
+
+__device__ __forceinline__ float fast_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void mma_16816(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+template <typename T>
+__device__ __forceinline__ float to_f(T x);
+template <>
+__device__ __forceinline__ float to_f<__half>(__half x) { return __half2float(x); }
+template <>
+__device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+// Few query rows per key/value head (kv_decode.cu) and many (kv_prefill.cu).
+// With 256 elements a lane cannot hold the output of more than 8 rows in registers.
+inline int decode_max_rows(int head_dim) { return head_dim == 256 ? 8 : 16; }
+constexpr int PREFILL_ROWS = 128;
+sqap_status launch_kv_decode(const AttnArgs& a, int type, int dtype, cudaStream_t s);
+sqap_status launch_kv_prefill(const AttnArgs& a, int type, int dtype, cudaStream_t s);
+
+}  // namespace kv
+}  // namespace sqap

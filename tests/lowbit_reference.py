@@ -88,3 +88,90 @@ def mx4_values(codes, byte, fmt, g=1.0):
     n = E2M1[nibbles(codes)]
     M, K = n.shape
     return (n.reshape(M, -1, block(fmt)) * scale_bytes_to_values(byte, fmt)[..., None]).reshape(M, K) * (g if fmt == NVFP4 else 1.0)
+
+
+# ------------------------------------------------------------------------------------------- 8-bit key/value cache
+
+def kv_values(raw, kind):
+    """Codes (uint8 bytes) -> numbers without their scale."""
+    return raw.view(np.int8).astype(np.float64) if kind == INT8 else E4M3_VALUES[raw]
+
+
+def kv_scale(amax, kind):
+    """fp32 scale of a block, from the fp32 largest magnitude."""
+    amax = np.float32(amax)
+    if kind == INT8:
+        s = np.float32(amax / np.float32(127))
+        return s if s >= 2.0 ** -100 else np.float32(0)
+    if not amax > 0:
+        return np.float32(0)
+    e = -100
+    while float(amax) > 448 * 2.0 ** e:
+        e += 1
+    return np.float32(2.0 ** e)
+
+
+def kv_round(y, kind):
+    """fp32 quotients -> codes, as numbers."""
+    y = np.asarray(y, np.float32).astype(np.float64)
+    return np.clip(np.rint(y), -127, 127) if kind == INT8 else to_e4m3(y)
+
+
+def inverse(scale):
+    return np.float32(0) if scale == 0 else np.float32(1) / np.float32(scale)
+
+
+def kv_append(codes, scales, table, lens, cu, rows, kind, P):
+    """codes [pages, H, P, D] (numbers), scales [pages, H] fp32, rows [T, H, D] fp32: changed in place."""
+    pages, H = scales.shape
+    for b in range(len(lens)):
+        n = cu[b + 1] - cu[b]
+        start = lens[b] - n
+        for j in range(table.shape[1]):
+            lo, hi = j * P, (j + 1) * P
+            t0, t1 = max(start, 0, lo), min(lens[b], hi)
+            page = table[b, j]
+            if t0 >= t1 or not 0 <= page < pages:
+                continue
+            for h in range(H):
+                x = rows[cu[b] + t0 - start: cu[b] + t1 - start, h].astype(np.float32)
+                before = scales[page, h] if t0 > max(lo, 0) else np.float32(0)
+                s = max(before, kv_scale(np.abs(x).max(), kind))
+                if t0 > lo and s > before:
+                    codes[page, h, :t0 - lo] = kv_round(codes[page, h, :t0 - lo].astype(np.float32) * np.float32(before / s), kind)
+                codes[page, h, t0 - lo:t1 - lo] = kv_round(x * inverse(s), kind)
+                scales[page, h] = s
+
+
+def kv_tokens(codes, scales, table_row, n, P):
+    """Tokens 0 .. n-1 of a sequence [n, H, D] in 64 bits and whether each exists."""
+    pages, H = scales.shape
+    out, there = np.zeros((n, H, codes.shape[3])), np.zeros(n, bool)
+    for t in range(n):
+        page = table_row[t // P] if t // P < len(table_row) else -1
+        if 0 <= page < pages:
+            there[t] = True
+            out[t] = codes[page, :, t % P] * scales[page].astype(np.float64)[:, None]
+    return out, there
+
+
+def attention(q, k, v, there, n_q, causal, scale):
+    """q [n_q, Hq, D], k, v [len, H, D]: out [n_q, Hq, D], lse [n_q, Hq], and what the tolerances need: the largest sum
+    of |q k| scale of a row, sum p |v|, max p vs-weighted."""
+    G = q.shape[1] // k.shape[1]
+    n = k.shape[0]
+    kk, vv = np.repeat(k, G, 1), np.repeat(v, G, 1)
+    s = np.einsum("ihd,thd->iht", q, kk) * scale
+    mag = (np.einsum("ihd,thd->iht", np.abs(q), np.abs(kk)) * abs(scale)).max(-1) if n else np.zeros(q.shape[:2])
+    seen = np.broadcast_to(there[None, :], (n_q, n)).copy()
+    if causal:
+        seen &= np.arange(n)[None, :] <= (n - n_q + np.arange(n_q))[:, None]
+    s = np.where(seen[:, None, :], s, -np.inf)
+    top = s.max(-1, initial=-np.inf)
+    ref = np.where(np.isfinite(top), top, 0)
+    p = np.exp(s - ref[..., None])
+    total = p.sum(-1)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        p = np.where(total[..., None] > 0, p / np.where(total > 0, total, 1)[..., None], 0)
+        lse = np.where(total > 0, ref + np.log(total), -np.inf)
+    return np.einsum("iht,thd->ihd", p, vv), lse, mag, np.einsum("iht,thd->ihd", p, np.abs(vv)), p
