@@ -151,7 +151,9 @@ extern "C" sqap_status sqap_kv_attention(const sqap_kv_cache* cache, const int32
     a.part_o = static_cast<float*>(workspace);
     a.part_ml = p.splits > 1 ? reinterpret_cast<float2*>(a.part_o + parts * cache->head_dim) : nullptr;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    st = p.decode ? launch_kv_decode(a, cache->type, dtype, s) : launch_kv_prefill(a, cache->type, dtype, s);
+    if (p.decode) st = launch_kv_decode(a, cache->type, dtype, s);
+    else if (cache->head_dim <= 128) st = launch_kv_prefill_tc(a, cache->type, dtype, s);
+    else st = launch_kv_prefill(a, cache->type, dtype, s);
     if (st != SQAP_OK || p.splits <= 1) return st;
     return finish_launch(dtype == SQAP_FP16 ? combine_as<__half>(a, s) : combine_as<__nv_bfloat16>(a, s));
 }

@@ -96,11 +96,12 @@ __device__ __forceinline__ float to_f<__half>(__half x) { return __half2float(x)
 template <>
 __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// Few query rows per key/value head (kv_decode.cu) and many (kv_prefill.cu).
+// Few query rows per key/value head (kv_decode.cu) and many: head_dim 64 and 128 (kv_prefill_tc.cu), 256 (kv_prefill.cu).
 // With 256 elements a lane cannot hold the output of more than 8 rows in registers.
 inline int decode_max_rows(int head_dim) { return head_dim == 256 ? 8 : 16; }
 constexpr int PREFILL_ROWS = 128;
 sqap_status launch_kv_decode(const AttnArgs& a, int type, int dtype, cudaStream_t s);
+sqap_status launch_kv_prefill_tc(const AttnArgs& a, int type, int dtype, cudaStream_t s);
 sqap_status launch_kv_prefill(const AttnArgs& a, int type, int dtype, cudaStream_t s);
 
 }  // namespace kv

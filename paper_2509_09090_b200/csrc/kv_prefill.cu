@@ -1,4 +1,6 @@
-// Attention of many query rows (prompts) over the paged 8-bit cache.
+// Attention of many query rows (prompts) over the paged 8-bit cache, head_dim 256: there a tile's output alone takes 256 columns of
+// tensor memory and its operands 192 KB of shared memory, so that nothing could overlap; register matrix instructions
+// hold it in registers instead. (head_dim 64 and 128: kv_prefill_tc.cu.)
 //
 // One CTA takes 128 rows (query x head of the group, packed: the heads that share a key/value head share its tiles) of one
 // sequence and key/value head and walks the keys in tiles. A tile's codes are fetched one tile ahead into registers,
@@ -24,14 +26,14 @@ template <int D>
 struct Shape {
     static constexpr int WARPS = 8;
     static constexpr int THREADS = WARPS * 32;
-    static constexpr int KEYS = D == 256 ? 32 : 64;      // keys per tile
+    static constexpr int KEYS = 32;                      // keys per tile
     static constexpr int LD = D + 8;                     // halves per row in shared memory: rows 16 bytes apart in the banks
     static constexpr int CHUNKS = KEYS * D / 16 / THREADS;   // 16-byte pieces of codes per thread
     static constexpr int GROUPS = KEYS / 16;
 };
 
 template <typename T, int TYPE, int D>
-__global__ void __launch_bounds__(256, D == 64 ? 2 : 1) kv_prefill_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(256, 1) kv_prefill_kernel(AttnArgs a) {
     using S = Shape<D>;
     constexpr int KEYS = S::KEYS, LD = S::LD;
     static_assert(S::WARPS * 16 == PREFILL_ROWS && S::CHUNKS >= 1, "tile shape");
@@ -250,9 +252,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) kv_prefill_kernel(AttnAr
 }
 
 template <typename T, int TYPE>
-cudaError_t launch_dim(const AttnArgs& a, unsigned grid, cudaStream_t s) {
-    if (a.c.head_dim == 64) return launch_dependent(kv_prefill_kernel<T, TYPE, 64>, dim3(grid), dim3(256), 0, s, a);
-    if (a.c.head_dim == 128) return launch_dependent(kv_prefill_kernel<T, TYPE, 128>, dim3(grid), dim3(256), 0, s, a);
+cudaError_t launch_as(const AttnArgs& a, unsigned grid, cudaStream_t s) {
     return launch_dependent(kv_prefill_kernel<T, TYPE, 256>, dim3(grid), dim3(256), 0, s, a);
 }
 
@@ -261,9 +261,9 @@ cudaError_t launch_dim(const AttnArgs& a, unsigned grid, cudaStream_t s) {
 sqap_status launch_kv_prefill(const AttnArgs& a, int type, int dtype, cudaStream_t s) {
     const unsigned grid = static_cast<unsigned>(static_cast<int64_t>(a.batch) * a.c.kv_heads * a.splits * a.tiles);
     if (dtype == SQAP_FP16)
-        return finish_launch(type == SQAP_KV_INT8 ? launch_dim<__half, SQAP_KV_INT8>(a, grid, s) : launch_dim<__half, SQAP_KV_E4M3>(a, grid, s));
-    return finish_launch(type == SQAP_KV_INT8 ? launch_dim<__nv_bfloat16, SQAP_KV_INT8>(a, grid, s)
-                                              : launch_dim<__nv_bfloat16, SQAP_KV_E4M3>(a, grid, s));
+        return finish_launch(type == SQAP_KV_INT8 ? launch_as<__half, SQAP_KV_INT8>(a, grid, s) : launch_as<__half, SQAP_KV_E4M3>(a, grid, s));
+    return finish_launch(type == SQAP_KV_INT8 ? launch_as<__nv_bfloat16, SQAP_KV_INT8>(a, grid, s)
+                                              : launch_as<__nv_bfloat16, SQAP_KV_E4M3>(a, grid, s));
 }
 
 }  // namespace kv
