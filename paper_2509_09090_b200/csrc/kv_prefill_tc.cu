@@ -1,16 +1,17 @@
 // Attention of many query rows (prompts) over the paged 8-bit cache on tcgen05, head_dim 64 and 128.
 //
-// One CTA takes 128 rows (query x head of the group, packed: the heads that share a key/value head share its tiles) of
-// one sequence and key/value head and walks the keys 128 at a time. Per tile: S = Q K^T into tensor memory, the softmax's
-// weights back into tensor memory as the A operand, O += W V.
-//   warps 0-3  softmax: thread = row. Also load the queries at the start and store the output at the end.
-//   warps 4-7  codes from global memory (one tile ahead, in registers) to fp16 in shared memory, 128B-swizzled
-//   warp  8    issues the MMAs
-// Work per tile and what it costs an SM: MMAs 2 x 128 x 128 x D (1024 cycles at D = 128), 16384 exponentials (1024 cycles),
+// An item is 128 rows (query x head of the group, packed: the heads that share a key/value head share its tiles) of one
+// sequence and key/value head; its keys are walked 64 at a time. Per tile: S = Q K^T into tensor memory, the softmax's weights
+// back into tensor memory as the A operand, O += W V.
+//   warps 0-3  softmax: thread = row. Rescale the output where a maximum has grown, and store it at the end.
+//   warps 4-7  codes from global memory (one tile ahead, in registers) to fp16 in shared memory, 128B-swizzled; the next
+//              item's queries
+//   warp  8    issues the MMAs: the scores of a tile before the output of the tile in front of it, so that the tensor core
+//              works on them while the softmax is still busy
+// Work per 64 keys and what it costs an SM: MMAs 2 x 128 x 64 x D (512 cycles at D = 128), 8192 exponentials (512 cycles),
 // some 3 instructions per weight and 1.3 per code besides. None of it is far ahead of the others, so they have to
-// overlap: a CTA runs score - softmax - output in turn in 256 columns of tensor memory and half an SM's shared memory, and
-// two CTAs on an SM fill each other's gaps. Shared memory is single-buffered: the keys of the next tile are written during
-// the softmax of this one, its values during the next scores.
+// overlap. A CTA takes 256 columns of tensor memory (two tiles of scores, one output) and 96 KB of shared memory (queries,
+// two tiles of keys and values); two CTAs on an SM fill each other's gaps, each walking its share of the items.
 //
 // The running maximum is raised only when a row's maximum has grown by more than 2^8 (the weights then stay within fp16, at
 // the same relative precision): rescaling the output in tensor memory is rare after the first tiles. Weights and sums:
@@ -28,23 +29,25 @@ namespace {
 
 using namespace tc;
 
-constexpr int KEYS = 128;                   // keys per tile
+constexpr int KEYS = 64;                    // keys per tile
 constexpr int GROUPS = KEYS / 16;           // runs of 16 keys: a page never ends inside one
 constexpr int THREADS = 288;
-constexpr int BLOCK_BYTES = 128 * 128;      // 128 rows of 64 halves
-constexpr int TMEM_COLS = 256;              // scores (and weights) 0 .. 127, output from 128
+constexpr int Q_BLOCK = 128 * 128;          // 128 rows of 64 halves
+constexpr int KV_BLOCK = KEYS * 128;        // a tile's keys or values, 64 elements of each
+constexpr int TMEM_COLS = 256;              // scores (and weights) of two tiles 0 .. 127, output from 128
 constexpr int O_COL = 128;
 constexpr float RAISE = 8.0f;
 
 template <int D>
 struct Smem {
-    static constexpr int BLOCKS = D / 64;
-    static constexpr int Q = 0, K = BLOCKS * BLOCK_BYTES, V = 2 * K, TAIL = 3 * K;
-    static constexpr int BYTES = TAIL + 512 + 1024;      // scales, barriers, flags; slack for the alignment
+    static constexpr int BLOCKS = D / 64, TILE = BLOCKS * KV_BLOCK;
+    static constexpr int Q = 0, K = BLOCKS * Q_BLOCK, V = K + 2 * TILE, TAIL = V + 2 * TILE;
+    static constexpr int OFF_FAC = 256, OFF_BAR = OFF_FAC + 2 * 128 * 4, OFF_WORDS = OFF_BAR + 128;
+    static constexpr int BYTES = TAIL + OFF_WORDS + 64 + 1024;      // slack for the alignment
 };
-// scales of the two tiles in flight, by run of 16 keys
+// Scales of the tiles in flight, by run of 16 keys: the softmax may be reading those of tile n - 2 while n's are written.
 struct Scales {
-    float ks[2][GROUPS], lv[2][GROUPS], iv[2][GROUPS];
+    float ks[4][GROUPS], lv[4][GROUPS], iv[4][GROUPS];
 };
 
 __device__ __forceinline__ void tc_mma_f16(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate, uint32_t issue) {
@@ -83,17 +86,23 @@ __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t* r) {
           "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
-__device__ __forceinline__ void tc_st32_f(uint32_t taddr, const uint32_t* r) {
-    tc_st16(taddr, r);
-    tc_st16(taddr + 16, r + 16);
+__device__ __forceinline__ void tc_st8(uint32_t taddr, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
 }
 __device__ __forceinline__ void tc_wait_st_f() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // Values [key][element], elements contiguous (the operand's N dimension): 128B-swizzled blocks of 64 elements; 8 keys are 1024
-// bytes apart, blocks BLOCK_BYTES.
+// bytes apart, blocks KV_BLOCK.
 __device__ __forceinline__ uint64_t smem_desc_values(uint32_t addr) {
-    return static_cast<uint64_t>((addr >> 4) & 0x3FFFu) | (static_cast<uint64_t>(BLOCK_BYTES >> 4) << 16) | (64ull << 32) | (1ull << 46) |
+    return static_cast<uint64_t>((addr >> 4) & 0x3FFFu) | (static_cast<uint64_t>(KV_BLOCK >> 4) << 16) | (64ull << 32) | (1ull << 46) |
            (2ull << 61);
 }
+
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src, bool real) {   // zeros where there is nothing to copy
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // a * b + c of two pairs at once.
 __device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
@@ -146,19 +155,28 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* sm = smem_raw + (base - smem_u32(smem_raw));
     Scales* scales = reinterpret_cast<Scales*>(sm + S::TAIL);
-    static_assert(sizeof(Scales) <= 256, "tail layout");
-    const uint32_t bar0 = base + S::TAIL + 256;
-    const uint32_t k_full = bar0, s_full = bar0 + 8, p_full = bar0 + 16, v_full = bar0 + 24, o_done = bar0 + 32, q_full = bar0 + 40;
-    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + S::TAIL + 256 + 56);
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::TAIL + 256 + 64);
+    float* row_fac = reinterpret_cast<float*>(sm + S::TAIL + S::OFF_FAC);       // [2][128]: by parity of the item
+    static_assert(sizeof(Scales) <= S::OFF_FAC, "tail layout");
+    const uint32_t bar0 = base + S::TAIL + S::OFF_BAR;
+    // tile n uses the barriers of parity n & 1, in their phase n >> 1
+    auto k_full = [&](uint32_t n) { return bar0 + 8u * (n & 1); };
+    auto s_full = [&](uint32_t n) { return bar0 + 16u + 8u * (n & 1); };       // also: the keys have been read
+    auto p_full = [&](uint32_t n) { return bar0 + 32u + 8u * (n & 1); };
+    auto v_full = [&](uint32_t n) { return bar0 + 48u + 8u * (n & 1); };
+    auto o_done = [&](uint32_t n) { return bar0 + 64u + 8u * (n & 1); };       // also: values and weights have been read
+    const uint32_t q_full = bar0 + 80u;
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + S::TAIL + S::OFF_WORDS);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::TAIL + S::OFF_WORDS + 8);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        mbar_init(k_full, 4);
-        mbar_init(s_full, 5);       // the MMAs, and the four warps that wrote the tile's scales
-        mbar_init(p_full, 4);
-        mbar_init(v_full, 4);
-        mbar_init(o_done, 1);
+        for (uint32_t b = 0; b < 2; ++b) {
+            mbar_init(k_full(b), 4);
+            mbar_init(s_full(b), 5);       // the MMAs, and the four warps that wrote the tile's scales
+            mbar_init(p_full(b), 4);
+            mbar_init(v_full(b), 4);
+            mbar_init(o_done(b), 1);
+        }
         mbar_init(q_full, 4);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -175,190 +193,135 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
     const uint32_t tmem = *tmem_slot;
     const int G = a.group;
     bool failed = false;
-    uint32_t n = 0;                 // tiles so far, over all items: the barriers' phases
+    uint32_t n = 0;                 // tiles so far, over all items
+    auto wait = [&](uint32_t bar, uint32_t tile) { return __all_sync(0xffffffffu, mbar_wait(bar, (tile >> 1) & 1u, abort_flag)) != 0; };
 
     if (warp < 4) {
-        const uint32_t t_s = tmem + (static_cast<uint32_t>(warp * 32) << 16), t_o = t_s + O_COL;
-        const float sign = a.scale_log2 < 0.0f ? -1.0f : 1.0f;     // goes into the queries: no factor of a score is negative
-        // The warp's 32 rows of queries, scaled row by row to fit fp16, to shared memory; returns the factor of this lane's row.
-        auto load_queries = [&](const Item& x) {
-            constexpr int LPR = D / 8, RPI = 32 / LPR;             // lanes per row, rows per step
-            uint4 u[LPR];
-#pragma unroll
-            for (int i = 0; i < LPR; ++i) {
-                const int r = x.r_first + warp * 32 + i * RPI + lane / LPR;
-                u[i] = make_uint4(0, 0, 0, 0);
-                if (r < x.rows)
-                    u[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (static_cast<int64_t>(x.w.row0) + r / G) * a.ldq +
-                                                                static_cast<int64_t>(x.w.h * G + r % G) * D) + lane % LPR);
-            }
-            float mine = 0.0f;
-#pragma unroll
-            for (int i = 0; i < LPR; ++i) {
-                float v[8];
-                unpack8<T>(u[i], v);
-                float amax = 0.0f, back;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(v[e]));
-#pragma unroll
-                for (int o = 1; o < LPR; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-                const float up = fit_exponent(amax, &back) * sign;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= up;
-                const int row = warp * 32 + i * RPI + lane / LPR, c = lane % LPR;
-                *reinterpret_cast<uint4*>(sm + S::Q + (c >> 3) * BLOCK_BYTES + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = pack8<__half>(v);
-                back = __shfl_sync(0xffffffffu, back, (lane % RPI) * LPR);
-                if (lane / RPI == i) mine = back;
-            }
-            fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(q_full);
-            return mine * fabsf(a.scale_log2);
-        };
-        // Maximum of the tile's exponents for this row: first the scores of a run of 16, then one scaling (the factors are >= 0).
-        auto tile_max = [&](auto masked, float fac, int seen, const float* ks, const float* lv) {
-            constexpr bool MASKED = decltype(masked)::value;
-            float top = -INFINITY;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t v[32];
-                tc_ld32(t_s + 32 * c, v);
-                tc_wait_ld();
-                if (MASKED) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (32 * c + i >= seen) v[i] = 0xFF800000u;
-                }
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float x = __uint_as_float(v[16 * h]);
-#pragma unroll
-                    for (int i = 1; i < 15; i += 2) x = fmaxf(fmaxf(x, __uint_as_float(v[16 * h + i])), __uint_as_float(v[16 * h + i + 1]));
-                    x = fmaxf(x, __uint_as_float(v[16 * h + 15]));
-                    // a missing page has lv = -inf (and scores of zero); a masked run stays -inf whatever the factor
-                    const float y = fmaf(x, fac * ks[2 * c + h], lv[2 * c + h]);
-                    top = fmaxf(top, MASKED && x == -INFINITY ? x : y);
-                }
-            }
-            return top;
-        };
-        // The weights of the tile, into the columns that its scores leave; returns the growth of the denominator.
-        auto tile_weights = [&](auto masked, float fac, float ref, int seen, const float* ks, const float* lv, const float* iv) {
-            constexpr bool MASKED = decltype(masked)::value;
-            float grow = 0.0f;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t v[32], p[16];
-                tc_ld32(t_s + 32 * c, v);
-                tc_wait_ld();
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float f = fac * ks[2 * c + h], z = lv[2 * c + h] - ref;
-                    const uint64_t f2 = pair_of(f, f), z2 = pair_of(z, z);
-                    uint64_t sum = 0;
-#pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        float x0, x1;
-                        unpair(fma_pair(pair_of(__uint_as_float(v[16 * h + i]), __uint_as_float(v[16 * h + i + 1])), f2, z2), &x0, &x1);
-                        x0 = fast_exp2(x0);
-                        x1 = fast_exp2(x1);
-                        if (MASKED) {
-                            if (32 * c + 16 * h + i >= seen) x0 = 0.0f;
-                            if (32 * c + 16 * h + i + 1 >= seen) x1 = 0.0f;
-                        }
-                        sum = add_pair(sum, pair_of(x0, x1));
-                        p[8 * h + i / 2] = half2_of(x0, x1);
-                    }
-                    float s0, s1;
-                    unpair(sum, &s0, &s1);
-                    grow = fmaf(s0 + s1, iv[2 * c + h], grow);
-                }
-                tc_st16(t_s + 16 * c, p);                // columns already read
-            }
-            return grow;
-        };
-
-        unsigned id = blockIdx.x;
-        Item x = item_of(a, id);
-        float fac = x.steps > 0 ? load_queries(x) : 0.0f;
-        for (;;) {
+        // Registers: 96 a thread at launch, 288 threads. Four softmax warps at 128, four at 64 and one at 96 take as many.
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
+        const uint32_t t_lane = tmem + (static_cast<uint32_t>(warp * 32) << 16), t_o = t_lane + O_COL;
+        uint32_t full_items = 0;
+        for (unsigned id = blockIdx.x; id < items; id += gridDim.x) {
+            const Item x = item_of(a, id);
             const int r = x.r_first + static_cast<int>(threadIdx.x);
             const bool real = r < x.rows;
-            const int qi = real ? r / G : 0, head = x.w.h * G + (real ? r % G : 0);
+            const int qi = real ? r / G : 0, head = x.w.h * G + (real ? r - qi * G : 0);
             const int lim = real ? min(visible(a, x.w, qi), x.end) : 0;
-            float m = -INFINITY, l = 0.0f;
+            const bool idle = x.r_first + warp * 32 >= x.rows;          // no rows: whatever these lanes hold goes nowhere
+            float m = -INFINITY, l = 0.0f, fac = 0.0f;
             for (int j = 0; j < x.steps; ++j, ++n) {
-                if (!__all_sync(0xffffffffu, mbar_wait(s_full, n & 1, abort_flag))) { failed = true; break; }
-                tc_fence_after();
-                const float* ks = scales->ks[n & 1];
-                const float* lv = scales->lv[n & 1];
-                const float* iv = scales->iv[n & 1];
-                const int seen = lim - (x.key0 + j * KEYS);    // this row sees the first `seen` keys of the tile
-                const bool whole = __all_sync(0xffffffffu, seen >= KEYS);
-                const float top = whole ? tile_max(std::false_type(), fac, seen, ks, lv) : tile_max(std::true_type(), fac, seen, ks, lv);
-                const bool raise = m == -INFINITY ? top != -INFINITY : top > m + RAISE;
-                if (__any_sync(0xffffffffu, raise)) {
-                    const float f = raise ? fast_exp2(m - top) : 1.0f;      // m = -inf: 0
-                    if (raise) m = top;
-                    l *= f;
-                    if (j > 0) {
-#pragma unroll 1
-                        for (int c = 0; c < D / 32; ++c) {
-                            uint32_t v[32];
-                            tc_ld32(t_o + 32 * c, v);
-                            tc_wait_ld();
+                if (!wait(s_full(n), n)) { failed = true; break; }
+                if (!idle) {
+                    tc_fence_after();
+                    if (j == 0) fac = row_fac[(full_items & 1) * 128 + threadIdx.x];
+                    const float* ks = scales->ks[n & 3];
+                    const float* lv = scales->lv[n & 3];
+                    const float* iv = scales->iv[n & 3];
+                    const int seen = lim - (x.key0 + j * KEYS);         // this row sees the first `seen` keys of the tile
+                    const uint32_t t_s = t_lane + KEYS * (n & 1);
+                    uint32_t v[KEYS];
+                    tc_ld32(t_s, v);
+                    tc_ld32(t_s + 32, v + 32);
+                    tc_wait_ld();
+                    if (!__all_sync(0xffffffffu, seen >= KEYS)) {
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
-                            tc_st32_f(t_o + 32 * c, v);
+                        for (int i = 0; i < KEYS; ++i)
+                            if (i >= seen) v[i] = 0xFF800000u;
+                    }
+                    // of a run's scores; never 0, so that what is masked stays at -inf
+                    auto factor = [&](int run) { return fmaxf(fac * ks[run], 1e-37f); };
+                    // the maximum of the scores of a run of 16, then one scaling
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int run = 0; run < GROUPS; ++run) {
+                        float y = __uint_as_float(v[16 * run]);
+#pragma unroll
+                        for (int i = 1; i < 15; i += 2)
+                            y = fmaxf(fmaxf(y, __uint_as_float(v[16 * run + i])), __uint_as_float(v[16 * run + i + 1]));
+                        y = fmaxf(y, __uint_as_float(v[16 * run + 15]));
+                        // a missing page has lv = -inf, and scores of zero
+                        top = fmaxf(top, fmaf(y, factor(run), lv[run]));
+                    }
+                    const bool raise = m == -INFINITY ? top != -INFINITY : top > m + RAISE;
+                    if (__any_sync(0xffffffffu, raise)) {
+                        const float f = raise ? fast_exp2(m - top) : 1.0f;      // m = -inf: 0
+                        if (raise) m = top;
+                        l *= f;
+                        if (j > 0) {
+                            if (!wait(o_done(n - 1), n - 1)) { failed = true; break; }
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int c = 0; c < D / 16; ++c) {
+                                uint32_t u[16];
+                                tc_ld16(t_o + 16 * c, u);
+                                tc_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(__uint_as_float(u[i]) * f);
+                                tc_st16(t_o + 16 * c, u);
+                            }
                         }
                     }
+                    const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+                    for (int run = 0; run < GROUPS; ++run) {
+                        const float f = factor(run), z = lv[run] - ref;
+                        const uint64_t f2 = pair_of(f, f), z2 = pair_of(z, z);
+                        uint32_t p[8];
+                        uint64_t sum = 0;
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) {
+                            float w0, w1;
+                            unpair(fma_pair(pair_of(__uint_as_float(v[16 * run + i]), __uint_as_float(v[16 * run + i + 1])), f2, z2), &w0, &w1);
+                            w0 = fast_exp2(w0);
+                            w1 = fast_exp2(w1);
+                            sum = add_pair(sum, pair_of(w0, w1));
+                            p[i / 2] = half2_of(w0, w1);
+                        }
+                        float s0, s1;
+                        unpair(sum, &s0, &s1);
+                        l = fmaf(s0 + s1, iv[run], l);
+                        tc_st8(t_s + 8 * run, p);                       // the scores are in registers
+                    }
+                    tc_wait_st_f();
+                    tc_fence_before();
                 }
-                const float ref = m == -INFINITY ? 0.0f : m;
-                l += whole ? tile_weights(std::false_type(), fac, ref, seen, ks, lv, iv) : tile_weights(std::true_type(), fac, ref, seen, ks, lv, iv);
-                tc_wait_st_f();
-                tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full);
+                if (lane == 0) mbar_arrive(p_full(n));
             }
             if (failed) break;
-            // the next item's queries while the last output product runs (the last scores have been taken: s_full)
-            const Item y = x;
-            id += gridDim.x;
-            const bool more = id < items;
-            if (more) {
-                x = item_of(a, id);
-                if (x.steps > 0) fac = load_queries(x);
-            }
-            if (y.steps > 0) {
-                if (!__all_sync(0xffffffffu, mbar_wait(o_done, (n - 1) & 1, abort_flag))) { failed = true; break; }
+            if (x.steps > 0) {
+                ++full_items;
+                if (!wait(o_done(n - 1), n - 1)) { failed = true; break; }
                 tc_fence_after();
             }
+            if (idle) continue;
             const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-            const int64_t row = static_cast<int64_t>(y.w.row0) + qi;
-            const int64_t at = a.splits > 1 && real ? part_index(a, y.w.b, head, qi, y.w.split) : 0;
-#pragma unroll 1
-            for (int c = 0; c < (y.r_first < y.rows ? D / 32 : 0); ++c) {
-                uint32_t v[32];
-                if (y.steps > 0) {
-                    tc_ld32(t_o + 32 * c, v);
+            const int64_t row = static_cast<int64_t>(x.w.row0) + qi;
+            const int64_t at = a.splits > 1 && real ? part_index(a, x.w.b, head, qi, x.w.split) : 0;
+            T* out = static_cast<T*>(a.out) + row * a.ldo + static_cast<int64_t>(head) * D;
+            float* po = a.part_o + at * D;
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) {
+                uint32_t v[64];
+                if (x.steps > 0) {
+                    tc_ld32(t_o + 64 * c, v);
+                    tc_ld32(t_o + 64 * c + 32, v + 32);
                     tc_wait_ld();
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = 0;
+                    for (int i = 0; i < 64; ++i) v[i] = 0;
                 }
                 if (!real) continue;
                 if (a.splits > 1) {
-                    uint4* po = reinterpret_cast<uint4*>(a.part_o + at * D + 32 * c);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) po[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                    for (int i = 0; i < 16; ++i) reinterpret_cast<uint4*>(po + 64 * c)[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
                 } else {
-                    uint4* out = reinterpret_cast<uint4*>(static_cast<T*>(a.out) + row * a.ldo + static_cast<int64_t>(head) * D + 32 * c);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < 8; ++i) {
                         float z[8];
 #pragma unroll
                         for (int e = 0; e < 8; ++e) z[e] = __uint_as_float(v[8 * i + e]) * inv;
-                        out[i] = pack8<T>(z);
+                        reinterpret_cast<uint4*>(out + 64 * c)[i] = pack8<T>(z);
                     }
                 }
             }
@@ -366,44 +329,42 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
                 if (a.splits > 1) a.part_ml[at] = make_float2(m, l);
                 else if (a.lse) a.lse[row * a.heads + head] = l > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
             }
-            if (!more) break;
+            tc_fence_before();
         }
     } else if (warp < 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         const int tid = threadIdx.x - 128;
         const int shift = a.c.page_shift, mask = (1 << shift) - 1;
         // A thread's pieces of a tile: 16 codes of keys tid / 4 + 32 i, elements 64 b + 16 (tid % 4) on. Eight lanes then
         // write eight different 16-byte units, and a thread's place in the swizzle never changes.
-        constexpr int BLOCKS = S::BLOCKS;
-        uint4 held[4][BLOCKS];      // keys and values in turn: either is fetched while the other's place is still in use
+        constexpr int BLOCKS = S::BLOCKS, ROWS = KEYS / 32;
+        uint4 kc[ROWS][BLOCKS], vc[ROWS][BLOCKS];
         const int32_t* table = nullptr;
         int h = 0, end = 0;
         auto page_at = [&](int key) {
             const int j = key >> shift;
             return key < end && j < a.ldt ? checked_page(a.c, __ldg(table + j)) : -1;
         };
-        auto fetch = [&](const Half& half, int k0) {
-            int page[4];
+        auto fetch = [&](const Half& half, int k0, uint4 (&to)[ROWS][BLOCKS]) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) page[i] = page_at(k0 + (tid >> 2) + 32 * i);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint8_t* p = half.codes + (page_codes(a.c, page[i], h) + ((k0 + (tid >> 2) + 32 * i) & mask)) * D + (tid & 3) * 16;
+            for (int i = 0; i < ROWS; ++i) {
+                const int key = k0 + (tid >> 2) + 32 * i, page = page_at(key);
+                const uint8_t* p = half.codes + (page_codes(a.c, page, h) + (key & mask)) * D + (tid & 3) * 16;
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b) {
-                    held[i][b] = make_uint4(0, 0, 0, 0);       // behind the end: zero codes, whatever lies there
-                    if (page[i] >= 0) held[i][b] = __ldg(reinterpret_cast<const uint4*>(p + 64 * b));
+                    to[i][b] = make_uint4(0, 0, 0, 0);         // behind the end: zero codes, whatever lies there
+                    if (page >= 0) to[i][b] = __ldg(reinterpret_cast<const uint4*>(p + 64 * b));
                 }
             }
         };
         const int row = tid >> 2, unit = (tid & 3) * 2;
-        uint8_t* const to0 = sm + row * 128 + ((unit ^ (row & 7)) << 4);
-        uint8_t* const to1 = sm + row * 128 + (((unit + 1) ^ (row & 7)) << 4);
-        auto put = [&](int region) {
+        const uint32_t to0 = row * 128 + ((unit ^ (row & 7)) << 4), to1 = row * 128 + (((unit + 1) ^ (row & 7)) << 4);
+        auto put = [&](int region, const uint4 (&from)[ROWS][BLOCKS]) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < ROWS; ++i)
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b) {
-                    const uint32_t in[4] = {held[i][b].x, held[i][b].y, held[i][b].z, held[i][b].w};
+                    const uint32_t in[4] = {from[i][b].x, from[i][b].y, from[i][b].z, from[i][b].w};
                     uint32_t out[8];
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
@@ -415,16 +376,83 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
                             out[2 * q + 1] = e4m3x2_to_half2(in[q] >> 16);
                         }
                     }
-                    *reinterpret_cast<uint4*>(to0 + region + b * BLOCK_BYTES + i * 32 * 128) = make_uint4(out[0], out[1], out[2], out[3]);
-                    *reinterpret_cast<uint4*>(to1 + region + b * BLOCK_BYTES + i * 32 * 128) = make_uint4(out[4], out[5], out[6], out[7]);
+                    uint8_t* to = sm + region + b * KV_BLOCK + i * 32 * 128;
+                    *reinterpret_cast<uint4*>(to + to0) = make_uint4(out[0], out[1], out[2], out[3]);
+                    *reinterpret_cast<uint4*>(to + to1) = make_uint4(out[4], out[5], out[6], out[7]);
                 }
         };
+        // Queries: a warp brings 32 rows, LPR lanes to a row.
+        constexpr int LPR = D / 8, RPI = 32 / LPR;
+        const int qc = lane % LPR, q_row0 = (warp - 4) * 32 + lane / LPR;
+        auto q_at = [&](int i) {
+            const int rr = q_row0 + i * RPI;
+            return static_cast<uint32_t>(S::Q + (qc >> 3) * Q_BLOCK + rr * 128 + (((qc & 7) ^ (rr & 7)) << 4));
+        };
+        uint32_t full_items = 0;
         for (unsigned id = blockIdx.x; id < items && !failed; id += gridDim.x) {
             const Item x = item_of(a, id);
+            if (x.steps == 0) continue;
+            // the last scores of the item before have been taken
+            if (n > 0 && !wait(s_full(n - 1), n - 1)) { failed = true; break; }
+            {
+                const int first = x.r_first + q_row0;
+                int qi = first / G, g = first - qi * G;
+                const T* q = static_cast<const T*>(a.q) + static_cast<int64_t>(x.w.row0) * a.ldq + static_cast<int64_t>(x.w.h) * G * D + 8 * qc;
+#pragma unroll 4
+                for (int i = 0; i < LPR; ++i) {
+                    const bool there = first + i * RPI < x.rows;
+                    cp_async_16(base + q_at(i), there ? q + qi * a.ldq + g * D : q, there);
+                    g += RPI;
+                    if (G == 1) {
+                        qi += RPI;
+                        g = 0;
+                    } else {
+                        while (g >= G) {
+                            g -= G;
+                            ++qi;
+                        }
+                    }
+                }
+            }
             table = a.table + x.w.b * a.ldt;
             h = x.w.h;
             end = x.end;
-            if (x.steps > 0) fetch(a.c.k, x.key0);
+            fetch(a.c.k, x.key0, kc);
+            fetch(a.c.v, x.key0, vc);
+            cp_async_wait();
+            // bf16 rows are scaled one by one to fit fp16; a negative scale goes into the queries, so that no factor is negative
+            float* fac = row_fac + (full_items & 1) * 128;
+            ++full_items;
+            if (std::is_same<T, __half>::value) {
+                if (a.scale_log2 < 0.0f)
+                    for (int i = 0; i < LPR; ++i) {
+                        uint4* u = reinterpret_cast<uint4*>(sm + q_at(i));
+                        *u = make_uint4(u->x ^ 0x80008000u, u->y ^ 0x80008000u, u->z ^ 0x80008000u, u->w ^ 0x80008000u);
+                    }
+                fac[(warp - 4) * 32 + lane] = fabsf(a.scale_log2);
+            } else {
+#pragma unroll 4
+                for (int i = 0; i < LPR; ++i) {
+                    uint4* u = reinterpret_cast<uint4*>(sm + q_at(i));
+                    float v[8];
+                    unpack8<T>(*u, v);
+                    float amax = 0.0f, back;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(v[e]));
+#pragma unroll
+                    for (int o = 1; o < LPR; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+                    float up = fit_exponent(amax, &back);
+                    if (a.scale_log2 < 0.0f) up = -up;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] *= up;
+                    *u = pack8<__half>(v);
+                    if (qc == 0) fac[q_row0 + i * RPI] = back * fabsf(a.scale_log2);
+                }
+            }
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_full);
+
             for (int j = 0; j < x.steps; ++j, ++n) {
                 const int k0 = x.key0 + j * KEYS;
                 float ks = 0.0f, vs = 0.0f;
@@ -437,29 +465,29 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
                         vs = __ldg(a.c.v.scales + s);
                     }
                 }
-                // keys: the scores of the tile before have been taken
-                if (n > 0 && !__all_sync(0xffffffffu, mbar_wait(s_full, (n - 1) & 1, abort_flag))) { failed = true; break; }
-                put(S::K);
+                // keys: the scores of the tile that was here have been taken
+                if (n > 1 && !wait(s_full(n), n - 2)) { failed = true; break; }
+                put(S::K + (n & 1) * S::TILE, kc);
                 if (tid < GROUPS) {
                     const float lv = __log2f(vs > 0.0f ? vs : ZERO_PAGE_SCALE);
-                    scales->ks[n & 1][tid] = ks;
-                    scales->lv[n & 1][tid] = page >= 0 ? lv : -INFINITY;
-                    scales->iv[n & 1][tid] = fast_exp2(-lv);
+                    scales->ks[n & 3][tid] = ks;
+                    scales->lv[n & 3][tid] = page >= 0 ? lv : -INFINITY;
+                    scales->iv[n & 3][tid] = fast_exp2(-lv);
                 }
                 fence_proxy_async();
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_arrive(s_full);
-                    mbar_arrive(k_full);
+                    mbar_arrive(s_full(n));
+                    mbar_arrive(k_full(n));
                 }
-                fetch(a.c.v, k0);
-                // values: the output of the tile before has taken them
-                if (n > 0 && !__all_sync(0xffffffffu, mbar_wait(o_done, (n - 1) & 1, abort_flag))) { failed = true; break; }
-                put(S::V);
+                if (j + 1 < x.steps) fetch(a.c.k, k0 + KEYS, kc);
+                // values: the output of the tile that was here has taken them
+                if (n > 1 && !wait(o_done(n), n - 2)) { failed = true; break; }
+                put(S::V + (n & 1) * S::TILE, vc);
                 fence_proxy_async();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(v_full);
-                if (j + 1 < x.steps) fetch(a.c.k, k0 + KEYS);
+                if (lane == 0) mbar_arrive(v_full(n));
+                if (j + 1 < x.steps) fetch(a.c.v, k0 + KEYS, vc);
             }
         }
     } else {
@@ -467,28 +495,32 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
         const uint32_t idesc_s = (1u << 4) | (static_cast<uint32_t>(KEYS >> 3) << 17) | (128u >> 4 << 24);
         const uint32_t idesc_o = (1u << 4) | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17) | (128u >> 4 << 24);
         uint32_t full_items = 0;
+        auto scores = [&](uint32_t t) {
+            // two tiles earlier these columns held weights: they have been read
+            if (!wait(k_full(t), t) || (t > 1 && !wait(o_done(t), t - 2))) return false;
+            tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+                tc_mma_f16(tmem + KEYS * (t & 1), smem_desc_sw128(base + S::Q + (k >> 2) * Q_BLOCK) + 2u * (k & 3),
+                           smem_desc_sw128(base + S::K + (t & 1) * S::TILE + (k >> 2) * KV_BLOCK) + 2u * (k & 3), idesc_s, k != 0 ? 1u : 0u, issue);
+            tc_commit_if(s_full(t), issue);
+            return true;
+        };
         for (unsigned id = blockIdx.x; id < items && !failed; id += gridDim.x) {
             const Item x = item_of(a, id);
             if (x.steps == 0) continue;
             if (!__all_sync(0xffffffffu, mbar_wait(q_full, full_items & 1, abort_flag))) { failed = true; break; }
             ++full_items;
+            if (!scores(n)) { failed = true; break; }
             for (int j = 0; j < x.steps; ++j, ++n) {
-                bool ok = mbar_wait(k_full, n & 1, abort_flag);
-                if (ok && n > 0) ok = mbar_wait(o_done, (n - 1) & 1, abort_flag);     // the weights in the score columns have been read
-                if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
-                tc_fence_after();
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k)
-                    tc_mma_f16(tmem, smem_desc_sw128(base + S::Q + (k >> 2) * BLOCK_BYTES) + 2u * (k & 3),
-                               smem_desc_sw128(base + S::K + (k >> 2) * BLOCK_BYTES) + 2u * (k & 3), idesc_s, k != 0 ? 1u : 0u, issue);
-                tc_commit_if(s_full, issue);
-                ok = mbar_wait(v_full, n & 1, abort_flag) && mbar_wait(p_full, n & 1, abort_flag);
-                if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
+                if (j + 1 < x.steps && !scores(n + 1)) { failed = true; break; }
+                if (!wait(v_full(n), n) || !wait(p_full(n), n)) { failed = true; break; }
                 tc_fence_after();
 #pragma unroll
                 for (int k = 0; k < KEYS / 16; ++k)
-                    tc_mma_f16_ts(tmem + O_COL, tmem + 8u * k, smem_desc_values(base + S::V) + 128u * k, idesc_o, (j | k) != 0 ? 1u : 0u, issue);
-                tc_commit_if(o_done, issue);
+                    tc_mma_f16_ts(tmem + O_COL, tmem + KEYS * (n & 1) + 8u * k, smem_desc_values(base + S::V + (n & 1) * S::TILE) + 128u * k, idesc_o,
+                                  (j | k) != 0 ? 1u : 0u, issue);
+                tc_commit_if(o_done(n), issue);
             }
         }
     }
