@@ -40,12 +40,17 @@ struct Where {
     int b, h, split, tile;
     int row0, n_q, len;    // first row of the sequence, its query rows, its keys
 };
-__device__ __forceinline__ Where locate(const AttnArgs& a, unsigned id) {
+__device__ __forceinline__ Where locate(const AttnArgs& a, unsigned id, int tiles) {
     Where w;
-    w.tile = static_cast<int>(id % a.tiles);
-    id /= a.tiles;
-    w.split = static_cast<int>(id % a.splits);
-    id /= a.splits;
+    w.tile = w.split = 0;
+    if (tiles > 1) {
+        w.tile = static_cast<int>(id % tiles);
+        id /= tiles;
+    }
+    if (a.splits > 1) {
+        w.split = static_cast<int>(id % a.splits);
+        id /= a.splits;
+    }
     w.h = static_cast<int>(id % a.c.kv_heads);
     w.b = static_cast<int>(id / a.c.kv_heads);
     w.row0 = a.cu[w.b];

@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(WARPS * 32) kv_decode_kernel(AttnArgs a) {
 
     pdl_launch_dependents();
     pdl_wait();
-    const Where w = locate(a, blockIdx.x);
+    const Where w = locate(a, blockIdx.x, 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int G = a.group;
     const int nq = w.n_q < a.max_q ? w.n_q : a.max_q;

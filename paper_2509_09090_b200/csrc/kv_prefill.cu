@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(256, 1) kv_prefill_kernel(AttnArgs a) {
 
     pdl_launch_dependents();
     pdl_wait();
-    Where w = locate(a, blockIdx.x);
+    Where w = locate(a, blockIdx.x, a.tiles);
     w.tile = a.tiles - 1 - w.tile;                       // the rows that see the most first
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int G = a.group;

@@ -133,7 +133,7 @@ __device__ __forceinline__ Item item_of(const AttnArgs& a, unsigned id) {
     // tiles outermost, the rows that see the most first
     const unsigned per_tile = static_cast<unsigned>(a.batch) * a.c.kv_heads * a.splits;
     const unsigned tile = id / per_tile;
-    x.w = locate(a, (id - tile * per_tile) * a.tiles);
+    x.w = locate(a, id - tile * per_tile, 1);
     x.w.tile = a.tiles - 1 - static_cast<int>(tile);
     x.rows = (x.w.n_q < a.max_q ? x.w.n_q : a.max_q) * a.group;
     x.r_first = x.w.tile * PREFILL_ROWS;
@@ -201,8 +201,9 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
         asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
         const uint32_t t_lane = tmem + (static_cast<uint32_t>(warp * 32) << 16), t_o = t_lane + O_COL;
         uint32_t full_items = 0;
+        Item next = item_of(a, blockIdx.x);
         for (unsigned id = blockIdx.x; id < items; id += gridDim.x) {
-            const Item x = item_of(a, id);
+            const Item x = next;
             const int r = x.r_first + static_cast<int>(threadIdx.x);
             const bool real = r < x.rows;
             const int qi = real ? r / G : 0, head = x.w.h * G + (real ? r - qi * G : 0);
@@ -289,6 +290,7 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
                 if (lane == 0) mbar_arrive(p_full(n));
             }
             if (failed) break;
+            if (id + gridDim.x < items) next = item_of(a, id + gridDim.x);      // while the last output product runs
             if (x.steps > 0) {
                 ++full_items;
                 if (!wait(o_done(n - 1), n - 1)) { failed = true; break; }
@@ -339,21 +341,65 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
         // write eight different 16-byte units, and a thread's place in the swizzle never changes.
         constexpr int BLOCKS = S::BLOCKS, ROWS = KEYS / 32;
         uint4 kc[ROWS][BLOCKS], vc[ROWS][BLOCKS];
-        const int32_t* table = nullptr;
-        int h = 0, end = 0;
-        auto page_at = [&](int key) {
-            const int j = key >> shift;
-            return key < end && j < a.ldt ? checked_page(a.c, __ldg(table + j)) : -1;
+        // The tiles of this CTA's items, one after another.
+        struct Tile {
+            const int32_t* table;
+            int h, k0, end;            // keys k0 .. of a sequence of `end` keys that count; end = 0: no more tiles
+            int row0, r_first, rows;   // rows > 0: the first tile of an item, whose queries are wanted
         };
-        auto fetch = [&](const Half& half, int k0, uint4 (&to)[ROWS][BLOCKS]) {
+        unsigned id = blockIdx.x;
+        Item gen = item_of(a, id);
+        int gen_j = 0;
+        auto next_tile = [&]() {
+            Tile t = {};
+            while (gen_j >= gen.steps) {
+                id += gridDim.x;
+                if (id >= items || id < gridDim.x) return t;
+                gen = item_of(a, id);
+                gen_j = 0;
+            }
+            t.table = a.table + gen.w.b * a.ldt;
+            t.h = gen.w.h;
+            t.k0 = gen.key0 + gen_j * KEYS;
+            t.end = gen.end;
+            t.row0 = gen.w.row0;
+            t.r_first = gen.r_first;
+            t.rows = gen_j == 0 ? gen.rows : 0;
+            ++gen_j;
+            return t;
+        };
+        auto page_at = [&](const Tile& t, int key) {
+            const int j = key >> shift;
+            return key < t.end && j < a.ldt ? checked_page(a.c, __ldg(t.table + j)) : -1;
+        };
+        auto pages_of_tile = [&](const Tile& t, int (&page)[ROWS]) {
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) page[i] = page_at(t, t.k0 + (tid >> 2) + 32 * i);
+        };
+        auto fetch = [&](const Half& half, const Tile& t, const int (&page)[ROWS], uint4 (&to)[ROWS][BLOCKS]) {
 #pragma unroll
             for (int i = 0; i < ROWS; ++i) {
-                const int key = k0 + (tid >> 2) + 32 * i, page = page_at(key);
-                const uint8_t* p = half.codes + (page_codes(a.c, page, h) + (key & mask)) * D + (tid & 3) * 16;
+                const int key = t.k0 + (tid >> 2) + 32 * i;
+                const uint8_t* p = half.codes + (page_codes(a.c, page[i], t.h) + (key & mask)) * D + (tid & 3) * 16;
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b) {
                     to[i][b] = make_uint4(0, 0, 0, 0);         // behind the end: zero codes, whatever lies there
-                    if (page >= 0) to[i][b] = __ldg(reinterpret_cast<const uint4*>(p + 64 * b));
+                    if (page[i] >= 0) to[i][b] = __ldg(reinterpret_cast<const uint4*>(p + 64 * b));
+                }
+            }
+        };
+        // Scales: thread 8 g of the first 64 holds a key of run g (tid / 4 = 16 (g % 2), i = g / 2) and with it the run's page.
+        float ks[ROWS], vs[ROWS];
+        const bool scaler = (tid & 63) == 0;
+        auto fetch_scales = [&](const Tile& t, const int (&page)[ROWS]) {
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+                ks[i] = 0.0f;
+                vs[i] = -1.0f;                                 // no page
+                if (scaler && page[i] >= 0) {
+                    const int64_t s = static_cast<int64_t>(page[i]) * a.c.kv_heads + t.h;
+                    ks[i] = __ldg(a.c.k.scales + s);
+                    vs[i] = __ldg(a.c.v.scales + s);
                 }
             }
         };
@@ -388,41 +434,33 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
             const int rr = q_row0 + i * RPI;
             return static_cast<uint32_t>(S::Q + (qc >> 3) * Q_BLOCK + rr * 128 + (((qc & 7) ^ (rr & 7)) << 4));
         };
-        uint32_t full_items = 0;
-        for (unsigned id = blockIdx.x; id < items && !failed; id += gridDim.x) {
-            const Item x = item_of(a, id);
-            if (x.steps == 0) continue;
-            // the last scores of the item before have been taken
-            if (n > 0 && !wait(s_full(n - 1), n - 1)) { failed = true; break; }
-            {
-                const int first = x.r_first + q_row0;
+        auto begin_queries = [&](const Tile& t) {
+            const int first = t.r_first + q_row0;
+            const T* q = static_cast<const T*>(a.q) + static_cast<int64_t>(t.row0) * a.ldq + static_cast<int64_t>(t.h) * G * D + 8 * qc;
+            if (G == 1) {
+                const T* p = q + first * a.ldq;
+#pragma unroll
+                for (int i = 0; i < LPR; ++i, p += RPI * a.ldq) {
+                    const bool there = first + i * RPI < t.rows;
+                    cp_async_16(base + q_at(i), there ? p : q, there);
+                }
+            } else {
                 int qi = first / G, g = first - qi * G;
-                const T* q = static_cast<const T*>(a.q) + static_cast<int64_t>(x.w.row0) * a.ldq + static_cast<int64_t>(x.w.h) * G * D + 8 * qc;
 #pragma unroll 4
                 for (int i = 0; i < LPR; ++i) {
-                    const bool there = first + i * RPI < x.rows;
+                    const bool there = first + i * RPI < t.rows;
                     cp_async_16(base + q_at(i), there ? q + qi * a.ldq + g * D : q, there);
                     g += RPI;
-                    if (G == 1) {
-                        qi += RPI;
-                        g = 0;
-                    } else {
-                        while (g >= G) {
-                            g -= G;
-                            ++qi;
-                        }
+                    while (g >= G) {
+                        g -= G;
+                        ++qi;
                     }
                 }
             }
-            table = a.table + x.w.b * a.ldt;
-            h = x.w.h;
-            end = x.end;
-            fetch(a.c.k, x.key0, kc);
-            fetch(a.c.v, x.key0, vc);
+        };
+        auto finish_queries = [&](float* fac) {
             cp_async_wait();
             // bf16 rows are scaled one by one to fit fp16; a negative scale goes into the queries, so that no factor is negative
-            float* fac = row_fac + (full_items & 1) * 128;
-            ++full_items;
             if (std::is_same<T, __half>::value) {
                 if (a.scale_log2 < 0.0f)
                     for (int i = 0; i < LPR; ++i) {
@@ -449,46 +487,61 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
                     if (qc == 0) fac[q_row0 + i * RPI] = back * fabsf(a.scale_log2);
                 }
             }
+        };
+
+        // The tile being written, its codes in registers; and the one after, its pages known.
+        int pages[ROWS];
+        Tile now = next_tile();
+        pages_of_tile(now, pages);
+        fetch(a.c.k, now, pages, kc);
+        fetch(a.c.v, now, pages, vc);
+        fetch_scales(now, pages);
+        Tile then = next_tile();
+        pages_of_tile(then, pages);
+        uint32_t full_items = 0;
+        for (; now.end > 0; ++n) {
+            const bool opens = now.rows > 0;
+            if (opens) {
+                // the last scores of the item before have been taken
+                if (n > 0 && !wait(s_full(n - 1), n - 1)) { failed = true; break; }
+                begin_queries(now);
+            }
+            // keys: the scores of the tile that was here have been taken
+            if (n > 1 && !wait(s_full(n), n - 2)) { failed = true; break; }
+            put(S::K + (n & 1) * S::TILE, kc);
+            if (scaler) {
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) {
+                    const int run = 2 * i + (tid >> 6);
+                    const float lv = __log2f(vs[i] > 0.0f ? vs[i] : ZERO_PAGE_SCALE);
+                    scales->ks[n & 3][run] = ks[i];
+                    scales->lv[n & 3][run] = vs[i] < 0.0f ? -INFINITY : lv;
+                    scales->iv[n & 3][run] = fast_exp2(-lv);
+                }
+            }
+            if (opens) {
+                finish_queries(row_fac + (full_items & 1) * 128);
+                ++full_items;
+            }
             fence_proxy_async();
             __syncwarp();
-            if (lane == 0) mbar_arrive(q_full);
-
-            for (int j = 0; j < x.steps; ++j, ++n) {
-                const int k0 = x.key0 + j * KEYS;
-                float ks = 0.0f, vs = 0.0f;
-                int page = -1;
-                if (tid < GROUPS) {
-                    page = page_at(k0 + 16 * tid);
-                    if (page >= 0) {
-                        const int64_t s = static_cast<int64_t>(page) * a.c.kv_heads + h;
-                        ks = __ldg(a.c.k.scales + s);
-                        vs = __ldg(a.c.v.scales + s);
-                    }
-                }
-                // keys: the scores of the tile that was here have been taken
-                if (n > 1 && !wait(s_full(n), n - 2)) { failed = true; break; }
-                put(S::K + (n & 1) * S::TILE, kc);
-                if (tid < GROUPS) {
-                    const float lv = __log2f(vs > 0.0f ? vs : ZERO_PAGE_SCALE);
-                    scales->ks[n & 3][tid] = ks;
-                    scales->lv[n & 3][tid] = page >= 0 ? lv : -INFINITY;
-                    scales->iv[n & 3][tid] = fast_exp2(-lv);
-                }
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(s_full(n));
-                    mbar_arrive(k_full(n));
-                }
-                if (j + 1 < x.steps) fetch(a.c.k, k0 + KEYS, kc);
-                // values: the output of the tile that was here has taken them
-                if (n > 1 && !wait(o_done(n), n - 2)) { failed = true; break; }
-                put(S::V + (n & 1) * S::TILE, vc);
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(v_full(n));
-                if (j + 1 < x.steps) fetch(a.c.v, k0 + KEYS, vc);
+            if (lane == 0) {
+                mbar_arrive(s_full(n));
+                mbar_arrive(k_full(n));
+                if (opens) mbar_arrive(q_full);
             }
+            fetch(a.c.k, then, pages, kc);
+            fetch_scales(then, pages);
+            // values: the output of the tile that was here has taken them
+            if (n > 1 && !wait(o_done(n), n - 2)) { failed = true; break; }
+            put(S::V + (n & 1) * S::TILE, vc);
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(v_full(n));
+            fetch(a.c.v, then, pages, vc);
+            now = then;
+            then = next_tile();
+            pages_of_tile(then, pages);
         }
     } else {
         const uint32_t issue = elect_one();
