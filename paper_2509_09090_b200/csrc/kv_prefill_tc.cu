@@ -368,13 +368,14 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
             ++gen_j;
             return t;
         };
-        auto page_at = [&](const Tile& t, int key) {
-            const int j = key >> shift;
-            return key < t.end && j < a.ldt ? checked_page(a.c, __ldg(t.table + j)) : -1;
-        };
+        // Table entries as they are; checked when they are used, so that nothing waits for them here.
         auto pages_of_tile = [&](const Tile& t, int (&page)[ROWS]) {
 #pragma unroll
-            for (int i = 0; i < ROWS; ++i) page[i] = page_at(t, t.k0 + (tid >> 2) + 32 * i);
+            for (int i = 0; i < ROWS; ++i) {
+                const int key = t.k0 + (tid >> 2) + 32 * i, j = key >> shift;
+                page[i] = -1;
+                if (key < t.end && j < a.ldt) page[i] = __ldg(t.table + j);
+            }
         };
         auto fetch = [&](const Half& half, const Tile& t, const int (&page)[ROWS], uint4 (&to)[ROWS][BLOCKS]) {
 #pragma unroll
@@ -384,7 +385,7 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b) {
                     to[i][b] = make_uint4(0, 0, 0, 0);         // behind the end: zero codes, whatever lies there
-                    if (page[i] >= 0) to[i][b] = __ldg(reinterpret_cast<const uint4*>(p + 64 * b));
+                    if (checked_page(a.c, page[i]) >= 0) to[i][b] = __ldg(reinterpret_cast<const uint4*>(p + 64 * b));
                 }
             }
         };
@@ -396,7 +397,7 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
             for (int i = 0; i < ROWS; ++i) {
                 ks[i] = 0.0f;
                 vs[i] = -1.0f;                                 // no page
-                if (scaler && page[i] >= 0) {
+                if (scaler && checked_page(a.c, page[i]) >= 0) {
                     const int64_t s = static_cast<int64_t>(page[i]) * a.c.kv_heads + t.h;
                     ks[i] = __ldg(a.c.k.scales + s);
                     vs[i] = __ldg(a.c.v.scales + s);
