@@ -4,9 +4,10 @@
 // sequence and key/value head; its keys are walked 64 at a time. Per tile: S = Q K^T into tensor memory, the softmax's weights
 // back into tensor memory as the A operand, O += W V.
 //   warps 0-3  softmax: thread = row. Rescale the output where a maximum has grown, and store it at the end.
-//   warps 4-7  codes from global memory (one tile ahead, in registers) to fp16 in shared memory, 128B-swizzled; the next
-//              item's queries
-//   warp  8    issues the MMAs: the scores of a tile before the output of the tile in front of it, so that the tensor core
+//   warps 4-11 codes from global memory (one tile ahead, in registers) to fp16 in shared memory, 128B-swizzled; the next
+//              item's queries. (Four warps for it took 3000 cycles a tile, a chain of short latencies, and were the
+//              slowest part.)
+//   warp  12   issues the MMAs: the scores of a tile before the output of the tile in front of it, so that the tensor core
 //              works on them while the softmax is still busy
 // Work per 64 keys and what it costs an SM: MMAs 2 x 128 x 64 x D (512 cycles at D = 128), 8192 exponentials (512 cycles),
 // some 3 instructions per weight and 1.3 per code besides. None of it is far ahead of the others, so they have to
@@ -31,7 +32,12 @@ using namespace tc;
 
 constexpr int KEYS = 64;                    // keys per tile
 constexpr int GROUPS = KEYS / 16;           // runs of 16 keys: a page never ends inside one
-constexpr int THREADS = 288;
+constexpr int CONV_WARPS = 8;
+constexpr int MMA_WARP = 4 + CONV_WARPS;
+constexpr int THREADS = 32 * (MMA_WARP + 1);
+// Registers: LAUNCH_REGS a thread at launch, of which the converting warps give up what the softmax takes (in all as many).
+constexpr int LAUNCH_REGS = 72, SOFTMAX_REGS = 120, CONV_REGS = 48;
+static_assert(4 * SOFTMAX_REGS + CONV_WARPS * CONV_REGS + LAUNCH_REGS <= (MMA_WARP + 1) * LAUNCH_REGS, "register split");
 constexpr int Q_BLOCK = 128 * 128;          // 128 rows of 64 halves
 constexpr int KV_BLOCK = KEYS * 128;        // a tile's keys or values, 64 elements of each
 constexpr int TMEM_COLS = 256;              // scores (and weights) of two tiles 0 .. 127, output from 128
@@ -171,17 +177,17 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (uint32_t b = 0; b < 2; ++b) {
-            mbar_init(k_full(b), 4);
-            mbar_init(s_full(b), 5);       // the MMAs, and the four warps that wrote the tile's scales
+            mbar_init(k_full(b), CONV_WARPS);
+            mbar_init(s_full(b), 1 + CONV_WARPS);       // the MMAs, and the warps that wrote the tile's scales (and factors)
             mbar_init(p_full(b), 4);
-            mbar_init(v_full(b), 4);
+            mbar_init(v_full(b), CONV_WARPS);
             mbar_init(o_done(b), 1);
         }
-        mbar_init(q_full, 4);
+        mbar_init(q_full, CONV_WARPS);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 8) {
+    if (warp == MMA_WARP) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(const_cast<uint32_t*>(tmem_slot))), "n"(TMEM_COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -197,8 +203,7 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
     auto wait = [&](uint32_t bar, uint32_t tile) { return __all_sync(0xffffffffu, mbar_wait(bar, (tile >> 1) & 1u, abort_flag)) != 0; };
 
     if (warp < 4) {
-        // Registers: 96 a thread at launch, 288 threads. Four softmax warps at 128, four at 64 and one at 96 take as many.
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
         const uint32_t t_lane = tmem + (static_cast<uint32_t>(warp * 32) << 16), t_o = t_lane + O_COL;
         uint32_t full_items = 0;
         Item next = item_of(a, blockIdx.x);
@@ -333,14 +338,16 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
             }
             tc_fence_before();
         }
-    } else if (warp < 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    } else if (warp < MMA_WARP) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CONV_REGS));
         const int tid = threadIdx.x - 128;
         const int shift = a.c.page_shift, mask = (1 << shift) - 1;
-        // A thread's pieces of a tile: 16 codes of keys tid / 4 + 32 i, elements 64 b + 16 (tid % 4) on. Eight lanes then
-        // write eight different 16-byte units, and a thread's place in the swizzle never changes.
-        constexpr int BLOCKS = S::BLOCKS, ROWS = KEYS / 32;
-        uint4 kc[ROWS][BLOCKS], vc[ROWS][BLOCKS];
+        // A thread's pieces of a tile: 16 codes of key tid / 4, elements 64 b + 16 (tid % 4) on. Eight lanes then write eight
+        // different 16-byte units.
+        constexpr int BLOCKS = S::BLOCKS;
+        static_assert(CONV_WARPS * 8 == KEYS, "one key for four threads");
+        uint4 kc[BLOCKS], vc[BLOCKS];
+        const int row = tid >> 2;
         // The tiles of this CTA's items, one after another.
         struct Tile {
             const int32_t* table;
@@ -368,69 +375,59 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
             ++gen_j;
             return t;
         };
-        // Table entries as they are; checked when they are used, so that nothing waits for them here.
-        auto pages_of_tile = [&](const Tile& t, int (&page)[ROWS]) {
+        // The table entry as it is; checked when it is used, so that nothing waits for it here.
+        auto entry_of = [&](const Tile& t) {
+            const int key = t.k0 + row, j = key >> shift;
+            return key < t.end && j < a.ldt ? __ldg(t.table + j) : -1;
+        };
+        // Place of this thread's codes in the cache; -1 behind the end or where there is no page.
+        auto place_of = [&](const Tile& t, int entry) {
+            return checked_page(a.c, entry) < 0 ? -1 : (page_codes(a.c, entry, t.h) + ((t.k0 + row) & mask)) * D + (tid & 3) * 16;
+        };
+        auto fetch = [&](const uint8_t* codes, int64_t place, uint4 (&to)[BLOCKS]) {
 #pragma unroll
-            for (int i = 0; i < ROWS; ++i) {
-                const int key = t.k0 + (tid >> 2) + 32 * i, j = key >> shift;
-                page[i] = -1;
-                if (key < t.end && j < a.ldt) page[i] = __ldg(t.table + j);
+            for (int b = 0; b < BLOCKS; ++b) {
+                to[b] = make_uint4(0, 0, 0, 0);                // zero codes, whatever lies there
+                if (place >= 0) to[b] = __ldg(reinterpret_cast<const uint4*>(codes + place + 64 * b));
             }
         };
-        auto fetch = [&](const Half& half, const Tile& t, const int (&page)[ROWS], uint4 (&to)[ROWS][BLOCKS]) {
-#pragma unroll
-            for (int i = 0; i < ROWS; ++i) {
-                const int key = t.k0 + (tid >> 2) + 32 * i;
-                const uint8_t* p = half.codes + (page_codes(a.c, page[i], t.h) + (key & mask)) * D + (tid & 3) * 16;
-#pragma unroll
-                for (int b = 0; b < BLOCKS; ++b) {
-                    to[i][b] = make_uint4(0, 0, 0, 0);         // behind the end: zero codes, whatever lies there
-                    if (checked_page(a.c, page[i]) >= 0) to[i][b] = __ldg(reinterpret_cast<const uint4*>(p + 64 * b));
-                }
-            }
-        };
-        // Scales: thread 8 g of the first 64 holds a key of run g (tid / 4 = 16 (g % 2), i = g / 2) and with it the run's page.
-        float ks[ROWS], vs[ROWS];
+        // Scales: one thread of each run of 16 keys.
+        float ks = 0.0f, vs = -1.0f;                           // vs < 0: no page
         const bool scaler = (tid & 63) == 0;
-        auto fetch_scales = [&](const Tile& t, const int (&page)[ROWS]) {
-#pragma unroll
-            for (int i = 0; i < ROWS; ++i) {
-                ks[i] = 0.0f;
-                vs[i] = -1.0f;                                 // no page
-                if (scaler && checked_page(a.c, page[i]) >= 0) {
-                    const int64_t s = static_cast<int64_t>(page[i]) * a.c.kv_heads + t.h;
-                    ks[i] = __ldg(a.c.k.scales + s);
-                    vs[i] = __ldg(a.c.v.scales + s);
-                }
+        auto fetch_scales = [&](const Tile& t, int entry) {
+            ks = 0.0f;
+            vs = -1.0f;
+            if (scaler && checked_page(a.c, entry) >= 0) {
+                const int64_t s = static_cast<int64_t>(entry) * a.c.kv_heads + t.h;
+                ks = __ldg(a.c.k.scales + s);
+                vs = __ldg(a.c.v.scales + s);
             }
         };
-        const int row = tid >> 2, unit = (tid & 3) * 2;
+        const int unit = (tid & 3) * 2;
         const uint32_t to0 = row * 128 + ((unit ^ (row & 7)) << 4), to1 = row * 128 + (((unit + 1) ^ (row & 7)) << 4);
-        auto put = [&](int region, const uint4 (&from)[ROWS][BLOCKS]) {
+        auto put = [&](int region, const uint4 (&from)[BLOCKS]) {
 #pragma unroll
-            for (int i = 0; i < ROWS; ++i)
+            for (int b = 0; b < BLOCKS; ++b) {
+                const uint32_t in[4] = {from[b].x, from[b].y, from[b].z, from[b].w};
+                uint32_t out[8];
 #pragma unroll
-                for (int b = 0; b < BLOCKS; ++b) {
-                    const uint32_t in[4] = {from[i][b].x, from[i][b].y, from[i][b].z, from[i][b].w};
-                    uint32_t out[8];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        if (TYPE == SQAP_KV_INT8) {
-                            out[2 * q] = biased_to_half2<0>(in[q] ^ 0x80808080u);
-                            out[2 * q + 1] = biased_to_half2<1>(in[q] ^ 0x80808080u);
-                        } else {
-                            out[2 * q] = e4m3x2_to_half2(in[q] & 0xFFFFu);
-                            out[2 * q + 1] = e4m3x2_to_half2(in[q] >> 16);
-                        }
+                for (int q = 0; q < 4; ++q) {
+                    if (TYPE == SQAP_KV_INT8) {
+                        out[2 * q] = biased_to_half2<0>(in[q] ^ 0x80808080u);
+                        out[2 * q + 1] = biased_to_half2<1>(in[q] ^ 0x80808080u);
+                    } else {
+                        out[2 * q] = e4m3x2_to_half2(in[q] & 0xFFFFu);
+                        out[2 * q + 1] = e4m3x2_to_half2(in[q] >> 16);
                     }
-                    uint8_t* to = sm + region + b * KV_BLOCK + i * 32 * 128;
-                    *reinterpret_cast<uint4*>(to + to0) = make_uint4(out[0], out[1], out[2], out[3]);
-                    *reinterpret_cast<uint4*>(to + to1) = make_uint4(out[4], out[5], out[6], out[7]);
                 }
+                uint8_t* to = sm + region + b * KV_BLOCK;
+                *reinterpret_cast<uint4*>(to + to0) = make_uint4(out[0], out[1], out[2], out[3]);
+                *reinterpret_cast<uint4*>(to + to1) = make_uint4(out[4], out[5], out[6], out[7]);
+            }
         };
-        // Queries: a warp brings 32 rows, LPR lanes to a row.
-        constexpr int LPR = D / 8, RPI = 32 / LPR;
-        const int qc = lane % LPR, q_row0 = (warp - 4) * 32 + lane / LPR;
+        // Queries: a warp brings Q_ROWS rows, LPR lanes to a row.
+        constexpr int Q_ROWS = 128 / CONV_WARPS, LPR = D / 8, RPI = 32 / LPR, Q_STEPS = Q_ROWS / RPI;
+        const int qc = lane % LPR, q_row0 = (warp - 4) * Q_ROWS + lane / LPR;
         auto q_at = [&](int i) {
             const int rr = q_row0 + i * RPI;
             return static_cast<uint32_t>(S::Q + (qc >> 3) * Q_BLOCK + rr * 128 + (((qc & 7) ^ (rr & 7)) << 4));
@@ -441,14 +438,14 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
             if (G == 1) {
                 const T* p = q + first * a.ldq;
 #pragma unroll
-                for (int i = 0; i < LPR; ++i, p += RPI * a.ldq) {
+                for (int i = 0; i < Q_STEPS; ++i, p += RPI * a.ldq) {
                     const bool there = first + i * RPI < t.rows;
                     cp_async_16(base + q_at(i), there ? p : q, there);
                 }
             } else {
                 int qi = first / G, g = first - qi * G;
 #pragma unroll 4
-                for (int i = 0; i < LPR; ++i) {
+                for (int i = 0; i < Q_STEPS; ++i) {
                     const bool there = first + i * RPI < t.rows;
                     cp_async_16(base + q_at(i), there ? q + qi * a.ldq + g * D : q, there);
                     g += RPI;
@@ -464,14 +461,14 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
             // bf16 rows are scaled one by one to fit fp16; a negative scale goes into the queries, so that no factor is negative
             if (std::is_same<T, __half>::value) {
                 if (a.scale_log2 < 0.0f)
-                    for (int i = 0; i < LPR; ++i) {
+                    for (int i = 0; i < Q_STEPS; ++i) {
                         uint4* u = reinterpret_cast<uint4*>(sm + q_at(i));
                         *u = make_uint4(u->x ^ 0x80008000u, u->y ^ 0x80008000u, u->z ^ 0x80008000u, u->w ^ 0x80008000u);
                     }
-                fac[(warp - 4) * 32 + lane] = fabsf(a.scale_log2);
+                if (lane < Q_ROWS) fac[(warp - 4) * Q_ROWS + lane] = fabsf(a.scale_log2);
             } else {
 #pragma unroll 4
-                for (int i = 0; i < LPR; ++i) {
+                for (int i = 0; i < Q_STEPS; ++i) {
                     uint4* u = reinterpret_cast<uint4*>(sm + q_at(i));
                     float v[8];
                     unpack8<T>(*u, v);
@@ -490,15 +487,15 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
             }
         };
 
-        // The tile being written, its codes in registers; and the one after, its pages known.
-        int pages[ROWS];
+        // The tile being written, its codes in registers; and the one after, its table entry on its way.
         Tile now = next_tile();
-        pages_of_tile(now, pages);
-        fetch(a.c.k, now, pages, kc);
-        fetch(a.c.v, now, pages, vc);
-        fetch_scales(now, pages);
+        int entry = entry_of(now);
+        int64_t place = place_of(now, entry);
+        fetch(a.c.k.codes, place, kc);
+        fetch(a.c.v.codes, place, vc);
+        fetch_scales(now, entry);
         Tile then = next_tile();
-        pages_of_tile(then, pages);
+        entry = entry_of(then);
         uint32_t full_items = 0;
         for (; now.end > 0; ++n) {
             const bool opens = now.rows > 0;
@@ -511,14 +508,10 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
             if (n > 1 && !wait(s_full(n), n - 2)) { failed = true; break; }
             put(S::K + (n & 1) * S::TILE, kc);
             if (scaler) {
-#pragma unroll
-                for (int i = 0; i < ROWS; ++i) {
-                    const int run = 2 * i + (tid >> 6);
-                    const float lv = __log2f(vs[i] > 0.0f ? vs[i] : ZERO_PAGE_SCALE);
-                    scales->ks[n & 3][run] = ks[i];
-                    scales->lv[n & 3][run] = vs[i] < 0.0f ? -INFINITY : lv;
-                    scales->iv[n & 3][run] = fast_exp2(-lv);
-                }
+                const float lv = __log2f(vs > 0.0f ? vs : ZERO_PAGE_SCALE);
+                scales->ks[n & 3][tid >> 6] = ks;
+                scales->lv[n & 3][tid >> 6] = vs < 0.0f ? -INFINITY : lv;
+                scales->iv[n & 3][tid >> 6] = fast_exp2(-lv);
             }
             if (opens) {
                 finish_queries(row_fac + (full_items & 1) * 128);
@@ -531,18 +524,19 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
                 mbar_arrive(k_full(n));
                 if (opens) mbar_arrive(q_full);
             }
-            fetch(a.c.k, then, pages, kc);
-            fetch_scales(then, pages);
+            place = place_of(then, entry);
+            fetch(a.c.k.codes, place, kc);
+            fetch_scales(then, entry);
             // values: the output of the tile that was here has taken them
             if (n > 1 && !wait(o_done(n), n - 2)) { failed = true; break; }
             put(S::V + (n & 1) * S::TILE, vc);
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) mbar_arrive(v_full(n));
-            fetch(a.c.v, then, pages, vc);
+            fetch(a.c.v.codes, place, vc);
             now = then;
             then = next_tile();
-            pages_of_tile(then, pages);
+            entry = entry_of(then);
         }
     } else {
         const uint32_t issue = elect_one();
@@ -586,13 +580,24 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(TMEM_COLS) : "memory");
+    if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(TMEM_COLS) : "memory");
 }
 
 template <typename T, int TYPE, int D>
 sqap_status launch_as(const AttnArgs& a, unsigned items, int* status, cudaStream_t s) {
     static PerDevice<int> setup;
-    const sqap_status st = setup.run([](int*) { return set_max_dynamic_smem(kv_prefill_tc_kernel<T, TYPE, D>, Smem<D>::BYTES); });
+    const sqap_status st = setup.run([](int*) {
+        // the softmax's registers come out of those that the kernel is launched with: with fewer, it would wait for them for ever
+        cudaFuncAttributes f;
+        const cudaError_t e = cudaFuncGetAttributes(&f, kv_prefill_tc_kernel<T, TYPE, D>);
+        if (e != cudaSuccess) {
+            note_cuda_error(e);
+            cudaGetLastError();
+            return SQAP_ERR_CUDA;
+        }
+        if (f.numRegs < LAUNCH_REGS) return SQAP_ERR_UNSUPPORTED;
+        return set_max_dynamic_smem(kv_prefill_tc_kernel<T, TYPE, D>, Smem<D>::BYTES);
+    });
     if (st != SQAP_OK) return st;
     const unsigned slots = 2u * static_cast<unsigned>(sm_count());
     return finish_launch(launch_dependent(kv_prefill_tc_kernel<T, TYPE, D>, dim3(items < slots ? items : slots), dim3(THREADS),
