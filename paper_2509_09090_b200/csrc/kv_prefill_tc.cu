@@ -165,22 +165,20 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
     static_assert(sizeof(Scales) <= S::OFF_FAC, "tail layout");
     const uint32_t bar0 = base + S::TAIL + S::OFF_BAR;
     // tile n uses the barriers of parity n & 1, in their phase n >> 1
-    auto k_full = [&](uint32_t n) { return bar0 + 8u * (n & 1); };
+    auto kv_full = [&](uint32_t n) { return bar0 + 8u * (n & 1); };
     auto s_full = [&](uint32_t n) { return bar0 + 16u + 8u * (n & 1); };       // also: the keys have been read
     auto p_full = [&](uint32_t n) { return bar0 + 32u + 8u * (n & 1); };
-    auto v_full = [&](uint32_t n) { return bar0 + 48u + 8u * (n & 1); };
-    auto o_done = [&](uint32_t n) { return bar0 + 64u + 8u * (n & 1); };       // also: values and weights have been read
-    const uint32_t q_full = bar0 + 80u;
+    auto o_done = [&](uint32_t n) { return bar0 + 48u + 8u * (n & 1); };       // also: values and weights have been read
+    const uint32_t q_full = bar0 + 64u;
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + S::TAIL + S::OFF_WORDS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::TAIL + S::OFF_WORDS + 8);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (uint32_t b = 0; b < 2; ++b) {
-            mbar_init(k_full(b), CONV_WARPS);
+            mbar_init(kv_full(b), CONV_WARPS);
             mbar_init(s_full(b), 1 + CONV_WARPS);       // the MMAs, and the warps that wrote the tile's scales (and factors)
             mbar_init(p_full(b), 4);
-            mbar_init(v_full(b), CONV_WARPS);
             mbar_init(o_done(b), 1);
         }
         mbar_init(q_full, CONV_WARPS);
@@ -517,22 +515,20 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
                 finish_queries(row_fac + (full_items & 1) * 128);
                 ++full_items;
             }
-            fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(s_full(n));
-                mbar_arrive(k_full(n));
-                if (opens) mbar_arrive(q_full);
-            }
             place = place_of(then, entry);
             fetch(a.c.k.codes, place, kc);
             fetch_scales(then, entry);
             // values: the output of the tile that was here has taken them
             if (n > 1 && !wait(o_done(n), n - 2)) { failed = true; break; }
             put(S::V + (n & 1) * S::TILE, vc);
+            // one fence for both: the scores of this tile wait for the output of tile n - 2 anyway
             fence_proxy_async();
             __syncwarp();
-            if (lane == 0) mbar_arrive(v_full(n));
+            if (lane == 0) {
+                mbar_arrive(s_full(n));
+                mbar_arrive(kv_full(n));
+                if (opens) mbar_arrive(q_full);
+            }
             fetch(a.c.v.codes, place, vc);
             now = then;
             then = next_tile();
@@ -545,7 +541,7 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
         uint32_t full_items = 0;
         auto scores = [&](uint32_t t) {
             // two tiles earlier these columns held weights: they have been read
-            if (!wait(k_full(t), t) || (t > 1 && !wait(o_done(t), t - 2))) return false;
+            if (!wait(kv_full(t), t) || (t > 1 && !wait(o_done(t), t - 2))) return false;
             tc_fence_after();
 #pragma unroll
             for (int k = 0; k < D / 16; ++k)
@@ -562,7 +558,7 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
             if (!scores(n)) { failed = true; break; }
             for (int j = 0; j < x.steps; ++j, ++n) {
                 if (j + 1 < x.steps && !scores(n + 1)) { failed = true; break; }
-                if (!wait(v_full(n), n) || !wait(p_full(n), n)) { failed = true; break; }
+                if (!wait(p_full(n), n)) { failed = true; break; }
                 tc_fence_after();
 #pragma unroll
                 for (int k = 0; k < KEYS / 16; ++k)
