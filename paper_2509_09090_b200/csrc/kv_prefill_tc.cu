@@ -353,25 +353,33 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
             int row0, r_first, rows;   // rows > 0: the first tile of an item, whose queries are wanted
         };
         unsigned id = blockIdx.x;
-        Item gen = item_of(a, id);
-        int gen_j = 0;
-        auto next_tile = [&]() {
-            Tile t = {};
-            while (gen_j >= gen.steps) {
+        Tile then = {};
+        int left = 0;                  // tiles of the item behind `then`
+        auto open_item = [&]() {
+            then.end = 0;
+            while (id < items) {
+                const Item x = item_of(a, id);
                 id += gridDim.x;
-                if (id >= items || id < gridDim.x) return t;
-                gen = item_of(a, id);
-                gen_j = 0;
+                if (x.steps == 0) continue;
+                then.table = a.table + x.w.b * a.ldt;
+                then.h = x.w.h;
+                then.k0 = x.key0;
+                then.end = x.end;
+                then.row0 = x.w.row0;
+                then.r_first = x.r_first;
+                then.rows = x.rows;
+                left = x.steps - 1;
+                break;
             }
-            t.table = a.table + gen.w.b * a.ldt;
-            t.h = gen.w.h;
-            t.k0 = gen.key0 + gen_j * KEYS;
-            t.end = gen.end;
-            t.row0 = gen.w.row0;
-            t.r_first = gen.r_first;
-            t.rows = gen_j == 0 ? gen.rows : 0;
-            ++gen_j;
-            return t;
+        };
+        auto advance = [&]() {
+            if (left > 0) {
+                --left;
+                then.k0 += KEYS;
+                then.rows = 0;
+            } else {
+                open_item();
+            }
         };
         // The table entry as it is; checked when it is used, so that nothing waits for it here.
         auto entry_of = [&](const Tile& t) {
@@ -379,8 +387,11 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
             return key < t.end && j < a.ldt ? __ldg(t.table + j) : -1;
         };
         // Place of this thread's codes in the cache; -1 behind the end or where there is no page.
+        const uint32_t page_bytes = static_cast<uint32_t>(a.c.kv_heads * D) << shift;      // 2^31 at most
         auto place_of = [&](const Tile& t, int entry) {
-            return checked_page(a.c, entry) < 0 ? -1 : (page_codes(a.c, entry, t.h) + ((t.k0 + row) & mask)) * D + (tid & 3) * 16;
+            const int64_t at = static_cast<int64_t>(static_cast<uint64_t>(static_cast<uint32_t>(entry)) * page_bytes) +
+                               (((static_cast<uint32_t>(t.h) << shift) + ((t.k0 + row) & mask)) * D + (tid & 3) * 16);
+            return checked_page(a.c, entry) < 0 ? -1 : at;
         };
         auto fetch = [&](const uint8_t* codes, int64_t place, uint4 (&to)[BLOCKS]) {
 #pragma unroll
@@ -486,13 +497,14 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
         };
 
         // The tile being written, its codes in registers; and the one after, its table entry on its way.
-        Tile now = next_tile();
+        open_item();
+        Tile now = then;
         int entry = entry_of(now);
         int64_t place = place_of(now, entry);
         fetch(a.c.k.codes, place, kc);
         fetch(a.c.v.codes, place, vc);
         fetch_scales(now, entry);
-        Tile then = next_tile();
+        advance();
         entry = entry_of(then);
         uint32_t full_items = 0;
         for (; now.end > 0; ++n) {
@@ -531,8 +543,10 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
             }
             fetch(a.c.v.codes, place, vc);
             now = then;
-            then = next_tile();
-            entry = entry_of(then);
+            if (now.end > 0) {
+                advance();
+                entry = entry_of(then);
+            }
         }
     } else {
         const uint32_t issue = elect_one();
