@@ -67,7 +67,8 @@ Plan plan_for(int64_t batch, int kv_heads, int group, int head_dim, int64_t max_
     Plan p;
     const int64_t rows = max_q * group;
     p.decode = rows <= decode_max_rows(head_dim);
-    p.tiles = p.decode ? 1 : static_cast<int>((rows + PREFILL_ROWS - 1) / PREFILL_ROWS);
+    const int per_tile = head_dim <= 128 ? PREFILL_TC_ROWS : PREFILL_ROWS;
+    p.tiles = p.decode ? 1 : static_cast<int>((rows + per_tile - 1) / per_tile);
     const int64_t ctas = batch * kv_heads * p.tiles;
     int64_t want;
     if (p.decode) want = max_len > 1024 ? 148 * 16 : 148 * 3;

@@ -104,7 +104,7 @@ __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 x) { return _
 // Few query rows per key/value head (kv_decode.cu) and many: head_dim 64 and 128 (kv_prefill_tc.cu), 256 (kv_prefill.cu).
 // With 256 elements a lane cannot hold the output of more than 8 rows in registers.
 inline int decode_max_rows(int head_dim) { return head_dim == 256 ? 8 : 16; }
-constexpr int PREFILL_ROWS = 128;
+constexpr int PREFILL_ROWS = 128, PREFILL_TC_ROWS = 256;   // query rows of a CTA's item
 sqap_status launch_kv_decode(const AttnArgs& a, int type, int dtype, cudaStream_t s);
 sqap_status launch_kv_prefill_tc(const AttnArgs& a, int type, int dtype, cudaStream_t s);
 sqap_status launch_kv_prefill(const AttnArgs& a, int type, int dtype, cudaStream_t s);

@@ -1,18 +1,19 @@
 // Attention of many query rows (prompts) over the paged 8-bit cache on tcgen05, head_dim 64 and 128.
 //
-// An item is 128 rows (query x head of the group, packed: the heads that share a key/value head share its tiles) of one
-// sequence and key/value head; its keys are walked 64 at a time. Per tile: S = Q K^T into tensor memory, the softmax's weights
-// back into tensor memory as the A operand, O += W V.
-//   warps 0-3  softmax: thread = row. Rescale the output where a maximum has grown, and store it at the end.
-//   warps 4-11 codes from global memory (one tile ahead, in registers) to fp16 in shared memory, 128B-swizzled; the next
-//              item's queries. (Four warps for it took 3000 cycles a tile, a chain of short latencies, and were the
-//              slowest part.)
-//   warp  12   issues the MMAs: the scores of a tile before the output of the tile in front of it, so that the tensor core
-//              works on them while the softmax is still busy
-// Work per 64 keys and what it costs an SM: MMAs 2 x 128 x 64 x D (512 cycles at D = 128), 8192 exponentials (512 cycles),
-// some 3 instructions per weight and 1.3 per code besides. None of it is far ahead of the others, so they have to
-// overlap. A CTA takes 256 columns of tensor memory (two tiles of scores, one output) and 96 KB of shared memory (queries,
-// two tiles of keys and values); two CTAs on an SM fill each other's gaps, each walking its share of the items.
+// An item is 256 rows (query x head of the group, packed: the heads that share a key/value head share its tiles) of one
+// sequence and key/value head, in two halves of 128; its keys are walked 64 at a time. Per tile and half: S = Q K^T into tensor
+// memory, the softmax's weights back into tensor memory as the A operand, O += W V.
+//   warps 0-3, 4-7  softmax of the two halves: thread = row. Rescale the output where a maximum has grown, and store it.
+//   warps 8-15      codes from global memory (one tile ahead, in registers) to fp16 in shared memory, 128B-swizzled; the next
+//                   item's queries
+//   warp  16        issues the MMAs: the scores of a tile before the output of the tile in front of it, half by half, so that
+//                   the tensor core works on one half while the softmax of the other is busy
+// Work per 64 keys and half, and what it costs an SM: MMAs 2 x 128 x 64 x D (640 cycles at D = 128: the scores read both
+// operands from shared memory), 8192 exponentials (512 cycles), some 3 instructions per weight; and per 64 keys 1.3 per code. It
+// is the instructions that bound it: an earlier form with 128 rows an item and two CTAs to an SM, which converted every tile
+// for 128 rows only, issued 8200 warp instructions per 128 x 128 scores, 5000 of them for the conversion, at 64 % of
+// the issue slots. Persistent CTAs, one to an SM; 512 columns of tensor memory: two tiles of scores and one output for
+// each half.
 //
 // The running maximum is raised only when a row's maximum has grown by more than 2^8 (the weights then stay within fp16, at
 // the same relative precision): rescaling the output in tensor memory is rare after the first tiles. Weights and sums:
@@ -33,27 +34,29 @@ using namespace tc;
 constexpr int KEYS = 64;                    // keys per tile
 constexpr int GROUPS = KEYS / 16;           // runs of 16 keys: a page never ends inside one
 constexpr int CONV_WARPS = 8;
-constexpr int MMA_WARP = 4 + CONV_WARPS;
+constexpr int CONV_WARP0 = 8, MMA_WARP = CONV_WARP0 + CONV_WARPS;
 constexpr int THREADS = 32 * (MMA_WARP + 1);
-// Registers: LAUNCH_REGS a thread at launch, of which the converting warps give up what the softmax takes (in all as many).
-constexpr int LAUNCH_REGS = 72, SOFTMAX_REGS = 120, CONV_REGS = 48;
-static_assert(4 * SOFTMAX_REGS + CONV_WARPS * CONV_REGS + LAUNCH_REGS <= (MMA_WARP + 1) * LAUNCH_REGS, "register split");
+constexpr int ROWS = PREFILL_TC_ROWS;       // of an item
+// Registers: LAUNCH_REGS a thread at launch, of which the converting warps give up what the softmax takes on.
+constexpr int LAUNCH_REGS = 96, SOFTMAX_REGS = 120, CONV_REGS = 64;
+static_assert(CONV_WARP0 * SOFTMAX_REGS + CONV_WARPS * CONV_REGS <= MMA_WARP * LAUNCH_REGS, "register split");
+constexpr int RING = 4;                     // tiles of keys and values in shared memory
 constexpr int Q_BLOCK = 128 * 128;          // 128 rows of 64 halves
 constexpr int KV_BLOCK = KEYS * 128;        // a tile's keys or values, 64 elements of each
-constexpr int TMEM_COLS = 256;              // scores (and weights) of two tiles 0 .. 127, output from 128
-constexpr int O_COL = 128;
+constexpr int TMEM_COLS = 512;              // half g: scores (and weights) of two tiles from 128 g, output from 256 + 128 g
+constexpr int O_COL = 256;
 constexpr float RAISE = 8.0f;
 
 template <int D>
 struct Smem {
-    static constexpr int BLOCKS = D / 64, TILE = BLOCKS * KV_BLOCK;
-    static constexpr int Q = 0, K = BLOCKS * Q_BLOCK, V = K + 2 * TILE, TAIL = V + 2 * TILE;
-    static constexpr int OFF_FAC = 256, OFF_BAR = OFF_FAC + 2 * 128 * 4, OFF_WORDS = OFF_BAR + 128;
+    static constexpr int BLOCKS = D / 64, TILE = BLOCKS * KV_BLOCK, HALF_Q = BLOCKS * Q_BLOCK;
+    static constexpr int Q = 0, K = 2 * HALF_Q, V = K + RING * TILE, TAIL = V + RING * TILE;
+    static constexpr int OFF_FAC = 256, OFF_BAR = OFF_FAC + 2 * ROWS * 4, OFF_WORDS = OFF_BAR + 256;
     static constexpr int BYTES = TAIL + OFF_WORDS + 64 + 1024;      // slack for the alignment
 };
-// Scales of the tiles in flight, by run of 16 keys: the softmax may be reading those of tile n - 2 while n's are written.
+// Scales of the tiles in the ring, by run of 16 keys.
 struct Scales {
-    float ks[4][GROUPS], lv[4][GROUPS], iv[4][GROUPS];
+    float ks[RING][GROUPS], lv[RING][GROUPS], iv[RING][GROUPS];
 };
 
 __device__ __forceinline__ void tc_mma_f16(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate, uint32_t issue) {
@@ -129,10 +132,11 @@ __device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
     return d;
 }
 
-// One item: 128 rows of a sequence and key/value head (and one piece of its history, where those are cut).
+// One item: 256 rows of a sequence and key/value head (and one piece of its history, where those are cut).
 struct Item {
     Where w;
     int rows, r_first, key0, end, steps;
+    int steps_lo;     // tiles that the lower half of the rows looks at (the upper half: all, or there is no upper half)
 };
 __device__ __forceinline__ Item item_of(const AttnArgs& a, unsigned id) {
     Item x;
@@ -142,46 +146,60 @@ __device__ __forceinline__ Item item_of(const AttnArgs& a, unsigned id) {
     x.w = locate(a, id - tile * per_tile, 1);
     x.w.tile = a.tiles - 1 - static_cast<int>(tile);
     x.rows = (x.w.n_q < a.max_q ? x.w.n_q : a.max_q) * a.group;
-    x.r_first = x.w.tile * PREFILL_ROWS;
+    x.r_first = x.w.tile * ROWS;
     x.key0 = x.w.split * a.chunk;
     x.end = 0;
+    x.steps = x.steps_lo = 0;
     if (x.r_first < x.rows && a.c.pages > 0) {
-        const int last = min(x.rows, x.r_first + PREFILL_ROWS) - 1;
         const int key1 = a.splits > 1 ? min(x.key0 + a.chunk, x.w.len) : x.w.len;
+        const int last = min(x.rows, x.r_first + ROWS) - 1, last_lo = min(x.rows, x.r_first + ROWS / 2) - 1;
         x.end = min(key1, visible(a, x.w, last / a.group));
+        const int end_lo = min(key1, visible(a, x.w, last_lo / a.group));
+        x.steps = x.end > x.key0 ? (x.end - x.key0 + KEYS - 1) / KEYS : 0;
+        x.steps_lo = end_lo > x.key0 ? (end_lo - x.key0 + KEYS - 1) / KEYS : 0;
     }
-    x.steps = x.end > x.key0 ? (x.end - x.key0 + KEYS - 1) / KEYS : 0;
     return x;
+}
+// Tiles of half g, 0 where it has no rows.
+__device__ __forceinline__ int half_steps(const Item& x, int g) {
+    if (g == 0) return x.steps_lo;
+    return x.r_first + ROWS / 2 < x.rows ? x.steps : 0;
 }
 
 template <typename T, int TYPE, int D>
-__global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, unsigned items, int* status) {
+__global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, unsigned items, int* status) {
     using S = Smem<D>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* sm = smem_raw + (base - smem_u32(smem_raw));
     Scales* scales = reinterpret_cast<Scales*>(sm + S::TAIL);
-    float* row_fac = reinterpret_cast<float*>(sm + S::TAIL + S::OFF_FAC);       // [2][128]: by parity of the item
+    float* row_fac = reinterpret_cast<float*>(sm + S::TAIL + S::OFF_FAC);       // [2][ROWS]: by parity of the item
     static_assert(sizeof(Scales) <= S::OFF_FAC, "tail layout");
     const uint32_t bar0 = base + S::TAIL + S::OFF_BAR;
-    // tile n uses the barriers of parity n & 1, in their phase n >> 1
-    auto kv_full = [&](uint32_t n) { return bar0 + 8u * (n & 1); };
-    auto s_full = [&](uint32_t n) { return bar0 + 16u + 8u * (n & 1); };       // also: the keys have been read
-    auto p_full = [&](uint32_t n) { return bar0 + 32u + 8u * (n & 1); };
-    auto o_done = [&](uint32_t n) { return bar0 + 48u + 8u * (n & 1); };       // also: values and weights have been read
-    const uint32_t q_full = bar0 + 64u;
+    // Tile n of the CTA lies in slot n % RING, in that barrier's phase n / RING. Tile c of a half (its own count) uses the
+    // half's barriers of parity c & 1, in their phase c >> 1.
+    auto kv_full = [&](uint32_t slot) { return bar0 + 8u * slot; };                                // keys, values, scales (and row factors)
+    auto kv_free = [&](uint32_t slot) { return bar0 + 8u * (RING + slot); };
+    auto s_full = [&](int g, uint32_t c) { return bar0 + 8u * (2 * RING + 2 * g + (c & 1)); };     // scores are there
+    auto p_full = [&](int g, uint32_t c) { return bar0 + 8u * (2 * RING + 4 + 2 * g + (c & 1)); }; // weights are there
+    auto o_done = [&](int g, uint32_t c) { return bar0 + 8u * (2 * RING + 8 + 2 * g + (c & 1)); }; // the output has taken them
+    const uint32_t q_full = bar0 + 8u * (2 * RING + 12), q_free = q_full + 8u;
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + S::TAIL + S::OFF_WORDS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::TAIL + S::OFF_WORDS + 8);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (uint32_t b = 0; b < 2; ++b) {
+        for (uint32_t b = 0; b < RING; ++b) {
             mbar_init(kv_full(b), CONV_WARPS);
-            mbar_init(s_full(b), 1 + CONV_WARPS);       // the MMAs, and the warps that wrote the tile's scales (and factors)
-            mbar_init(p_full(b), 4);
-            mbar_init(o_done(b), 1);
+            mbar_init(kv_free(b), 1);
+        }
+        for (uint32_t b = 0; b < 4; ++b) {
+            mbar_init(s_full(b >> 1, b), 1);
+            mbar_init(p_full(b >> 1, b), 4);
+            mbar_init(o_done(b >> 1, b), 1);
         }
         mbar_init(q_full, CONV_WARPS);
+        mbar_init(q_free, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -197,12 +215,21 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
     const uint32_t tmem = *tmem_slot;
     const int G = a.group;
     bool failed = false;
-    uint32_t n = 0;                 // tiles so far, over all items
-    auto wait = [&](uint32_t bar, uint32_t tile) { return __all_sync(0xffffffffu, mbar_wait(bar, (tile >> 1) & 1u, abort_flag)) != 0; };
+    auto wait_phase = [&](uint32_t bar, uint32_t phase) { return __all_sync(0xffffffffu, mbar_wait(bar, phase & 1u, abort_flag)) != 0; };
+    // the place of the CTA's next tile in the ring, and how often the ring has been walked
+    uint32_t slot = 0, walk = 0;
+    auto next_slot = [&]() {
+        if (++slot == RING) {
+            slot = 0;
+            ++walk;
+        }
+    };
 
-    if (warp < 4) {
+    if (warp < CONV_WARP0) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
-        const uint32_t t_lane = tmem + (static_cast<uint32_t>(warp * 32) << 16), t_o = t_lane + O_COL;
+        const int half = warp >> 2;
+        const uint32_t t_lane = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + 128 * half, t_o = t_lane + O_COL;
+        uint32_t n = 0;             // tiles of this half so far
         uint32_t full_items = 0;
         Item next = item_of(a, blockIdx.x);
         for (unsigned id = blockIdx.x; id < items; id += gridDim.x) {
@@ -212,15 +239,17 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
             const int qi = real ? r / G : 0, head = x.w.h * G + (real ? r - qi * G : 0);
             const int lim = real ? min(visible(a, x.w, qi), x.end) : 0;
             const bool idle = x.r_first + warp * 32 >= x.rows;          // no rows: whatever these lanes hold goes nowhere
+            const int steps = half_steps(x, half);
             float m = -INFINITY, l = 0.0f, fac = 0.0f;
-            for (int j = 0; j < x.steps; ++j, ++n) {
-                if (!wait(s_full(n), n)) { failed = true; break; }
+            for (int j = 0; j < steps; ++j, ++n, next_slot()) {
+                // (the tile's scales and the rows' factors are written before kv_full)
+                if (!wait_phase(kv_full(slot), walk) || !wait_phase(s_full(half, n), n >> 1)) { failed = true; break; }
                 if (!idle) {
                     tc_fence_after();
-                    if (j == 0) fac = row_fac[(full_items & 1) * 128 + threadIdx.x];
-                    const float* ks = scales->ks[n & 3];
-                    const float* lv = scales->lv[n & 3];
-                    const float* iv = scales->iv[n & 3];
+                    if (j == 0) fac = row_fac[(full_items & 1) * ROWS + threadIdx.x];
+                    const float* ks = scales->ks[slot];
+                    const float* lv = scales->lv[slot];
+                    const float* iv = scales->iv[slot];
                     const int seen = lim - (x.key0 + j * KEYS);         // this row sees the first `seen` keys of the tile
                     const uint32_t t_s = t_lane + KEYS * (n & 1);
                     uint32_t v[KEYS];
@@ -252,7 +281,7 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
                         if (raise) m = top;
                         l *= f;
                         if (j > 0) {
-                            if (!wait(o_done(n - 1), n - 1)) { failed = true; break; }
+                            if (!wait_phase(o_done(half, n - 1), (n - 1) >> 1)) { failed = true; break; }
                             tc_fence_after();
 #pragma unroll 1
                             for (int c = 0; c < D / 16; ++c) {
@@ -290,13 +319,14 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
                     tc_fence_before();
                 }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full(n));
+                if (lane == 0) mbar_arrive(p_full(half, n));
             }
             if (failed) break;
             if (id + gridDim.x < items) next = item_of(a, id + gridDim.x);      // while the last output product runs
-            if (x.steps > 0) {
-                ++full_items;
-                if (!wait(o_done(n - 1), n - 1)) { failed = true; break; }
+            for (int j = steps; j < x.steps; ++j) next_slot();          // tiles that the other half alone looks at
+            if (x.steps > 0) ++full_items;
+            if (steps > 0) {
+                if (!wait_phase(o_done(half, n - 1), (n - 1) >> 1)) { failed = true; break; }
                 tc_fence_after();
             }
             if (idle) continue;
@@ -308,7 +338,7 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
 #pragma unroll
             for (int c = 0; c < D / 64; ++c) {
                 uint32_t v[64];
-                if (x.steps > 0) {
+                if (steps > 0) {
                     tc_ld32(t_o + 64 * c, v);
                     tc_ld32(t_o + 64 * c + 32, v + 32);
                     tc_wait_ld();
@@ -338,7 +368,7 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
         }
     } else if (warp < MMA_WARP) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CONV_REGS));
-        const int tid = threadIdx.x - 128;
+        const int tid = threadIdx.x - 32 * CONV_WARP0;
         const int shift = a.c.page_shift, mask = (1 << shift) - 1;
         // A thread's pieces of a tile: 16 codes of key tid / 4, elements 64 b + 16 (tid % 4) on. Eight lanes then write eight
         // different 16-byte units.
@@ -435,11 +465,12 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
             }
         };
         // Queries: a warp brings Q_ROWS rows, LPR lanes to a row.
-        constexpr int Q_ROWS = 128 / CONV_WARPS, LPR = D / 8, RPI = 32 / LPR, Q_STEPS = Q_ROWS / RPI;
-        const int qc = lane % LPR, q_row0 = (warp - 4) * Q_ROWS + lane / LPR;
+        constexpr int Q_ROWS = ROWS / CONV_WARPS, LPR = D / 8, RPI = 32 / LPR, Q_STEPS = Q_ROWS / RPI;
+        static_assert(Q_ROWS == 32, "the lanes of a warp write its rows' factors");
+        const int qc = lane % LPR, q_row0 = (warp - CONV_WARP0) * Q_ROWS + lane / LPR;
         auto q_at = [&](int i) {
             const int rr = q_row0 + i * RPI;
-            return static_cast<uint32_t>(S::Q + (qc >> 3) * Q_BLOCK + rr * 128 + (((qc & 7) ^ (rr & 7)) << 4));
+            return static_cast<uint32_t>(S::Q + (rr >> 7) * S::HALF_Q + (qc >> 3) * Q_BLOCK + (rr & 127) * 128 + (((qc & 7) ^ (rr & 7)) << 4));
         };
         auto begin_queries = [&](const Tile& t) {
             const int first = t.r_first + q_row0;
@@ -474,7 +505,7 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
                         uint4* u = reinterpret_cast<uint4*>(sm + q_at(i));
                         *u = make_uint4(u->x ^ 0x80008000u, u->y ^ 0x80008000u, u->z ^ 0x80008000u, u->w ^ 0x80008000u);
                     }
-                if (lane < Q_ROWS) fac[(warp - 4) * Q_ROWS + lane] = fabsf(a.scale_log2);
+                fac[tid] = fabsf(a.scale_log2);
             } else {
 #pragma unroll 4
                 for (int i = 0; i < Q_STEPS; ++i) {
@@ -507,41 +538,37 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
         advance();
         entry = entry_of(then);
         uint32_t full_items = 0;
-        for (; now.end > 0; ++n) {
+        for (; now.end > 0; next_slot()) {
             const bool opens = now.rows > 0;
             if (opens) {
                 // the last scores of the item before have been taken
-                if (n > 0 && !wait(s_full(n - 1), n - 1)) { failed = true; break; }
+                if (full_items > 0 && !wait_phase(q_free, full_items - 1)) { failed = true; break; }
                 begin_queries(now);
             }
-            // keys: the scores of the tile that was here have been taken
-            if (n > 1 && !wait(s_full(n), n - 2)) { failed = true; break; }
-            put(S::K + (n & 1) * S::TILE, kc);
+            // whoever was in this slot has been used up
+            if (walk > 0 && !wait_phase(kv_free(slot), walk - 1)) { failed = true; break; }
+            put(S::K + slot * S::TILE, kc);
             if (scaler) {
                 const float lv = __log2f(vs > 0.0f ? vs : ZERO_PAGE_SCALE);
-                scales->ks[n & 3][tid >> 6] = ks;
-                scales->lv[n & 3][tid >> 6] = vs < 0.0f ? -INFINITY : lv;
-                scales->iv[n & 3][tid >> 6] = fast_exp2(-lv);
-            }
-            if (opens) {
-                finish_queries(row_fac + (full_items & 1) * 128);
-                ++full_items;
+                scales->ks[slot][tid >> 6] = ks;
+                scales->lv[slot][tid >> 6] = vs < 0.0f ? -INFINITY : lv;
+                scales->iv[slot][tid >> 6] = fast_exp2(-lv);
             }
             place = place_of(then, entry);
             fetch(a.c.k.codes, place, kc);
             fetch_scales(then, entry);
-            // values: the output of the tile that was here has taken them
-            if (n > 1 && !wait(o_done(n), n - 2)) { failed = true; break; }
-            put(S::V + (n & 1) * S::TILE, vc);
-            // one fence for both: the scores of this tile wait for the output of tile n - 2 anyway
+            put(S::V + slot * S::TILE, vc);
+            fetch(a.c.v.codes, place, vc);
+            if (opens) {
+                finish_queries(row_fac + (full_items & 1) * ROWS);
+                ++full_items;
+            }
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) {
-                mbar_arrive(s_full(n));
-                mbar_arrive(kv_full(n));
+                mbar_arrive(kv_full(slot));
                 if (opens) mbar_arrive(q_full);
             }
-            fetch(a.c.v.codes, place, vc);
             now = then;
             if (now.end > 0) {
                 advance();
@@ -553,32 +580,55 @@ __global__ void __launch_bounds__(THREADS, 2) kv_prefill_tc_kernel(AttnArgs a, u
         const uint32_t idesc_s = (1u << 4) | (static_cast<uint32_t>(KEYS >> 3) << 17) | (128u >> 4 << 24);
         const uint32_t idesc_o = (1u << 4) | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17) | (128u >> 4 << 24);
         uint32_t full_items = 0;
-        auto scores = [&](uint32_t t) {
+        uint32_t n[2] = {0, 0};                 // tiles of either half so far, and up to which the scores have been issued
+        uint32_t s_slot = 0, s_walk = 0;        // place of the tile whose scores are issued next
+        // Scores of half g's tile c, from slot s_slot.
+        auto scores = [&](int g, uint32_t c) {
             // two tiles earlier these columns held weights: they have been read
-            if (!wait(kv_full(t), t) || (t > 1 && !wait(o_done(t), t - 2))) return false;
+            if (c > 1 && !wait_phase(o_done(g, c), (c - 2) >> 1)) return false;
             tc_fence_after();
 #pragma unroll
             for (int k = 0; k < D / 16; ++k)
-                tc_mma_f16(tmem + KEYS * (t & 1), smem_desc_sw128(base + S::Q + (k >> 2) * Q_BLOCK) + 2u * (k & 3),
-                           smem_desc_sw128(base + S::K + (t & 1) * S::TILE + (k >> 2) * KV_BLOCK) + 2u * (k & 3), idesc_s, k != 0 ? 1u : 0u, issue);
-            tc_commit_if(s_full(t), issue);
+                tc_mma_f16(tmem + 128 * g + KEYS * (c & 1), smem_desc_sw128(base + S::Q + g * S::HALF_Q + (k >> 2) * Q_BLOCK) + 2u * (k & 3),
+                           smem_desc_sw128(base + S::K + s_slot * S::TILE + (k >> 2) * KV_BLOCK) + 2u * (k & 3), idesc_s, k != 0 ? 1u : 0u, issue);
+            tc_commit_if(s_full(g, c), issue);
+            return true;
+        };
+        auto output = [&](int g, uint32_t c, bool first) {
+            if (!wait_phase(p_full(g, c), c >> 1)) return false;
+            tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < KEYS / 16; ++k)
+                tc_mma_f16_ts(tmem + O_COL + 128 * g, tmem + 128 * g + KEYS * (c & 1) + 8u * k, smem_desc_values(base + S::V + slot * S::TILE) + 128u * k,
+                              idesc_o, first && k == 0 ? 0u : 1u, issue);
+            tc_commit_if(o_done(g, c), issue);
             return true;
         };
         for (unsigned id = blockIdx.x; id < items && !failed; id += gridDim.x) {
             const Item x = item_of(a, id);
             if (x.steps == 0) continue;
-            if (!__all_sync(0xffffffffu, mbar_wait(q_full, full_items & 1, abort_flag))) { failed = true; break; }
+            const int steps[2] = {half_steps(x, 0), half_steps(x, 1)};
+            if (!wait_phase(q_full, full_items)) { failed = true; break; }
             ++full_items;
-            if (!scores(n)) { failed = true; break; }
-            for (int j = 0; j < x.steps; ++j, ++n) {
-                if (j + 1 < x.steps && !scores(n + 1)) { failed = true; break; }
-                if (!wait(p_full(n), n)) { failed = true; break; }
-                tc_fence_after();
+            // tile j of the item: its scores first, then the output of the tile before
+            for (int j = 0; j <= x.steps && !failed; ++j) {
+                if (j < x.steps && !wait_phase(kv_full(s_slot), s_walk)) { failed = true; break; }
 #pragma unroll
-                for (int k = 0; k < KEYS / 16; ++k)
-                    tc_mma_f16_ts(tmem + O_COL, tmem + KEYS * (n & 1) + 8u * k, smem_desc_values(base + S::V + (n & 1) * S::TILE) + 128u * k, idesc_o,
-                                  (j | k) != 0 ? 1u : 0u, issue);
-                tc_commit_if(o_done(n), issue);
+                for (int g = 0; g < 2; ++g) {
+                    if (j < steps[g] && !scores(g, n[g])) { failed = true; break; }
+                    if (j > 0 && j <= steps[g] && !output(g, n[g] - 1, j == 1)) { failed = true; break; }
+                    if (j < steps[g]) ++n[g];
+                }
+                if (failed) break;
+                if (j + 1 == x.steps) tc_commit_if(q_free, issue);
+                if (j > 0) {
+                    tc_commit_if(kv_free(slot), issue);
+                    next_slot();
+                }
+                if (j < x.steps && ++s_slot == RING) {
+                    s_slot = 0;
+                    ++s_walk;
+                }
             }
         }
     }
@@ -609,7 +659,7 @@ sqap_status launch_as(const AttnArgs& a, unsigned items, int* status, cudaStream
         return set_max_dynamic_smem(kv_prefill_tc_kernel<T, TYPE, D>, Smem<D>::BYTES);
     });
     if (st != SQAP_OK) return st;
-    const unsigned slots = 2u * static_cast<unsigned>(sm_count());
+    const unsigned slots = static_cast<unsigned>(sm_count());
     return finish_launch(launch_dependent(kv_prefill_tc_kernel<T, TYPE, D>, dim3(items < slots ? items : slots), dim3(THREADS),
                                           Smem<D>::BYTES, s, a, items, status));
 }
