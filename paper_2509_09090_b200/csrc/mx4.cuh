@@ -16,6 +16,21 @@ sqap_status launch_mx4_quantize(const void* x, int x_dtype, int M, int K, int64_
 sqap_status check_mx4_quantize(const void* x, int x_dtype, int M, int K, int64_t ldx, int format, const void* codes,
                                const void* scales);
 
+// One product (arguments checked by the caller). early: the kernel in front of it in the stream is this library's activation
+// quantizer, which lets its dependents start only after its own dependency wait. Whatever wrote the weights has then
+// completed, and they may be fetched while the quantizer still runs. Without it the weights may be the output of the kernel
+// right in front.
+struct Mx4Product {
+    const uint8_t *x_codes, *x_scales, *w_codes, *w_scales;
+    const float *gx, *gw;
+    void* out;
+    int64_t ldo;
+    int M, N, K, format, out_dtype;
+    bool early;
+};
+// The kernel for many tokens (mx4_pair.cu).
+sqap_status launch_mx4_pair(const Mx4Product& q, cudaStream_t s);
+
 inline int type_bytes(int dtype) { return dtype == SQAP_FP32 ? 4 : 2; }
 
 }  // namespace sqap

@@ -29,6 +29,7 @@ using namespace tc;
 constexpr int BM = 128;                   // weight rows per tile
 constexpr int BK = 256;                   // elements of K per stage
 constexpr int BN_MAX = 256;
+constexpr int PAIR_ROWS = 256;            // more tokens than this go to the CTA-pair kernel (mx4_pair.cu)
 constexpr int S_MAX = 10;
 constexpr int KSPLIT_MAX = 8;
 constexpr int A_BYTES = BM * BK / 2;      // 16 KB
@@ -328,24 +329,21 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constan
     }
 }
 
-// early: the kernel in front of this one in the stream is this library's activation quantizer, which lets its dependents
-// start only after its own dependency wait. Whatever wrote the weights has then completed, and they may be fetched
-// while the quantizer still runs. Without it the weights may be the output of the kernel right in front.
-static sqap_status launch(const uint8_t* xc, const uint8_t* xs, int M, const uint8_t* wc, const uint8_t* ws, int N, int K,
-                          int format, const float* gx, const float* gw, void* out, int64_t ldo, int out_dtype, bool early,
-                          cudaStream_t s) {
+static sqap_status launch(const Mx4Product& q, cudaStream_t s) {
+    const int M = q.M, N = q.N, K = q.K, format = q.format;
+    if (M > PAIR_ROWS) return launch_mx4_pair(q, s);
     MxArgs k;
-    k.early = early ? 1 : 0;
-    k.x_sf = xs;
-    k.w_sf = ws;
-    k.gx = format == SQAP_MX_NVFP4 ? gx : nullptr;   // MXFP4 has no scale of the tensor
-    k.gw = format == SQAP_MX_NVFP4 ? gw : nullptr;
-    k.out = out;
-    k.ldo = ldo;
+    k.early = q.early ? 1 : 0;
+    k.x_sf = q.x_scales;
+    k.w_sf = q.w_scales;
+    k.gx = q.gx;
+    k.gw = q.gw;
+    k.out = q.out;
+    k.ldo = q.ldo;
     k.M = M;
     k.N = N;
     k.K = K;
-    k.out_dtype = out_dtype;
+    k.out_dtype = q.out_dtype;
     k.status = device_status_word();
     if (!k.status) return SQAP_ERR_CUDA;
     if (!device_is_sm100()) return SQAP_ERR_UNSUPPORTED;
@@ -388,8 +386,8 @@ static sqap_status launch(const uint8_t* xc, const uint8_t* xs, int M, const uin
     const int smem = ring_bytes + TAIL_BYTES + 1024;
 
     CUtensorMap tm_w, tm_x;
-    if (!make_map(&tm_w, wc, N, K / 2, BM, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !make_map(&tm_x, xc, M, K / 2, k.BN, 128, CU_TENSOR_MAP_SWIZZLE_128B))
+    if (!make_map(&tm_w, q.w_codes, N, K / 2, BM, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !make_map(&tm_x, q.x_codes, M, K / 2, k.BN, 128, CU_TENSOR_MAP_SWIZZLE_128B))
         return SQAP_ERR_CUDA;
     static PerDevice<int> setup;
     const sqap_status st = setup.run([](int*) {
@@ -435,6 +433,12 @@ static sqap_status check(int M, const void* wc, const void* ws, int N, int K, in
     return SQAP_OK;
 }
 
+static Mx4Product product(const uint8_t* xc, const uint8_t* xs, const float* gx, int M, const uint8_t* wc, const uint8_t* ws, const float* gw,
+                          int N, int K, int format, void* out, int64_t ldo, int out_dtype, bool early) {
+    const bool g = format == SQAP_MX_NVFP4;   // MXFP4 has no scale of the tensor
+    return {xc, xs, wc, ws, g ? gx : nullptr, g ? gw : nullptr, out, ldo, M, N, K, format, out_dtype, early};
+}
+
 static size_t codes_bytes(int M, int K) { return (static_cast<size_t>(M) * (K / 2) + 255) / 256 * 256; }
 
 }  // namespace mx4
@@ -455,7 +459,7 @@ extern "C" sqap_status sqap_mx4_linear(const uint8_t* x_codes, const uint8_t* x_
     if (st != SQAP_OK || M == 0) return st;
     if (!x_codes || !x_scales) return SQAP_ERR_INVALID;
     if (!aligned16(x_codes) || !aligned16(x_scales)) return SQAP_ERR_ALIGN;
-    return mx4::launch(x_codes, x_scales, M, w_codes, w_scales, N, K, format, x_tensor_scale, w_tensor_scale, out, ldo, out_dtype, false,
+    return mx4::launch(mx4::product(x_codes, x_scales, x_tensor_scale, M, w_codes, w_scales, w_tensor_scale, N, K, format, out, ldo, out_dtype, false),
                        static_cast<cudaStream_t>(stream));
 }
 
@@ -474,5 +478,5 @@ extern "C" sqap_status sqap_mx4_quantize_linear(const void* x, int x_dtype, int 
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     st = launch_mx4_quantize(x, x_dtype, M, K, ldx, row_index, format, x_tensor_scale, codes, scales, s);
     if (st != SQAP_OK) return st;
-    return mx4::launch(codes, scales, M, w_codes, w_scales, N, K, format, x_tensor_scale, w_tensor_scale, out, ldo, out_dtype, true, s);
+    return mx4::launch(mx4::product(codes, scales, x_tensor_scale, M, w_codes, w_scales, w_tensor_scale, N, K, format, out, ldo, out_dtype, true), s);
 }

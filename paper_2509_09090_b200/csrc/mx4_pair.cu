@@ -1,0 +1,419 @@
+// Product of two microscaled 4-bit matrices for many tokens, on CTA pairs (tcgen05 cta_group::2). Mathematics, operands and scale
+// layout: mx4_linear.cu.
+//
+// A cluster of two CTAs computes 256 x BN tiles (BN 64, 128 or 192 tokens): each CTA holds 128 weight rows and half of the
+// token rows, and the pair's tensor cores share both halves, so an SM fetches 28 KB of codes instead of 40 per 256
+// elements of K at BN = 192; the four-bit MMAs take 384 cycles for that, and fetching is what bounds the kernel. The scales of
+// the tokens are wanted in full by both CTAs (4 KB), those of the weights by their own (2 KB). All loads are TMA boxes whose
+// bytes are counted on the leader's barrier, where the MMAs are issued (the scale tiles go as rows of 512 bytes).
+// Tensor memory (512 columns): two accumulators of 192 columns, so that a tile is stored while the next is computed, and two
+// sets of scale columns.
+//   warp 0     TMA      warp 1  MMA (leader)      warps 2-9  epilogue: four lane quadrants x two halves of the tokens
+// A token tile may start in the middle of a 128-row scale tile (BN = 64, 192): 64 rows are two columns of a tile in tensor
+// memory, so the scales start two columns further on.
+// Every wait on a barrier is bounded; on expiry the kernel records SQAP_ERR_TIMEOUT in the device status word, drains, and
+// returns through the cluster barrier.
+#include "mx4.cuh"
+#include "tc_common.cuh"
+
+namespace sqap {
+namespace mx4p {
+
+using namespace tc;
+
+constexpr int BM = 128;                   // weight rows per CTA
+constexpr int BK = 256;                   // elements of K per stage
+constexpr int BN_MAX = 192;
+constexpr int S = 6;
+constexpr int A_BYTES = BM * BK / 2;      // 16 KB
+constexpr int B_BYTES = BN_MAX / 2 * BK / 2;   // 12 KB: this CTA's half of the tokens
+constexpr int SF_TILE = 512;
+constexpr int SFB_TILES = 2;              // row tiles that a token tile can reach into
+constexpr int OFF_A = 0, OFF_B = OFF_A + S * A_BYTES;
+constexpr int OFF_SFA = OFF_B + S * B_BYTES, SF_BYTES = 4 * SF_TILE;
+constexpr int OFF_SFB = OFF_SFA + S * SF_BYTES;
+constexpr int OFF_STAGE = OFF_SFB + S * SFB_TILES * SF_BYTES;   // staging of the coalesced stores: two halves x two buffers
+constexpr int OFF_BAR = OFF_STAGE + EPI_STAGE_TOTAL;
+constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;
+constexpr int EPI_WARPS = 8;
+constexpr int THREADS = 32 * (2 + EPI_WARPS);
+constexpr int SF_COL = 2 * BN_MAX;        // scale columns: two sets of (4 + 4 x SFB_TILES) columns for each scale tile along K
+constexpr int SET_COLS = 4 * 4 * (1 + SFB_TILES);
+static_assert(SMEM_BYTES <= 227 * 1024 && SF_COL + 2 * SET_COLS <= 512, "budgets");
+static_assert(8 * (2 * S + 4) + 16 <= 256, "barrier block");
+
+struct PairArgs {
+    const float* gx;
+    const float* gw;
+    void* out;
+    int64_t ldo;
+    int M, N, K;
+    int BN, m_tiles, n_tiles;
+    int out_dtype;
+    int k_tiles;
+    int early;
+    int* status;
+};
+
+__device__ __forceinline__ uint32_t cluster_ctarank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t map_to_cta(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// Into this CTA's shared memory; the bytes are counted on a barrier that may live in the peer CTA.
+__device__ __forceinline__ void tma_pair_if(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar_cluster, uint32_t issue) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "@q cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(bar_cluster), "r"(issue)
+        : "memory");
+}
+__device__ __forceinline__ void tc_commit_pair(uint32_t bar, uint32_t issue) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %2, 0;\n\t"
+        "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}"
+        ::"r"(bar), "h"(static_cast<uint16_t>(3)), "r"(issue)
+        : "memory");
+}
+__device__ __forceinline__ uint64_t smem_desc_scales(uint32_t addr) {
+    return static_cast<uint64_t>((addr >> 4) & 0x3FFFu) | (8ull << 32) | (1ull << 46);
+}
+__device__ __forceinline__ void tc_copy_scales(uint32_t taddr, uint64_t desc, uint32_t issue) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %2, 0;\n\t"
+        "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}"
+        ::"r"(taddr), "l"(desc), "r"(issue)
+        : "memory");
+}
+template <int FMT>
+__device__ __forceinline__ void tc_mma_mx4(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                           uint32_t accumulate, uint32_t issue) {
+    if (FMT == SQAP_MX_NVFP4)
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "setp.ne.b32 q, %7, 0;\n\t"
+            "@q tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+            ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(issue)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "setp.ne.b32 q, %7, 0;\n\t"
+            "@q tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+            ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(issue)
+            : "memory");
+}
+
+template <int FMT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
+mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_wsf,
+                const __grid_constant__ CUtensorMap tm_xsf, PairArgs a) {
+    constexpr int TILES = FMT == SQAP_MX_NVFP4 ? 4 : 2;     // scale tiles along K per stage
+    constexpr int PER_TILE = 4 / TILES;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;   // identical in both CTAs of the pair
+    uint8_t* sm = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t bar0 = base + OFF_BAR;
+    auto full = [&](int s) { return bar0 + 8u * s; };                  // leader's: both CTAs' loads of the stage have landed
+    auto done = [&](int s) { return bar0 + 8u * (S + s); };            // the MMAs of the stage in slot s are done (both CTAs)
+    auto acc_full = [&](int b) { return bar0 + 8u * (2 * S + b); };
+    auto acc_empty = [&](int b) { return bar0 + 8u * (2 * S + 2 + b); };   // leader's
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + OFF_BAR + 8 * (2 * S + 4));
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + OFF_BAR + 8 * (2 * S + 4) + 8);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();          // 0 = leader
+    const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+    const int half_bn = a.BN >> 1;
+    const int k_steps = (a.K + BK - 1) / BK;
+    const int total_tiles = a.m_tiles * a.n_tiles;
+    const uint32_t stage_tx = 2u * static_cast<uint32_t>(A_BYTES + half_bn * (BK / 2) + TILES * SF_TILE * (1 + SFB_TILES));
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(done(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(acc_full(b), 1);
+            mbar_init(acc_empty(b), 2 * EPI_WARPS);
+        }
+        abort_flag[0] = 0;
+        abort_flag[1] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(const_cast<uint32_t*>(tmem_slot))) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    pdl_launch_dependents();
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();   // the peer's barriers exist before anything signals them
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    bool failed = false;
+    // first scale-row tile of a token tile, and how many columns into it the tokens start
+    auto sf_row = [&](int m_tile) { return m_tile * a.BN / 128; };
+
+    if (warp == 0) {
+        const uint32_t issue = elect_one();
+        auto weights = [&](int s, int ks, int n_tile, uint32_t bar) {
+            const int nt = 2 * n_tile + static_cast<int>(rank);        // 128-row tile of the weights
+            tma_pair_if(base + OFF_A + s * A_BYTES, &tm_w, ks * (BK / 2), nt * BM, bar, issue);
+            tma_pair_if(base + OFF_SFA + s * SF_BYTES, &tm_wsf, 0, nt * a.k_tiles + ks * TILES, bar, issue);
+        };
+        auto tokens = [&](int s, int ks, int m_tile, uint32_t bar) {
+            tma_pair_if(base + OFF_B + s * B_BYTES, &tm_x, ks * (BK / 2), m_tile * a.BN + static_cast<int>(rank) * half_bn, bar, issue);
+#pragma unroll
+            for (int r = 0; r < SFB_TILES; ++r)
+                tma_pair_if(base + OFF_SFB + (s * SFB_TILES + r) * SF_BYTES, &tm_xsf, 0, (sf_row(m_tile) + r) * a.k_tiles + ks * TILES, bar, issue);
+        };
+        uint32_t early = 0;
+        if (a.early && pair < total_tiles) {
+            early = static_cast<uint32_t>(k_steps < S ? k_steps : S);
+            for (uint32_t ks = 0; ks < early; ++ks) weights(static_cast<int>(ks), static_cast<int>(ks), pair % a.n_tiles, map_to_cta(full(ks), 0));
+        }
+        pdl_wait();
+        uint32_t it = 0;
+        for (int tile = pair; tile < total_tiles && !failed; tile += n_pairs) {
+            const int n_tile = tile % a.n_tiles, m_tile = tile / a.n_tiles;
+            for (int ks = 0; ks < k_steps; ++ks, ++it) {
+                const int s = it % S;
+                if (it >= S && !__all_sync(0xffffffffu, mbar_wait(done(s), (it / S - 1) & 1u, abort_flag))) { failed = true; break; }
+                if (rank == 0) mbar_expect_tx_if(full(s), stage_tx, issue);
+                const uint32_t bar = map_to_cta(full(s), 0);
+                if (it >= early) weights(s, ks, n_tile, bar);
+                tokens(s, ks, m_tile, bar);
+            }
+        }
+        if (failed) {
+            // the loads in flight are counted on the leader's barrier: give them a fixed while to land
+            const long long t0 = clock64();
+            while (clock64() - t0 < 200000) {}
+        }
+    } else if (warp == 1) {
+        pdl_wait();
+        if (rank == 0) {
+            const uint32_t issue = elect_one();
+            const uint32_t idesc = (1u << 7) | (1u << 10) | (static_cast<uint32_t>(a.BN >> 3) << 17) | (FMT == SQAP_MX_MXFP4 ? 1u << 23 : 0u) |
+                                   (static_cast<uint32_t>((2 * BM) >> 4) << 24);
+            uint32_t it = 0, lt = 0;
+            for (int tile = pair; tile < total_tiles && !failed; tile += n_pairs, ++lt) {
+                const int b = lt & 1;
+                if (!__all_sync(0xffffffffu, mbar_wait(acc_empty(b), ((lt >> 1) & 1u) ^ 1u, abort_flag))) { failed = true; break; }
+                tc_fence_after();
+                const uint32_t d = tmem_base + static_cast<uint32_t>(b * BN_MAX);
+                const uint32_t skip = ((tile / a.n_tiles) * a.BN % 128) / 32;      // columns into the first scale tile
+                for (int ks = 0; ks < k_steps; ++ks, ++it) {
+                    const int s = it % S;
+                    if (!__all_sync(0xffffffffu, mbar_wait(full(s), (it / S) & 1u, abort_flag))) { failed = true; break; }
+                    tc_fence_after();
+                    const uint32_t sfa = tmem_base + SF_COL + (it & 1) * SET_COLS, sfb = sfa + 4 * TILES;
+                    const int mmas = a.K - ks * BK >= BK ? 4 : (a.K - ks * BK + 63) / 64;
+                    const int tiles = (mmas + PER_TILE - 1) / PER_TILE;
+                    for (int t = 0; t < tiles; ++t) {
+                        tc_copy_scales(sfa + 4u * t, smem_desc_scales(base + OFF_SFA + s * SF_BYTES + t * SF_TILE), issue);
+#pragma unroll
+                        for (int r = 0; r < SFB_TILES; ++r)
+                            tc_copy_scales(sfb + 4u * (t * SFB_TILES + r),
+                                           smem_desc_scales(base + OFF_SFB + (s * SFB_TILES + r) * SF_BYTES + t * SF_TILE), issue);
+                    }
+                    const uint64_t adesc = smem_desc_sw128(base + OFF_A + s * A_BYTES), bdesc = smem_desc_sw128(base + OFF_B + s * B_BYTES);
+                    for (int k = 0; k < mmas; ++k) {
+                        const int t = k / PER_TILE;
+                        const uint32_t id = FMT == SQAP_MX_MXFP4 ? ((k & 1) ? (2u << 4) | (2u << 29) : 0u) : 0u;
+                        tc_mma_mx4<FMT>(d, adesc + 2u * k, bdesc + 2u * k, idesc | id, sfa + 4u * t, sfb + 4u * SFB_TILES * t + skip,
+                                        (ks | k) != 0 ? 1u : 0u, issue);
+                    }
+                    tc_commit_pair(done(s), issue);
+                }
+                if (failed) break;
+                tc_commit_pair(acc_full(b), issue);
+            }
+        }
+    } else {
+        pdl_wait();
+        const float alpha = __fmul_rn(a.gx ? __ldg(a.gx) : 1.0f, a.gw ? __ldg(a.gw) : 1.0f);
+        const int quad = warp & 3, row = quad * 32 + lane;
+        const int hf = (warp - 2) >> 2, tid_half = static_cast<int>(threadIdx.x) - (2 + 4 * hf) * 32;
+        const int split = ((a.BN / 16 + 1) / 2) * 16;
+        const int c_begin = hf == 0 ? 0 : split, c_end = hf == 0 ? split : a.BN;
+        uint8_t* stage_half = sm + OFF_STAGE + hf * 2 * EPI_STAGE_BYTES;
+        uint32_t lt = 0;
+        for (int tile = pair; tile < total_tiles && !failed; tile += n_pairs, ++lt) {
+            const int b = lt & 1;
+            const int n0 = (tile % a.n_tiles) * (2 * BM) + static_cast<int>(rank) * BM, m0 = (tile / a.n_tiles) * a.BN;
+            // all epilogue warps leave the loop together if any wait ran out, so the barriers below never hang
+            if (bar_or(1, 32 * EPI_WARPS, !mbar_wait(acc_full(b), (lt >> 1) & 1u, abort_flag))) { failed = true; break; }
+            tc_fence_after();
+            const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + static_cast<uint32_t>(b * BN_MAX);
+            int flip = 0;
+            for (int c = c_begin; c < c_end; c += 16, flip ^= 1) {
+                uint32_t v[16];
+                tc_ld16(taddr + c, v);
+                tc_wait_ld();
+                if (a.out_dtype == SQAP_FP32) {                        // a warp's 32 channels of a token are 128 bytes
+                    float* o = static_cast<float*>(a.out) + static_cast<int64_t>(m0 + c) * a.ldo + n0 + row;
+                    if (n0 + row < a.N)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (m0 + c + j < a.M) o[j * a.ldo] = __uint_as_float(v[j]) * alpha;
+                    continue;
+                }
+                uint8_t* stage = stage_half + flip * EPI_STAGE_BYTES;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float y = __uint_as_float(v[j]) * alpha;
+                    *reinterpret_cast<uint16_t*>(stage + j * (BM * 2) + row * 2) = a.out_dtype == SQAP_FP16 ? bits16<SQAP_FP16>(y) : bits16<SQAP_BF16>(y);
+                }
+                // Two buffers in turn: a thread can only be two chunks ahead of the slowest after passing the barrier in between
+                bar_sync_named(2 + hf, 128);
+#pragma unroll
+                for (int p = tid_half; p < 16 * (BM / 8); p += 128) {
+                    const int token = p / (BM / 8), piece = p % (BM / 8);
+                    const int m = m0 + c + token, n = n0 + piece * 8;
+                    if (m < a.M && n < a.N) {
+                        const uint16_t* src = reinterpret_cast<const uint16_t*>(stage + token * (BM * 2) + piece * 16);
+                        uint16_t* dst = static_cast<uint16_t*>(a.out) + static_cast<int64_t>(m) * a.ldo + n;
+                        if (n + 8 <= a.N) {
+                            *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(src);
+                        } else {
+                            for (int e = 0; e < a.N - n; ++e) dst[e] = src[e];
+                        }
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty(b), 0));
+        }
+    }
+
+    if (failed) {
+        *abort_flag = 1;
+        atomicOr(a.status, SQAP_ERR_TIMEOUT);
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();   // neither CTA leaves (or frees tensor memory) while the other may still signal it
+    tc_fence_after();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem_base) : "memory");
+}
+
+// Scale tiles as a matrix of 512-byte rows, boxes of `box_rows` of them.
+static bool make_scale_map(CUtensorMap* m, const void* ptr, uint64_t tiles, uint32_t box_rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {SF_TILE / 4, tiles};
+    const cuuint64_t strides[1] = {SF_TILE};
+    const cuuint32_t box[2] = {SF_TILE / 4, box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int FMT>
+static sqap_status resident_pairs(int* pairs) {
+    static PerDevice<int> setup;
+    const int* p = nullptr;
+    const sqap_status st = setup.run(
+        [](int* out) {
+            const sqap_status s0 = set_max_dynamic_smem(mx4_pair_kernel<FMT>, SMEM_BYTES);
+            if (s0 != SQAP_OK) return s0;
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(static_cast<unsigned>(sm_count() / 2 * 2));
+            cfg.blockDim = dim3(THREADS);
+            cfg.dynamicSmemBytes = SMEM_BYTES;
+            cudaLaunchAttribute attr;
+            attr.id = cudaLaunchAttributeClusterDimension;
+            attr.val.clusterDim.x = 2;
+            attr.val.clusterDim.y = 1;
+            attr.val.clusterDim.z = 1;
+            cfg.attrs = &attr;
+            cfg.numAttrs = 1;
+            int n = 0;
+            if (cudaOccupancyMaxActiveClusters(&n, mx4_pair_kernel<FMT>, &cfg) != cudaSuccess || n <= 0) {
+                cudaGetLastError();
+                n = sm_count() / 2;
+            }
+            *out = n;
+            return SQAP_OK;
+        },
+        &p);
+    if (st == SQAP_OK) *pairs = *p;
+    return st;
+}
+
+}  // namespace mx4p
+
+sqap_status launch_mx4_pair(const Mx4Product& q, cudaStream_t s) {
+    using namespace mx4p;
+    PairArgs k;
+    k.gx = q.gx;
+    k.gw = q.gw;
+    k.out = q.out;
+    k.ldo = q.ldo;
+    k.M = q.M;
+    k.N = q.N;
+    k.K = q.K;
+    k.out_dtype = q.out_dtype;
+    k.early = q.early ? 1 : 0;
+    k.k_tiles = mx4_k_tiles(q.K, q.format);
+    k.status = device_status_word();
+    if (!k.status) return SQAP_ERR_CUDA;
+    if (!device_is_sm100()) return SQAP_ERR_UNSUPPORTED;
+    int pairs = 0;
+    const sqap_status st = q.format == SQAP_MX_NVFP4 ? resident_pairs<SQAP_MX_NVFP4>(&pairs) : resident_pairs<SQAP_MX_MXFP4>(&pairs);
+    if (st != SQAP_OK) return st;
+    k.n_tiles = (q.N + 2 * BM - 1) / (2 * BM);
+    // Tokens per tile: waves of tiles over the pairs x time per stage (what is fetched, at about 75 bytes a clock)
+    double best = -1.0;
+    for (int bn = 64; bn <= BN_MAX; bn += 64) {
+        const int mt = (q.M + bn - 1) / bn;
+        const long tiles = static_cast<long>(mt) * k.n_tiles;
+        const double cost = static_cast<double>((tiles + pairs - 1) / pairs) * (A_BYTES + bn * 64 + 6144);
+        if (best < 0 || cost < best) {
+            best = cost;
+            k.BN = bn;
+            k.m_tiles = mt;
+        }
+    }
+    const uint32_t stage_tiles = q.format == SQAP_MX_NVFP4 ? 4 : 2;
+    CUtensorMap tm_w, tm_x, tm_wsf, tm_xsf;
+    if (!make_map(&tm_w, q.w_codes, q.N, q.K / 2, BM, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !make_map(&tm_x, q.x_codes, q.M, q.K / 2, k.BN / 2, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !make_scale_map(&tm_wsf, q.w_scales, static_cast<uint64_t>((q.N + 127) / 128) * k.k_tiles, stage_tiles) ||
+        !make_scale_map(&tm_xsf, q.x_scales, static_cast<uint64_t>((q.M + 127) / 128) * k.k_tiles, stage_tiles))
+        return SQAP_ERR_CUDA;
+    const int tiles = k.m_tiles * k.n_tiles;
+    if (tiles < pairs) pairs = tiles;
+    const cudaError_t e = q.format == SQAP_MX_NVFP4
+                              ? launch_dependent(mx4_pair_kernel<SQAP_MX_NVFP4>, dim3(2 * pairs), dim3(THREADS), SMEM_BYTES, s, tm_w, tm_x, tm_wsf, tm_xsf, k)
+                              : launch_dependent(mx4_pair_kernel<SQAP_MX_MXFP4>, dim3(2 * pairs), dim3(THREADS), SMEM_BYTES, s, tm_w, tm_x, tm_wsf, tm_xsf, k);
+    if (e != cudaSuccess) {
+        note_cuda_error(e);
+        cudaGetLastError();
+        return SQAP_ERR_CUDA;
+    }
+    count_launch();
+    return check_launch();
+}
+
+}  // namespace sqap
