@@ -226,21 +226,30 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
                     if (!__all_sync(0xffffffffu, mbar_wait(full(s), (it / S) & 1u, abort_flag))) { failed = true; break; }
                     tc_fence_after();
                     const uint32_t sfa = tmem_base + SF_COL + (it & 1) * SET_COLS, sfb = sfa + 4 * TILES;
+                    const uint64_t adesc = smem_desc_sw128(base + OFF_A + s * A_BYTES), bdesc = smem_desc_sw128(base + OFF_B + s * B_BYTES);
+                    const uint64_t da = smem_desc_scales(base + OFF_SFA + s * SF_BYTES), db = smem_desc_scales(base + OFF_SFB + s * SFB_TILES * SF_BYTES);
                     const int mmas = a.K - ks * BK >= BK ? 4 : (a.K - ks * BK + 63) / 64;
-                    const int tiles = (mmas + PER_TILE - 1) / PER_TILE;
-                    for (int t = 0; t < tiles; ++t) {
-                        tc_copy_scales(sfa + 4u * t, smem_desc_scales(base + OFF_SFA + s * SF_BYTES + t * SF_TILE), issue);
+                    // Descriptors count in units of 16 bytes. Whole stages are unrolled: every address is then one addition.
+                    auto scale_tile = [&](int t) {
+                        tc_copy_scales(sfa + 4u * t, da + t * (SF_TILE / 16), issue);
 #pragma unroll
                         for (int r = 0; r < SFB_TILES; ++r)
-                            tc_copy_scales(sfb + 4u * (t * SFB_TILES + r),
-                                           smem_desc_scales(base + OFF_SFB + (s * SFB_TILES + r) * SF_BYTES + t * SF_TILE), issue);
-                    }
-                    const uint64_t adesc = smem_desc_sw128(base + OFF_A + s * A_BYTES), bdesc = smem_desc_sw128(base + OFF_B + s * B_BYTES);
-                    for (int k = 0; k < mmas; ++k) {
+                            tc_copy_scales(sfb + 4u * (t * SFB_TILES + r), db + (r * SF_BYTES + t * SF_TILE) / 16, issue);
+                    };
+                    auto mma = [&](int k) {
                         const int t = k / PER_TILE;
-                        const uint32_t id = FMT == SQAP_MX_MXFP4 ? ((k & 1) ? (2u << 4) | (2u << 29) : 0u) : 0u;
+                        const uint32_t id = FMT == SQAP_MX_MXFP4 && (k & 1) ? (2u << 4) | (2u << 29) : 0u;
                         tc_mma_mx4<FMT>(d, adesc + 2u * k, bdesc + 2u * k, idesc | id, sfa + 4u * t, sfb + 4u * SFB_TILES * t + skip,
                                         (ks | k) != 0 ? 1u : 0u, issue);
+                    };
+                    if (mmas == 4) {
+#pragma unroll
+                        for (int t = 0; t < TILES; ++t) scale_tile(t);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) mma(k);
+                    } else {
+                        for (int t = 0; t < (mmas + PER_TILE - 1) / PER_TILE; ++t) scale_tile(t);
+                        for (int k = 0; k < mmas; ++k) mma(k);
                     }
                     tc_commit_pair(done(s), issue);
                 }
