@@ -331,6 +331,7 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constan
 
 static sqap_status launch(const Mx4Product& q, cudaStream_t s) {
     const int M = q.M, N = q.N, K = q.K, format = q.format;
+    if (mx4_gemv_supports(M, K, format)) return launch_mx4_gemv(q, nullptr, 0, 0, nullptr, s);
     if (M > PAIR_ROWS) return launch_mx4_pair(q, s);
     MxArgs k;
     k.early = q.early ? 1 : 0;
@@ -476,6 +477,9 @@ extern "C" sqap_status sqap_mx4_quantize_linear(const void* x, int x_dtype, int 
     if (st != SQAP_OK || M == 0) return st;
     if (workspace_bytes < sqap_mx4_workspace_bytes(M, N, K, format)) return SQAP_ERR_NOMEM;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (mx4_gemv_supports(M, K, format))   // quantizes its few rows itself
+        return launch_mx4_gemv(mx4::product(nullptr, nullptr, x_tensor_scale, M, w_codes, w_scales, w_tensor_scale, N, K, format, out, ldo, out_dtype, false),
+                               x, x_dtype, ldx, row_index, s);
     st = launch_mx4_quantize(x, x_dtype, M, K, ldx, row_index, format, x_tensor_scale, codes, scales, s);
     if (st != SQAP_OK) return st;
     return mx4::launch(mx4::product(codes, scales, x_tensor_scale, M, w_codes, w_scales, w_tensor_scale, N, K, format, out, ldo, out_dtype, true), s);
