@@ -8,9 +8,10 @@
 // (the code's sign) replaces the byte by its sign bit, 0 here, so one permute gives the positive codes and a second, with the
 // signs flipped, the negative ones.
 // The tokens are quantized by every CTA itself (a few hundred instructions, while its first weights travel) where the call
-// brings them as rows; they lie in shared memory as int8, with their scales.
-// Rows: a 32-byte sector of the scale tiles holds rows r, r + 1 and those 32, 64 and 96 further down, so a CTA of four warps takes
-// those eight, a warp two of them (which share the tokens' reads).
+// brings them as rows; they lie in shared memory as int8, with their scales. Two CTAs to an SM walk the rows, so that this is
+// done once for many of them.
+// Rows: a 32-byte sector of the scale tiles holds rows r, r + 1 and those 32, 64 and 96 further down, so four warps take those
+// eight together, a warp two of them (which share the tokens' reads).
 #include <type_traits>
 
 #include "mx4_device.cuh"
@@ -18,7 +19,7 @@
 namespace sqap {
 namespace mx4v {
 
-constexpr int WARPS = 4, THREADS = 32 * WARPS;
+constexpr int WARPS = 8, TEAMS = WARPS / 4, THREADS = 32 * WARPS;   // a team of four warps takes eight rows
 constexpr int AHEAD = 4;               // steps (1024 elements: 32 a lane, one 16-byte load per row) whose loads are in flight together
 
 struct GemvArgs {
@@ -51,7 +52,7 @@ __device__ __forceinline__ uint2 codes_to_int8(uint32_t w) {
 
 // T = void: the tokens come as codes and scales.
 template <typename T, int FMT, int MM>
-__global__ void __launch_bounds__(THREADS) mx4_gemv_kernel(GemvArgs a) {
+__global__ void __launch_bounds__(THREADS, 2) mx4_gemv_kernel(GemvArgs a) {
     constexpr int BLK = FMT == SQAP_MX_NVFP4 ? 16 : 32;
     extern __shared__ uint8_t smem[];
     const int K = a.K, groups = K / 32;                  // 32 elements: a lane's share of a step
@@ -63,17 +64,25 @@ __global__ void __launch_bounds__(THREADS) mx4_gemv_kernel(GemvArgs a) {
     pdl_launch_dependents();
     pdl_wait();
 
-    // this warp's rows
-    const int tile = blockIdx.x >> 4, r = (blockIdx.x & 15) * 2 + warp * 32;
-    const int n0 = tile * 128 + r;
-    const bool live0 = n0 < a.N, live1 = n0 + 1 < a.N;
-    const uint4* w0 = reinterpret_cast<const uint4*>(a.w_codes + static_cast<size_t>(live0 ? n0 : 0) * (K / 2));
-    const uint4* w1 = reinterpret_cast<const uint4*>(a.w_codes + static_cast<size_t>(live1 ? n0 + 1 : 0) * (K / 2));
-    // scale bytes of rows r and r + 1 of the tile: 16 bytes apart
-    const uint8_t* sc = a.w_scales + static_cast<size_t>(tile) * a.k_tiles * 512 + (r & 31) * 16 + (r >> 5) * 4;
+    // The rows of this team, eight at a time; this warp's share r, r + 1 of a 128-row tile. Loads run AHEAD steps in front of
+    // the sums, across the change of rows.
+    const int total = (a.N + 127) / 128 * 16, steps = (groups + 31) / 32;
+    const int stride = gridDim.x * TEAMS, team = blockIdx.x * TEAMS + (warp >> 2);
     uint4 c[AHEAD][2];
     uint32_t s[AHEAD][2];
-    auto fetch = [&](int i, int g) {                    // g: the lane's 32 elements
+    int f_rows = team, f_step = 0;                       // what is fetched next
+    const uint4 *w0 = nullptr, *w1 = nullptr;
+    const uint8_t* sc = nullptr;
+    auto aim = [&]() {
+        const int tile = f_rows >> 4, r = (f_rows & 15) * 2 + (warp & 3) * 32, n0 = tile * 128 + r;
+        w0 = reinterpret_cast<const uint4*>(a.w_codes + static_cast<size_t>(n0 < a.N ? n0 : 0) * (K / 2));
+        w1 = reinterpret_cast<const uint4*>(a.w_codes + static_cast<size_t>(n0 + 1 < a.N ? n0 + 1 : 0) * (K / 2));
+        // scale bytes of rows r and r + 1 of the tile: 16 bytes apart
+        sc = a.w_scales + static_cast<size_t>(tile) * a.k_tiles * 512 + (r & 31) * 16 + (r >> 5) * 4;
+    };
+    auto fetch = [&](int i) {
+        if (f_rows >= total) return;
+        const int g = lane + 32 * f_step;                // the lane's 32 elements
         if (g < groups) {
             c[i][0] = __ldg(w0 + g);
             c[i][1] = __ldg(w1 + g);
@@ -87,9 +96,15 @@ __global__ void __launch_bounds__(THREADS) mx4_gemv_kernel(GemvArgs a) {
                 s[i][1] = __ldg(p + 16);
             }
         }
+        if (++f_step == steps) {
+            f_step = 0;
+            f_rows += stride;
+            if (f_rows < total) aim();
+        }
     };
+    if (f_rows < total) aim();
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) fetch(i, lane + 32 * i);
+    for (int i = 0; i < AHEAD; ++i) fetch(i);
 
     // the tokens
     const float gs = a.gx ? __ldg(a.gx) : 1.0f;
@@ -123,12 +138,15 @@ __global__ void __launch_bounds__(THREADS) mx4_gemv_kernel(GemvArgs a) {
     }
     __syncthreads();
 
+    const float alpha = (FMT == SQAP_MX_NVFP4 ? __fmul_rn(gs, a.gw ? __ldg(a.gw) : 1.0f) : 1.0f) * 0.25f;
     float acc[2][MM] = {};
-    for (int g0 = lane; g0 < groups; g0 += 32 * AHEAD) {
+    int rows = team, step = 0;
+    while (rows < total) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            const int g = g0 + 32 * i;
-            if (g >= groups) break;
+            if (rows >= total) break;
+            const int g = lane + 32 * step;
+            if (g < groups) {
             uint4 xl[MM], xh[MM];
 #pragma unroll
             for (int m = 0; m < MM; ++m) {
@@ -181,25 +199,30 @@ __global__ void __launch_bounds__(THREADS) mx4_gemv_kernel(GemvArgs a) {
                         acc[row][m] = fmaf(static_cast<float>(dot[m][0] + dot[m][1]) * xs[m * (K / 32) + g], s0, acc[row][m]);
                 }
             }
-            fetch(i, g + 32 * AHEAD);
+            }
+            fetch(i);
+            if (++step < steps) continue;
+            const int n0 = (rows >> 4) * 128 + (rows & 15) * 2 + (warp & 3) * 32;
+#pragma unroll
+            for (int row = 0; row < 2; ++row)
+#pragma unroll
+                for (int m = 0; m < MM; ++m) {
+                    float y = acc[row][m];
+                    acc[row][m] = 0.0f;
+#pragma unroll
+                    for (int o = 16; o; o >>= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
+                    if (lane == 0 && n0 + row < a.N) {
+                        y *= alpha;
+                        const int64_t at = m * a.ldo + n0 + row;
+                        if (a.out_dtype == SQAP_FP16) static_cast<__half*>(a.out)[at] = __float2half_rn(y);
+                        else if (a.out_dtype == SQAP_BF16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(y);
+                        else static_cast<float*>(a.out)[at] = y;
+                    }
+                }
+            step = 0;
+            rows += stride;
         }
     }
-    const float alpha = (FMT == SQAP_MX_NVFP4 ? __fmul_rn(gs, a.gw ? __ldg(a.gw) : 1.0f) : 1.0f) * 0.25f;
-#pragma unroll
-    for (int row = 0; row < 2; ++row)
-#pragma unroll
-        for (int m = 0; m < MM; ++m) {
-            float y = acc[row][m];
-#pragma unroll
-            for (int o = 16; o; o >>= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
-            if (lane == 0 && (row ? live1 : live0)) {
-                y *= alpha;
-                const int64_t at = m * a.ldo + n0 + row;
-                if (a.out_dtype == SQAP_FP16) static_cast<__half*>(a.out)[at] = __float2half_rn(y);
-                else if (a.out_dtype == SQAP_BF16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(y);
-                else static_cast<float*>(a.out)[at] = y;
-            }
-        }
 }
 
 template <typename T, int FMT, int MM>
@@ -208,7 +231,8 @@ static sqap_status launch_as(const GemvArgs& a, cudaStream_t s) {
     const sqap_status st = setup.run([](int*) { return set_max_dynamic_smem(mx4_gemv_kernel<T, FMT, MM>, 227 * 1024); });
     if (st != SQAP_OK) return st;
     const size_t smem = static_cast<size_t>(MM) * a.K + static_cast<size_t>(MM) * (a.K / mx4_block(FMT)) * sizeof(float);
-    const unsigned grid = static_cast<unsigned>((a.N + 127) / 128) * 16u;
+    const unsigned teams = static_cast<unsigned>((a.N + 127) / 128) * 16u, most = 2u * static_cast<unsigned>(sm_count());
+    const unsigned grid = teams / TEAMS < most ? teams / TEAMS : most;
     const cudaError_t e = launch_dependent(mx4_gemv_kernel<T, FMT, MM>, dim3(grid), dim3(THREADS), smem, s, a);
     if (e != cudaSuccess) {
         note_cuda_error(e);
