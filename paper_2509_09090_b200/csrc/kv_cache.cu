@@ -10,6 +10,7 @@ namespace kv {
 namespace {
 
 constexpr int THREADS = 128;
+constexpr int HELD = 8;      // 16-byte pieces that a thread keeps between the two passes
 
 // Maximum over the block, known to every thread.
 __device__ __forceinline__ float block_max(float v, float* red) {
@@ -72,14 +73,26 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(AppendArgs a) {
     const T* row0 = src + (static_cast<int64_t>(first_row) + (t0 - start)) * ld;
     const int items = (t1 - t0) * per_row;
 
+    // The new tokens' share of a thread: kept in registers where it is small enough (the usual pages), read again otherwise.
+    auto source = [&](int i) { return __ldg(reinterpret_cast<const uint4*>(row0 + (i / per_row) * ld) + i % per_row); };
+    uint4 held[HELD];
     float amax = 0.0f;
-    for (int i = threadIdx.x; i < items; i += THREADS) {
-        float v[8];
-        unpack8<T>(__ldg(reinterpret_cast<const uint4*>(row0 + (i / per_row) * ld) + i % per_row), v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(v[e]));
+    for (int q = 0; q < HELD; ++q) {
+        const int i = threadIdx.x + q * THREADS;
+        held[q] = make_uint4(0, 0, 0, 0);
+        if (i < items) held[q] = source(i);
     }
     const float before = t0 > lo ? *scale_at : 0.0f;        // tokens in front of the new ones keep their place
+    auto widen = [&](uint4 u) {
+        float v[8];
+        unpack8<T>(u, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(v[e]));
+    };
+#pragma unroll
+    for (int q = 0; q < HELD; ++q) widen(held[q]);
+    for (int i = threadIdx.x + HELD * THREADS; i < items; i += THREADS) widen(source(i));
     amax = block_max(amax, red);                            // (every thread has read *scale_at before thread 0 writes it)
     const float scale = fmaxf(before, scale_for<TYPE>(amax));
     if (threadIdx.x == 0) *scale_at = scale;
@@ -96,13 +109,17 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(AppendArgs a) {
     }
     const float inv = inverse_of(scale);
     uint2* to = reinterpret_cast<uint2*>(codes + static_cast<int64_t>(t0 - lo) * D);
-    for (int i = threadIdx.x; i < items; i += THREADS) {
+    auto write = [&](int i, uint4 u) {
         float v[8];
-        unpack8<T>(__ldg(reinterpret_cast<const uint4*>(row0 + (i / per_row) * ld) + i % per_row), v);
+        unpack8<T>(u, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = __fmul_rn(v[e], inv);
         to[i] = encode8<TYPE>(v);
-    }
+    };
+#pragma unroll
+    for (int q = 0; q < HELD; ++q)
+        if (threadIdx.x + q * THREADS < items) write(threadIdx.x + q * THREADS, held[q]);
+    for (int i = threadIdx.x + HELD * THREADS; i < items; i += THREADS) write(i, source(i));
 }
 
 struct ReadArgs {
@@ -117,33 +134,55 @@ struct ReadArgs {
     int64_t ldk, ldv;
 };
 
-// One CTA = one token of one sequence, all heads, keys and values.
+// One warp = one token of one sequence, keys or values, of 16 codes a lane and step; up to four steps' loads in flight.
 template <typename T, int TYPE>
-__global__ void __launch_bounds__(THREADS) kv_read_kernel(ReadArgs a) {
+__global__ void __launch_bounds__(THREADS) kv_read_kernel(ReadArgs a, unsigned total) {
     pdl_launch_dependents();
     pdl_wait();
     const Cache& c = a.c;
-    const int b = blockIdx.x / a.max_rows, i = blockIdx.x % a.max_rows;
-    const int r0 = a.cu[b];
-    if (i >= a.cu[b + 1] - r0) return;
+    const unsigned id = blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
+    if (id >= total) return;
+    const int which = id & 1, lane = threadIdx.x & 31;
+    const int b = static_cast<int>((id >> 1) / a.max_rows), i = static_cast<int>((id >> 1) % a.max_rows);
+    T* out = static_cast<T*>(which ? a.v : a.k);
+    const int r0 = a.cu[b], r1 = a.cu[b + 1];
     const int64_t pos = static_cast<int64_t>(a.first ? a.first[b] : 0) + i, j = pos >> c.page_shift;
-    const int D = c.head_dim, per_row = D / 8;
+    if (!out || i >= r1 - r0) return;
+    const int D = c.head_dim, pieces = c.kv_heads * D / 16;
     const int page = pos >= 0 && j < a.ldt ? checked_page(c, a.table[b * a.ldt + j]) : -1;
     const int t = static_cast<int>(pos) & ((1 << c.page_shift) - 1);
-    const int items = c.kv_heads * per_row;
-    for (int x = threadIdx.x; x < 2 * items; x += THREADS) {
-        const int which = x >= items, y = which ? x - items : x, h = y / per_row, e = y % per_row;
-        const Half half = which ? c.v : c.k;
-        T* out = static_cast<T*>(which ? a.v : a.k);
-        if (!out) continue;
-        float v[8] = {};
-        if (page >= 0) {
-            const float s = __ldg(half.scales + static_cast<int64_t>(page) * c.kv_heads + h);
-            decode8<TYPE>(__ldg(reinterpret_cast<const uint2*>(half.codes + (page_codes(c, page, h) + t) * D) + e), v);
+    const Half half = which ? c.v : c.k;
+    const int dshift = 31 - __clz(D / 16);                   // pieces per head, a power of two
+    const float* scales = half.scales + static_cast<int64_t>(page) * c.kv_heads;
+    const uint8_t* codes = half.codes + (page_codes(c, page, 0) + t) * D;
+    const int64_t head_stride = static_cast<int64_t>(D) << c.page_shift;
+    uint4* to = reinterpret_cast<uint4*>(out + (static_cast<int64_t>(r0) + i) * (which ? a.ldv : a.ldk));
+    for (int x0 = lane; x0 < pieces; x0 += 128) {
+        uint4 u[4];
+        float s[4];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] = __fmul_rn(v[q], s);
+        for (int q = 0; q < 4; ++q) {
+            const int x = x0 + 32 * q, h = x >> dshift;
+            u[q] = make_uint4(0, 0, 0, 0);
+            s[q] = 0.0f;                                     // a missing page reads as zero
+            if (page >= 0 && x < pieces) {
+                u[q] = __ldg(reinterpret_cast<const uint4*>(codes + h * head_stride + (x - (h << dshift)) * 16));
+                s[q] = __ldg(scales + h);
+            }
         }
-        *(reinterpret_cast<uint4*>(out + (static_cast<int64_t>(r0) + i) * (which ? a.ldv : a.ldk)) + y) = pack8<T>(v);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int x = x0 + 32 * q;
+            if (x >= pieces) break;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                decode8<TYPE>(e ? make_uint2(u[q].z, u[q].w) : make_uint2(u[q].x, u[q].y), v);
+#pragma unroll
+                for (int f = 0; f < 8; ++f) v[f] = __fmul_rn(v[f], s[q]);
+                to[2 * x + e] = pack8<T>(v);
+            }
+        }
     }
 }
 
@@ -204,7 +243,7 @@ __global__ void __launch_bounds__(THREADS) kv_compact_kernel(CompactArgs a) {
     const int h = static_cast<int>(id % c.kv_heads);
     id /= c.kv_heads;
     const int slot = static_cast<int>(id % a.slots), i = static_cast<int>(id / a.slots);
-    const int P = 1 << c.page_shift, D = c.head_dim, per_row = D / 8;
+    const int P = 1 << c.page_shift, D = c.head_dim;
     int n = a.n_kept[i];
     n = n < 0 ? 0 : (n > a.max_kept ? a.max_kept : n);
     const int lo = slot << c.page_shift;
@@ -230,31 +269,54 @@ __global__ void __launch_bounds__(THREADS) kv_compact_kernel(CompactArgs a) {
         of[threadIdx.x] = s;
     }
     __syncthreads();
-    float amax = 0.0f;
-    const int items = P * per_row;
-    for (int x = threadIdx.x; x < items; x += THREADS) {
-        const int t = x / per_row;
-        if (at[t] < 0) continue;
-        float v[8];
-        decode8<TYPE>(__ldg(reinterpret_cast<const uint2*>(half.codes + at[t] * D) + x % per_row), v);
+    // 16 codes a piece: at most 16 pieces a thread, of which HELD / 2 stay in registers between the two passes
+    const int per16 = D / 16, items = P * per16;
+    auto source = [&](int x) {
+        const int64_t where = at[x / per16];
+        return where < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(half.codes + where * D) + x % per16);
+    };
+    uint4 held[HELD / 2];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(__fmul_rn(v[e], of[t])));
+    for (int q = 0; q < HELD / 2; ++q) {
+        const int x = threadIdx.x + q * THREADS;
+        held[q] = make_uint4(0, 0, 0, 0);
+        if (x < items) held[q] = source(x);
     }
+    float amax = 0.0f;
+    auto widen = [&](int x, uint4 u) {
+        const float s = of[x / per16];
+        float v[8];
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            decode8<TYPE>(f ? make_uint2(u.z, u.w) : make_uint2(u.x, u.y), v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(__fmul_rn(v[e], s)));
+        }
+    };
+#pragma unroll
+    for (int q = 0; q < HELD / 2; ++q)
+        if (threadIdx.x + q * THREADS < items) widen(threadIdx.x + q * THREADS, held[q]);
+    for (int x = threadIdx.x + HELD / 2 * THREADS; x < items; x += THREADS) widen(x, source(x));
     const float scale = scale_for<TYPE>(block_max(amax, red)), inv = inverse_of(scale);
     if (threadIdx.x == 0) half.scales[static_cast<int64_t>(page) * c.kv_heads + h] = scale;
-    uint2* to = reinterpret_cast<uint2*>(half.codes + page_codes(c, page, h) * D);
-    for (int x = threadIdx.x; x < items; x += THREADS) {
-        const int t = x / per_row;
-        uint2 r = make_uint2(0, 0);
-        if (at[t] >= 0) {
-            float v[8];
-            decode8<TYPE>(__ldg(reinterpret_cast<const uint2*>(half.codes + at[t] * D) + x % per_row), v);
+    uint4* to = reinterpret_cast<uint4*>(half.codes + page_codes(c, page, h) * D);
+    auto write = [&](int x, uint4 u) {
+        const float s = of[x / per16];
+        float v[8];
+        uint2 r[2];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = __fmul_rn(__fmul_rn(v[e], of[t]), inv);
-            r = encode8<TYPE>(v);
+        for (int f = 0; f < 2; ++f) {
+            decode8<TYPE>(f ? make_uint2(u.z, u.w) : make_uint2(u.x, u.y), v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = __fmul_rn(__fmul_rn(v[e], s), inv);
+            r[f] = encode8<TYPE>(v);
         }
-        to[x] = r;
-    }
+        to[x] = make_uint4(r[0].x, r[0].y, r[1].x, r[1].y);
+    };
+#pragma unroll
+    for (int q = 0; q < HELD / 2; ++q)
+        if (threadIdx.x + q * THREADS < items) write(threadIdx.x + q * THREADS, held[q]);
+    for (int x = threadIdx.x + HELD / 2 * THREADS; x < items; x += THREADS) write(x, source(x));
 }
 
 constexpr int64_t MAX_GRID = 0x7FFFFFFF;
@@ -265,9 +327,10 @@ cudaError_t append_as(const AppendArgs& a, int type, unsigned grid, cudaStream_t
     return launch_dependent(kv_append_kernel<T, SQAP_KV_E4M3>, dim3(grid), dim3(THREADS), 0, s, a);
 }
 template <typename T>
-cudaError_t read_as(const ReadArgs& a, int type, unsigned grid, cudaStream_t s) {
-    if (type == SQAP_KV_INT8) return launch_dependent(kv_read_kernel<T, SQAP_KV_INT8>, dim3(grid), dim3(THREADS), 0, s, a);
-    return launch_dependent(kv_read_kernel<T, SQAP_KV_E4M3>, dim3(grid), dim3(THREADS), 0, s, a);
+cudaError_t read_as(const ReadArgs& a, int type, unsigned total, cudaStream_t s) {
+    const dim3 grid((total + THREADS / 32 - 1) / (THREADS / 32));
+    if (type == SQAP_KV_INT8) return launch_dependent(kv_read_kernel<T, SQAP_KV_INT8>, grid, dim3(THREADS), 0, s, a, total);
+    return launch_dependent(kv_read_kernel<T, SQAP_KV_E4M3>, grid, dim3(THREADS), 0, s, a, total);
 }
 
 }  // namespace
@@ -311,7 +374,7 @@ extern "C" sqap_status sqap_kv_read(const sqap_kv_cache* cache, const int32_t* t
     if ((k && ldk % 8 != 0) || (v && ldv % 8 != 0) || !aligned16(k) || !aligned16(v)) return SQAP_ERR_ALIGN;
     if (batch == 0 || max_rows == 0 || (!k && !v)) return SQAP_OK;
     if (!cu_rows || (ldt > 0 && !table)) return SQAP_ERR_INVALID;
-    const int64_t grid = static_cast<int64_t>(batch) * max_rows;
+    const int64_t grid = 2 * static_cast<int64_t>(batch) * max_rows;        // warps
     if (grid > MAX_GRID) return SQAP_ERR_UNSUPPORTED;
     const ReadArgs a = {device_view(cache), table, ldt, first, cu_rows, max_rows, k, v, ldk, ldv};
     cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -63,9 +63,8 @@ __device__ __forceinline__ void word_to_half2x2(uint32_t w, uint32_t* lo, uint32
     }
 }
 
-template <typename T, int TYPE, int D, int NT>
+template <typename T, int TYPE, int D, int NT, int GROUPS>
 __global__ void __launch_bounds__(WARPS * 32) kv_decode_kernel(AttnArgs a) {
-    constexpr int GROUPS = D == 256 ? 1 : 2;       // 16-token groups per step
     constexpr int STEP = 16 * GROUPS;
     constexpr int KC = D / 64;                     // 16-byte chunks of a key row per lane
     constexpr int VB = D / 8;                      // bytes of a value row per lane
@@ -143,34 +142,42 @@ __global__ void __launch_bounds__(WARPS * 32) kv_decode_kernel(AttnArgs a) {
     }
     const int32_t* table = a.table + w.b * a.ldt;
     const int shift = a.c.page_shift, mask = (1 << shift) - 1;
-    auto page_at = [&](int key) {
-        const int j = key >> shift;
-        return key < end && j < a.ldt ? checked_page(a.c, __ldg(table + j)) : -1;
-    };
 
-    int next_page[GROUPS];
-#pragma unroll
-    for (int u = 0; u < GROUPS; ++u) next_page[u] = page_at(key0 + warp * STEP + 16 * u);
-    for (int k0 = key0 + warp * STEP; k0 < end; k0 += WARPS * STEP) {
-        int page[GROUPS];
-        Bytes<16> kw[GROUPS][2][KC];
-        Bytes<VB> vw[GROUPS][4];
-        float ks[GROUPS], vs[GROUPS];
+    // A step's loads are issued as soon as their registers are free: the next keys during this step's softmax, the next values
+    // at its end, the pages' numbers a step earlier still.
+    int entry[GROUPS], page[GROUPS] = {};
+    Bytes<16> kw[GROUPS][2][KC];
+    Bytes<VB> vw[GROUPS][4];
+    float ks[GROUPS], vs[GROUPS];
+    auto entries = [&](int k0) {
 #pragma unroll
         for (int u = 0; u < GROUPS; ++u) {
-            page[u] = next_page[u];
-            const int safe = page[u] < 0 ? 0 : page[u];        // a page that does not exist is read as page 0 and masked
-            const int64_t tok = page_codes(a.c, safe, w.h) + ((k0 + 16 * u) & mask);
-            const uint8_t* kp = a.c.k.codes + (tok + g) * D + 16 * t;
-            const uint8_t* vp = a.c.v.codes + (tok + 2 * t) * D + (VB > 16 ? 16 : VB) * g;
+            const int key = k0 + 16 * u, j = key >> shift;
+            entry[u] = -1;
+            if (key < end && j < a.ldt) entry[u] = __ldg(table + j);
+        }
+    };
+    // a page that does not exist is read as page 0 and masked
+    auto token_at = [&](int k0, int u) { return page_codes(a.c, max(page[u], 0), w.h) + ((k0 + 16 * u) & mask); };
+    auto load_keys = [&](int k0) {
+#pragma unroll
+        for (int u = 0; u < GROUPS; ++u) {
+            page[u] = checked_page(a.c, entry[u]);
+            const uint8_t* kp = a.c.k.codes + (token_at(k0, u) + g) * D + 16 * t;
 #pragma unroll
             for (int c = 0; c < KC; ++c) {
                 kw[u][0][c] = load_bytes<16>(kp + 64 * c);
                 kw[u][1][c] = load_bytes<16>(kp + 8 * D + 64 * c);
             }
-            const int64_t s = static_cast<int64_t>(safe) * a.c.kv_heads + w.h;
+            const int64_t s = static_cast<int64_t>(max(page[u], 0)) * a.c.kv_heads + w.h;
             ks[u] = __ldg(a.c.k.scales + s);
             vs[u] = __ldg(a.c.v.scales + s);
+        }
+    };
+    auto load_values = [&](int k0) {
+#pragma unroll
+        for (int u = 0; u < GROUPS; ++u) {
+            const uint8_t* vp = a.c.v.codes + (token_at(k0, u) + 2 * t) * D + (VB > 16 ? 16 : VB) * g;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint8_t* p = vp + ((i & 1) + (i >> 1) * 8) * D;
@@ -186,9 +193,16 @@ __global__ void __launch_bounds__(WARPS * 32) kv_decode_kernel(AttnArgs a) {
                 }
             }
         }
-#pragma unroll
-        for (int u = 0; u < GROUPS; ++u) next_page[u] = page_at(k0 + WARPS * STEP + 16 * u);
-
+    };
+    const int first = key0 + warp * STEP;
+    if (first < end) {
+        entries(first);
+        load_keys(first);
+        load_values(first);
+        entries(first + WARPS * STEP);
+    }
+    for (int k0 = first; k0 < end; k0 += WARPS * STEP) {
+        const bool more = k0 + WARPS * STEP < end;
         // scores
         float sc[GROUPS][NT][4];
 #pragma unroll
@@ -208,8 +222,18 @@ __global__ void __launch_bounds__(WARPS * 32) kv_decode_kernel(AttnArgs a) {
                     for (int n = 0; n < NT; ++n) mma_16816(sc[u][n], af, qf[n][c][j][0], qf[n][c][j][1]);
                 }
         }
+        // (the page and scales of this step, before the next step's take their place)
+        bool there[GROUPS];
+        float this_ks[GROUPS], lv[GROUPS], iv[GROUPS];
+#pragma unroll
+        for (int u = 0; u < GROUPS; ++u) {
+            there[u] = page[u] >= 0;
+            this_ks[u] = ks[u];
+            lv[u] = __log2f(vs[u] > 0.0f ? vs[u] : ZERO_PAGE_SCALE);
+            iv[u] = fast_exp2(-lv[u]);             // the reciprocal of what lv stands for: the weights use lv
+        }
+        if (more) load_keys(k0 + WARPS * STEP);
         // scale, mask, maximum
-        float lv[GROUPS], iv[GROUPS];
         float top[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -218,24 +242,21 @@ __global__ void __launch_bounds__(WARPS * 32) kv_decode_kernel(AttnArgs a) {
         }
 #pragma unroll
         for (int u = 0; u < GROUPS; ++u) {
-            const float x = vs[u] > 0.0f ? vs[u] : ZERO_PAGE_SCALE;
-            lv[u] = __log2f(x);
-            iv[u] = fast_exp2(-lv[u]);             // the reciprocal of what lv stands for, not of x: the weights use lv
             const int base = k0 + 16 * u;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int key = base + g + (e >> 1) * 8;
-                    const bool seen = page[u] >= 0 && key < min(lim[n][e & 1], end);
-                    sc[u][n][e] = seen ? fmaf(sc[u][n][e], fac[n][e & 1] * ks[u], lv[u]) : -INFINITY;
+                    const bool seen = there[u] && key < min(lim[n][e & 1], end);
+                    sc[u][n][e] = seen ? fmaf(sc[u][n][e], fac[n][e & 1] * this_ks[u], lv[u]) : -INFINITY;
                     top[n][e & 1] = fmaxf(top[n][e & 1], sc[u][n][e]);
                 }
-            if (page[u] < 0 || base + 16 > end) {
+            if (!there[u] || base + 16 > end) {
                 // what lies behind the end of a history may be anything, not-a-numbers included: weight 0 is not enough
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (page[u] < 0 || base + 2 * t + (i & 1) + (i >> 1) * 8 >= end)
+                    if (!there[u] || base + 2 * t + (i & 1) + (i >> 1) * 8 >= end)
 #pragma unroll
                         for (int q = 0; q < VB / 4; ++q) vw[u][i].w[q] = 0;
             }
@@ -291,6 +312,10 @@ __global__ void __launch_bounds__(WARPS * 32) kv_decode_kernel(AttnArgs a) {
                     for (int n = 0; n < NT; ++n) mma_16816(o[n][2 * q + p], af, pf[u][n][0], pf[u][n][1]);
                 }
             }
+        if (more) {
+            load_values(k0 + WARPS * STEP);
+            entries(k0 + 2 * WARPS * STEP);
+        }
     }
 
     // the warps of the CTA meet
@@ -351,9 +376,10 @@ __global__ void __launch_bounds__(WARPS * 32) kv_decode_kernel(AttnArgs a) {
 
 template <typename T, int TYPE, int D>
 cudaError_t launch_rows(const AttnArgs& a, unsigned grid, cudaStream_t s) {
-    if (static_cast<int64_t>(a.max_q) * a.group <= 8) return launch_dependent(kv_decode_kernel<T, TYPE, D, 1>, dim3(grid), dim3(WARPS * 32), 0, s, a);
+    constexpr int GROUPS = D == 256 ? 1 : 2;       // 16-token groups per step
+    if (static_cast<int64_t>(a.max_q) * a.group <= 8) return launch_dependent(kv_decode_kernel<T, TYPE, D, 1, GROUPS>, dim3(grid), dim3(WARPS * 32), 0, s, a);
     if (D == 256) return cudaErrorInvalidValue;     // not reached: see decode_max_rows()
-    return launch_dependent(kv_decode_kernel<T, TYPE, D == 256 ? 128 : D, 2>, dim3(grid), dim3(WARPS * 32), 0, s, a);
+    return launch_dependent(kv_decode_kernel<T, TYPE, D == 256 ? 128 : D, 2, GROUPS>, dim3(grid), dim3(WARPS * 32), 0, s, a);
 }
 template <typename T, int TYPE>
 cudaError_t launch_dim(const AttnArgs& a, unsigned grid, cudaStream_t s) {
