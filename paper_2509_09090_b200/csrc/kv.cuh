@@ -1,6 +1,8 @@
 // Internal: the paged 8-bit key/value cache as the kernels see it, conversions and checks.
 #pragma once
 
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace sqap {
@@ -106,21 +108,36 @@ __device__ __forceinline__ void decode8(uint2 w, float* v) {
         v[4 * i + 3] = g.y;
     }
 }
-// Eight numbers, already divided by the scale -> eight codes.
+// Largest magnitude of eight 16-bit floats, as a pair to be folded by the caller; exact, a NaN loses.
+template <typename T>
+__device__ __forceinline__ void widen8(uint4 u, uint32_t* top) {
+    const uint32_t w[4] = {u.x & 0x7FFF7FFFu, u.y & 0x7FFF7FFFu, u.z & 0x7FFF7FFFu, u.w & 0x7FFF7FFFu};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (std::is_same<T, __half>::value) asm("max.f16x2 %0, %0, %1;" : "+r"(*top) : "r"(w[i]));
+        else asm("max.bf16x2 %0, %0, %1;" : "+r"(*top) : "r"(w[i]));
+    }
+}
+template <typename T>
+__device__ __forceinline__ float fold_pair(uint32_t top) {
+    if (std::is_same<T, __half>::value) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&top));
+        return fmaxf(f.x, f.y);
+    }
+    return fmaxf(__uint_as_float(top << 16), __uint_as_float(top & 0xFFFF0000u));
+}
+// Eight numbers, already divided by the scale (magnitude 127 or 448 at most, by a rounding or two) -> eight codes.
+// int8: adding 1.5 * 2^23 leaves the nearest whole number, ties to even, in the low bits; its low byte is the code.
 template <int TYPE>
 __device__ __forceinline__ uint2 encode8(const float* y) {
     uint32_t w[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         if (TYPE == SQAP_KV_INT8) {
-            uint32_t r = 0;
+            uint32_t b[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                int q = __float2int_rn(y[4 * i + j]);
-                q = max(-127, min(127, q));
-                r |= (static_cast<uint32_t>(q) & 0xFFu) << (8 * j);
-            }
-            w[i] = r;
+            for (int j = 0; j < 4; ++j) b[j] = __float_as_uint(__fadd_rn(y[4 * i + j], 12582912.0f));
+            w[i] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
         } else {
             uint16_t a, b;
             asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;" : "=h"(a) : "f"(y[4 * i]), "f"(y[4 * i + 1]));

@@ -10,6 +10,7 @@ namespace kv {
 namespace {
 
 constexpr int THREADS = 128;
+constexpr int READ_AHEAD = 8;
 constexpr int HELD = 8;      // 16-byte pieces that a thread keeps between the two passes
 
 // Maximum over the block, known to every thread.
@@ -76,7 +77,6 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(AppendArgs a) {
     // The new tokens' share of a thread: kept in registers where it is small enough (the usual pages), read again otherwise.
     auto source = [&](int i) { return __ldg(reinterpret_cast<const uint4*>(row0 + (i / per_row) * ld) + i % per_row); };
     uint4 held[HELD];
-    float amax = 0.0f;
 #pragma unroll
     for (int q = 0; q < HELD; ++q) {
         const int i = threadIdx.x + q * THREADS;
@@ -84,16 +84,11 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(AppendArgs a) {
         if (i < items) held[q] = source(i);
     }
     const float before = t0 > lo ? *scale_at : 0.0f;        // tokens in front of the new ones keep their place
-    auto widen = [&](uint4 u) {
-        float v[8];
-        unpack8<T>(u, v);
+    uint32_t top = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(v[e]));
-    };
-#pragma unroll
-    for (int q = 0; q < HELD; ++q) widen(held[q]);
-    for (int i = threadIdx.x + HELD * THREADS; i < items; i += THREADS) widen(source(i));
-    amax = block_max(amax, red);                            // (every thread has read *scale_at before thread 0 writes it)
+    for (int q = 0; q < HELD; ++q) widen8<T>(held[q], &top);
+    for (int i = threadIdx.x + HELD * THREADS; i < items; i += THREADS) widen8<T>(source(i), &top);
+    const float amax = block_max(fold_pair<T>(top), red);   // (every thread has read *scale_at before thread 0 writes it)
     const float scale = fmaxf(before, scale_for<TYPE>(amax));
     if (threadIdx.x == 0) *scale_at = scale;
     if (scale > before && t0 > lo) {                        // they are rounded again to the larger scale
@@ -134,7 +129,8 @@ struct ReadArgs {
     int64_t ldk, ldv;
 };
 
-// One warp = one token of one sequence, keys or values, of 16 codes a lane and step; up to four steps' loads in flight.
+// One warp = one token of one sequence, keys or values: 8 codes a lane and step (16-byte stores, side by side), eight steps'
+// loads in flight.
 template <typename T, int TYPE>
 __global__ void __launch_bounds__(THREADS) kv_read_kernel(ReadArgs a, unsigned total) {
     pdl_launch_dependents();
@@ -148,40 +144,37 @@ __global__ void __launch_bounds__(THREADS) kv_read_kernel(ReadArgs a, unsigned t
     const int r0 = a.cu[b], r1 = a.cu[b + 1];
     const int64_t pos = static_cast<int64_t>(a.first ? a.first[b] : 0) + i, j = pos >> c.page_shift;
     if (!out || i >= r1 - r0) return;
-    const int D = c.head_dim, pieces = c.kv_heads * D / 16;
+    const int D = c.head_dim, pieces = c.kv_heads * D / 8;
     const int page = pos >= 0 && j < a.ldt ? checked_page(c, a.table[b * a.ldt + j]) : -1;
     const int t = static_cast<int>(pos) & ((1 << c.page_shift) - 1);
     const Half half = which ? c.v : c.k;
-    const int dshift = 31 - __clz(D / 16);                   // pieces per head, a power of two
+    const int dshift = 31 - __clz(D / 8);                    // pieces per head, a power of two
     const float* scales = half.scales + static_cast<int64_t>(page) * c.kv_heads;
     const uint8_t* codes = half.codes + (page_codes(c, page, 0) + t) * D;
     const int64_t head_stride = static_cast<int64_t>(D) << c.page_shift;
     uint4* to = reinterpret_cast<uint4*>(out + (static_cast<int64_t>(r0) + i) * (which ? a.ldv : a.ldk));
-    for (int x0 = lane; x0 < pieces; x0 += 128) {
-        uint4 u[4];
-        float s[4];
+    for (int x0 = lane; x0 < pieces; x0 += 32 * READ_AHEAD) {
+        uint2 u[READ_AHEAD];
+        float s[READ_AHEAD];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < READ_AHEAD; ++q) {
             const int x = x0 + 32 * q, h = x >> dshift;
-            u[q] = make_uint4(0, 0, 0, 0);
+            u[q] = make_uint2(0, 0);
             s[q] = 0.0f;                                     // a missing page reads as zero
             if (page >= 0 && x < pieces) {
-                u[q] = __ldg(reinterpret_cast<const uint4*>(codes + h * head_stride + (x - (h << dshift)) * 16));
+                u[q] = __ldg(reinterpret_cast<const uint2*>(codes + h * head_stride) + (x - (h << dshift)));
                 s[q] = __ldg(scales + h);
             }
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < READ_AHEAD; ++q) {
             const int x = x0 + 32 * q;
             if (x >= pieces) break;
             float v[8];
+            decode8<TYPE>(u[q], v);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                decode8<TYPE>(e ? make_uint2(u[q].z, u[q].w) : make_uint2(u[q].x, u[q].y), v);
-#pragma unroll
-                for (int f = 0; f < 8; ++f) v[f] = __fmul_rn(v[f], s[q]);
-                to[2 * x + e] = pack8<T>(v);
-            }
+            for (int f = 0; f < 8; ++f) v[f] = __fmul_rn(v[f], s[q]);
+            to[x] = pack8<T>(v);
         }
     }
 }

@@ -81,12 +81,19 @@ mx4_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restri
         const uint32_t b = __ldg(scales + scale_offset(row, 8 * g / mx4_block(FMT), k_tiles));
         const float sc = FMT == SQAP_MX_NVFP4 ? __fmul_rn(scale_value<FMT>(b), gs) : scale_value<FMT>(b);
         alignas(16) T y[8];
+        uint32_t h[4];                                // pairs of codes as fp16, exactly
+        asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+            "mov.b32 {a, b, c, d}, %4;\n\t"
+            "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+            "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+            "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+            "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+            : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(c));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t n = (c >> (4 * i)) & 15u, e = (n >> 1) & 3u, m = n & 1u;
-            // code magnitude: m/2 for e = 0, else (1 + m/2) 2^(e-1)
-            const float mag = e ? __uint_as_float(((126u + e) << 23) | (m << 22)) : 0.5f * static_cast<float>(m);
-            y[i] = from_float<T>(__fmul_rn((n & 8u) ? -mag : mag, sc));
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+            y[2 * i] = from_float<T>(__fmul_rn(f.x, sc));
+            y[2 * i + 1] = from_float<T>(__fmul_rn(f.y, sc));
         }
         uint4* o = reinterpret_cast<uint4*>(out + static_cast<int64_t>(row) * ldo + 8 * g);
 #pragma unroll
