@@ -162,7 +162,7 @@ __device__ __forceinline__ float scale_for(float amax) {
     x = x < MIN_EXP ? MIN_EXP : x;
     return __uint_as_float(static_cast<uint32_t>(x + 127) << 23);
 }
-__device__ __forceinline__ float inverse_of(float scale) { return scale > 0.0f ? __fdiv_rn(1.0f, scale) : 0.0f; }
+__device__ __forceinline__ float inverse_of(float scale) { return scale > 0.0f ? __frcp_rn(scale) : 0.0f; }
 
 template <typename T>
 __device__ __forceinline__ void unpack8(uint4 u, float* v);

@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(AppendArgs a) {
     const int page = checked_page(c, a.table[b * a.ldt + j]);
     if (page < 0) return;
     const Half half = which ? c.v : c.k;
-    const int D = c.head_dim, per_row = D / 8;
+    const int D = c.head_dim, per_row = D / 8, rshift = 31 - __clz(per_row);      // a power of two
     uint8_t* codes = half.codes + page_codes(c, page, h) * D;
     float* scale_at = half.scales + static_cast<int64_t>(page) * c.kv_heads + h;
     const T* src = static_cast<const T*>(which ? a.v : a.k) + static_cast<int64_t>(h) * D;
@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(AppendArgs a) {
     const int items = (t1 - t0) * per_row;
 
     // The new tokens' share of a thread: kept in registers where it is small enough (the usual pages), read again otherwise.
-    auto source = [&](int i) { return __ldg(reinterpret_cast<const uint4*>(row0 + (i / per_row) * ld) + i % per_row); };
+    auto source = [&](int i) { return __ldg(reinterpret_cast<const uint4*>(row0 + (i >> rshift) * ld) + (i & (per_row - 1))); };
     uint4 held[HELD];
 #pragma unroll
     for (int q = 0; q < HELD; ++q) {
@@ -129,52 +129,49 @@ struct ReadArgs {
     int64_t ldk, ldv;
 };
 
-// One warp = one token of one sequence, keys or values: 8 codes a lane and step (16-byte stores, side by side), eight steps'
-// loads in flight.
-template <typename T, int TYPE>
-__global__ void __launch_bounds__(THREADS) kv_read_kernel(ReadArgs a, unsigned total) {
+// One warp = 16 consecutive places of a page (a run: contiguous codes) of one sequence and head, keys or values: 8 codes a lane
+// and step, 16-byte stores side by side, READ_AHEAD steps' loads in flight. (By tokens instead, all heads of one after the
+// other, every 128 bytes come from another page's worth of codes: 31 us where this takes 19, for 16 x 288 tokens, 32 heads.)
+template <typename T, int TYPE, int D>
+__global__ void __launch_bounds__(THREADS) kv_read_kernel(ReadArgs a, unsigned total, int runs) {
+    constexpr int LANES = D / 8, STEPS = 16 * LANES / 32, AHEAD = STEPS < READ_AHEAD ? STEPS : READ_AHEAD;
     pdl_launch_dependents();
     pdl_wait();
     const Cache& c = a.c;
-    const unsigned id = blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
+    unsigned id = blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
     if (id >= total) return;
-    const int which = id & 1, lane = threadIdx.x & 31;
-    const int b = static_cast<int>((id >> 1) / a.max_rows), i = static_cast<int>((id >> 1) % a.max_rows);
+    const int lane = threadIdx.x & 31;
+    const int h = static_cast<int>(id % c.kv_heads);
+    id /= c.kv_heads;
+    const int which = id & 1;
+    id >>= 1;
+    const int run = static_cast<int>(id % runs), b = static_cast<int>(id / runs);
     T* out = static_cast<T*>(which ? a.v : a.k);
-    const int r0 = a.cu[b], r1 = a.cu[b + 1];
-    const int64_t pos = static_cast<int64_t>(a.first ? a.first[b] : 0) + i, j = pos >> c.page_shift;
-    if (!out || i >= r1 - r0) return;
-    const int D = c.head_dim, pieces = c.kv_heads * D / 8;
-    const int page = pos >= 0 && j < a.ldt ? checked_page(c, a.table[b * a.ldt + j]) : -1;
-    const int t = static_cast<int>(pos) & ((1 << c.page_shift) - 1);
+    const int r0 = a.cu[b];
+    const int n = min(a.cu[b + 1] - r0, a.max_rows);
+    const int64_t first = a.first ? a.first[b] : 0;
+    const int64_t pos0 = ((first >> 4) + run) << 4, j = pos0 >> c.page_shift;      // first place of the run
+    if (!out || pos0 >= first + n) return;
+    const int page = pos0 >= 0 && j < a.ldt ? checked_page(c, a.table[b * a.ldt + j]) : -1;
     const Half half = which ? c.v : c.k;
-    const int dshift = 31 - __clz(D / 8);                    // pieces per head, a power of two
-    const float* scales = half.scales + static_cast<int64_t>(page) * c.kv_heads;
-    const uint8_t* codes = half.codes + (page_codes(c, page, 0) + t) * D;
-    const int64_t head_stride = static_cast<int64_t>(D) << c.page_shift;
-    uint4* to = reinterpret_cast<uint4*>(out + (static_cast<int64_t>(r0) + i) * (which ? a.ldv : a.ldk));
-    for (int x0 = lane; x0 < pieces; x0 += 32 * READ_AHEAD) {
-        uint2 u[READ_AHEAD];
-        float s[READ_AHEAD];
+    const int64_t ld = which ? a.ldv : a.ldk;
+    const uint2* codes = reinterpret_cast<const uint2*>(half.codes + (page_codes(c, page, h) + (static_cast<int>(pos0) & ((1 << c.page_shift) - 1))) * D);
+    const float s = page >= 0 ? __ldg(half.scales + static_cast<int64_t>(page) * c.kv_heads + h) : 0.0f;     // a missing page reads as zero
 #pragma unroll
-        for (int q = 0; q < READ_AHEAD; ++q) {
-            const int x = x0 + 32 * q, h = x >> dshift;
-            u[q] = make_uint2(0, 0);
-            s[q] = 0.0f;                                     // a missing page reads as zero
-            if (page >= 0 && x < pieces) {
-                u[q] = __ldg(reinterpret_cast<const uint2*>(codes + h * head_stride) + (x - (h << dshift)));
-                s[q] = __ldg(scales + h);
-            }
-        }
+    for (int s0 = 0; s0 < STEPS; s0 += AHEAD) {
+        uint2 u[AHEAD];
 #pragma unroll
-        for (int q = 0; q < READ_AHEAD; ++q) {
-            const int x = x0 + 32 * q;
-            if (x >= pieces) break;
+        for (int q = 0; q < AHEAD; ++q) u[q] = page >= 0 ? __ldg(codes + 32 * (s0 + q) + lane) : make_uint2(0, 0);
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q) {
+            const int piece = 32 * (s0 + q) + lane;
+            const int64_t i = pos0 + piece / LANES - first;                        // row of the sequence
+            if (i < 0 || i >= n) continue;
             float v[8];
             decode8<TYPE>(u[q], v);
 #pragma unroll
-            for (int f = 0; f < 8; ++f) v[f] = __fmul_rn(v[f], s[q]);
-            to[x] = pack8<T>(v);
+            for (int f = 0; f < 8; ++f) v[f] = __fmul_rn(v[f], s);
+            *(reinterpret_cast<uint4*>(out + (r0 + i) * ld + h * D) + piece % LANES) = pack8<T>(v);
         }
     }
 }
@@ -263,10 +260,10 @@ __global__ void __launch_bounds__(THREADS) kv_compact_kernel(CompactArgs a) {
     }
     __syncthreads();
     // 16 codes a piece: at most 16 pieces a thread, of which HELD / 2 stay in registers between the two passes
-    const int per16 = D / 16, items = P * per16;
+    const int per16 = D / 16, rshift = 31 - __clz(per16), items = P * per16;
     auto source = [&](int x) {
-        const int64_t where = at[x / per16];
-        return where < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(half.codes + where * D) + x % per16);
+        const int64_t where = at[x >> rshift];
+        return where < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(half.codes + where * D) + (x & (per16 - 1)));
     };
     uint4 held[HELD / 2];
 #pragma unroll
@@ -277,7 +274,7 @@ __global__ void __launch_bounds__(THREADS) kv_compact_kernel(CompactArgs a) {
     }
     float amax = 0.0f;
     auto widen = [&](int x, uint4 u) {
-        const float s = of[x / per16];
+        const float s = of[x >> rshift];
         float v[8];
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
@@ -294,7 +291,7 @@ __global__ void __launch_bounds__(THREADS) kv_compact_kernel(CompactArgs a) {
     if (threadIdx.x == 0) half.scales[static_cast<int64_t>(page) * c.kv_heads + h] = scale;
     uint4* to = reinterpret_cast<uint4*>(half.codes + page_codes(c, page, h) * D);
     auto write = [&](int x, uint4 u) {
-        const float s = of[x / per16];
+        const float s = of[x >> rshift];
         float v[8];
         uint2 r[2];
 #pragma unroll
@@ -319,11 +316,16 @@ cudaError_t append_as(const AppendArgs& a, int type, unsigned grid, cudaStream_t
     if (type == SQAP_KV_INT8) return launch_dependent(kv_append_kernel<T, SQAP_KV_INT8>, dim3(grid), dim3(THREADS), 0, s, a);
     return launch_dependent(kv_append_kernel<T, SQAP_KV_E4M3>, dim3(grid), dim3(THREADS), 0, s, a);
 }
-template <typename T>
-cudaError_t read_as(const ReadArgs& a, int type, unsigned total, cudaStream_t s) {
+template <typename T, int TYPE>
+cudaError_t read_dim(const ReadArgs& a, unsigned total, int runs, cudaStream_t s) {
     const dim3 grid((total + THREADS / 32 - 1) / (THREADS / 32));
-    if (type == SQAP_KV_INT8) return launch_dependent(kv_read_kernel<T, SQAP_KV_INT8>, grid, dim3(THREADS), 0, s, a, total);
-    return launch_dependent(kv_read_kernel<T, SQAP_KV_E4M3>, grid, dim3(THREADS), 0, s, a, total);
+    if (a.c.head_dim == 64) return launch_dependent(kv_read_kernel<T, TYPE, 64>, grid, dim3(THREADS), 0, s, a, total, runs);
+    if (a.c.head_dim == 128) return launch_dependent(kv_read_kernel<T, TYPE, 128>, grid, dim3(THREADS), 0, s, a, total, runs);
+    return launch_dependent(kv_read_kernel<T, TYPE, 256>, grid, dim3(THREADS), 0, s, a, total, runs);
+}
+template <typename T>
+cudaError_t read_as(const ReadArgs& a, int type, unsigned total, int runs, cudaStream_t s) {
+    return type == SQAP_KV_INT8 ? read_dim<T, SQAP_KV_INT8>(a, total, runs, s) : read_dim<T, SQAP_KV_E4M3>(a, total, runs, s);
 }
 
 }  // namespace
@@ -367,12 +369,13 @@ extern "C" sqap_status sqap_kv_read(const sqap_kv_cache* cache, const int32_t* t
     if ((k && ldk % 8 != 0) || (v && ldv % 8 != 0) || !aligned16(k) || !aligned16(v)) return SQAP_ERR_ALIGN;
     if (batch == 0 || max_rows == 0 || (!k && !v)) return SQAP_OK;
     if (!cu_rows || (ldt > 0 && !table)) return SQAP_ERR_INVALID;
-    const int64_t grid = 2 * static_cast<int64_t>(batch) * max_rows;        // warps
-    if (grid > MAX_GRID) return SQAP_ERR_UNSUPPORTED;
+    // runs of 16 places that max_rows tokens can touch
+    const int64_t runs = (static_cast<int64_t>(max_rows) + 14) / 16 + 1, warps = 2 * static_cast<int64_t>(batch) * runs * cache->kv_heads;
+    if (warps > MAX_GRID) return SQAP_ERR_UNSUPPORTED;
     const ReadArgs a = {device_view(cache), table, ldt, first, cu_rows, max_rows, k, v, ldk, ldv};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return finish_launch(dtype == SQAP_FP16 ? read_as<__half>(a, cache->type, static_cast<unsigned>(grid), s)
-                                            : read_as<__nv_bfloat16>(a, cache->type, static_cast<unsigned>(grid), s));
+    return finish_launch(dtype == SQAP_FP16 ? read_as<__half>(a, cache->type, static_cast<unsigned>(warps), static_cast<int>(runs), s)
+                                            : read_as<__nv_bfloat16>(a, cache->type, static_cast<unsigned>(warps), static_cast<int>(runs), s));
 }
 
 extern "C" sqap_status sqap_kv_copy_pages(const sqap_kv_cache* cache, const int32_t* pairs, int n, void* stream) {

@@ -27,13 +27,13 @@ mx4_quantize_kernel(const T* __restrict__ x, int M, int K, int64_t ldx, const in
     const float gs = tensor_scale ? __ldg(tensor_scale) : 1.0f;
     for (int row = blockIdx.y; row < M; row += gridDim.y) {
         const int src = row_index ? __ldg(row_index + row) : row;
-        float v[16];
-        if (g < groups) load16<T>(x + static_cast<int64_t>(src) * ldx + 16 * g, v);
+        float v[16], amax = 0.0f;
+        if (g < groups) amax = load16<T>(x + static_cast<int64_t>(src) * ldx + 16 * g, v);
         else {
 #pragma unroll
             for (int i = 0; i < 16; ++i) v[i] = 0.0f;
         }
-        uint32_t sbyte = quantize16<FMT>(v, gs);
+        uint32_t sbyte = quantize16<FMT>(v, amax, gs);
         if (g < groups) {
             const uint2 c = make_uint2(to_e2m1x8(v), to_e2m1x8(v + 8));
             *reinterpret_cast<uint2*>(codes + static_cast<size_t>(row) * (K / 2) + 8 * static_cast<size_t>(g)) = c;

@@ -5,10 +5,12 @@
 
 namespace sqap {
 
+// Sixteen consecutive elements, and the largest magnitude among them (two at a time where they have 16 bits).
 template <typename T>
-__device__ __forceinline__ void load16(const T* p, float* v);
+__device__ __forceinline__ float load16(const T* p, float* v);
 template <>
-__device__ __forceinline__ void load16<__half>(const __half* p, float* v) {
+__device__ __forceinline__ float load16<__half>(const __half* p, float* v) {
+    uint32_t top = 0;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const uint4 u = __ldg(reinterpret_cast<const uint4*>(p) + h);
@@ -18,11 +20,15 @@ __device__ __forceinline__ void load16<__half>(const __half* p, float* v) {
             const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
             v[8 * h + 2 * i] = f.x;
             v[8 * h + 2 * i + 1] = f.y;
+            asm("max.f16x2 %0, %0, %1;" : "+r"(top) : "r"(w[i] & 0x7FFF7FFFu));
         }
     }
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&top));
+    return fmaxf(f.x, f.y);
 }
 template <>
-__device__ __forceinline__ void load16<__nv_bfloat16>(const __nv_bfloat16* p, float* v) {
+__device__ __forceinline__ float load16<__nv_bfloat16>(const __nv_bfloat16* p, float* v) {
+    uint32_t top = 0;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const uint4 u = __ldg(reinterpret_cast<const uint4*>(p) + h);
@@ -31,11 +37,14 @@ __device__ __forceinline__ void load16<__nv_bfloat16>(const __nv_bfloat16* p, fl
         for (int i = 0; i < 4; ++i) {
             v[8 * h + 2 * i] = __uint_as_float(w[i] << 16);
             v[8 * h + 2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            asm("max.bf16x2 %0, %0, %1;" : "+r"(top) : "r"(w[i] & 0x7FFF7FFFu));
         }
     }
+    return fmaxf(__uint_as_float(top << 16), __uint_as_float(top & 0xFFFF0000u));
 }
 template <>
-__device__ __forceinline__ void load16<float>(const float* p, float* v) {
+__device__ __forceinline__ float load16<float>(const float* p, float* v) {
+    float top = 0.0f;
 #pragma unroll
     for (int h = 0; h < 4; ++h) {
         const float4 f = __ldg(reinterpret_cast<const float4*>(p) + h);
@@ -43,7 +52,9 @@ __device__ __forceinline__ void load16<float>(const float* p, float* v) {
         v[4 * h + 1] = f.y;
         v[4 * h + 2] = f.z;
         v[4 * h + 3] = f.w;
+        top = fmaxf(fmaxf(fmaxf(top, fabsf(f.x)), fmaxf(fabsf(f.y), fabsf(f.z))), fabsf(f.w));
     }
+    return top;
 }
 
 // Eight numbers -> eight e2m1 codes (round to nearest, ties to even, at most 6), element 0 in the lowest nibble.
@@ -76,22 +87,33 @@ __device__ __forceinline__ size_t scale_offset(int row, int block, int k_tiles) 
     return (static_cast<size_t>(row >> 7) * k_tiles + (block >> 2)) * 512u + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3);
 }
 
-// Sixteen consecutive elements of a row: returns the scale byte of their block, and in v what their codes are rounded from.
+// Sixteen consecutive elements of a row and their largest magnitude: returns the scale byte of their block, and in v what
+// their codes are rounded from.
 // MXFP4: the block's other half is in the neighbouring lane (lane ^ 1); every lane of the warp calls it.
 template <int FMT>
-__device__ __forceinline__ uint32_t quantize16(float* v, float gs) {
-    float amax = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) amax = fmaxf(amax, fabsf(v[i]));
+__device__ __forceinline__ uint32_t quantize16(float* v, float amax, float gs) {
     if (FMT == SQAP_MX_NVFP4) {
         // scale = e4m3(amax / 6 / g); the codes are those of x / (scale g)
         const uint32_t sbyte = to_e4m3x2(__fdiv_rn(__fdiv_rn(amax, 6.0f), gs), 0.0f) & 0xFFu;
         const float sc = e4m3_to_float(sbyte);
-        const float inv = sc > 0.0f ? __fdiv_rn(1.0f, __fmul_rn(sc, gs)) : 0.0f;
+        const float inv = sc > 0.0f ? __frcp_rn(__fmul_rn(sc, gs)) : 0.0f;
         // Adding and taking away 24 rounds to a multiple of 2^-19: a quotient that lies exactly halfway between two codes,
         // which the rounded reciprocal may miss by an ulp, comes out halfway again.
+        // (The additions two at a time; a multiplication in the same form would be contracted with them.)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = __fadd_rn(__fadd_rn(__fmul_rn(v[i], inv), 24.0f), -24.0f);
+        for (int i = 0; i < 16; i += 2) {
+            float2 y = make_float2(__fmul_rn(v[i], inv), __fmul_rn(v[i + 1], inv));
+            asm("{\n\t.reg .b64 y, c;\n\t"
+                "mov.b64 y, {%0, %1};\n\t"
+                "mov.b64 c, {%2, %2};\n\t"
+                "add.rn.f32x2 y, y, c;\n\t"
+                "mov.b64 c, {%3, %3};\n\t"
+                "add.rn.f32x2 y, y, c;\n\t"
+                "mov.b64 {%0, %1}, y;\n\t}"
+                : "+f"(y.x), "+f"(y.y) : "f"(24.0f), "f"(-24.0f));
+            v[i] = y.x;
+            v[i + 1] = y.y;
+        }
         return sbyte;
     }
     amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));

@@ -115,15 +115,15 @@ __global__ void __launch_bounds__(THREADS, 2) mx4_gemv_kernel(GemvArgs a) {
             uint2 q;
             float scale;
             if constexpr (!std::is_same<T, void>::value) {
-                float v[16];
+                float v[16], amax = 0.0f;
                 if (h < 2 * groups) {
                     const int64_t src = a.row_index ? __ldg(a.row_index + m) : m;
-                    load16<T>(static_cast<const T*>(a.x) + src * a.ldx + 16 * h, v);
+                    amax = load16<T>(static_cast<const T*>(a.x) + src * a.ldx + 16 * h, v);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) v[i] = 0.0f;
                 }
-                scale = scale_value<FMT>(quantize16<FMT>(v, gs));
+                scale = scale_value<FMT>(quantize16<FMT>(v, amax, gs));
                 q = make_uint2(to_e2m1x8(v), to_e2m1x8(v + 8));
             } else if (h < 2 * groups) {
                 q = __ldg(reinterpret_cast<const uint2*>(a.x_codes + static_cast<size_t>(m) * (K / 2)) + h);
