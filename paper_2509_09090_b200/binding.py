@@ -128,10 +128,12 @@ def _ptr(t):
     """Address of a torch tensor / numpy array / int / None."""
     if t is None:
         return None
+    try:
+        return t.data_ptr()
+    except AttributeError:
+        pass
     if isinstance(t, int):
         return t
-    if hasattr(t, "data_ptr"):
-        return t.data_ptr()
     if hasattr(t, "ctypes"):
         return t.ctypes.data
     raise TypeError(f"cannot take the address of {type(t)}")
