@@ -34,8 +34,9 @@ constexpr int S_MAX = 10;
 constexpr int KSPLIT_MAX = 8;
 constexpr int A_BYTES = BM * BK / 2;      // 16 KB
 constexpr int SF_TILE = 512;              // scales of 128 rows x 4 blocks
-constexpr int THREADS = 192;              // warp 0: TMA, warp 1: MMA, all: exchange, epilogue
-constexpr int CHUNK_BYTES = BM * 16 * 4;  // 16 tokens of a partial sum: [16][128] fp32
+constexpr int THREADS = 256;              // warp 0: TMA, warp 1: MMA, all: exchange and epilogue, in two groups of four
+constexpr int CHUNK_BYTES = BM * 16 * 4;  // 16 tokens of a partial sum: four planes [128 rows][4 tokens] fp32
+constexpr int STAGE_BYTES = BM * 16 * 2;  // a chunk of 16-bit outputs on its way out
 constexpr int TAIL_BYTES = 512;           // barriers and flags behind the ring
 
 struct MxArgs {
@@ -69,8 +70,8 @@ __device__ __forceinline__ uint32_t map_to_cta(uint32_t addr, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
-__device__ __forceinline__ void st_cluster(uint32_t cluster_addr, uint32_t v) {
-    asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
+__device__ __forceinline__ void st_cluster_v4(uint32_t cluster_addr, const uint32_t* v) {
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
 // Untiled bulk copy global -> this CTA's shared memory (both addresses and the size are multiples of 16).
 __device__ __forceinline__ void bulk_load_if(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint32_t issue) {
@@ -252,7 +253,7 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constan
     }
 
     // ---------------- partial sums -> the CTA that owns their tokens. 16-token chunk c belongs to rank c % ksplit,
-    // which keeps the part of source r at (r * own_max + c / ksplit) * CHUNK_BYTES as [16 tokens][128 channels].
+    // which keeps the part of source r at (r * own_max + c / ksplit) * CHUNK_BYTES: thread = weight row, 16 bytes to a plane.
     const int chunks = a.BN >> 4;
     const int own_max = (chunks + a.ksplit - 1) / a.ksplit;
     if (!failed && !mbar_wait(acc_full, 0u, abort_flag)) failed = true;
@@ -263,17 +264,17 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constan
     failed = __syncthreads_or(failed ? 1 : 0) != 0;
     tc_fence_after();
     cluster_sync_all();   // every CTA's MMAs are done (or given up): the rings are idle
-    if (warp < 4 && !failed) {
-        const uint32_t taddr = tmem_base + (static_cast<uint32_t>(warp * 32) << 16);
-        const int row = warp * 32 + lane;
-        for (int c = 0; c < chunks; ++c) {
+    const int quad = warp & 3, group = warp >> 2, row = quad * 32 + lane;
+    if (!failed) {
+        const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quad * 32) << 16);
+        for (int c = group; c < chunks; c += 2) {
             uint32_t v[16];
             tc_ld16(taddr + 16 * c, v);
-            const uint32_t dst = map_to_cta(base + static_cast<uint32_t>((rank * own_max + c / a.ksplit) * CHUNK_BYTES + row * 4),
+            const uint32_t dst = map_to_cta(base + static_cast<uint32_t>((rank * own_max + c / a.ksplit) * CHUNK_BYTES + row * 16),
                                             static_cast<uint32_t>(c % a.ksplit));
             tc_wait_ld();
 #pragma unroll
-            for (int j = 0; j < 16; ++j) st_cluster(dst + j * (BM * 4), v[j]);
+            for (int q = 0; q < 4; ++q) st_cluster_v4(dst + q * (BM * 16), v + 4 * q);
         }
     }
     tc_fence_before();
@@ -286,44 +287,51 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constan
     if (failed) return;
     const float alpha = __fmul_rn(a.gx ? __ldg(a.gx) : 1.0f, a.gw ? __ldg(a.gw) : 1.0f);
     const int own = (chunks - rank + a.ksplit - 1) / a.ksplit;
-    for (int p = threadIdx.x; p < own * 256; p += THREADS) {      // 8 channels of one token
-        const int lc = p >> 8, token = (p >> 4) & 15, piece = p & 15;
-        const int m = m0 + 16 * (lc * a.ksplit + rank) + token, n = n0 + 8 * piece;
-        if (m >= a.M || n >= a.N) continue;
-        const float4* part = reinterpret_cast<const float4*>(sm + lc * CHUNK_BYTES + (token * BM + 8 * piece) * 4);
-        float4 lo = part[0], hi = part[1];
-        for (int r = 1; r < a.ksplit; ++r) {
-            part += own_max * (CHUNK_BYTES / 16);
-            const float4 l = part[0], h = part[1];
-            lo.x += l.x; lo.y += l.y; lo.z += l.z; lo.w += l.w;
-            hi.x += h.x; hi.y += h.y; hi.z += h.z; hi.w += h.w;
+    // 16-bit outputs go through shared memory ([token][channel], behind the exchange) so that a thread stores 16 bytes: two
+    // buffers a group in turn, one barrier of the group a chunk.
+    uint8_t* const stage0 = sm + own_max * a.ksplit * CHUNK_BYTES + group * 2 * STAGE_BYTES;
+    for (int lc = group, turn = 0; lc < own; lc += 2, turn ^= 1) {
+        const int m_first = m0 + 16 * (lc * a.ksplit + rank);
+        float y[16];
+        const uint8_t* part = sm + lc * CHUNK_BYTES + row * 16;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float4 f = *reinterpret_cast<const float4*>(part + q * (BM * 16));
+            y[4 * q] = f.x; y[4 * q + 1] = f.y; y[4 * q + 2] = f.z; y[4 * q + 3] = f.w;
         }
-        float y[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+        for (int r = 1; r < a.ksplit; ++r) {
+            part += own_max * CHUNK_BYTES;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] *= alpha;
-        const int64_t at = static_cast<int64_t>(m) * a.ldo + n;
-        if (a.out_dtype == SQAP_FP32) {
-            float* o = static_cast<float*>(a.out) + at;
-            if (n + 8 <= a.N) {
-                reinterpret_cast<float4*>(o)[0] = make_float4(y[0], y[1], y[2], y[3]);
-                reinterpret_cast<float4*>(o)[1] = make_float4(y[4], y[5], y[6], y[7]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (n + e < a.N) o[e] = y[e];
+            for (int q = 0; q < 4; ++q) {
+                const float4 f = *reinterpret_cast<const float4*>(part + q * (BM * 16));
+                y[4 * q] += f.x; y[4 * q + 1] += f.y; y[4 * q + 2] += f.z; y[4 * q + 3] += f.w;
             }
-        } else {
-            uint16_t b[8];
+        }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) b[e] = a.out_dtype == SQAP_FP16 ? bits16<SQAP_FP16>(y[e]) : bits16<SQAP_BF16>(y[e]);
-            uint16_t* o = static_cast<uint16_t*>(a.out) + at;
+        for (int e = 0; e < 16; ++e) y[e] *= alpha;
+        if (a.out_dtype == SQAP_FP32) {                              // a warp's 32 channels of a token are 128 bytes
+            float* o = static_cast<float*>(a.out) + static_cast<int64_t>(m_first) * a.ldo + n0 + row;
+            if (n0 + row < a.N)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (m_first + e < a.M) o[e * a.ldo] = y[e];
+            continue;
+        }
+        uint8_t* stage = stage0 + turn * STAGE_BYTES;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            *reinterpret_cast<uint16_t*>(stage + e * (BM * 2) + row * 2) = a.out_dtype == SQAP_FP16 ? bits16<SQAP_FP16>(y[e]) : bits16<SQAP_BF16>(y[e]);
+        bar_sync_named(1 + group, 128);
+#pragma unroll
+        for (int p = row; p < 16 * (BM / 8); p += 128) {
+            const int token = p / (BM / 8), piece = p % (BM / 8), m = m_first + token, n = n0 + 8 * piece;
+            if (m >= a.M || n >= a.N) continue;
+            const uint16_t* src = reinterpret_cast<const uint16_t*>(stage + token * (BM * 2) + piece * 16);
+            uint16_t* o = static_cast<uint16_t*>(a.out) + static_cast<int64_t>(m) * a.ldo + n;
             if (n + 8 <= a.N) {
-                *reinterpret_cast<uint4*>(o) = make_uint4(b[0] | (static_cast<uint32_t>(b[1]) << 16), b[2] | (static_cast<uint32_t>(b[3]) << 16),
-                                                          b[4] | (static_cast<uint32_t>(b[5]) << 16), b[6] | (static_cast<uint32_t>(b[7]) << 16));
+                *reinterpret_cast<uint4*>(o) = *reinterpret_cast<const uint4*>(src);
             } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (n + e < a.N) o[e] = b[e];
+                for (int e = 0; e < a.N - n; ++e) o[e] = src[e];
             }
         }
     }
@@ -378,7 +386,7 @@ static sqap_status launch(const Mx4Product& q, cudaStream_t s) {
         }
     }
     const int own_max = (k.BN / 16 + k.ksplit - 1) / k.ksplit;
-    const int need = own_max * k.ksplit * CHUNK_BYTES;            // the exchange lies in the idle ring
+    const int need = own_max * k.ksplit * CHUNK_BYTES + 4 * STAGE_BYTES;   // the exchange and the staging lie in the idle ring
     int ring_bytes = k.stages * k.stage_bytes;
     while (ring_bytes < need) {   // cannot happen with the depths above; keeps the invariant visible
         ++k.stages;
