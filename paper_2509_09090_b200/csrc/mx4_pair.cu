@@ -4,11 +4,15 @@
 // A cluster of two CTAs computes 256 x BN tiles (BN 64, 128 or 192 tokens): each CTA holds 128 weight rows and half of the
 // token rows, and the pair's tensor cores share both halves, so an SM fetches 28 KB of codes instead of 40 per 256
 // elements of K at BN = 192; the four-bit MMAs take 384 cycles for that, and fetching is what bounds the kernel. The scales of
-// the tokens are wanted in full by both CTAs (4 KB), those of the weights by their own (2 KB). All loads are TMA boxes whose
-// bytes are counted on the leader's barrier, where the MMAs are issued (the scale tiles go as rows of 512 bytes).
+// the tokens are wanted in full by both CTAs (4 KB), those of the weights by their own (2 KB). The codes' bytes are counted on the
+// leader's barrier, where the MMAs are issued.
+// The scales go to tensor memory through registers (four warps: shared memory -> tcgen05.st, one lane quadrant each): a
+// tcgen05.cp of a scale tile holds up the tensor pipe for some 24 cycles, and a stage has twelve of them beside 374 cycles of
+// MMAs (measured: pipe busy 78 %, with MMAs 44 %; 136 us where this takes @PAIR_US@ for 4608 x 12288 x 4096 with the quantizer).
 // Tensor memory (512 columns): two accumulators of 192 columns, so that a tile is stored while the next is computed, and two
 // sets of scale columns.
 //   warp 0     TMA      warp 1  MMA (leader)      warps 2-9  epilogue: four lane quadrants x two halves of the tokens
+//   warps 10-13  scales to tensor memory
 // A token tile may start in the middle of a 128-row scale tile (BN = 64, 192): 64 rows are two columns of a tile in tensor
 // memory, so the scales start two columns further on.
 // Every wait on a barrier is bounded; on expiry the kernel records SQAP_ERR_TIMEOUT in the device status word, drains, and
@@ -36,11 +40,12 @@ constexpr int OFF_STAGE = OFF_SFB + S * SFB_TILES * SF_BYTES;   // staging of th
 constexpr int OFF_BAR = OFF_STAGE + EPI_STAGE_TOTAL;
 constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;
 constexpr int EPI_WARPS = 8;
-constexpr int THREADS = 32 * (2 + EPI_WARPS);
+constexpr int SF_WARP0 = 2 + EPI_WARPS;
+constexpr int THREADS = 32 * (SF_WARP0 + 4);
 constexpr int SF_COL = 2 * BN_MAX;        // scale columns: two sets of (4 + 4 x SFB_TILES) columns for each scale tile along K
 constexpr int SET_COLS = 4 * 4 * (1 + SFB_TILES);
 static_assert(SMEM_BYTES <= 227 * 1024 && SF_COL + 2 * SET_COLS <= 512, "budgets");
-static_assert(8 * (2 * S + 4) + 16 <= 256, "barrier block");
+static_assert(8 * (3 * S + 6) + 16 <= 256, "barrier block");
 
 struct PairArgs {
     const float* gx;
@@ -88,17 +93,13 @@ __device__ __forceinline__ void tc_commit_pair(uint32_t bar, uint32_t issue) {
         ::"r"(bar), "h"(static_cast<uint16_t>(3)), "r"(issue)
         : "memory");
 }
-__device__ __forceinline__ uint64_t smem_desc_scales(uint32_t addr) {
-    return static_cast<uint64_t>((addr >> 4) & 0x3FFFu) | (8ull << 32) | (1ull << 46);
+// Eight columns of this thread's tensor-memory lane.
+__device__ __forceinline__ void tc_st8(uint32_t taddr, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
 }
-__device__ __forceinline__ void tc_copy_scales(uint32_t taddr, uint64_t desc, uint32_t issue) {
-    asm volatile(
-        "{\n\t.reg .pred q;\n\t"
-        "setp.ne.b32 q, %2, 0;\n\t"
-        "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}"
-        ::"r"(taddr), "l"(desc), "r"(issue)
-        : "memory");
-}
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 template <int FMT>
 __device__ __forceinline__ void tc_mma_mx4(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                            uint32_t accumulate, uint32_t issue) {
@@ -134,8 +135,10 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
     auto done = [&](int s) { return bar0 + 8u * (S + s); };            // the MMAs of the stage in slot s are done (both CTAs)
     auto acc_full = [&](int b) { return bar0 + 8u * (2 * S + b); };
     auto acc_empty = [&](int b) { return bar0 + 8u * (2 * S + 2 + b); };   // leader's
-    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + OFF_BAR + 8 * (2 * S + 4));
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + OFF_BAR + 8 * (2 * S + 4) + 8);
+    auto sf_full = [&](int s) { return bar0 + 8u * (2 * S + 4 + s); };     // this CTA's scale tiles of the stage have landed
+    auto sf_ready = [&](int b) { return bar0 + 8u * (3 * S + 4 + b); };    // leader's: a set of scale columns is there in both CTAs
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + OFF_BAR + 8 * (3 * S + 6));
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + OFF_BAR + 8 * (3 * S + 6) + 8);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();          // 0 = leader
@@ -143,16 +146,18 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
     const int half_bn = a.BN >> 1;
     const int k_steps = (a.K + BK - 1) / BK;
     const int total_tiles = a.m_tiles * a.n_tiles;
-    const uint32_t stage_tx = 2u * static_cast<uint32_t>(A_BYTES + half_bn * (BK / 2) + TILES * SF_TILE * (1 + SFB_TILES));
+    const uint32_t stage_tx = 2u * static_cast<uint32_t>(A_BYTES + half_bn * (BK / 2)), sf_tx = TILES * SF_TILE * (1 + SFB_TILES);
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
             mbar_init(full(s), 1);
             mbar_init(done(s), 1);
+            mbar_init(sf_full(s), 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full(b), 1);
             mbar_init(acc_empty(b), 2 * EPI_WARPS);
+            mbar_init(sf_ready(b), 8);   // four warps of either CTA
         }
         abort_flag[0] = 0;
         abort_flag[1] = 0;
@@ -177,13 +182,14 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
         auto weights = [&](int s, int ks, int n_tile, uint32_t bar) {
             const int nt = 2 * n_tile + static_cast<int>(rank);        // 128-row tile of the weights
             tma_pair_if(base + OFF_A + s * A_BYTES, &tm_w, ks * (BK / 2), nt * BM, bar, issue);
-            tma_pair_if(base + OFF_SFA + s * SF_BYTES, &tm_wsf, 0, nt * a.k_tiles + ks * TILES, bar, issue);
+            mbar_expect_tx_if(sf_full(s), sf_tx, issue);
+            tma_load_2d_if(base + OFF_SFA + s * SF_BYTES, &tm_wsf, 0, nt * a.k_tiles + ks * TILES, sf_full(s), issue);
         };
         auto tokens = [&](int s, int ks, int m_tile, uint32_t bar) {
             tma_pair_if(base + OFF_B + s * B_BYTES, &tm_x, ks * (BK / 2), m_tile * a.BN + static_cast<int>(rank) * half_bn, bar, issue);
 #pragma unroll
             for (int r = 0; r < SFB_TILES; ++r)
-                tma_pair_if(base + OFF_SFB + (s * SFB_TILES + r) * SF_BYTES, &tm_xsf, 0, (sf_row(m_tile) + r) * a.k_tiles + ks * TILES, bar, issue);
+                tma_load_2d_if(base + OFF_SFB + (s * SFB_TILES + r) * SF_BYTES, &tm_xsf, 0, (sf_row(m_tile) + r) * a.k_tiles + ks * TILES, sf_full(s), issue);
         };
         uint32_t early = 0;
         if (a.early && pair < total_tiles) {
@@ -223,38 +229,61 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
                 const uint32_t skip = ((tile / a.n_tiles) * a.BN % 128) / 32;      // columns into the first scale tile
                 for (int ks = 0; ks < k_steps; ++ks, ++it) {
                     const int s = it % S;
-                    if (!__all_sync(0xffffffffu, mbar_wait(full(s), (it / S) & 1u, abort_flag))) { failed = true; break; }
+                    const bool ok = mbar_wait(full(s), (it / S) & 1u, abort_flag) && mbar_wait(sf_ready(it & 1), (it >> 1) & 1u, abort_flag);
+                    if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
                     tc_fence_after();
-                    const uint32_t sfa = tmem_base + SF_COL + (it & 1) * SET_COLS, sfb = sfa + 4 * TILES;
+                    const uint32_t sfa = tmem_base + SF_COL + (it & 1) * SET_COLS, sfb = sfa + 4 * TILES + skip;
                     const uint64_t adesc = smem_desc_sw128(base + OFF_A + s * A_BYTES), bdesc = smem_desc_sw128(base + OFF_B + s * B_BYTES);
-                    const uint64_t da = smem_desc_scales(base + OFF_SFA + s * SF_BYTES), db = smem_desc_scales(base + OFF_SFB + s * SFB_TILES * SF_BYTES);
                     const int mmas = a.K - ks * BK >= BK ? 4 : (a.K - ks * BK + 63) / 64;
-                    // Descriptors count in units of 16 bytes. Whole stages are unrolled: every address is then one addition.
-                    auto scale_tile = [&](int t) {
-                        tc_copy_scales(sfa + 4u * t, da + t * (SF_TILE / 16), issue);
-#pragma unroll
-                        for (int r = 0; r < SFB_TILES; ++r)
-                            tc_copy_scales(sfb + 4u * (t * SFB_TILES + r), db + (r * SF_BYTES + t * SF_TILE) / 16, issue);
-                    };
                     auto mma = [&](int k) {
                         const int t = k / PER_TILE;
                         const uint32_t id = FMT == SQAP_MX_MXFP4 && (k & 1) ? (2u << 4) | (2u << 29) : 0u;
-                        tc_mma_mx4<FMT>(d, adesc + 2u * k, bdesc + 2u * k, idesc | id, sfa + 4u * t, sfb + 4u * SFB_TILES * t + skip,
-                                        (ks | k) != 0 ? 1u : 0u, issue);
+                        tc_mma_mx4<FMT>(d, adesc + 2u * k, bdesc + 2u * k, idesc | id, sfa + 4u * t, sfb + 4u * SFB_TILES * t, (ks | k) != 0 ? 1u : 0u,
+                                        issue);
                     };
                     if (mmas == 4) {
 #pragma unroll
-                        for (int t = 0; t < TILES; ++t) scale_tile(t);
-#pragma unroll
                         for (int k = 0; k < 4; ++k) mma(k);
                     } else {
-                        for (int t = 0; t < (mmas + PER_TILE - 1) / PER_TILE; ++t) scale_tile(t);
                         for (int k = 0; k < mmas; ++k) mma(k);
                     }
                     tc_commit_pair(done(s), issue);
                 }
                 if (failed) break;
                 tc_commit_pair(acc_full(b), issue);
+            }
+        }
+    } else if (warp >= SF_WARP0) {
+        // ---------------- scales: lane i of every quadrant holds rows i, 32 + i, 64 + i, 96 + i of a tile, a column each
+        const int quad = warp & 3;
+        const uint32_t mine = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + SF_COL;
+        uint32_t it = 0;
+        for (int tile = pair; tile < total_tiles && !failed; tile += n_pairs) {
+            for (int ks = 0; ks < k_steps; ++ks, ++it) {
+                const int s = it % S;
+                bool ok = mbar_wait(sf_full(s), (it / S) & 1u, abort_flag);
+                // the MMAs that read this set two stages ago are done
+                if (ok && it >= 2) ok = mbar_wait(done((it - 2) % S), ((it - 2) / S) & 1u, abort_flag);
+                if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
+                tc_fence_after();
+                uint32_t r[4 * TILES * (1 + SFB_TILES)];
+                auto get = [&](int at, int off) {
+                    const uint4 u = *reinterpret_cast<const uint4*>(sm + off + lane * 16);
+                    r[at] = u.x; r[at + 1] = u.y; r[at + 2] = u.z; r[at + 3] = u.w;
+                };
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) get(4 * t, OFF_SFA + s * SF_BYTES + t * SF_TILE);
+#pragma unroll
+                for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                    for (int q = 0; q < SFB_TILES; ++q)
+                        get(4 * TILES + 4 * (t * SFB_TILES + q), OFF_SFB + (s * SFB_TILES + q) * SF_BYTES + t * SF_TILE);
+#pragma unroll
+                for (int c = 0; c < 4 * TILES * (1 + SFB_TILES); c += 8) tc_st8(mine + (it & 1) * SET_COLS + c, r + c);
+                tc_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(map_to_cta(sf_ready(it & 1), 0));
             }
         }
     } else {
