@@ -9,12 +9,12 @@
 // The scales go to tensor memory through registers (four warps: shared memory -> tcgen05.st, one lane quadrant each): a
 // tcgen05.cp of a scale tile holds up the tensor pipe for some 24 cycles, and a stage has twelve of them beside 374 cycles of
 // MMAs (measured: pipe busy 78 %, with MMAs 44 %; 136 us where this takes @PAIR_US@ for 4608 x 12288 x 4096 with the quantizer).
-// Tensor memory (512 columns): two accumulators of 192 columns, so that a tile is stored while the next is computed, and two
+// Tensor memory (512 columns): two accumulators of 192 columns, so that a tile is stored while the next is computed, and three
 // sets of scale columns.
 //   warp 0     TMA      warp 1  MMA (leader)      warps 2-9  epilogue: four lane quadrants x two halves of the tokens
 //   warps 10-13  scales to tensor memory
-// A token tile may start in the middle of a 128-row scale tile (BN = 64, 192): 64 rows are two columns of a tile in tensor
-// memory, so the scales start two columns further on.
+// A token tile may start in the middle of a 128-row scale tile (BN = 64, 192): 64 rows are two columns of a tile, so its scales
+// are taken from two columns further on.
 // Every wait on a barrier is bounded; on expiry the kernel records SQAP_ERR_TIMEOUT in the device status word, drains, and
 // returns through the cluster barrier.
 #include "mx4.cuh"
@@ -42,10 +42,12 @@ constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;
 constexpr int EPI_WARPS = 8;
 constexpr int SF_WARP0 = 2 + EPI_WARPS;
 constexpr int THREADS = 32 * (SF_WARP0 + 4);
-constexpr int SF_COL = 2 * BN_MAX;        // scale columns: two sets of (4 + 4 x SFB_TILES) columns for each scale tile along K
-constexpr int SET_COLS = 4 * 4 * (1 + SFB_TILES);
-static_assert(SMEM_BYTES <= 227 * 1024 && SF_COL + 2 * SET_COLS <= 512, "budgets");
-static_assert(8 * (3 * S + 6) + 16 <= 256, "barrier block");
+// Scale columns: a stage's set has, for each scale tile along K, 4 columns of weight scales and 6 of token scales (192 rows,
+// from where the token tile starts). Three sets: writing one and signalling it takes longer than a stage's MMAs.
+constexpr int SETS = 3, SFB_COLS = BN_MAX / 32;
+constexpr int SF_COL = 2 * BN_MAX, SET_COLS = 4 * (4 + SFB_COLS);
+static_assert(SMEM_BYTES <= 227 * 1024 && SF_COL + SETS * SET_COLS <= 512, "budgets");
+static_assert(8 * (3 * S + 4 + SETS) + 16 <= 256, "barrier block");
 
 struct PairArgs {
     const float* gx;
@@ -137,8 +139,8 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
     auto acc_empty = [&](int b) { return bar0 + 8u * (2 * S + 2 + b); };   // leader's
     auto sf_full = [&](int s) { return bar0 + 8u * (2 * S + 4 + s); };     // this CTA's scale tiles of the stage have landed
     auto sf_ready = [&](int b) { return bar0 + 8u * (3 * S + 4 + b); };    // leader's: a set of scale columns is there in both CTAs
-    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + OFF_BAR + 8 * (3 * S + 6));
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + OFF_BAR + 8 * (3 * S + 6) + 8);
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + OFF_BAR + 8 * (3 * S + 4 + SETS));
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + OFF_BAR + 8 * (3 * S + 4 + SETS) + 8);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();          // 0 = leader
@@ -157,8 +159,9 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full(b), 1);
             mbar_init(acc_empty(b), 2 * EPI_WARPS);
-            mbar_init(sf_ready(b), 8);   // four warps of either CTA
+
         }
+        for (int b = 0; b < SETS; ++b) mbar_init(sf_ready(b), 8);   // four warps of either CTA
         abort_flag[0] = 0;
         abort_flag[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -226,19 +229,18 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
                 if (!__all_sync(0xffffffffu, mbar_wait(acc_empty(b), ((lt >> 1) & 1u) ^ 1u, abort_flag))) { failed = true; break; }
                 tc_fence_after();
                 const uint32_t d = tmem_base + static_cast<uint32_t>(b * BN_MAX);
-                const uint32_t skip = ((tile / a.n_tiles) * a.BN % 128) / 32;      // columns into the first scale tile
                 for (int ks = 0; ks < k_steps; ++ks, ++it) {
                     const int s = it % S;
-                    const bool ok = mbar_wait(full(s), (it / S) & 1u, abort_flag) && mbar_wait(sf_ready(it & 1), (it >> 1) & 1u, abort_flag);
+                    const bool ok = mbar_wait(full(s), (it / S) & 1u, abort_flag) && mbar_wait(sf_ready(it % SETS), (it / SETS) & 1u, abort_flag);
                     if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
                     tc_fence_after();
-                    const uint32_t sfa = tmem_base + SF_COL + (it & 1) * SET_COLS, sfb = sfa + 4 * TILES + skip;
+                    const uint32_t sfa = tmem_base + SF_COL + (it % SETS) * SET_COLS, sfb = sfa + 4 * TILES;
                     const uint64_t adesc = smem_desc_sw128(base + OFF_A + s * A_BYTES), bdesc = smem_desc_sw128(base + OFF_B + s * B_BYTES);
                     const int mmas = a.K - ks * BK >= BK ? 4 : (a.K - ks * BK + 63) / 64;
                     auto mma = [&](int k) {
                         const int t = k / PER_TILE;
                         const uint32_t id = FMT == SQAP_MX_MXFP4 && (k & 1) ? (2u << 4) | (2u << 29) : 0u;
-                        tc_mma_mx4<FMT>(d, adesc + 2u * k, bdesc + 2u * k, idesc | id, sfa + 4u * t, sfb + 4u * SFB_TILES * t, (ks | k) != 0 ? 1u : 0u,
+                        tc_mma_mx4<FMT>(d, adesc + 2u * k, bdesc + 2u * k, idesc | id, sfa + 4u * t, sfb + SFB_COLS * t, (ks | k) != 0 ? 1u : 0u,
                                         issue);
                     };
                     if (mmas == 4) {
@@ -259,31 +261,36 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
         const uint32_t mine = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + SF_COL;
         uint32_t it = 0;
         for (int tile = pair; tile < total_tiles && !failed; tile += n_pairs) {
+            const bool middle = (tile / a.n_tiles) * a.BN % 128 != 0;          // the token tile starts 64 rows into a scale tile
             for (int ks = 0; ks < k_steps; ++ks, ++it) {
                 const int s = it % S;
                 bool ok = mbar_wait(sf_full(s), (it / S) & 1u, abort_flag);
-                // the MMAs that read this set two stages ago are done
-                if (ok && it >= 2) ok = mbar_wait(done((it - 2) % S), ((it - 2) / S) & 1u, abort_flag);
+                // the MMAs that read this set SETS stages ago are done
+                if (ok && it >= SETS) ok = mbar_wait(done((it - SETS) % S), ((it - SETS) / S) & 1u, abort_flag);
                 if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
                 tc_fence_after();
-                uint32_t r[4 * TILES * (1 + SFB_TILES)];
-                auto get = [&](int at, int off) {
-                    const uint4 u = *reinterpret_cast<const uint4*>(sm + off + lane * 16);
-                    r[at] = u.x; r[at + 1] = u.y; r[at + 2] = u.z; r[at + 3] = u.w;
-                };
+                constexpr int COLS = TILES * (4 + SFB_COLS);
+                uint32_t r[(COLS + 7) / 8 * 8] = {};
+                auto get = [&](int off) { return *reinterpret_cast<const uint4*>(sm + off + lane * 16); };
 #pragma unroll
-                for (int t = 0; t < TILES; ++t) get(4 * t, OFF_SFA + s * SF_BYTES + t * SF_TILE);
+                for (int t = 0; t < TILES; ++t) {
+                    const uint4 w = get(OFF_SFA + s * SF_BYTES + t * SF_TILE);
+                    const uint4 x = get(OFF_SFB + s * SFB_TILES * SF_BYTES + t * SF_TILE), y = get(OFF_SFB + (s * SFB_TILES + 1) * SF_BYTES + t * SF_TILE);
+                    r[4 * t] = w.x; r[4 * t + 1] = w.y; r[4 * t + 2] = w.z; r[4 * t + 3] = w.w;
+                    uint32_t* b = r + 4 * TILES + SFB_COLS * t;
+                    b[0] = middle ? x.z : x.x;
+                    b[1] = middle ? x.w : x.y;
+                    b[2] = middle ? y.x : x.z;
+                    b[3] = middle ? y.y : x.w;
+                    b[4] = middle ? y.z : y.x;
+                    b[5] = middle ? y.w : y.y;
+                }
 #pragma unroll
-                for (int t = 0; t < TILES; ++t)
-#pragma unroll
-                    for (int q = 0; q < SFB_TILES; ++q)
-                        get(4 * TILES + 4 * (t * SFB_TILES + q), OFF_SFB + (s * SFB_TILES + q) * SF_BYTES + t * SF_TILE);
-#pragma unroll
-                for (int c = 0; c < 4 * TILES * (1 + SFB_TILES); c += 8) tc_st8(mine + (it & 1) * SET_COLS + c, r + c);
+                for (int c = 0; c < COLS; c += 8) tc_st8(mine + (it % SETS) * SET_COLS + c, r + c);
                 tc_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(map_to_cta(sf_ready(it & 1), 0));
+                if (lane == 0) mbar_arrive_cluster(map_to_cta(sf_ready(it % SETS), 0));
             }
         }
     } else {
