@@ -41,13 +41,15 @@ constexpr int OFF_BAR = OFF_STAGE + EPI_STAGE_TOTAL;
 constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;
 constexpr int EPI_WARPS = 8;
 constexpr int SF_WARP0 = 2 + EPI_WARPS;
-constexpr int THREADS = 32 * (SF_WARP0 + 4);
+constexpr int SF_GROUPS = 2;              // of four scale warps; they take the stages in turn
+constexpr int SF_LOADER = SF_WARP0 + 4 * SF_GROUPS;
+constexpr int THREADS = 32 * (SF_LOADER + 1);
 // Scale columns: a stage's set has, for each scale tile along K, 4 columns of weight scales and 6 of token scales (192 rows,
 // from where the token tile starts). Three sets: writing one and signalling it takes longer than a stage's MMAs.
 constexpr int SETS = 3, SFB_COLS = BN_MAX / 32;
 constexpr int SF_COL = 2 * BN_MAX, SET_COLS = 4 * (4 + SFB_COLS);
 static_assert(SMEM_BYTES <= 227 * 1024 && SF_COL + SETS * SET_COLS <= 512, "budgets");
-static_assert(8 * (3 * S + 4 + SETS) + 16 <= 256, "barrier block");
+static_assert(8 * (4 * S + 4) + 16 <= 256, "barrier block");
 
 struct PairArgs {
     const float* gx;
@@ -87,12 +89,10 @@ __device__ __forceinline__ void tma_pair_if(uint32_t dst, const CUtensorMap* map
         ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(bar_cluster), "r"(issue)
         : "memory");
 }
-__device__ __forceinline__ void tc_commit_pair(uint32_t bar, uint32_t issue) {
+__device__ __forceinline__ void tc_commit_pair(uint32_t bar) {
     asm volatile(
-        "{\n\t.reg .pred q;\n\t"
-        "setp.ne.b32 q, %2, 0;\n\t"
-        "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}"
-        ::"r"(bar), "h"(static_cast<uint16_t>(3)), "r"(issue)
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+        ::"r"(bar), "h"(static_cast<uint16_t>(3))
         : "memory");
 }
 // Eight columns of this thread's tensor-memory lane.
@@ -104,22 +104,20 @@ __device__ __forceinline__ void tc_st8(uint32_t taddr, const uint32_t* r) {
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 template <int FMT>
 __device__ __forceinline__ void tc_mma_mx4(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb,
-                                           uint32_t accumulate, uint32_t issue) {
+                                           uint32_t accumulate) {
     if (FMT == SQAP_MX_NVFP4)
         asm volatile(
-            "{\n\t.reg .pred p, q;\n\t"
+            "{\n\t.reg .pred p;\n\t"
             "setp.ne.b32 p, %6, 0;\n\t"
-            "setp.ne.b32 q, %7, 0;\n\t"
-            "@q tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-            ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(issue)
+            "tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+            ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
             : "memory");
     else
         asm volatile(
-            "{\n\t.reg .pred p, q;\n\t"
+            "{\n\t.reg .pred p;\n\t"
             "setp.ne.b32 p, %6, 0;\n\t"
-            "setp.ne.b32 q, %7, 0;\n\t"
-            "@q tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-            ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(issue)
+            "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+            ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
             : "memory");
 }
 
@@ -133,14 +131,15 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;   // identical in both CTAs of the pair
     uint8_t* sm = smem_raw + (base - smem_u32(smem_raw));
     const uint32_t bar0 = base + OFF_BAR;
-    auto full = [&](int s) { return bar0 + 8u * s; };                  // leader's: both CTAs' loads of the stage have landed
+    auto full = [&](int s) { return bar0 + 8u * s; };                  // leader's: the stage's codes have landed and its scales are in
+                                                                       // tensor memory, in both CTAs
     auto done = [&](int s) { return bar0 + 8u * (S + s); };            // the MMAs of the stage in slot s are done (both CTAs)
     auto acc_full = [&](int b) { return bar0 + 8u * (2 * S + b); };
     auto acc_empty = [&](int b) { return bar0 + 8u * (2 * S + 2 + b); };   // leader's
     auto sf_full = [&](int s) { return bar0 + 8u * (2 * S + 4 + s); };     // this CTA's scale tiles of the stage have landed
-    auto sf_ready = [&](int b) { return bar0 + 8u * (3 * S + 4 + b); };    // leader's: a set of scale columns is there in both CTAs
-    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + OFF_BAR + 8 * (3 * S + 4 + SETS));
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + OFF_BAR + 8 * (3 * S + 4 + SETS) + 8);
+    auto sf_empty = [&](int s) { return bar0 + 8u * (3 * S + 4 + s); };    // ... and have been read
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + OFF_BAR + 8 * (4 * S + 4));
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + OFF_BAR + 8 * (4 * S + 4) + 8);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();          // 0 = leader
@@ -152,16 +151,15 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
-            mbar_init(full(s), 1);
+            mbar_init(full(s), 1 + 8);   // the loads; four scale warps of either CTA
             mbar_init(done(s), 1);
             mbar_init(sf_full(s), 1);
+            mbar_init(sf_empty(s), 4);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full(b), 1);
             mbar_init(acc_empty(b), 2 * EPI_WARPS);
-
         }
-        for (int b = 0; b < SETS; ++b) mbar_init(sf_ready(b), 8);   // four warps of either CTA
         abort_flag[0] = 0;
         abort_flag[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -177,22 +175,12 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
     bool failed = false;
-    // first scale-row tile of a token tile, and how many columns into it the tokens start
-    auto sf_row = [&](int m_tile) { return m_tile * a.BN / 128; };
 
     if (warp == 0) {
         const uint32_t issue = elect_one();
         auto weights = [&](int s, int ks, int n_tile, uint32_t bar) {
             const int nt = 2 * n_tile + static_cast<int>(rank);        // 128-row tile of the weights
             tma_pair_if(base + OFF_A + s * A_BYTES, &tm_w, ks * (BK / 2), nt * BM, bar, issue);
-            mbar_expect_tx_if(sf_full(s), sf_tx, issue);
-            tma_load_2d_if(base + OFF_SFA + s * SF_BYTES, &tm_wsf, 0, nt * a.k_tiles + ks * TILES, sf_full(s), issue);
-        };
-        auto tokens = [&](int s, int ks, int m_tile, uint32_t bar) {
-            tma_pair_if(base + OFF_B + s * B_BYTES, &tm_x, ks * (BK / 2), m_tile * a.BN + static_cast<int>(rank) * half_bn, bar, issue);
-#pragma unroll
-            for (int r = 0; r < SFB_TILES; ++r)
-                tma_load_2d_if(base + OFF_SFB + (s * SFB_TILES + r) * SF_BYTES, &tm_xsf, 0, (sf_row(m_tile) + r) * a.k_tiles + ks * TILES, sf_full(s), issue);
         };
         uint32_t early = 0;
         if (a.early && pair < total_tiles) {
@@ -209,39 +197,62 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
                 if (rank == 0) mbar_expect_tx_if(full(s), stage_tx, issue);
                 const uint32_t bar = map_to_cta(full(s), 0);
                 if (it >= early) weights(s, ks, n_tile, bar);
-                tokens(s, ks, m_tile, bar);
+                tma_pair_if(base + OFF_B + s * B_BYTES, &tm_x, ks * (BK / 2), m_tile * a.BN + static_cast<int>(rank) * half_bn, bar, issue);
             }
         }
-        if (failed) {
-            // the loads in flight are counted on the leader's barrier: give them a fixed while to land
-            const long long t0 = clock64();
-            while (clock64() - t0 < 200000) {}
+    } else if (warp == SF_LOADER) {
+        const uint32_t issue = elect_one();
+        auto weights = [&](int s, int ks, int n_tile) {
+            mbar_expect_tx_if(sf_full(s), sf_tx, issue);
+            tma_load_2d_if(base + OFF_SFA + s * SF_BYTES, &tm_wsf, 0, (2 * n_tile + static_cast<int>(rank)) * a.k_tiles + ks * TILES, sf_full(s), issue);
+        };
+        uint32_t early = 0;
+        if (a.early && pair < total_tiles) {
+            early = static_cast<uint32_t>(k_steps < S ? k_steps : S);
+            for (uint32_t ks = 0; ks < early; ++ks) weights(static_cast<int>(ks), static_cast<int>(ks), pair % a.n_tiles);
+        }
+        pdl_wait();
+        uint32_t it = 0;
+        for (int tile = pair; tile < total_tiles && !failed; tile += n_pairs) {
+            const int n_tile = tile % a.n_tiles, row_tile = tile / a.n_tiles * a.BN / 128;
+            for (int ks = 0; ks < k_steps; ++ks, ++it) {
+                const int s = it % S;
+                if (it >= S && !__all_sync(0xffffffffu, mbar_wait(sf_empty(s), (it / S - 1) & 1u, abort_flag))) { failed = true; break; }
+                if (it >= early) weights(s, ks, n_tile);
+#pragma unroll
+                for (int r = 0; r < SFB_TILES; ++r)
+                    tma_load_2d_if(base + OFF_SFB + (s * SFB_TILES + r) * SF_BYTES, &tm_xsf, 0, (row_tile + r) * a.k_tiles + ks * TILES, sf_full(s), issue);
+            }
         }
     } else if (warp == 1) {
         pdl_wait();
-        if (rank == 0) {
-            const uint32_t issue = elect_one();
+        if (rank == 0 && elect_one()) {
+            // One thread alone: its instructions are what the tensor core waits for, so no votes, and the barrier of the next stage is
+            // looked at before this stage's products are issued.
             const uint32_t idesc = (1u << 7) | (1u << 10) | (static_cast<uint32_t>(a.BN >> 3) << 17) | (FMT == SQAP_MX_MXFP4 ? 1u << 23 : 0u) |
                                    (static_cast<uint32_t>((2 * BM) >> 4) << 24);
-            uint32_t it = 0, lt = 0;
+            const uint64_t adesc0 = smem_desc_sw128(base + OFF_A), bdesc0 = smem_desc_sw128(base + OFF_B);
+            uint32_t lt = 0, ph = 0, set = tmem_base + SF_COL;
+            int s = 0;
+            bool ready = false;
             for (int tile = pair; tile < total_tiles && !failed; tile += n_pairs, ++lt) {
                 const int b = lt & 1;
-                if (!__all_sync(0xffffffffu, mbar_wait(acc_empty(b), ((lt >> 1) & 1u) ^ 1u, abort_flag))) { failed = true; break; }
+                if (!mbar_wait(acc_empty(b), ((lt >> 1) & 1u) ^ 1u, abort_flag)) { failed = true; break; }
                 tc_fence_after();
                 const uint32_t d = tmem_base + static_cast<uint32_t>(b * BN_MAX);
-                for (int ks = 0; ks < k_steps; ++ks, ++it) {
-                    const int s = it % S;
-                    const bool ok = mbar_wait(full(s), (it / S) & 1u, abort_flag) && mbar_wait(sf_ready(it % SETS), (it / SETS) & 1u, abort_flag);
-                    if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
+                for (int ks = 0; ks < k_steps; ++ks) {
+                    if (!ready && !mbar_wait(full(s), ph, abort_flag)) { failed = true; break; }
                     tc_fence_after();
-                    const uint32_t sfa = tmem_base + SF_COL + (it % SETS) * SET_COLS, sfb = sfa + 4 * TILES;
-                    const uint64_t adesc = smem_desc_sw128(base + OFF_A + s * A_BYTES), bdesc = smem_desc_sw128(base + OFF_B + s * B_BYTES);
+                    const int next = s + 1 == S ? 0 : s + 1;
+                    const uint32_t next_ph = s + 1 == S ? ph ^ 1u : ph;
+                    ready = mbar_test_wait(full(next), next_ph);
+                    const uint32_t sfa = set, sfb = sfa + 4 * TILES;
+                    const uint64_t adesc = adesc0 + static_cast<uint32_t>(s * (A_BYTES / 16)), bdesc = bdesc0 + static_cast<uint32_t>(s * (B_BYTES / 16));
                     const int mmas = a.K - ks * BK >= BK ? 4 : (a.K - ks * BK + 63) / 64;
                     auto mma = [&](int k) {
                         const int t = k / PER_TILE;
                         const uint32_t id = FMT == SQAP_MX_MXFP4 && (k & 1) ? (2u << 4) | (2u << 29) : 0u;
-                        tc_mma_mx4<FMT>(d, adesc + 2u * k, bdesc + 2u * k, idesc | id, sfa + 4u * t, sfb + SFB_COLS * t, (ks | k) != 0 ? 1u : 0u,
-                                        issue);
+                        tc_mma_mx4<FMT>(d, adesc + 2u * k, bdesc + 2u * k, idesc | id, sfa + 4u * t, sfb + SFB_COLS * t, k != 0 || ks != 0 ? 1u : 0u);
                     };
                     if (mmas == 4) {
 #pragma unroll
@@ -249,49 +260,57 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
                     } else {
                         for (int k = 0; k < mmas; ++k) mma(k);
                     }
-                    tc_commit_pair(done(s), issue);
+                    tc_commit_pair(done(s));
+                    s = next;
+                    ph = next_ph;
+                    set = set == tmem_base + SF_COL + (SETS - 1) * SET_COLS ? tmem_base + SF_COL : set + SET_COLS;
                 }
                 if (failed) break;
-                tc_commit_pair(acc_full(b), issue);
+                tc_commit_pair(acc_full(b));
             }
         }
+        __syncwarp();
     } else if (warp >= SF_WARP0) {
         // ---------------- scales: lane i of every quadrant holds rows i, 32 + i, 64 + i, 96 + i of a tile, a column each
         const int quad = warp & 3;
         const uint32_t mine = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + SF_COL;
-        uint32_t it = 0;
-        for (int tile = pair; tile < total_tiles && !failed; tile += n_pairs) {
-            const bool middle = (tile / a.n_tiles) * a.BN % 128 != 0;          // the token tile starts 64 rows into a scale tile
-            for (int ks = 0; ks < k_steps; ++ks, ++it) {
-                const int s = it % S;
-                bool ok = mbar_wait(sf_full(s), (it / S) & 1u, abort_flag);
-                // the MMAs that read this set SETS stages ago are done
-                if (ok && it >= SETS) ok = mbar_wait(done((it - SETS) % S), ((it - SETS) / S) & 1u, abort_flag);
-                if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
-                tc_fence_after();
-                constexpr int COLS = TILES * (4 + SFB_COLS);
-                uint32_t r[(COLS + 7) / 8 * 8] = {};
-                auto get = [&](int off) { return *reinterpret_cast<const uint4*>(sm + off + lane * 16); };
-#pragma unroll
-                for (int t = 0; t < TILES; ++t) {
-                    const uint4 w = get(OFF_SFA + s * SF_BYTES + t * SF_TILE);
-                    const uint4 x = get(OFF_SFB + s * SFB_TILES * SF_BYTES + t * SF_TILE), y = get(OFF_SFB + (s * SFB_TILES + 1) * SF_BYTES + t * SF_TILE);
-                    r[4 * t] = w.x; r[4 * t + 1] = w.y; r[4 * t + 2] = w.z; r[4 * t + 3] = w.w;
-                    uint32_t* b = r + 4 * TILES + SFB_COLS * t;
-                    b[0] = middle ? x.z : x.x;
-                    b[1] = middle ? x.w : x.y;
-                    b[2] = middle ? y.x : x.z;
-                    b[3] = middle ? y.y : x.w;
-                    b[4] = middle ? y.z : y.x;
-                    b[5] = middle ? y.w : y.y;
-                }
-#pragma unroll
-                for (int c = 0; c < COLS; c += 8) tc_st8(mine + (it % SETS) * SET_COLS + c, r + c);
-                tc_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(map_to_cta(sf_ready(it % SETS), 0));
+        const uint32_t my_tiles = pair < total_tiles ? (total_tiles - 1 - pair) / n_pairs + 1 : 0, stages = my_tiles * k_steps;
+        int tile = pair, ks = (warp - SF_WARP0) >> 2;
+        for (uint32_t it = ks; it < stages; it += SF_GROUPS, ks += SF_GROUPS) {
+            while (ks >= k_steps) {
+                ks -= k_steps;
+                tile += n_pairs;
             }
+            const bool middle = (tile / a.n_tiles) * a.BN % 128 != 0;          // the token tile starts 64 rows into a scale tile
+            const int s = it % S;
+            if (!__all_sync(0xffffffffu, mbar_wait(sf_full(s), (it / S) & 1u, abort_flag))) { failed = true; break; }
+            constexpr int COLS = TILES * (4 + SFB_COLS);
+            uint32_t r[(COLS + 7) / 8 * 8] = {};
+            auto get = [&](int off) { return *reinterpret_cast<const uint4*>(sm + off + lane * 16); };
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                const uint4 w = get(OFF_SFA + s * SF_BYTES + t * SF_TILE);
+                const uint4 x = get(OFF_SFB + s * SFB_TILES * SF_BYTES + t * SF_TILE), y = get(OFF_SFB + (s * SFB_TILES + 1) * SF_BYTES + t * SF_TILE);
+                r[4 * t] = w.x; r[4 * t + 1] = w.y; r[4 * t + 2] = w.z; r[4 * t + 3] = w.w;
+                uint32_t* b = r + 4 * TILES + SFB_COLS * t;
+                b[0] = middle ? x.z : x.x;
+                b[1] = middle ? x.w : x.y;
+                b[2] = middle ? y.x : x.z;
+                b[3] = middle ? y.y : x.w;
+                b[4] = middle ? y.z : y.x;
+                b[5] = middle ? y.w : y.y;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sf_empty(s));
+            // the MMAs that read this set SETS stages ago are done
+            if (it >= SETS && !__all_sync(0xffffffffu, mbar_wait(done((it - SETS) % S), ((it - SETS) / S) & 1u, abort_flag))) { failed = true; break; }
+            tc_fence_after();
+#pragma unroll
+            for (int c = 0; c < COLS; c += 8) tc_st8(mine + (it % SETS) * SET_COLS + c, r + c);
+            tc_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(map_to_cta(full(s), 0));
         }
     } else {
         pdl_wait();
@@ -357,6 +376,11 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
     }
     tc_fence_before();
     __syncthreads();
+    if (*abort_flag) {
+        // the loads in flight are counted on barriers that no one waits for any more: give them a fixed while to land
+        const long long t0 = clock64();
+        while (clock64() - t0 < 200000) {}
+    }
     cluster_sync_all();   // neither CTA leaves (or frees tensor memory) while the other may still signal it
     tc_fence_after();
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem_base) : "memory");
