@@ -101,6 +101,26 @@ __device__ __forceinline__ void tc_st8(uint32_t taddr, const uint32_t* r) {
                  ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                  : "memory");
 }
+// 16 lanes x 32 columns as fragments of 8 x 8: r[4 u + 2 h + e] is row 8 h + lane / 4, column 8 u + 2 (lane % 4) + e.
+__device__ __forceinline__ void tc_ld_fragments(uint32_t taddr, uint32_t* r) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr));
+}
+// Four 8 x 8 fragments of 16-bit values, turned, to the rows of 16 bytes that lanes 0-7, 8-15, ... address.
+__device__ __forceinline__ void store_turned(uint32_t row, const uint32_t* p) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(row), "r"(p[0]), "r"(p[1]), "r"(p[2]), "r"(p[3]) : "memory");
+}
+template <int OUT>
+__device__ __forceinline__ uint32_t bits16x2(float lo, float hi) {
+    if (OUT == SQAP_FP16) {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 template <int FMT>
 __device__ __forceinline__ void tc_mma_mx4(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb,
@@ -320,6 +340,52 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
         const int split = ((a.BN / 16 + 1) / 2) * 16;
         const int c_begin = hf == 0 ? 0 : split, c_end = hf == 0 ? split : a.BN;
         uint8_t* stage_half = sm + OFF_STAGE + hf * 2 * EPI_STAGE_BYTES;
+        // 32 tokens at a time in the layout of 8 x 8 fragments (channel lane / 4, tokens 2 (lane % 4) and the next), turned on the way
+        // to shared memory; the 16-byte pieces of a token's row there are permuted by the token against bank conflicts. A thread
+        // copies out piece tid_half % 16 of tokens tid_half / 16 and 8 further on.
+        const int out_token = tid_half >> 4, out_piece = tid_half & 15;
+        const uint32_t put = smem_u32(stage_half) + (lane & 7) * (BM * 2) + ((quad * 4 + (lane >> 3)) ^ (lane & 7)) * 16;
+        const uint8_t* take = stage_half + out_token * (BM * 2) + (out_piece ^ out_token) * 16;
+        auto store_tile = [&](auto out_type, uint32_t taddr, int m0, int n0) {
+            constexpr int OUT = decltype(out_type)::value;
+            const int n = n0 + out_piece * 8, n_left = a.N - n;
+            int m = m0 + c_begin + out_token;
+            uint16_t* dst = static_cast<uint16_t*>(a.out) + static_cast<int64_t>(m) * a.ldo + n;
+            for (int c = c_begin; c < c_end; c += 32) {
+                uint32_t v[2][16];
+                tc_ld_fragments(taddr + c, v[0]);
+                tc_ld_fragments(taddr + c + (16u << 16), v[1]);
+                tc_wait_ld();
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {             // 16 tokens each, into two buffers in turn
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        uint32_t p[4];
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const uint32_t* x = v[g >> 1] + 8 * part + 4 * u + 2 * (g & 1);
+                            p[g] = bits16x2<OUT>(__uint_as_float(x[0]) * alpha, __uint_as_float(x[1]) * alpha);
+                        }
+                        store_turned(put + part * EPI_STAGE_BYTES + u * 8 * (BM * 2), p);
+                    }
+                    // A thread can only be two buffers ahead of the slowest after passing the barrier in between
+                    bar_sync_named(2 + hf, 128);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i, m += 8, dst += 8 * a.ldo) {
+                        if (m >= a.M || n_left <= 0) continue;
+                        const uint4 y = *reinterpret_cast<const uint4*>(take + part * EPI_STAGE_BYTES + i * 8 * (BM * 2));
+                        if (n_left >= 8) {
+                            *reinterpret_cast<uint4*>(dst) = y;
+                        } else {
+                            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                            for (int e = 0; e < 7; ++e)
+                                if (e < n_left) dst[e] = static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)));
+                        }
+                    }
+                }
+            }
+        };
         uint32_t lt = 0;
         for (int tile = pair; tile < total_tiles && !failed; tile += n_pairs, ++lt) {
             const int b = lt & 1;
@@ -328,41 +394,21 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
             if (bar_or(1, 32 * EPI_WARPS, !mbar_wait(acc_full(b), (lt >> 1) & 1u, abort_flag))) { failed = true; break; }
             tc_fence_after();
             const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + static_cast<uint32_t>(b * BN_MAX);
-            int flip = 0;
-            for (int c = c_begin; c < c_end; c += 16, flip ^= 1) {
-                uint32_t v[16];
-                tc_ld16(taddr + c, v);
-                tc_wait_ld();
-                if (a.out_dtype == SQAP_FP32) {                        // a warp's 32 channels of a token are 128 bytes
+            if (a.out_dtype == SQAP_FP32) {                            // a warp's 32 channels of a token are 128 bytes
+                for (int c = c_begin; c < c_end; c += 16) {
+                    uint32_t v[16];
+                    tc_ld16(taddr + c, v);
+                    tc_wait_ld();
                     float* o = static_cast<float*>(a.out) + static_cast<int64_t>(m0 + c) * a.ldo + n0 + row;
                     if (n0 + row < a.N)
 #pragma unroll
                         for (int j = 0; j < 16; ++j)
                             if (m0 + c + j < a.M) o[j * a.ldo] = __uint_as_float(v[j]) * alpha;
-                    continue;
                 }
-                uint8_t* stage = stage_half + flip * EPI_STAGE_BYTES;
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const float y = __uint_as_float(v[j]) * alpha;
-                    *reinterpret_cast<uint16_t*>(stage + j * (BM * 2) + row * 2) = a.out_dtype == SQAP_FP16 ? bits16<SQAP_FP16>(y) : bits16<SQAP_BF16>(y);
-                }
-                // Two buffers in turn: a thread can only be two chunks ahead of the slowest after passing the barrier in between
-                bar_sync_named(2 + hf, 128);
-#pragma unroll
-                for (int p = tid_half; p < 16 * (BM / 8); p += 128) {
-                    const int token = p / (BM / 8), piece = p % (BM / 8);
-                    const int m = m0 + c + token, n = n0 + piece * 8;
-                    if (m < a.M && n < a.N) {
-                        const uint16_t* src = reinterpret_cast<const uint16_t*>(stage + token * (BM * 2) + piece * 16);
-                        uint16_t* dst = static_cast<uint16_t*>(a.out) + static_cast<int64_t>(m) * a.ldo + n;
-                        if (n + 8 <= a.N) {
-                            *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(src);
-                        } else {
-                            for (int e = 0; e < a.N - n; ++e) dst[e] = src[e];
-                        }
-                    }
-                }
+            } else if (a.out_dtype == SQAP_FP16) {
+                store_tile(std::integral_constant<int, SQAP_FP16>{}, taddr, m0, n0);
+            } else {
+                store_tile(std::integral_constant<int, SQAP_BF16>{}, taddr, m0, n0);
             }
             tc_fence_before();
             __syncwarp();
