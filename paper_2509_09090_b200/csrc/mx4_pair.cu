@@ -45,10 +45,11 @@ constexpr int SF_GROUPS = 2;              // of four scale warps; they take the 
 constexpr int SF_LOADER = SF_WARP0 + 4 * SF_GROUPS;
 constexpr int THREADS = 32 * (SF_LOADER + 1);
 // Scale columns: a stage's set has, for each scale tile along K, 4 columns of weight scales and 6 of token scales (192 rows,
-// from where the token tile starts). Three sets: writing one and signalling it takes longer than a stage's MMAs.
-constexpr int SETS = 3, SFB_COLS = BN_MAX / 32;
-constexpr int SF_COL = 2 * BN_MAX, SET_COLS = 4 * (4 + SFB_COLS);
-static_assert(SMEM_BYTES <= 227 * 1024 && SF_COL + SETS * SET_COLS <= 512, "budgets");
+// from where the token tile starts). As many sets as the accumulators leave room for, a stage of the ring each at most:
+// from the end of a stage's MMAs to the set written again and signalled takes some 1000 cycles, the MMAs of a stage 2 BN.
+constexpr int SFB_COLS = BN_MAX / 32, SET_COLS = 4 * (4 + SFB_COLS);
+__host__ __device__ constexpr int sets_for(int bn) { return (512 - 2 * bn) / SET_COLS < S ? (512 - 2 * bn) / SET_COLS : S; }
+static_assert(SMEM_BYTES <= 227 * 1024 && sets_for(BN_MAX) >= 2, "budgets");
 static_assert(8 * (4 * S + 4) + 16 <= 256, "barrier block");
 
 struct PairArgs {
@@ -167,6 +168,7 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
     const int half_bn = a.BN >> 1;
     const int k_steps = (a.K + BK - 1) / BK;
     const int total_tiles = a.m_tiles * a.n_tiles;
+    const uint32_t sets = sets_for(a.BN);
     const uint32_t stage_tx = 2u * static_cast<uint32_t>(A_BYTES + half_bn * (BK / 2)), sf_tx = TILES * SF_TILE * (1 + SFB_TILES);
 
     if (threadIdx.x == 0) {
@@ -252,14 +254,16 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
             const uint32_t idesc = (1u << 7) | (1u << 10) | (static_cast<uint32_t>(a.BN >> 3) << 17) | (FMT == SQAP_MX_MXFP4 ? 1u << 23 : 0u) |
                                    (static_cast<uint32_t>((2 * BM) >> 4) << 24);
             const uint64_t adesc0 = smem_desc_sw128(base + OFF_A), bdesc0 = smem_desc_sw128(base + OFF_B);
-            uint32_t lt = 0, ph = 0, set = tmem_base + SF_COL;
+            uint32_t lt = 0, ph = 0;
+            const uint32_t set0 = tmem_base + 2u * a.BN, last_set = set0 + (sets - 1) * SET_COLS;
+            uint32_t set = set0;
             int s = 0;
             bool ready = false;
             for (int tile = pair; tile < total_tiles && !failed; tile += n_pairs, ++lt) {
                 const int b = lt & 1;
                 if (!mbar_wait(acc_empty(b), ((lt >> 1) & 1u) ^ 1u, abort_flag)) { failed = true; break; }
                 tc_fence_after();
-                const uint32_t d = tmem_base + static_cast<uint32_t>(b * BN_MAX);
+                const uint32_t d = tmem_base + static_cast<uint32_t>(b * a.BN);
                 for (int ks = 0; ks < k_steps; ++ks) {
                     if (!ready && !mbar_wait(full(s), ph, abort_flag)) { failed = true; break; }
                     tc_fence_after();
@@ -283,7 +287,7 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
                     tc_commit_pair(done(s));
                     s = next;
                     ph = next_ph;
-                    set = set == tmem_base + SF_COL + (SETS - 1) * SET_COLS ? tmem_base + SF_COL : set + SET_COLS;
+                    set = set == last_set ? set0 : set + SET_COLS;
                 }
                 if (failed) break;
                 tc_commit_pair(acc_full(b));
@@ -293,10 +297,12 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
     } else if (warp >= SF_WARP0) {
         // ---------------- scales: lane i of every quadrant holds rows i, 32 + i, 64 + i, 96 + i of a tile, a column each
         const int quad = warp & 3;
-        const uint32_t mine = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + SF_COL;
+        const uint32_t mine = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + 2u * a.BN;
         const uint32_t my_tiles = pair < total_tiles ? (total_tiles - 1 - pair) / n_pairs + 1 : 0, stages = my_tiles * k_steps;
         int tile = pair, ks = (warp - SF_WARP0) >> 2;
-        for (uint32_t it = ks; it < stages; it += SF_GROUPS, ks += SF_GROUPS) {
+        uint32_t set = ks;
+        for (uint32_t it = ks; it < stages; it += SF_GROUPS, ks += SF_GROUPS, set += SF_GROUPS) {
+            if (set >= sets) set -= sets;
             while (ks >= k_steps) {
                 ks -= k_steps;
                 tile += n_pairs;
@@ -322,11 +328,11 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(sf_empty(s));
-            // the MMAs that read this set SETS stages ago are done
-            if (it >= SETS && !__all_sync(0xffffffffu, mbar_wait(done((it - SETS) % S), ((it - SETS) / S) & 1u, abort_flag))) { failed = true; break; }
+            // the MMAs that read this set `sets` stages ago are done
+            if (it >= sets && !__all_sync(0xffffffffu, mbar_wait(done((it - sets) % S), ((it - sets) / S) & 1u, abort_flag))) { failed = true; break; }
             tc_fence_after();
 #pragma unroll
-            for (int c = 0; c < COLS; c += 8) tc_st8(mine + (it % SETS) * SET_COLS + c, r + c);
+            for (int c = 0; c < COLS; c += 8) tc_st8(mine + set * SET_COLS + c, r + c);
             tc_wait_st();
             tc_fence_before();
             __syncwarp();
@@ -393,7 +399,7 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
             // all epilogue warps leave the loop together if any wait ran out, so the barriers below never hang
             if (bar_or(1, 32 * EPI_WARPS, !mbar_wait(acc_full(b), (lt >> 1) & 1u, abort_flag))) { failed = true; break; }
             tc_fence_after();
-            const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + static_cast<uint32_t>(b * BN_MAX);
+            const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + static_cast<uint32_t>(b * a.BN);
             if (a.out_dtype == SQAP_FP32) {                            // a warp's 32 channels of a token are 128 bytes
                 for (int c = c_begin; c < c_end; c += 16) {
                     uint32_t v[16];
