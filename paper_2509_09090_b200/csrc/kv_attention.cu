@@ -6,18 +6,23 @@ namespace sqap {
 namespace kv {
 namespace {
 
-// One warp per row: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
-template <typename T, int D>
+// Pieces from which on four warps join a row (32 heads, 4096 keys in 16 pieces: 10.5 -> 8.7 us with the attention).
+constexpr int COMBINE_SPLITS = 8;
+
+// out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s. A row is joined by WARPS warps, which take its pieces in turn and meet in
+// shared memory; four rows / WARPS to a CTA.
+template <typename T, int D, int WARPS>
 __global__ void __launch_bounds__(128) kv_combine_kernel(AttnArgs a) {
+    __shared__ float red[WARPS > 1 ? WARPS : 1][WARPS > 1 ? D : 1], red_l[4];
     pdl_launch_dependents();
     pdl_wait();
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % WARPS;
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * (4 / WARPS) + warp / WARPS;
     const int i = static_cast<int>(id % a.max_q);
     const int64_t bh = id / a.max_q;
     const int head = static_cast<int>(bh % a.heads);
     const int64_t b = bh / a.heads;
-    if (b >= a.batch) return;
+    if (b >= a.batch) return;                                    // WARPS == 4: the whole CTA
     const int row0 = a.cu[b];
     if (i >= a.cu[b + 1] - row0) return;
     const int64_t at = part_index(a, static_cast<int>(b), head, i, 0);
@@ -27,10 +32,10 @@ __global__ void __launch_bounds__(128) kv_combine_kernel(AttnArgs a) {
     for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     const float ref = m == -INFINITY ? 0.0f : m;
     float l = 0.0f, y[D / 32] = {};
-    for (int s = 0; s < a.splits; ++s) {
+#pragma unroll 4
+    for (int s = part; s < a.splits; s += WARPS) {
         const float2 ml = a.part_ml[at + s];
-        if (!(ml.y > 0.0f)) continue;
-        const float f = fast_exp2(ml.x - ref);
+        const float f = fast_exp2(ml.x - ref);                   // 0 for a piece without keys, whose output and denominator are 0
         l = fmaf(ml.y, f, l);
         const float2* p = reinterpret_cast<const float2*>(a.part_o + (at + s) * D) + lane;
 #pragma unroll
@@ -40,29 +45,54 @@ __global__ void __launch_bounds__(128) kv_combine_kernel(AttnArgs a) {
             y[2 * e + 1] = fmaf(x.y, f, y[2 * e + 1]);
         }
     }
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    if (WARPS > 1) {
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) *reinterpret_cast<float2*>(&red[part][64 * e + 2 * lane]) = make_float2(y[2 * e], y[2 * e + 1]);
+        if (lane == 0) red_l[part] = l;
+        __syncthreads();
+        if (part != 0) return;
+#pragma unroll
+        for (int w = 1; w < WARPS; ++w) {
+            l += red_l[w];
+#pragma unroll
+            for (int e = 0; e < D / 64; ++e) {
+                const float2 x = *reinterpret_cast<const float2*>(&red[w][64 * e + 2 * lane]);
+                y[2 * e] += x.x;
+                y[2 * e + 1] += x.y;
+            }
+        }
+    }
+    const float inv = l != 0.0f ? 1.0f / l : 0.0f;
     const int64_t row = static_cast<int64_t>(row0) + i;
     uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + row * a.ldo + static_cast<int64_t>(head) * D) + lane;
 #pragma unroll
     for (int e = 0; e < D / 64; ++e) out[32 * e] = pack2<T>(y[2 * e] * inv, y[2 * e + 1] * inv);
-    if (lane == 0 && a.lse) a.lse[row * a.heads + head] = l > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+    if (lane == 0 && a.lse) a.lse[row * a.heads + head] = l != 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
 }
 
+template <typename T, int D>
+cudaError_t combine_dim(const AttnArgs& a, cudaStream_t s) {
+    const int64_t rows = static_cast<int64_t>(a.batch) * a.heads * a.max_q;
+    if (a.splits >= COMBINE_SPLITS && rows <= 0x7FFFFFFF) return launch_dependent(kv_combine_kernel<T, D, 4>, dim3(static_cast<unsigned>(rows)), dim3(128), 0, s, a);
+    return launch_dependent(kv_combine_kernel<T, D, 1>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(128), 0, s, a);
+}
 template <typename T>
 cudaError_t combine_as(const AttnArgs& a, cudaStream_t s) {
-    const int64_t rows = static_cast<int64_t>(a.batch) * a.heads * a.max_q;
-    const dim3 grid(static_cast<unsigned>((rows + 3) / 4));
-    if (a.c.head_dim == 64) return launch_dependent(kv_combine_kernel<T, 64>, grid, dim3(128), 0, s, a);
-    if (a.c.head_dim == 128) return launch_dependent(kv_combine_kernel<T, 128>, grid, dim3(128), 0, s, a);
-    return launch_dependent(kv_combine_kernel<T, 256>, grid, dim3(128), 0, s, a);
+    if (a.c.head_dim == 64) return combine_dim<T, 64>(a, s);
+    if (a.c.head_dim == 128) return combine_dim<T, 128>(a, s);
+    return combine_dim<T, 256>(a, s);
 }
 
 struct Plan {
     bool decode;
     int tiles, splits, chunk;
 };
-// From the sizes alone, so that the workspace can be asked for ahead: enough CTAs to fill the device a few times over
-// (uneven histories then even out), pieces of 256 keys at least.
+// From the sizes alone, so that the workspace can be asked for ahead. Decode: up to 1024 keys a history is cut only where there
+// are fewer than three CTAs to an SM, beyond that to four, and to sixteen as long as pieces keep 1024 keys (uneven histories then even
+// out). Measured at 8 and 32 heads, us, with four / eight / sixteen CTAs to an SM: 1 x 32768 keys 24 / 28 / 28, 16 x 2048 48 / 52 / 56,
+// 32 x 4096 48 / 50 / 53, 32 uneven ones of up to 16384 145 / 139 / 137; three / four at 16 x 290: 8.9 / 12.8.
+// Prompts: two rounds of CTAs where there is less than one, in pieces of 1024 keys at least: cut / whole, us, 256 rows behind 1000
+// keys (8 heads, groups of 4) 38 / 31, behind 8000 92 / 153; 288 rows behind 4096 (32 heads) 73 / 85.
 Plan plan_for(int64_t batch, int kv_heads, int group, int head_dim, int64_t max_q, int64_t max_len) {
     Plan p;
     const int64_t rows = max_q * group;
@@ -70,12 +100,15 @@ Plan plan_for(int64_t batch, int kv_heads, int group, int head_dim, int64_t max_
     const int per_tile = head_dim <= 128 ? PREFILL_TC_ROWS : PREFILL_ROWS;
     p.tiles = p.decode ? 1 : static_cast<int>((rows + per_tile - 1) / per_tile);
     const int64_t ctas = batch * kv_heads * p.tiles;
-    int64_t want;
-    if (p.decode) want = max_len > 1024 ? 148 * 16 : 148 * 3;
-    else want = ctas < 148 ? 148 * 2 : 0;
-    int64_t splits = ctas > 0 ? (want + ctas - 1) / ctas : 1;
-    const int64_t most = (max_len + 255) / 256;
-    if (splits > most) splits = most;
+    auto pieces = [&](int per_sm) { return ctas > 0 ? (148 * per_sm + ctas - 1) / ctas : 1; };
+    auto least = [](int64_t x, int64_t y) { return x < y ? x : y; };
+    int64_t splits;
+    if (p.decode) {
+        const int64_t fill = least(pieces(max_len > 1024 ? 4 : 3), (max_len + 255) / 256), even = least(pieces(16), max_len / 1024);
+        splits = fill > even ? fill : even;
+    } else {
+        splits = ctas < 148 ? least(pieces(2), max_len / 1024) : 1;
+    }
     if (splits < 1) splits = 1;
     const int64_t chunk = ((max_len + splits - 1) / splits + 127) / 128 * 128;
     p.chunk = static_cast<int>(chunk < 128 ? 128 : chunk);

@@ -9,9 +9,10 @@
 //   output  O[element][row] = V^T w:  lane (g, t) loads D/8 consecutive bytes of the values of tokens 2t, 2t+1, 2t+8, 2t+9; byte
 //           permutes pair up the tokens of an element. The weights turn from the score layout (token down, row across)
 //           into the operand layout by one transposition of 8 x 8 halves (movmatrix) per eight tokens.
-// A warp keeps a running maximum, denominator and output of its own over 32-token steps (16 at D = 256); the warps of a
+// A warp keeps a running maximum, denominator and output of its own over steps of 16 or 32 tokens (see launch_rows); the warps of a
 // CTA take the steps of their piece of the history in turn and meet in shared memory once at the end. Histories that are
-// too few to fill the device are cut into pieces, joined by kv_combine_kernel.
+// too few to fill the device are cut into pieces, joined by kv_combine_kernel. 32 uneven histories of up to 16384 tokens, 8 heads of
+// 128 in e4m3, groups of 4: 125 us, 4.8 TB/s; what is left is the start and end of uneven pieces and 16 warps an SM.
 #include "kv_attention.cuh"
 
 namespace sqap {
@@ -376,14 +377,15 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
 
 template <typename T, int TYPE, int D>
 cudaError_t launch_rows(const AttnArgs& a, unsigned grid, cudaStream_t s) {
-    // 16-token groups per step. Short histories are a matter of latency: with one group a fourth CTA fits an SM, so that e.g.
-    // 16 sequences x 32 heads run in one wave (step of 16 x 290 tokens: 24.2 us with two groups, 22.9 with one).
-    constexpr int GROUPS = D == 256 ? 1 : 2;
-    if (static_cast<int64_t>(a.max_q) * a.group <= 8 && a.max_len <= 1024)
-        return launch_dependent(kv_decode_kernel<T, TYPE, D, 1, 1>, dim3(grid), dim3(WARPS * 32), 0, s, a);
-    if (static_cast<int64_t>(a.max_q) * a.group <= 8) return launch_dependent(kv_decode_kernel<T, TYPE, D, 1, GROUPS>, dim3(grid), dim3(WARPS * 32), 0, s, a);
+    // 16-token groups per step. With one group of 128 elements a fourth CTA fits an SM, at 64 elements a second group's loads in
+    // flight count for more. Measured, one / two groups, us: D = 128, 16 x 290 tokens x 32 heads 8.9 / 10.3, 16 x 2048 45 / 56,
+    // 32 sequences of up to 16384 x 8 heads 125 / 137; D = 64, the same, 6.9 / 6.6, 32 / 30, 82 / 75.
+    constexpr int GROUPS = D == 64 ? 2 : 1;
+    if (static_cast<int64_t>(a.max_q) * a.group <= 8)
+        return launch_dependent(kv_decode_kernel<T, TYPE, D, 1, GROUPS>, dim3(grid), dim3(WARPS * 32), 0, s, a);
+    // 9 to 16 rows: one / two groups, 32 x 8192 tokens x 8 heads of 128, 12 rows, 127 / 107; 16 x 2048, 16 rows, 33 / 30.
     if (D == 256) return cudaErrorInvalidValue;     // not reached: see decode_max_rows()
-    return launch_dependent(kv_decode_kernel<T, TYPE, D == 256 ? 128 : D, 2, GROUPS>, dim3(grid), dim3(WARPS * 32), 0, s, a);
+    return launch_dependent(kv_decode_kernel<T, TYPE, D == 256 ? 128 : D, 2, 2>, dim3(grid), dim3(WARPS * 32), 0, s, a);
 }
 template <typename T, int TYPE>
 cudaError_t launch_dim(const AttnArgs& a, unsigned grid, cudaStream_t s) {

@@ -5,7 +5,8 @@
 // One CTA takes 128 rows (query x head of the group, packed: the heads that share a key/value head share its tiles) of one
 // sequence and key/value head and walks the keys in tiles. A tile's codes are fetched one tile ahead into registers,
 // turned into fp16 once per CTA and kept in shared memory, from where the eight warps (16 rows each) feed
-// register matrix instructions: scores, running maximum and denominator, weights times values.
+// register matrix instructions: scores, running maximum and denominator, weights times values. Bounded by their rate, an
+// eighth of tcgen05's, and by the registers that allow one CTA an SM (16 prompts' last 8 tokens behind 290, 32 heads: 119 us).
 #include "kv_attention.cuh"
 
 namespace sqap {

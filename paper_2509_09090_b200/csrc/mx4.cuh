@@ -31,7 +31,7 @@ struct Mx4Product {
 // The weight stream for a handful of tokens (mx4_gemv.cu). x: rows that it quantizes itself (x_codes and x_scales are then not
 // read), or null.
 constexpr int MX4_GEMV_MAX_ROWS = 4;
-bool mx4_gemv_supports(int M, int K, int format);
+bool mx4_gemv_takes(int M, int N, int K, int format);
 sqap_status launch_mx4_gemv(const Mx4Product& q, const void* x, int x_dtype, int64_t ldx, const int32_t* row_index, cudaStream_t s);
 // The kernel for many tokens (mx4_pair.cu).
 sqap_status launch_mx4_pair(const Mx4Product& q, cudaStream_t s);

@@ -4,8 +4,9 @@
 // scales and accumulates in fp32; nothing is unpacked on the way. Weights are the MMA-M operand (128 rows of a tile),
 // tokens the MMA-N operand (BN columns), so that a handful of tokens costs a narrow tile and not a mostly empty one.
 //
-// What bounds it. Few tokens: the weight stream (0.5625 or 0.53 bytes per weight). Many tokens: the tensor cores, four
-// times the bf16 rate, for which an SM has to be fed two 16 KB operand tiles per 256 elements of K.
+// This kernel is for few tokens, few weight rows and long K (use_clusters()); many tokens or rows: mx4_pair.cu. What bounds it: the
+// weight stream (0.5625 or 0.53 bytes per weight, 3.7 us of HBM for 4096 x 11008), and around it the set-up (some 2400 cycles)
+// and the exchange of partial sums (3000 to 4000 at 160 tokens). 160 x 4096 x 11008 in MXFP4 with the quantizer: 14.6 us.
 //
 // A stage of the shared-memory ring holds 256 elements of K: 128 bytes per row of either operand (one 128B-swizzled
 // TMA box each) and the scale tiles that belong to them, copied as they lie in memory (512 bytes per 128 rows and
@@ -29,7 +30,6 @@ using namespace tc;
 constexpr int BM = 128;                   // weight rows per tile
 constexpr int BK = 256;                   // elements of K per stage
 constexpr int BN_MAX = 256;
-constexpr int PAIR_ROWS = 256;            // more tokens than this go to the CTA-pair kernel (mx4_pair.cu)
 constexpr int S_MAX = 10;
 constexpr int KSPLIT_MAX = 8;
 constexpr int A_BYTES = BM * BK / 2;      // 16 KB
@@ -47,7 +47,7 @@ struct MxArgs {
     void* out;
     int64_t ldo;
     int M, N, K;
-    int BN, m_tiles, n_tiles;
+    int BN;
     int out_dtype;
     int stages, stage_bytes;
     int k_tiles;       // scale tiles along K
@@ -140,14 +140,13 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constan
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = static_cast<int>(cluster_ctarank());
-    const int tile = static_cast<int>(blockIdx.x) / a.ksplit;
-    const int nt = tile % a.n_tiles, n0 = nt * BM, m0 = (tile / a.n_tiles) * a.BN;
+    const int nt = static_cast<int>(blockIdx.x) / a.ksplit, n0 = nt * BM;
     const int k_steps = (a.K + BK - 1) / BK;
     const int ks_begin = rank * k_steps / a.ksplit, ks_end = (rank + 1) * k_steps / a.ksplit;
     const int my_steps = ks_end - ks_begin;
     const int sfb_rows = (a.BN + 127) / 128;                 // scale tiles across a token tile
     const int m_sf_tiles = (a.M + 127) / 128;
-    const int sfb_here = m_sf_tiles - m0 / 128 < sfb_rows ? m_sf_tiles - m0 / 128 : sfb_rows;   // those that exist
+    const int sfb_here = m_sf_tiles < sfb_rows ? m_sf_tiles : sfb_rows;   // those that exist
     auto a_addr = [&](int s) { return base + static_cast<uint32_t>(s * a.stage_bytes); };
     auto b_addr = [&](int s) { return a_addr(s) + A_BYTES; };
     auto sfa_addr = [&](int s) { return b_addr(s) + static_cast<uint32_t>(a.BN * 128); };
@@ -163,9 +162,9 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constan
     };
     auto issue_tokens = [&](int ks, int s, uint32_t issue) {
         const uint32_t sf = static_cast<uint32_t>(sf_tiles(ks) * SF_TILE);
-        tma_load_2d_if(b_addr(s), &tm_x, ks * (BK / 2), m0, full(s), issue);
+        tma_load_2d_if(b_addr(s), &tm_x, ks * (BK / 2), 0, full(s), issue);
         for (int r = 0; r < sfb_here; ++r)
-            bulk_load_if(sfb_addr(s, r), a.x_sf + (static_cast<size_t>(m0 / 128 + r) * a.k_tiles + ks * TILES) * SF_TILE, sf, full(s), issue);
+            bulk_load_if(sfb_addr(s, r), a.x_sf + (static_cast<size_t>(r) * a.k_tiles + ks * TILES) * SF_TILE, sf, full(s), issue);
     };
     const int pre = my_steps < S ? my_steps : S;   // stages issued before the main loop
     if (warp == 0) {
@@ -291,7 +290,7 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constan
     // buffers a group in turn, one barrier of the group a chunk.
     uint8_t* const stage0 = sm + own_max * a.ksplit * CHUNK_BYTES + group * 2 * STAGE_BYTES;
     for (int lc = group, turn = 0; lc < own; lc += 2, turn ^= 1) {
-        const int m_first = m0 + 16 * (lc * a.ksplit + rank);
+        const int m_first = 16 * (lc * a.ksplit + rank);
         float y[16];
         const uint8_t* part = sm + lc * CHUNK_BYTES + row * 16;
 #pragma unroll
@@ -337,10 +336,21 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constan
     }
 }
 
+// Which kernel. The pairs (mx4_pair.cu) take 256 weight rows and up to 192 tokens each and walk K alone: some 5 us and 0.25 us
+// per 256 elements of K and round. The clusters here split K where there are few tiles, but then exchange 4 bytes per token and
+// weight row of every slice. So they are for long K, few weight rows and few tokens. Measured with the quantizer, clusters / pairs,
+// us: 4096 x 11008 (rows x K): 14.9 / 15.9 for 64 tokens, 14.7 / 16.6 for 128, 17.3 / 17.6 for 192, 25.9 / 19.6 for 320;
+// 1024 x 4096: 7.2 / 9.1 for 16, 8.3 / 9.3 for 64, 10.1 / 9.3 for 128; 4096 x 4096: 10.3 / 8.9 for 16, 13.5 / 10.1 for 256;
+// 12288 x 4096: 16.4 / 10.0 for 16, 21.0 / 17.1 for 256.
+static bool use_clusters(int M, int N, int K) {
+    const int64_t steps = (K + BK - 1) / BK, weight_tiles = (N + 2 * BM - 1) / (2 * BM);
+    return M <= BN_MAX && 64ll * M <= K && steps * (sm_count() / 2) > 128 * weight_tiles;
+}
+
 static sqap_status launch(const Mx4Product& q, cudaStream_t s) {
     const int M = q.M, N = q.N, K = q.K, format = q.format;
-    if (mx4_gemv_supports(M, K, format)) return launch_mx4_gemv(q, nullptr, 0, 0, nullptr, s);
-    if (M > PAIR_ROWS) return launch_mx4_pair(q, s);
+    if (mx4_gemv_takes(M, N, K, format)) return launch_mx4_gemv(q, nullptr, 0, 0, nullptr, s);
+    if (!use_clusters(M, N, K)) return launch_mx4_pair(q, s);
     MxArgs k;
     k.early = q.early ? 1 : 0;
     k.x_sf = q.x_scales;
@@ -357,9 +367,7 @@ static sqap_status launch(const Mx4Product& q, cudaStream_t s) {
     if (!k.status) return SQAP_ERR_CUDA;
     if (!device_is_sm100()) return SQAP_ERR_UNSUPPORTED;
     k.k_tiles = mx4_k_tiles(K, format);
-    k.BN = M <= BN_MAX ? (M + 15) / 16 * 16 : BN_MAX;
-    k.m_tiles = (M + k.BN - 1) / k.BN;
-    k.n_tiles = (N + BM - 1) / BM;
+    k.BN = (M + 15) / 16 * 16;   // one token tile: use_clusters()
     const int tiles_k = format == SQAP_MX_NVFP4 ? 4 : 2, sfb_rows = (k.BN + 127) / 128;
     k.stage_bytes = (A_BYTES + k.BN * 128 + tiles_k * SF_TILE * (1 + sfb_rows) + 1023) / 1024 * 1024;
     // Narrow tiles: two CTAs to an SM, so that one streams while the other exchanges and stores.
@@ -374,7 +382,7 @@ static sqap_status launch(const Mx4Product& q, cudaStream_t s) {
 
     // K split: rounds of clusters over the device x (stages of a CTA + its fixed cost), in units of a stage
     const int slots = sm_count() * per_sm;
-    const long tiles = static_cast<long>(k.m_tiles) * k.n_tiles;
+    const long tiles = (N + BM - 1) / BM;
     double best = -1.0;
     k.ksplit = 1;
     for (int c = 1; c <= KSPLIT_MAX && c <= k_steps; ++c) {
@@ -485,7 +493,7 @@ extern "C" sqap_status sqap_mx4_quantize_linear(const void* x, int x_dtype, int 
     if (st != SQAP_OK || M == 0) return st;
     if (workspace_bytes < sqap_mx4_workspace_bytes(M, N, K, format)) return SQAP_ERR_NOMEM;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (mx4_gemv_supports(M, K, format))   // quantizes its few rows itself
+    if (mx4_gemv_takes(M, N, K, format))   // quantizes its few rows itself
         return launch_mx4_gemv(mx4::product(nullptr, nullptr, x_tensor_scale, M, w_codes, w_scales, w_tensor_scale, N, K, format, out, ldo, out_dtype, false),
                                x, x_dtype, ldx, row_index, s);
     st = launch_mx4_quantize(x, x_dtype, M, K, ldx, row_index, format, x_tensor_scale, codes, scales, s);

@@ -3,16 +3,20 @@
 //
 // A cluster of two CTAs computes 256 x BN tiles (BN 64, 128 or 192 tokens): each CTA holds 128 weight rows and half of the
 // token rows, and the pair's tensor cores share both halves, so an SM fetches 28 KB of codes instead of 40 per 256
-// elements of K at BN = 192; the four-bit MMAs take 384 cycles for that, and fetching is what bounds the kernel. The scales of
-// the tokens are wanted in full by both CTAs (4 KB), those of the weights by their own (2 KB). The codes' bytes are counted on the
-// leader's barrier, where the MMAs are issued.
+// elements of K at BN = 192. The scales of the tokens are wanted in full by both CTAs (4 KB), those of the weights by their own
+// (2 KB). The codes' bytes are counted on the leader's barrier, where the MMAs are issued.
+// What bounds it: the four-bit MMAs of a stage (256 elements of K) take 384 cycles at BN = 192. 4608 x 12288 x 4096 in NVFP4 with
+// the quantizer takes 111 us (4.2 PFLOP/s). A stage costs 0.32 us there; with one MMA of four issued it is 0.23, with no loads
+// 0.22, with neither 0.21: the round trip of a stage's signals (done -> scales written again -> issued) and the SM clock, which
+// the full load brings down to 1.6 GHz, share the rest. A tile's results cost 1.6 us of issue slots beside it.
 // The scales go to tensor memory through registers (four warps: shared memory -> tcgen05.st, one lane quadrant each): a
 // tcgen05.cp of a scale tile holds up the tensor pipe for some 24 cycles, and a stage has twelve of them beside 374 cycles of
-// MMAs (measured: pipe busy 78 %, with MMAs 44 %; 136 us where this takes @PAIR_US@ for 4608 x 12288 x 4096 with the quantizer).
-// Tensor memory (512 columns): two accumulators of 192 columns, so that a tile is stored while the next is computed, and three
-// sets of scale columns.
-//   warp 0     TMA      warp 1  MMA (leader)      warps 2-9  epilogue: four lane quadrants x two halves of the tokens
-//   warps 10-13  scales to tensor memory
+// MMAs (measured: pipe busy 78 %, with MMAs 44 %; 15 us more for 4608 x 12288 x 4096).
+// Tensor memory (512 columns): two accumulators of BN columns, so that a tile is stored while the next is computed, and three to six
+// sets of scale columns. A scale tile's place in shared memory is free as soon as it has been read, so the scales run ahead of
+// the codes and have a loading warp of their own; two groups of four warps copy them, a stage each in turn.
+//   warp 0     TMA      warp 1  MMA (one thread of the leader)      warps 2-9  epilogue: four lane quadrants x two halves of the tokens
+//   warps 10-17  scales to tensor memory      warp 18  scales' TMA
 // A token tile may start in the middle of a 128-row scale tile (BN = 64, 192): 64 rows are two columns of a tile, so its scales
 // are taken from two columns further on.
 // Every wait on a barrier is bounded; on expiry the kernel records SQAP_ERR_TIMEOUT in the device status word, drains, and
