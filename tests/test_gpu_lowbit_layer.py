@@ -185,7 +185,8 @@ def test_prompt_prune_fork_and_decode(kind, fmt):
 
 # eight pieces of a history and more are joined by four warps to a row; uneven lengths leave some pieces empty
 @pytest.mark.parametrize("dtype,heads,H,D_,lens,new", [("fp16", 4, 1, 64, [2300, 1, 0], [1, 1, 1]), ("bf16", 2, 2, 128, [5000, 1100], [1, 1]),
-                                                       ("fp16", 2, 1, 256, [2500, 300], [1, 0]), ("bf16", 16, 1, 128, [10000], [20])])
+                                                       ("fp16", 2, 1, 256, [2500, 300], [1, 0]), ("bf16", 16, 1, 128, [10000], [20]), ("fp16", 2, 1, 256, [4200, 300], [20, 9]),
+                                                       ("bf16", 4, 1, 64, [9000, 40, 0], [70, 40, 5])])
 def test_attention_in_many_pieces(dtype, heads, H, D_, lens, new):
     s = Setup(lens, H, D_, 64, R.E4M3, sum(lens), nan_behind=True)
     check_attention(s, new, heads, True, dtype, seed=3)
