@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(128) kv_share_kernel(Pool p, const int32_t* sr
     pdl_launch_dependents();
     pdl_wait();
     const int i = blockIdx.x;
-    if (pairs[i].x == -2) return;
+    if (pairs[i].y == -2) return;                     // not met (the page to copy is whatever number the source's row holds)
     const int32_t* from = p.table + src[i] * p.ldt;
     int32_t* to = p.table + dst[i] * p.ldt;
     const int full = p.lens[src[i]] >> p.page_shift, used = pages_of(p.lens[src[i]], p.page_shift);

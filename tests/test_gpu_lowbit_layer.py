@@ -209,3 +209,19 @@ def test_product_at_the_borders_of_the_rules(M, N, K, fmt):
         o = out.double().cpu().numpy()
         assert (o[M] == 7).all() and (o[:, N:] == 7).all()
         check_product(o[:M, :N], x, w, dtype, K)
+
+
+def test_fork_of_a_row_whose_last_page_is_missing():
+    """A number in the page table that is no page holds no tokens, whichever number it is: the full pages are shared all the same."""
+    for hole in (-1, -2, -7, 50):
+        layer = Layer(R.INT8)
+        B.sqap_kv_alloc(*layer.pool, ints([0]), ints([2 * P + 3]), 1)
+        layer.table[0, 2] = hole
+        pairs = torch.empty((1, 2), dtype=torch.int32, device=DEV)
+        granted = torch.empty(1, dtype=torch.int32, device=DEV)
+        B.sqap_kv_fork(*layer.pool, ints([0]), ints([1]), 1, pairs, granted)
+        B.sqap_kv_copy_pages(layer.cache, pairs, 1)
+        torch.cuda.synchronize()
+        assert granted.tolist() == [1] and pairs.tolist() == [[hole, 3]]
+        assert layer.table[1].tolist() == [0, 1, 3, -1, -1, -1] and layer.lens[:2].tolist() == [2 * P + 3] * 2
+        assert layer.refs[:5].tolist() == [2, 2, 1, 1, 0]
