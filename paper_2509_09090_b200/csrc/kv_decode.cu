@@ -230,7 +230,8 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
         for (int u = 0; u < GROUPS; ++u) {
             there[u] = page[u] >= 0;
             this_ks[u] = ks[u];
-            lv[u] = __log2f(vs[u] > 0.0f ? vs[u] : ZERO_PAGE_SCALE);
+            // (a place without a page has page 0's scales here: its weight is 0, but 0 times the reciprocal of what may stand there is not)
+            lv[u] = __log2f(there[u] && vs[u] > 0.0f ? vs[u] : ZERO_PAGE_SCALE);
             iv[u] = fast_exp2(-lv[u]);             // the reciprocal of what lv stands for: the weights use lv
         }
         if (more) load_keys(k0 + WARPS * STEP);
