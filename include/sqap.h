@@ -425,8 +425,8 @@ sqap_status sqap_kv_alloc(int32_t* refs, int pages, int page_tokens, int32_t* ta
 
 /*
  * sqap_kv_fork: row dst_rows[i], which must be empty (lens 0), becomes a copy of src_rows[i]: the full pages are shared (refs + 1),
- * an unfinished last page is copied into a fresh one. pairs: device int32 [n][2], 8-byte aligned, gets (page to copy, fresh
- * page), (-1, -1) where there is none to copy, (-2, -2) where the request was not met: no such row, a destination that is
+ * an unfinished last page is copied into a fresh one (if the source's entry is no page, the copy's is -1). pairs: device int32
+ * [n][2], 8-byte aligned, gets (page to copy, fresh page), (-1, -1) where there is none to copy, (-2, -2) where the request was not met: no such row, a destination that is
  * not empty, is named earlier or is also a source, no free page. Such a request changes nothing. The same source may
  * be forked many times.
  */

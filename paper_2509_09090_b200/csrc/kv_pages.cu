@@ -226,7 +226,11 @@ __global__ void __launch_bounds__(NT) kv_fork_kernel(Pool p, const int32_t* src,
         if (q.a < 0 || q.a >= p.rows || q.b < 0 || q.b >= p.rows || sh.first[q.b] != i) return q;
         q.len = p.lens[q.a];
         if (q.len < 0 || p.lens[q.b] != 0 || pages_of(q.len, p.page_shift) > p.ldt) return q;
-        q.need = (q.len & ((1 << p.page_shift) - 1)) != 0 ? 1 : 0;
+        // an unfinished last page is copied, if the source has it
+        if ((q.len & ((1 << p.page_shift) - 1)) != 0) {
+            const int last = p.table[q.a * p.ldt + (q.len >> p.page_shift)];
+            q.need = last >= 0 && last < p.pages ? 1 : 0;
+        }
         q.ok = true;
         return q;
     };
@@ -254,7 +258,8 @@ __global__ void __launch_bounds__(128) kv_share_kernel(Pool p, const int32_t* sr
     pdl_launch_dependents();
     pdl_wait();
     const int i = blockIdx.x;
-    if (pairs[i].y == -2) return;                     // not met (the page to copy is whatever number the source's row holds)
+    const int given = pairs[i].y;                     // -2: not met; -1: no page to copy; else the destination's last page, entered already
+    if (given == -2) return;
     const int32_t* from = p.table + src[i] * p.ldt;
     int32_t* to = p.table + dst[i] * p.ldt;
     const int full = p.lens[src[i]] >> p.page_shift, used = pages_of(p.lens[src[i]], p.page_shift);
@@ -263,8 +268,8 @@ __global__ void __launch_bounds__(128) kv_share_kernel(Pool p, const int32_t* sr
             const int page = from[j];
             to[j] = page;
             if (page >= 0 && page < p.pages) atomicAdd(p.refs + page, 1);
-        } else if (j >= used) {
-            to[j] = -1;
+        } else if (j >= used || given < 0) {
+            to[j] = -1;                               // a last page that the source lacks is lacking here as well
         }
     }
 }

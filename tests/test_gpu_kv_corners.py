@@ -50,3 +50,59 @@ def test_attention_does_not_look_at_scales_of_pages_it_does_not_have(dtype, head
     for value in (SMALLEST, 1e-40, math.inf, math.nan):
         unused_scales(s, np.float32(value))
         check_attention(s, new, heads, True, dtype, seed=len(lens))
+
+
+# ---------------------------------------------------------------------------------------------------------------- forks
+
+@pytest.mark.parametrize("kind", [R.INT8, R.E4M3])
+@pytest.mark.parametrize("hole", [-1, -2, 1000])
+def test_fork_of_a_row_without_its_last_page_is_a_copy(hole, kind):
+    """What the source's missing page does not hold, its copy does not hold either, whoever had the free pages before."""
+    P, H, D, n = 16, 2, 64, 2 * 16 + 3
+    g = np.random.default_rng(3)
+    pages, rows, width = 8, 3, 6
+    k, v = (dev(g.integers(1, 0x70, (pages, H, P, D)).astype(np.uint8)).view(torch.int8 if kind == R.INT8 else torch.float8_e4m3fn) for _ in range(2))
+    ks, vs = (dev(np.exp(g.standard_normal((pages, H))).astype(np.float32)) for _ in range(2))
+    cache = B.KvCache(k, v, ks, vs, kind)
+    refs, lens = (torch.zeros(m, dtype=torch.int32, device=DEV) for m in (pages, rows))
+    table = torch.full((rows, width), -1, dtype=torch.int32, device=DEV)
+    pool = (refs, pages, P, table, width, rows, lens)
+    x = dev(g.standard_normal((n, 2 * H * D)), torch.float16)
+    B.sqap_kv_alloc(*pool, ints([0]), ints([n]), 1)
+    B.sqap_kv_append(cache, table, width, 1, lens, ints([0, n]), n, x, 2 * H * D, x[:, H * D:], 2 * H * D, 0)
+    table[0, 2] = hole
+    pairs, granted = torch.empty((1, 2), dtype=torch.int32, device=DEV), torch.empty(1, dtype=torch.int32, device=DEV)
+    B.sqap_kv_fork(*pool, ints([0]), ints([1]), 1, pairs, granted)
+    B.sqap_kv_copy_pages(cache, pairs, 1)
+    assert granted.tolist() == [1] and pairs.tolist() == [[-1, -1]]
+    assert table[1].tolist() == [0, 1, -1, -1, -1, -1] and refs.tolist() == [2, 2, 1, 0, 0, 0, 0, 0]
+    for step in range(2):
+        m = n + step
+        assert lens[:2].tolist() == [m, m]
+        back = torch.full((2 * m, H * D), 9.0, dtype=torch.float16, device=DEV)
+        B.sqap_kv_read(cache, table, width, 2, None, ints([0, m, 2 * m]), m, None, 0, back, H * D, 0)
+        q = x[:2, :H * D].contiguous()
+        q[1] = q[0]
+        out, lse = torch.empty_like(q), torch.empty((2, H), device=DEV)
+        B.sqap_kv_attention(cache, table, width, 2, lens, ints([0, 1, 2]), 1, m, q, H * D, H, 0.125, 1, out, H * D, lse, 0, None, 0)
+        torch.cuda.synchronize()
+        assert torch.equal(back[:m], back[m:]) and (back[2 * P:m] == 0).all()
+        assert torch.equal(out[0], out[1]) and torch.equal(lse[0], lse[1])
+        # one more token for both: no page, so it is dropped for both
+        B.sqap_kv_alloc(*pool, ints([0, 1]), ints([1, 1]), 2)
+        B.sqap_kv_append(cache, table, width, 2, lens, ints([0, 1, 2]), 1, x, 2 * H * D, x[:, H * D:], 2 * H * D, 0)
+
+
+def test_fork_of_a_row_without_its_last_page_needs_no_free_page():
+    P, pages, rows, width = 16, 2, 3, 4
+    refs, lens = (torch.zeros(m, dtype=torch.int32, device=DEV) for m in (pages, rows))
+    table = torch.full((rows, width), -1, dtype=torch.int32, device=DEV)
+    pool = (refs, pages, P, table, width, rows, lens)
+    B.sqap_kv_alloc(*pool, ints([0]), ints([P + 1]), 1)
+    pairs, granted = torch.empty((2, 2), dtype=torch.int32, device=DEV), torch.empty(2, dtype=torch.int32, device=DEV)
+    B.sqap_kv_fork(*pool, ints([0]), ints([1]), 1, pairs, granted)                 # the pool is used up
+    assert granted[0] == 0 and pairs[0].tolist() == [-2, -2]
+    table[0, 1] = -1
+    B.sqap_kv_fork(*pool, ints([0, 0]), ints([1, 2]), 2, pairs, granted)
+    assert granted.tolist() == [1, 1] and pairs.tolist() == [[-1, -1]] * 2
+    assert table[1:].tolist() == [[0, -1, -1, -1]] * 2 and lens.tolist() == [P + 1] * 3 and refs.tolist() == [3, 1]
