@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(128) kv_combine_kernel(AttnArgs a) {
     uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + row * a.ldo + static_cast<int64_t>(head) * D) + lane;
 #pragma unroll
     for (int e = 0; e < D / 64; ++e) out[32 * e] = pack2<T>(y[2 * e] * inv, y[2 * e + 1] * inv);
-    if (lane == 0 && a.lse) a.lse[row * a.heads + head] = l != 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+    if (lane == 0 && a.lse) a.lse[row * a.heads + head] = l != 0.0f ? log_sum(m, l) : -INFINITY;
 }
 
 template <typename T, int D>

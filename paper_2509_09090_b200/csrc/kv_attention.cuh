@@ -10,8 +10,11 @@ namespace kv {
 // The codes enter the matrix instructions as they are (exact in fp16); the scale of a page's keys multiplies its scores, and
 // the scale of its values goes into the exponent:  w_t = 2^(s_t log2 e + log2 vs - m) is the weight of the value CODES, with m
 // the running maximum of the whole exponent, so w_t <= 1 whatever the scales are and fp16 holds it to 11 bits; the
-// denominator adds w_t / vs. A page of zero values has no say in m worth keeping: any scale does, and gets this one.
-constexpr float ZERO_PAGE_SCALE = 0.015625f;
+// denominator adds w_t / vs. A page of zero values adds to the denominator alone, and must not raise m: that would push the other
+// pages' weights into the subnormals of fp16. It is given a scale below all others: values of fp16 rows have scales of 2^-32 to
+// 2^9, and 2^-60 leaves 28 binary orders in which its own probability may be the larger one. Smaller still, and fp32 would lose
+// its w_t (which ends at 2^-126) where the denominator needs it: with 2^-60, next to scales of 2^9, below 2^-57 of the others.
+constexpr float ZERO_PAGE_SCALE = 8.673617379884035e-19f;   // 2^-60
 
 struct AttnArgs {
     Cache c;
@@ -83,6 +86,13 @@ __device__ __forceinline__ float fast_exp2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// ln of 2^m l, l > 0. The exponent of l meets m before the logarithm of its mantissa does: the exponents of the pages' scales, which
+// both contain, then cancel without a rounding at their size. An l that is not finite is the answer.
+__device__ __forceinline__ float log_sum(float m, float l) {
+    if (!(l < INFINITY)) return l;
+    const uint32_t b = __float_as_uint(l);
+    return (m + static_cast<float>(static_cast<int>(b >> 23) - 127) + log2f(__uint_as_float((b & 0x7FFFFFu) | 0x3F800000u))) * 0.69314718055994531f;
 }
 __device__ __forceinline__ void mma_16816(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"

@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
             for (int e = 0; e < 8; ++e) y[e] *= inv;
             const int64_t row = static_cast<int64_t>(w.row0) + i;
             *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + row * a.ldo + static_cast<int64_t>(head) * D + d) = pack8<T>(y);
-            if (d == 0 && a.lse) a.lse[row * a.heads + head] = ll > 0.0f ? (mm + log2f(ll)) * 0.69314718055994531f : -INFINITY;
+            if (d == 0 && a.lse) a.lse[row * a.heads + head] = ll > 0.0f ? log_sum(mm, ll) : -INFINITY;
         }
     }
 }

@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(256, 1) kv_prefill_kernel(AttnArgs a) {
             T* out = static_cast<T*>(a.out) + row * a.ldo + static_cast<int64_t>(head) * D + 2 * t;
 #pragma unroll
             for (int x = 0; x < D / 8; ++x) *reinterpret_cast<uint32_t*>(out + 8 * x) = pack2<T>(o[x][2 * e] * inv, o[x][2 * e + 1] * inv);
-            if (t == 0 && a.lse) a.lse[row * a.heads + head] = l[e] > 0.0f ? (m[e] + log2f(l[e])) * 0.69314718055994531f : -INFINITY;
+            if (t == 0 && a.lse) a.lse[row * a.heads + head] = l[e] > 0.0f ? log_sum(m[e], l[e]) : -INFINITY;
         }
     }
 }

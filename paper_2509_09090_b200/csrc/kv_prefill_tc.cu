@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
             }
             if (real) {
                 if (a.splits > 1) a.part_ml[at] = make_float2(m, l);
-                else if (a.lse) a.lse[row * a.heads + head] = l > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+                else if (a.lse) a.lse[row * a.heads + head] = l > 0.0f ? log_sum(m, l) : -INFINITY;
             }
             tc_fence_before();
         }

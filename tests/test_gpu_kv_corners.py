@@ -106,3 +106,19 @@ def test_fork_of_a_row_without_its_last_page_needs_no_free_page():
     B.sqap_kv_fork(*pool, ints([0, 0]), ints([1, 2]), 2, pairs, granted)
     assert granted.tolist() == [1, 1] and pairs.tolist() == [[-1, -1]] * 2
     assert table[1:].tolist() == [[0, -1, -1, -1]] * 2 and lens.tolist() == [P + 1] * 3 and refs.tolist() == [3, 1]
+
+
+# ---------------------------------------------------------------------------------------------------------- zero values
+
+@pytest.mark.parametrize("kind", [R.INT8, R.E4M3])
+@pytest.mark.parametrize("exponent", [-40, -30, -16, 8])
+@pytest.mark.parametrize("D,new", [(64, [1, 1]), (128, [1, 1]), (128, [40, 24]), (64, [30, 9]), (256, [1, 1]), (256, [40, 24])])
+def test_a_page_of_zero_values_leaves_the_weights_of_the_others_their_bits(D, new, exponent, kind):
+    s = Setup([300, 130], 2, D, 32, kind, 11)
+    s.scale["v"] = (2.0 ** exponent * (1 + s.g.random(s.scale["v"].shape))).astype(np.float32)
+    for z in (s.table[0, 4], s.table[1, 1]):
+        s.raw["v"][z] = 0
+        s.scale["v"][z] = 0
+    s.to_device()
+    for gain in (0.3, 2.0):
+        check_attention(s, new, 4, True, "bf16", q_gain=gain)
