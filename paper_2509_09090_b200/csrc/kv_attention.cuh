@@ -41,7 +41,8 @@ struct AttnArgs {
 // Work of a CTA, from its index.
 struct Where {
     int b, h, split, tile;
-    int row0, n_q, len;    // first row of the sequence, its query rows, its keys
+    int row0, n_q;         // first row of the sequence, its query rows
+    int tokens, len;       // its tokens, and how many of them are looked at (max_len at most)
 };
 __device__ __forceinline__ Where locate(const AttnArgs& a, unsigned id, int tiles) {
     Where w;
@@ -60,14 +61,15 @@ __device__ __forceinline__ Where locate(const AttnArgs& a, unsigned id, int tile
     const int n = a.cu[w.b + 1] - w.row0;
     w.n_q = n < 0 ? 0 : n;
     const int len = a.lens[w.b];
-    w.len = len < 0 ? 0 : (len > a.max_len ? a.max_len : len);
+    w.tokens = len < 0 ? 0 : len;
+    w.len = min(w.tokens, a.max_len);
     return w;
 }
 // Keys that query i of the sequence may look at (the first so many).
 __device__ __forceinline__ int visible(const AttnArgs& a, const Where& w, int i) {
     if (!a.causal) return w.len;
-    const int64_t n = static_cast<int64_t>(w.len) - w.n_q + i + 1;
-    return n < 0 ? 0 : static_cast<int>(n);
+    const int64_t n = static_cast<int64_t>(w.tokens) - w.n_q + i + 1;
+    return n < 0 ? 0 : static_cast<int>(min(n, static_cast<int64_t>(w.len)));
 }
 __device__ __forceinline__ int64_t part_index(const AttnArgs& a, int b, int head, int i, int split) {
     return ((static_cast<int64_t>(b) * a.heads + head) * a.max_q + i) * a.splits + split;

@@ -122,3 +122,27 @@ def test_a_page_of_zero_values_leaves_the_weights_of_the_others_their_bits(D, ne
     s.to_device()
     for gain in (0.3, 2.0):
         check_attention(s, new, 4, True, "bf16", q_gain=gain)
+
+
+# ---------------------------------------------------------------------------------------------------------- the maxima
+
+@pytest.mark.parametrize("D,new", [(64, [4, 1, 3]), (128, [2, 4, 1]), (128, [40, 33, 7]), (64, [20, 70, 9]), (256, [3, 1, 2]), (256, [40, 30, 9])])
+def test_causal_attention_beyond_max_len(D, new):
+    """Places from max_len on are not seen; which of the places in front of it a query sees does not change."""
+    lens, heads, H, P = [100, 90, 64], 4, 2, 16
+    s = Setup(lens, H, D, P, R.INT8, 5)
+    q = dev(np.random.default_rng(1).standard_normal((2 + sum(new), heads * D)), torch.bfloat16)
+    for max_len in (50, 64, 95):
+        o, l, cu = run_attention(s, q, new, heads, True, "bf16", max_len=max_len)
+        qn = q.double().cpu().numpy().reshape(-1, heads, D)
+        for b, n in enumerate(lens):
+            k, there = R.kv_tokens(s.codes("k"), s.scale["k"], s.table[b], n, P)
+            v, _ = R.kv_tokens(s.codes("v"), s.scale["v"], s.table[b], n, P)
+            there[max_len:] = False
+            ref, lse, mag, pv, _ = R.attention(qn[cu[b]:cu[b + 1]], k, v, there, new[b], True, 1 / math.sqrt(D))
+            d = 2.0 ** -19 * (1 + mag)
+            got = o[cu[b]:cu[b + 1]].reshape(ref.shape)
+            # (the scales of a head lie within 2^3 of one another here: no weight that counts is subnormal in fp16)
+            assert (np.abs(got - ref) <= np.abs(ref) * 2.0 ** -8 + pv * (2.0 ** -10 + 2 * d[..., None])).all()
+            gl, seen = l[cu[b]:cu[b + 1]], np.isfinite(lse)
+            assert (gl[~seen] == -np.inf).all() and (np.abs(gl - lse)[seen] <= (d + 2.0 ** -20)[seen] + np.abs(lse[seen]) * 2.0 ** -22).all()
