@@ -371,7 +371,7 @@ typedef struct {
  * Appends: rows cu_new[b] .. cu_new[b+1]-1 of k and v (dtype FP16 or BF16, rows ldk / ldv elements apart, head h in columns
  * h*head_dim ...: column slices of a fused QKV output are taken in place) become the LAST tokens of sequence b, whose
  * lens[b] counts them already; tokens that would lie before position 0 are dropped. max_new: no sequence brings more (rows
- * beyond that are not read). For each page and head that receives tokens:
+ * beyond that are not read; their places stay as they are). For each page and head that receives tokens:
  *   scale' = max(scale if the page holds earlier tokens of the sequence, else 0; scale of the new tokens' amax)
  *   earlier tokens, if the scale grew:  code' = round(code * (scale / scale'));  new tokens:  code = round(x * (1 / scale'))
  * in fp32, round to nearest even, int8 clamped to +-127, e4m3 to +-448. Powers of two make the first rule exact for e4m3

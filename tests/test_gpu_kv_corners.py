@@ -146,3 +146,24 @@ def test_causal_attention_beyond_max_len(D, new):
             assert (np.abs(got - ref) <= np.abs(ref) * 2.0 ** -8 + pv * (2.0 ** -10 + 2 * d[..., None])).all()
             gl, seen = l[cu[b]:cu[b + 1]], np.isfinite(lse)
             assert (gl[~seen] == -np.inf).all() and (np.abs(gl - lse)[seen] <= (d + 2.0 ** -20)[seen] + np.abs(lse[seen]) * 2.0 ** -22).all()
+
+
+@pytest.mark.parametrize("kind", [R.INT8, R.E4M3])
+@pytest.mark.parametrize("max_new", [1, 5, 16, 39])
+def test_append_of_more_rows_than_max_new(max_new, kind):
+    """The rows that are read go where they would go without the limit; the places of the others stay as they are."""
+    new, lens, H, D, P = [40, 3, 20], [50, 20, 12], 2, 64, 16
+    s = Setup(lens, H, D, P, kind, 8)
+    cu = np.concatenate([[0], np.cumsum(new)])
+    x = dev(s.g.standard_normal((sum(new), 2 * H * D)), torch.float16)
+    B.sqap_kv_append(s.cache, s.dtable, s.width, 3, ints(lens), ints(cu), max_new, x, 2 * H * D, x[:, H * D:], 2 * H * D, 0)
+    torch.cuda.synchronize()
+    xn = x.float().cpu().numpy()
+    for a, c0 in (("k", 0), ("v", H * D)):
+        codes, scale = s.codes(a), s.scale[a].copy()
+        for b in range(3):
+            m = min(new[b], max_new)
+            end = lens[b] - new[b] + m
+            if end > 0:
+                R.kv_append(codes, scale, s.table[b:b + 1], [end], [0, m], xn[cu[b]:cu[b] + m, c0:c0 + H * D].reshape(-1, H, D), kind, P)
+        assert np.array_equal(s.device_codes(a), codes) and np.array_equal(s.ds[a].cpu().numpy(), scale)
