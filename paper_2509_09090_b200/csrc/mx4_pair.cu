@@ -300,6 +300,7 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
         __syncwarp();
     } else if (warp >= SF_WARP0) {
         // ---------------- scales: lane i of every quadrant holds rows i, 32 + i, 64 + i, 96 + i of a tile, a column each
+        pdl_wait();   // the waits below are bounded, and the loads that they wait for may not start before the kernel in front is done
         const int quad = warp & 3;
         const uint32_t mine = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + 2u * a.BN;
         const uint32_t my_tiles = pair < total_tiles ? (total_tiles - 1 - pair) / n_pairs + 1 : 0, stages = my_tiles * k_steps;

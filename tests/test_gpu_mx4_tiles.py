@@ -1,0 +1,53 @@
+"""Products of microscaled 4-bit matrices over many tiles and at the ends of the scales' range."""
+import numpy as np
+import pytest
+
+import lowbit_reference as R
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if torch.cuda.is_available():
+    from paper_2509_09090_b200 import binding as B
+    from test_gpu_kv import ints
+    from test_gpu_mx4 import CODE, DEV, T, check_product, dev, product_case
+
+
+def test_product_behind_a_kernel_that_takes_longer_than_its_waits():
+    """The product's CTAs may be on the device while the kernel in front still runs; their limits on waiting (some 2 s) do not count that.
+    In front: attention of 149 heads on 148 SMs, so that all but one of them are free for the time of one head."""
+    H, D, P, heads = 149, 256, 128, 149
+    code = torch.zeros(1, H, P, D, dtype=torch.int8, device=DEV)
+    scale = torch.ones(1, H, device=DEV)
+    cache = B.KvCache(code, code, scale, scale, B.SQAP_KV_INT8)
+    nq = 9
+    q = torch.zeros(nq, heads * D, dtype=torch.float16, device=DEV)
+    out_a = torch.empty_like(q)
+
+    def attention(n):
+        table = torch.zeros(1, -(-n // P), dtype=torch.int32, device=DEV)
+        lens, cu = ints([n]), ints([0, nq])
+        torch.cuda.synchronize()
+        t = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+        t[0].record()
+        B.sqap_kv_attention(cache, table, table.shape[1], 1, lens, cu, nq, n, q, heads * D, heads, 0.1, 0, out_a, heads * D, None, 0, None, 0)
+        return table, t
+
+    attention(1 << 17)
+    torch.cuda.synchronize()
+    table, t = attention(1 << 20)
+    t[1].record()
+    torch.cuda.synchronize()
+    n = int((1 << 20) * 5200 / t[0].elapsed_time(t[1]))       # two heads, 2.6 s each, one after the other
+    assert n < 1 << 30
+    M, N, K, fmt = 300, 512, 512, R.NVFP4
+    xc, xs, wc, ws, x, w = product_case(M, N, K, fmt, seed=1)
+    xc, xs, wc, ws = (dev(a) for a in (xc, xs, wc, ws))
+    out = torch.full((M, N), 7.0, dtype=torch.float32, device=DEV)
+    table, t = attention(n)
+    B.sqap_mx4_linear(xc, xs, None, M, wc, ws, None, N, K, fmt, out, N, B.SQAP_FP32)
+    t[1].record()
+    torch.cuda.synchronize()
+    assert t[0].elapsed_time(t[1]) > 4400
+    assert B.sqap_device_status() == B.SQAP_OK
+    check_product(out.double().cpu().numpy(), x, w, "fp32", K)
