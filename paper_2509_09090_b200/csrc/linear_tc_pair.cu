@@ -259,8 +259,9 @@ w4a4_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
             }
         }
     } else if (warp < 6) {
-        // (no dependency wait here: these warps touch shared and tensor memory only, and may unpack the weights that
-        // were fetched early while the kernel before this one still runs)
+        // (These warps touch shared and tensor memory only, and may unpack the weights that were fetched early while the
+        // kernel before this one still runs. The dependency wait comes in front of the first bounded wait for what follows it.)
+        const uint32_t early = static_cast<uint32_t>(k_steps < U ? k_steps : U);
         // ---------------- unpack warps: thread = one tensor-memory lane = one weight row of the tile
         const int quad = warp & 3;                 // the lane quadrant this warp may write
         const int L = quad * 32 + lane;            // tensor-memory lane
@@ -274,6 +275,7 @@ w4a4_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
         for (int tile = pair; tile < total_tiles && !failed; tile += n_pairs) {
             for (int ks = 0; ks < k_steps; ++ks, ++it) {
                 const int s = it % S, j = it % U;
+                if (it == early) pdl_wait();
                 // weight tile j was last read by the MMAs of stage it - U, whose completion is done((it - U) % S)
                 bool ok = mbar_wait(full(s), (it / S) & 1u, abort_flag);
                 if (ok && it >= U) ok = mbar_wait(done((it - U) % S), ((it - U) / S) & 1u, abort_flag);

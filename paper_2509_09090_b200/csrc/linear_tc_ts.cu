@@ -223,8 +223,7 @@ w4a4_tc_ts_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constan
             }
         }
     } else if (warp < 6) {
-        // (no dependency wait here: these warps touch shared and tensor memory only, and may unpack the weights that
-        // were fetched early while the kernel before this one still runs)
+        pdl_wait();   // a stage is full when its activations are there as well, and the bounded waits count this kernel's own time only
         // ---------------- unpack warps: thread = one tensor-memory lane = one weight row of the tile
         const int quad = warp & 3;                 // the lane quadrant this warp may write
         const int L = quad * 32 + lane;            // tensor-memory lane

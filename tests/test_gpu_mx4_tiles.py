@@ -1,4 +1,4 @@
-"""Products of microscaled 4-bit matrices over many tiles and at the ends of the scales' range."""
+"""Products behind a long kernel, and of microscaled 4-bit matrices over many tiles and at the ends of the scales' range."""
 import numpy as np
 import pytest
 
@@ -9,12 +9,34 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 if torch.cuda.is_available():
     from paper_2509_09090_b200 import binding as B
+    import gpu_harness as G
     from test_gpu_kv import ints
     from test_gpu_mx4 import CODE, DEV, T, check_product, dev, product_case
 
 
-def test_product_behind_a_kernel_that_takes_longer_than_its_waits():
-    """The product's CTAs may be on the device while the kernel in front still runs; their limits on waiting (some 2 s) do not count that.
+def product_of_nvfp4():
+    M, N, K, fmt = 300, 512, 512, R.NVFP4
+    xc, xs, wc, ws, x, w = product_case(M, N, K, fmt, seed=1)
+    xc, xs, wc, ws = (dev(a) for a in (xc, xs, wc, ws))
+    out = torch.full((M, N), 7.0, dtype=torch.float32, device=DEV)
+    return out, lambda: B.sqap_mx4_linear(xc, xs, None, M, wc, ws, None, N, K, fmt, out, N, B.SQAP_FP32)
+
+
+def product_of_int4(flag):
+    """More tiles of the weights than SMs (or pairs of them), so that a CTA has a second one."""
+    M, N, K = 40, 19200 if flag == B.SQAP_L_FORCE_TCGEN05_TS else 38400, 512
+    g = np.random.default_rng(2)
+    w = G.pack(g.integers(-7, 8, (N, K)), np.full(N, 0.01))
+    q, sc = dev(g.integers(0, 256, (M, K // 2)).astype(np.uint8)), torch.full((M,), 0.02, device=DEV)
+    out = torch.zeros((M, N), dtype=torch.int32, device=DEV)
+    size = B.sqap_workspace_bytes(M, N, K, flag)
+    work = torch.empty(size + 256, dtype=torch.uint8, device=DEV)
+    at = (work.data_ptr() + 255) // 256 * 256
+    return out, lambda: (B.sqap_w4a4_linear(q, sc, M, w, None, out, N, B.SQAP_I32, flag, at, size), work)
+
+
+def test_products_behind_a_kernel_that_takes_longer_than_their_waits():
+    """A product's CTAs may be on the device while the kernel in front still runs; their limits on waiting (some 2 s) do not count that.
     In front: attention of 149 heads on 148 SMs, so that all but one of them are free for the time of one head."""
     H, D, P, heads = 149, 256, 128, 149
     code = torch.zeros(1, H, P, D, dtype=torch.int8, device=DEV)
@@ -40,14 +62,16 @@ def test_product_behind_a_kernel_that_takes_longer_than_its_waits():
     torch.cuda.synchronize()
     n = int((1 << 20) * 5200 / t[0].elapsed_time(t[1]))       # two heads, 2.6 s each, one after the other
     assert n < 1 << 30
-    M, N, K, fmt = 300, 512, 512, R.NVFP4
-    xc, xs, wc, ws, x, w = product_case(M, N, K, fmt, seed=1)
-    xc, xs, wc, ws = (dev(a) for a in (xc, xs, wc, ws))
-    out = torch.full((M, N), 7.0, dtype=torch.float32, device=DEV)
-    table, t = attention(n)
-    B.sqap_mx4_linear(xc, xs, None, M, wc, ws, None, N, K, fmt, out, N, B.SQAP_FP32)
-    t[1].record()
-    torch.cuda.synchronize()
-    assert t[0].elapsed_time(t[1]) > 4400
-    assert B.sqap_device_status() == B.SQAP_OK
-    check_product(out.double().cpu().numpy(), x, w, "fp32", K)
+    for make in (product_of_nvfp4, lambda: product_of_int4(B.SQAP_L_FORCE_TCGEN05_TS), lambda: product_of_int4(B.SQAP_L_FORCE_TCGEN05_PAIR)):
+        out, call = make()
+        keep = call()
+        torch.cuda.synchronize()
+        want = out.clone()
+        out.zero_()
+        table, t = attention(n)
+        keep = call(), keep
+        t[1].record()
+        torch.cuda.synchronize()
+        assert t[0].elapsed_time(t[1]) > 4400
+        assert B.sqap_device_status() == B.SQAP_OK
+        assert want.any() and torch.equal(out, want)
