@@ -366,12 +366,12 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
             po[0] = make_float4(y[0], y[1], y[2], y[3]);
             po[1] = make_float4(y[4], y[5], y[6], y[7]);
         } else {
-            const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
+            const float inv = ll != 0.0f ? 1.0f / ll : 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] *= inv;
             const int64_t row = static_cast<int64_t>(w.row0) + i;
             *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + row * a.ldo + static_cast<int64_t>(head) * D + d) = pack8<T>(y);
-            if (d == 0 && a.lse) a.lse[row * a.heads + head] = ll > 0.0f ? log_sum(mm, ll) : -INFINITY;
+            if (d == 0 && a.lse) a.lse[row * a.heads + head] = ll != 0.0f ? log_sum(mm, ll) : -INFINITY;
         }
     }
 }

@@ -242,12 +242,12 @@ __global__ void __launch_bounds__(256, 1) kv_prefill_kernel(AttnArgs a) {
 #pragma unroll
             for (int x = 0; x < D / 8; ++x) *reinterpret_cast<float2*>(po + 8 * x) = make_float2(o[x][2 * e], o[x][2 * e + 1]);
         } else {
-            const float inv = l[e] > 0.0f ? 1.0f / l[e] : 0.0f;
+            const float inv = l[e] != 0.0f ? 1.0f / l[e] : 0.0f;
             const int64_t row = static_cast<int64_t>(w.row0) + i;
             T* out = static_cast<T*>(a.out) + row * a.ldo + static_cast<int64_t>(head) * D + 2 * t;
 #pragma unroll
             for (int x = 0; x < D / 8; ++x) *reinterpret_cast<uint32_t*>(out + 8 * x) = pack2<T>(o[x][2 * e] * inv, o[x][2 * e + 1] * inv);
-            if (t == 0 && a.lse) a.lse[row * a.heads + head] = l[e] > 0.0f ? log_sum(m[e], l[e]) : -INFINITY;
+            if (t == 0 && a.lse) a.lse[row * a.heads + head] = l[e] != 0.0f ? log_sum(m[e], l[e]) : -INFINITY;
         }
     }
 }

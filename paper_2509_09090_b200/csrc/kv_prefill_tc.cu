@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
                 tc_fence_after();
             }
             if (idle) continue;
-            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+            const float inv = l != 0.0f ? 1.0f / l : 0.0f;
             const int64_t row = static_cast<int64_t>(x.w.row0) + qi;
             const int64_t at = a.splits > 1 && real ? part_index(a, x.w.b, head, qi, x.w.split) : 0;
             T* out = static_cast<T*>(a.out) + row * a.ldo + static_cast<int64_t>(head) * D;
@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
             }
             if (real) {
                 if (a.splits > 1) a.part_ml[at] = make_float2(m, l);
-                else if (a.lse) a.lse[row * a.heads + head] = l > 0.0f ? log_sum(m, l) : -INFINITY;
+                else if (a.lse) a.lse[row * a.heads + head] = l != 0.0f ? log_sum(m, l) : -INFINITY;
             }
             tc_fence_before();
         }

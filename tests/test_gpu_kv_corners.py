@@ -167,3 +167,25 @@ def test_append_of_more_rows_than_max_new(max_new, kind):
             if end > 0:
                 R.kv_append(codes, scale, s.table[b:b + 1], [end], [0, m], xn[cu[b]:cu[b] + m, c0:c0 + H * D].reshape(-1, H, D), kind, P)
         assert np.array_equal(s.device_codes(a), codes) and np.array_equal(s.ds[a].cpu().numpy(), scale)
+
+
+# ---------------------------------------------------------------------------------------------------------- not-a-numbers
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("D,lens,new", [(64, [40, 9], [1, 1]), (128, [3000, 70], [1, 1]), (128, [40, 60], [33, 20]), (64, [4000, 50], [20, 20]),
+                                        (256, [40, 9], [1, 1]), (256, [3000, 50], [40, 33])])
+def test_a_query_that_is_not_finite_spoils_its_own_row_alone(D, lens, new, bad):
+    """... and says so in the log-sum-exp as well, whether the history is cut into pieces or not: -inf means that nothing is seen."""
+    heads, H = 4, 2
+    s = Setup(lens, H, D, 16, R.INT8, 5)
+    rows = 2 + sum(new)
+    good = dev(np.random.default_rng(1).standard_normal((rows, heads * D)), torch.float16)
+    q = good.clone()
+    q[2, D + 5] = bad                     # the first sequence's first query, head 1
+    o0, l0, _ = run_attention(s, good, new, heads, True, "fp16")
+    o, l, _ = run_attention(s, q, new, heads, True, "fp16")
+    o0, o = (a[2:].reshape(-1, heads, D) for a in (o0, o))
+    assert np.isnan(l[2, 1]) and np.isnan(o[0, 1]).all()
+    l0[2, 1] = l[2, 1] = 0
+    o0[0, 1] = o[0, 1] = 0
+    assert np.array_equal(l, l0) and np.array_equal(o, o0)
