@@ -376,7 +376,8 @@ typedef struct {
  *   earlier tokens, if the scale grew:  code' = round(code * (scale / scale'));  new tokens:  code = round(x * (1 / scale'))
  * in fp32, round to nearest even, int8 clamped to +-127, e4m3 to +-448. Powers of two make the first rule exact for e4m3
  * but for its subnormal codes. A page that receives tokens must belong to one sequence. Other places of the page
- * keep their codes. cu_new: batch + 1 entries, not decreasing. Non-finite values give unspecified codes in their page.
+ * keep their codes. cu_new: batch + 1 entries, not decreasing. Non-finite values give unspecified codes in their page, but finite
+ * ones and a finite scale: queries that see no token of the page do not notice.
  */
 sqap_status sqap_kv_append(const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int batch, const int32_t* lens,
                            const int32_t* cu_new, int max_new, const void* k, int64_t ldk, const void* v, int64_t ldv,

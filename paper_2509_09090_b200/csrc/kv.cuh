@@ -147,6 +147,24 @@ __device__ __forceinline__ uint2 encode8(const float* y) {
     }
     return make_uint2(w[0], w[1]);
 }
+// Eight codes without not-a-numbers (e4m3 has them, 0x7F and 0xFF; they become zeros): a weight of 0 times one would reach rows that do
+// not see it. A byte's low seven bits plus one carry into its top bit for 0x7F alone.
+template <int TYPE>
+__device__ __forceinline__ uint2 finite_codes(uint2 w) {
+    if (TYPE == SQAP_KV_INT8) return w;
+    const uint32_t x = ((w.x & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u, y = ((w.y & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+    if (x | y) {
+        w.x &= ~((x >> 7) * 0x7Fu);
+        w.y &= ~((y >> 7) * 0x7Fu);
+    }
+    return w;
+}
+template <typename T>
+__device__ __forceinline__ float largest();
+template <>
+__device__ __forceinline__ float largest<__half>() { return 65504.0f; }
+template <>
+__device__ __forceinline__ float largest<__nv_bfloat16>() { return __uint_as_float(0x7F7F0000u); }
 // Scale of a block whose largest magnitude is amax.
 template <int TYPE>
 __device__ __forceinline__ float scale_for(float amax) {

@@ -89,7 +89,8 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(AppendArgs a) {
 #pragma unroll
     for (int q = 0; q < HELD; ++q) widen8<T>(held[q], &top);
     for (int i = threadIdx.x + HELD * THREADS; i < items; i += THREADS) widen8<T>(source(i), &top);
-    const float amax = block_max(fold_pair<T>(top), red);   // (every thread has read *scale_at before thread 0 writes it)
+    // (every thread has read *scale_at before thread 0 writes it; an infinity counts as the largest number: scales are finite)
+    const float amax = fminf(block_max(fold_pair<T>(top), red), largest<T>());
     const float scale = fmaxf(before, scale_for<TYPE>(amax));
     if (threadIdx.x == 0) *scale_at = scale;
     if (scale > before && t0 > lo) {                        // they are rounded again to the larger scale
@@ -110,7 +111,7 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(AppendArgs a) {
         unpack8<T>(u, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = __fmul_rn(v[e], inv);
-        to[i] = encode8<TYPE>(v);
+        to[i] = finite_codes<TYPE>(encode8<TYPE>(v));
     };
 #pragma unroll
     for (int q = 0; q < HELD; ++q)

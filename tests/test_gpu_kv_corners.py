@@ -189,3 +189,27 @@ def test_a_query_that_is_not_finite_spoils_its_own_row_alone(D, lens, new, bad):
     l0[2, 1] = l[2, 1] = 0
     o0[0, 1] = o[0, 1] = 0
     assert np.array_equal(l, l0) and np.array_equal(o, o0)
+
+
+@pytest.mark.parametrize("kind", [R.INT8, R.E4M3])
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("D,n", [(64, 3), (64, 60), (128, 4), (128, 200), (256, 3), (256, 60)])
+def test_a_token_that_is_not_finite_does_not_reach_queries_that_do_not_see_its_page(D, n, bad, dtype, kind):
+    H, P, old = 2, 16, 14                  # the new tokens begin two places in front of a page
+    g = np.random.default_rng(2)
+    got = []
+    rows = dev(g.standard_normal((n, 3 * H * D)), T[dtype])
+    for what in (0.5, bad):
+        s = Setup([old + n], H, D, P, kind, 4)
+        x = rows.clone()
+        x[2, H * D + 3] = x[2, 2 * H * D + 7] = what              # key and value of the first token of the second page
+        cu, lens = ints([0, n]), ints([old + n])
+        B.sqap_kv_append(s.cache, s.dtable, s.width, 1, lens, cu, n, x[:, H * D:], 3 * H * D, x[:, 2 * H * D:], 3 * H * D, CODE[dtype])
+        out, lse = torch.empty((n, H * D), dtype=T[dtype], device=DEV), torch.empty((n, H), device=DEV)
+        size = B.sqap_kv_attention_workspace_bytes(s.cache, 1, n, old + n, H)
+        work = torch.empty(size + 16, dtype=torch.uint8, device=DEV)
+        B.sqap_kv_attention(s.cache, s.dtable, s.width, 1, lens, cu, n, old + n, x, 3 * H * D, H, 0.1, 1, out, H * D, lse, CODE[dtype], work, size)
+        torch.cuda.synchronize()
+        got.append((out[:2].clone(), lse[:2].clone()))
+    assert torch.isfinite(got[0][0]).all() and torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
