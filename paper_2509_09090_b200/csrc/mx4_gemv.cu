@@ -4,7 +4,7 @@
 // a cluster's exchange and two launches for what is a few microseconds of streaming (1 x 12288 x 4096: 10.4 us, 2.7 TB/s; the
 // quantization that every CTA does first and some 2 instructions per code are what is left). Here a code's doubled value (0, 1, 2, 3, 4,
 // 6, 8, 12, with a sign) is an int8, so a block's sum of products is exact in integers:
-//   sum over the block of x w = (1/4) dp4a(...),  then one fp32 multiplication by each of the two block scales.
+//   sum over the block of x w = (1/4) dp4a(...),  then the two block scales in fp32 (the quarter is in the tokens').
 // Four nibbles become four bytes by one byte permute of an 8-byte table with the nibbles as selectors: the selector's top bit
 // (the code's sign) replaces the byte by its sign bit, 0 here, so one permute gives the positive codes and a second, with the
 // signs flipped, the negative ones.
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(THREADS, 2) mx4_gemv_kernel(GemvArgs a) {
     // int8 tokens: of each 32 elements the first 16 and the second 16 in arrays of their own (no bank conflicts)
     auto lo = [&](int m) { return reinterpret_cast<uint4*>(smem) + (2 * m) * groups; };
     auto hi = [&](int m) { return reinterpret_cast<uint4*>(smem) + (2 * m + 1) * groups; };
-    float* const xs = reinterpret_cast<float*>(smem + MM * K);            // [MM][K / BLK]
+    float* const xs = reinterpret_cast<float*>(smem + MM * K);            // [MM][K / BLK]: a quarter of the scales (codes are doubled)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_launch_dependents();
     pdl_wait();
@@ -133,13 +133,13 @@ __global__ void __launch_bounds__(THREADS, 2) mx4_gemv_kernel(GemvArgs a) {
             if (h < 2 * groups) {
                 const uint2 p0 = codes_to_int8(q.x), p1 = codes_to_int8(q.y);
                 ((h & 1) ? hi(m) : lo(m))[h >> 1] = make_uint4(p0.x, p0.y, p1.x, p1.y);
-                if (FMT == SQAP_MX_NVFP4 || (h & 1) == 0) xs[m * (K / BLK) + 16 * h / BLK] = scale;
+                if (FMT == SQAP_MX_NVFP4 || (h & 1) == 0) xs[m * (K / BLK) + 16 * h / BLK] = 0.25f * scale;
             }
         }
     }
     __syncthreads();
 
-    const float alpha = (FMT == SQAP_MX_NVFP4 ? __fmul_rn(gs, a.gw ? __ldg(a.gw) : 1.0f) : 1.0f) * 0.25f;
+    const float alpha = FMT == SQAP_MX_NVFP4 ? __fmul_rn(gs, a.gw ? __ldg(a.gw) : 1.0f) : 1.0f;
     float acc[2][MM] = {};
     int rows = team, step = 0;
     while (rows < total) {
@@ -195,9 +195,11 @@ __global__ void __launch_bounds__(THREADS, 2) mx4_gemv_kernel(GemvArgs a) {
                     }
                 } else {
                     const float s0 = scale_value<FMT>(s[i][row]);
+                    // The scales reach over the whole range of fp32: they meet before the sum of products does (which is up to 2^12),
+                    // bounded, so that a sum of 0 stays 0.
 #pragma unroll
                     for (int m = 0; m < MM; ++m)
-                        acc[row][m] = fmaf(static_cast<float>(dot[m][0] + dot[m][1]) * xs[m * (K / 32) + g], s0, acc[row][m]);
+                        acc[row][m] = fmaf(static_cast<float>(dot[m][0] + dot[m][1]), fminf(xs[m * (K / 32) + g] * s0, 3.4028235e38f), acc[row][m]);
                 }
             }
             }

@@ -75,3 +75,19 @@ def test_products_behind_a_kernel_that_takes_longer_than_their_waits():
         assert t[0].elapsed_time(t[1]) > 4400
         assert B.sqap_device_status() == B.SQAP_OK
         assert want.any() and torch.equal(out, want)
+
+
+# one to four tokens are multiplied on CUDA cores, five on tensor cores
+@pytest.mark.parametrize("M", [1, 2, 4, 5])
+@pytest.mark.parametrize("x_exp,w_exp", [(125, -100), (120, -60), (-100, 100), (-120, 20), (125, -127)])
+def test_power_of_two_scales_at_the_ends_of_their_range(M, x_exp, w_exp):
+    """A product of scales that fits fp32 is right wherever the scales themselves lie."""
+    N, K, fmt = 40, 256, R.MXFP4
+    g = np.random.default_rng(M)
+    xc, wc = (g.integers(0, 256, (r, K // 2)).astype(np.uint8) for r in (M, N))
+    xs, ws = ((127 + e + g.integers(0, 3, (r, K // 32)) - (e > 100)).clip(0, 254).astype(np.uint8) for e, r in ((x_exp, M), (w_exp, N)))
+    x, w = R.mx4_values(xc, xs, fmt), R.mx4_values(wc, ws, fmt)
+    out = torch.full((M, N), 7.0, dtype=torch.float32, device=DEV)
+    B.sqap_mx4_linear(dev(xc), dev(R.tile(xs, 0xFF)), None, M, dev(wc), dev(R.tile(ws, 0xFF)), None, N, K, fmt, out, N, B.SQAP_FP32)
+    torch.cuda.synchronize()
+    check_product(out.double().cpu().numpy(), x, w, "fp32", K)
