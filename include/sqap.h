@@ -388,7 +388,8 @@ sqap_status sqap_kv_append(const sqap_kv_cache* cache, const int32_t* table, int
  * sequence b, heads x head_dim elements each; query head h reads key/value head h / (heads / kv_heads).
  *   out[row][h] = sum_t p_t v_t,   p = softmax over the visible t of (q . k_t) * scale
  * With SQAP_KV_CAUSAL query i of n_q sees tokens 0 .. lens[b] - n_q + i, without it all lens[b]. A row that sees nothing is 0
- * (lse -inf); one whose query holds a NaN is NaN, its lse too, and no other row with it. lse (may be NULL): fp32 [rows][heads], log sum_t exp((q . k_t) scale).
+ * (lse -inf); one whose query holds a NaN is NaN, its lse too, and no other row with it. lse (may be NULL): fp32
+ * [rows][heads], log sum_t exp((q . k_t) scale).
  * dtype (of q and out): FP16 or BF16; rows ldq / ldo elements apart, 16-byte aligned, ldq, ldo % 8 == 0. Rows that belong to no
  * sequence are left as they are. max_q, max_len: no sequence has more queries or tokens (more are not computed / not
  * seen); they size the launch. Scores, maxima, denominators and sums are fp32; the queries enter the matrix

@@ -54,6 +54,15 @@ inline Cache device_view(const sqap_kv_cache* c) {
     d.head_dim = c->head_dim;
     return d;
 }
+// Product of sizes (none negative), at most 2^62: where 64 bits do not hold it, it is too large for every limit that it is held against.
+template <typename... I>
+inline int64_t size_product(I... sizes) {
+    constexpr int64_t TOP = int64_t{1} << 62;
+    int64_t p = 1;
+    for (const int64_t s : {static_cast<int64_t>(sizes)...})
+        if (__builtin_mul_overflow(p, s, &p) || p > TOP) p = TOP;
+    return p;
+}
 inline bool row_type(int t) { return t == SQAP_FP16 || t == SQAP_BF16; }
 inline sqap_status finish_launch(cudaError_t e) {
     if (e != cudaSuccess) {

@@ -99,7 +99,7 @@ Plan plan_for(int64_t batch, int kv_heads, int group, int head_dim, int64_t max_
     p.decode = rows <= decode_max_rows(head_dim);
     const int per_tile = head_dim <= 128 ? PREFILL_TC_ROWS : PREFILL_ROWS;
     p.tiles = p.decode ? 1 : static_cast<int>((rows + per_tile - 1) / per_tile);
-    const int64_t ctas = batch * kv_heads * p.tiles;
+    const int64_t ctas = size_product(batch, kv_heads, p.tiles);
     auto pieces = [&](int per_sm) { return ctas > 0 ? (148 * per_sm + ctas - 1) / ctas : 1; };
     auto least = [](int64_t x, int64_t y) { return x < y ? x : y; };
     int64_t splits;
@@ -116,6 +116,11 @@ Plan plan_for(int64_t batch, int kv_heads, int group, int head_dim, int64_t max_
     if (p.splits < 1) p.splits = 1;
     return p;
 }
+// What the kernels' 32-bit indexes hold.
+bool sizes_fit(int batch, int kv_heads, int heads, int max_q, int max_len) {
+    return size_product(max_q, heads / kv_heads) <= 1 << 30 && max_len <= 1 << 30 && size_product(batch, heads, max_q) <= 4ll * 0x7FFFFFFF;
+}
+bool grid_fits(int batch, int kv_heads, const Plan& p) { return size_product(batch, kv_heads, p.splits, p.tiles) <= 0x7FFFFFFF; }
 size_t part_bytes(int64_t batch, int heads, int64_t max_q, int head_dim, const Plan& p) {
     if (p.splits <= 1) return 0;
     const size_t parts = static_cast<size_t>(batch) * heads * max_q * p.splits;
@@ -129,8 +134,9 @@ size_t part_bytes(int64_t batch, int heads, int64_t max_q, int head_dim, const P
 extern "C" size_t sqap_kv_attention_workspace_bytes(const sqap_kv_cache* cache, int batch, int max_q, int max_len, int heads) {
     using namespace sqap::kv;
     if (check_cache(cache) != SQAP_OK || batch <= 0 || max_q <= 0 || max_len < 0 || heads <= 0 || heads % cache->kv_heads != 0) return 0;
-    return part_bytes(batch, heads, max_q, cache->head_dim,
-                      plan_for(batch, cache->kv_heads, heads / cache->kv_heads, cache->head_dim, max_q, max_len));
+    if (!sizes_fit(batch, cache->kv_heads, heads, max_q, max_len)) return 0;
+    const Plan p = plan_for(batch, cache->kv_heads, heads / cache->kv_heads, cache->head_dim, max_q, max_len);
+    return grid_fits(batch, cache->kv_heads, p) ? part_bytes(batch, heads, max_q, cache->head_dim, p) : 0;
 }
 
 extern "C" sqap_status sqap_kv_attention(const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int batch, const int32_t* lens,
@@ -153,10 +159,9 @@ extern "C" sqap_status sqap_kv_attention(const sqap_kv_cache* cache, const int32
     AttnArgs a;
     a.c = device_view(cache);
     a.group = heads / cache->kv_heads;
-    if (static_cast<int64_t>(max_q) * a.group > (1 << 30) || max_len > (1 << 30)) return SQAP_ERR_UNSUPPORTED;
+    if (!sizes_fit(batch, cache->kv_heads, heads, max_q, max_len)) return SQAP_ERR_UNSUPPORTED;
     const Plan p = plan_for(batch, cache->kv_heads, a.group, cache->head_dim, max_q, max_len);
-    const int64_t grid = static_cast<int64_t>(batch) * cache->kv_heads * p.splits * p.tiles;
-    if (grid > 0x7FFFFFFF || static_cast<int64_t>(batch) * heads * max_q > 4ll * 0x7FFFFFFF) return SQAP_ERR_UNSUPPORTED;
+    if (!grid_fits(batch, cache->kv_heads, p)) return SQAP_ERR_UNSUPPORTED;
     const size_t need = part_bytes(batch, heads, max_q, cache->head_dim, p);
     if (need > 0) {
         if (!workspace) return SQAP_ERR_INVALID;

@@ -351,7 +351,7 @@ extern "C" sqap_status sqap_kv_append(const sqap_kv_cache* cache, const int32_t*
     AppendArgs a = {device_view(cache), table, ldt, lens, cu_new, max_new, 0, k, v, ldk, ldv};
     // from an offset of page_tokens - 1 on, the tokens touch one page more
     a.slots = static_cast<int>((static_cast<int64_t>(max_new) - 1 + cache->page_tokens - 1) / cache->page_tokens + 1);
-    const int64_t grid = static_cast<int64_t>(batch) * a.slots * cache->kv_heads * 2;
+    const int64_t grid = size_product(batch, a.slots, cache->kv_heads, 2);
     if (grid > MAX_GRID) return SQAP_ERR_UNSUPPORTED;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return finish_launch(dtype == SQAP_FP16 ? append_as<__half>(a, cache->type, static_cast<unsigned>(grid), s)
@@ -372,7 +372,7 @@ extern "C" sqap_status sqap_kv_read(const sqap_kv_cache* cache, const int32_t* t
     if (batch == 0 || max_rows == 0 || (!k && !v)) return SQAP_OK;
     if (!cu_rows || (ldt > 0 && !table)) return SQAP_ERR_INVALID;
     // runs of 16 places that max_rows tokens can touch
-    const int64_t runs = (static_cast<int64_t>(max_rows) + 14) / 16 + 1, warps = 2 * static_cast<int64_t>(batch) * runs * cache->kv_heads;
+    const int64_t runs = (static_cast<int64_t>(max_rows) + 14) / 16 + 1, warps = size_product(2, batch, runs, cache->kv_heads);
     if (warps > MAX_GRID) return SQAP_ERR_UNSUPPORTED;
     const ReadArgs a = {device_view(cache), table, ldt, first, cu_rows, max_rows, k, v, ldk, ldv};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -391,7 +391,7 @@ extern "C" sqap_status sqap_kv_copy_pages(const sqap_kv_cache* cache, const int3
     if (reinterpret_cast<uintptr_t>(pairs) & 7u) return SQAP_ERR_ALIGN;
     if (cache->pages == 0) return SQAP_OK;
     const int64_t bytes = static_cast<int64_t>(cache->kv_heads) * cache->page_tokens * cache->head_dim;
-    const int64_t pieces = (bytes + COPY_BYTES - 1) / COPY_BYTES, grid = 2 * static_cast<int64_t>(n) * pieces;
+    const int64_t pieces = (bytes + COPY_BYTES - 1) / COPY_BYTES, grid = size_product(2, n, pieces);
     if (grid > MAX_GRID) return SQAP_ERR_UNSUPPORTED;
     return finish_launch(launch_dependent(kv_copy_pages_kernel, dim3(static_cast<unsigned>(grid)), dim3(THREADS), 0,
                                           static_cast<cudaStream_t>(stream), device_view(cache), pairs, static_cast<int>(pieces)));
@@ -410,7 +410,7 @@ extern "C" sqap_status sqap_kv_compact(const sqap_kv_cache* cache, const int32_t
     if (cache->pages == 0 || rows == 0 || ldt == 0) return SQAP_OK;
     CompactArgs a = {device_view(cache), table, ldt, rows, lens, src_rows, dst_rows, kept, ldkept, n_kept, max_kept, 0};
     a.slots = (max_kept - 1) / cache->page_tokens + 1;
-    const int64_t grid = static_cast<int64_t>(n) * a.slots * cache->kv_heads * 2;
+    const int64_t grid = size_product(n, a.slots, cache->kv_heads, 2);
     if (grid > MAX_GRID) return SQAP_ERR_UNSUPPORTED;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (cache->type == SQAP_KV_INT8)
