@@ -213,3 +213,62 @@ def test_a_token_that_is_not_finite_does_not_reach_queries_that_do_not_see_its_p
         torch.cuda.synchronize()
         got.append((out[:2].clone(), lse[:2].clone()))
     assert torch.isfinite(got[0][0]).all() and torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+# ------------------------------------------------------------------------------------------------- many items, threads
+
+# more items of 256 rows than CTAs; items without an upper half, and sequences without rows, in front of full ones
+@pytest.mark.parametrize("kind,dtype", [(R.INT8, "fp16"), (R.E4M3, "bf16")])
+@pytest.mark.parametrize("heads,H,D,P,old,new", [
+    (32, 32, 128, 64, [0, 300, 7, 500, 200, 0], [288, 20, 150, 1, 129, 0]),
+    (32, 32, 64, 16, [0, 300, 7, 0, 200, 100], [288, 20, 150, 1, 129, 300]),
+    (32, 8, 128, 32, [0, 300, 64, 500, 1, 90], [250, 3, 390, 30, 129, 5])])
+def test_prompts_of_several_items_to_a_cta(heads, H, D, P, old, new, kind, dtype):
+    s = Setup([a + b for a, b in zip(old, new)], H, D, P, kind, 17, nan_behind=True)
+    for causal in (True, False):
+        check_attention(s, new, heads, causal, dtype, seed=3)
+    q = dev(np.random.default_rng(0).standard_normal((2 + sum(new), heads * D)), T[dtype])
+    a, b = (run_attention(s, q, new, heads, True, dtype)[:2] for _ in range(2))
+    assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+    assert B.sqap_device_status() == B.SQAP_OK
+
+
+def test_calls_from_two_host_threads():
+    import threading
+    H, D, P = 4, 128, 64
+    sets, ref = [], []
+    for i in range(2):
+        s = Setup([1300, 200], H, D, P, R.INT8, 20 + i)
+        x = dev(s.g.standard_normal((2, 3 * H * D)), torch.float16)
+        n = B.sqap_kv_attention_workspace_bytes(s.cache, 2, 1, 1300, H)
+        sets.append((s, x, ints(s.lens), ints([0, 1, 2]), torch.empty(2, H * D, dtype=torch.float16, device=DEV),
+                     torch.empty(n, dtype=torch.uint8, device=DEV), n, torch.cuda.Stream()))
+
+    def step(i):
+        s, x, lens, cu, out, work, n, stream = sets[i]
+        B.sqap_kv_append(s.cache, s.dtable, s.width, 2, lens, cu, 1, x[:, H * D:], 3 * H * D, x[:, 2 * H * D:], 3 * H * D, 0, stream)
+        B.sqap_kv_attention(s.cache, s.dtable, s.width, 2, lens, cu, 1, 1300, x, 3 * H * D, H, 0.09, 1, out, H * D, None, 0, work, n, stream)
+
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        step(i)
+        torch.cuda.synchronize()
+        ref.append(sets[i][4].clone())
+        sets[i][4].zero_()
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(i):
+        try:
+            for _ in range(200):
+                step(i)
+        except Exception as e:  # noqa: BLE001
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in (0, 1)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed and all(torch.equal(sets[i][4], ref[i]) for i in (0, 1))

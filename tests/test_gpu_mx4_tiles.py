@@ -91,3 +91,24 @@ def test_power_of_two_scales_at_the_ends_of_their_range(M, x_exp, w_exp):
     B.sqap_mx4_linear(dev(xc), dev(R.tile(xs, 0xFF)), None, M, dev(wc), dev(R.tile(ws, 0xFF)), None, N, K, fmt, out, N, B.SQAP_FP32)
     torch.cuda.synchronize()
     check_product(out.double().cpu().numpy(), x, w, "fp32", K)
+
+
+# 64, 128 and 192 tokens a tile; two to seven tiles for each pair of CTAs of a B200, of one to five stages, the last one short or whole
+@pytest.mark.parametrize("fmt", [R.NVFP4, R.MXFP4])
+@pytest.mark.parametrize("M,N,K", [(200, 12300, 544), (330, 12300, 288), (1100, 5000, 1056), (700, 5000, 1280), (1100, 19000, 96), (60, 40000, 512)])
+def test_products_of_several_tiles_to_a_pair(M, N, K, fmt):
+    xc, xs, wc, ws, x, w = product_case(M, N, K, fmt, seed=M + N + K)
+    args = [dev(a) for a in (xc, xs)], [dev(a) for a in (wc, ws)]
+    ldo = (N + 7) // 8 * 8 + 8
+    for dtype in ("fp32", "bf16"):
+        got = []
+        for _ in range(2):
+            out = torch.full((M + 1, ldo), 7.0, dtype=T[dtype], device=DEV)
+            B.sqap_mx4_linear(*args[0], None, M, *args[1], None, N, K, fmt, out, ldo, CODE[dtype])
+            torch.cuda.synchronize()
+            assert B.sqap_device_status() == B.SQAP_OK
+            got.append(out)
+        assert torch.equal(got[0], got[1])
+        o = got[0].double().cpu().numpy()
+        assert (o[M] == 7).all() and (o[:, N:] == 7).all()
+        check_product(o[:M, :N], x, w, dtype, K)
