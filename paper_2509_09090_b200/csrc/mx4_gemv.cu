@@ -1,7 +1,7 @@
 // Product of two microscaled 4-bit matrices for one to four tokens: a weight stream on CUDA cores.
 //
 // Bounded by HBM: 0.5625 (MXFP4 0.53) bytes per weight, read once. The tensor-core kernel (mx4_linear.cu) needs tensor memory,
-// a cluster's exchange and two launches for what is a few microseconds of streaming (1 x 12288 x 4096: 10.4 us, 2.7 TB/s; the
+// a cluster's exchange and two launches for what is a few microseconds of streaming (1 x 12288 x 4096: 11.1 us, 2.6 TB/s; the
 // quantization that every CTA does first and some 2 instructions per code are what is left). Here a code's doubled value (0, 1, 2, 3, 4,
 // 6, 8, 12, with a sign) is an int8, so a block's sum of products is exact in integers:
 //   sum over the block of x w = (1/4) dp4a(...),  then the two block scales in fp32 (the quarter is in the tokens').
@@ -262,13 +262,18 @@ static sqap_status launch_format(const GemvArgs& a, int M, int format, cudaStrea
 }  // namespace mx4v
 
 // One token, or up to four with few elements and few products: their quantization is repeated by every CTA and the integer products
-// grow with them, where the tensor-core kernels take four tokens in the time of one. Measured, this / those with their quantizer, us,
-// for 1, 2, 3, 4 tokens: 4096 x 4096 (rows x K) 5.2 6.5 8.1 9.1 / 8.9; 4096 x 1024 2.8 3.8 4.7 5.3 / 6.1; 12288 x 4096
-// 10.4 12.9 16.3 18.3 / 9.5; 22016 x 4096 16.0 19.5 25.0 27.5 / 17.3; 4096 x 11008 10.6 13.9 18.3 21.4 / 12.0.
+// grow with them, where the tensor-core kernels take four tokens in the time of one. Measured with the quantizer, weights from HBM, this /
+// those in a graph, us (called one by one, those take 12 to 18 us for their two launches up to 4096 x 11008). NVFP4, one token: 4096 x 1024
+// (rows x K) 3.0 / 6.0, 4096 x 4096 6.1 / 9.6, 12288 x 4096 11.1 / 11.5, 22016 x 4096 16.3 / 17.5, 4096 x 11008 11.7 / 13.5, 8192 x 8192
+// 14.3 / 14.5, 4096 x 16384 15.4 / 14.8; two: 4096 x 4096 7.5 / 9.6; four: 1024 x 4096 7.5 / 7.5, 4096 x 1024 5.8 / 6.4.
+// MXFP4, one token: 4096 x 4096 5.4 / 9.3, 4096 x 11008 12.3 / 12.5, but 12288 x 4096 12.0 / 11.1, 8192 x 8192 16.1 / 13.9 and
+// 22016 x 4096 18.4 / 16.8.
 // The tokens as int8 and their scales have to fit shared memory, with room for a second CTA.
 bool mx4_gemv_takes(int M, int N, int K, int format) {
     if (M > MX4_GEMV_MAX_ROWS || static_cast<int64_t>(M) * (K + K / mx4_block(format) * 4) > 100 * 1024) return false;
-    return M == 1 || (static_cast<int64_t>(M) * K <= 12 * 1024 && static_cast<int64_t>(M) * N * K <= 48 << 20);
+    const int64_t products = static_cast<int64_t>(M) * N * K;
+    if (M == 1) return format == SQAP_MX_NVFP4 || products < 48 << 20;
+    return static_cast<int64_t>(M) * K <= 12 * 1024 && products <= 48 << 20;
 }
 
 sqap_status launch_mx4_gemv(const Mx4Product& q, const void* x, int x_dtype, int64_t ldx, const int32_t* row_index, cudaStream_t s) {

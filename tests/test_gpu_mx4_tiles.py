@@ -112,3 +112,15 @@ def test_products_of_several_tiles_to_a_pair(M, N, K, fmt):
         o = got[0].double().cpu().numpy()
         assert (o[M] == 7).all() and (o[:, N:] == 7).all()
         check_product(o[:M, :N], x, w, dtype, K)
+
+
+@pytest.mark.parametrize("fmt", [R.NVFP4, R.MXFP4])
+@pytest.mark.parametrize("M,N,K", [(1, 12280, 4096), (1, 12288, 4096), (1, 12304, 4096), (2, 4096, 6144), (2, 4104, 6144)])
+def test_one_and_two_tokens_on_either_side_of_the_rule(M, N, K, fmt):
+    xc, xs, wc, ws, x, w = product_case(M, N, K, fmt, seed=M + N + K)
+    out = torch.full((M + 1, N), 7.0, dtype=torch.float32, device=DEV)
+    B.sqap_mx4_linear(dev(xc), dev(xs), None, M, dev(wc), dev(ws), None, N, K, fmt, out, N, B.SQAP_FP32)
+    torch.cuda.synchronize()
+    o = out.double().cpu().numpy()
+    assert (o[M] == 7).all()
+    check_product(o[:M], x, w, "fp32", K)
