@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import glob
 import os
+import re
 import subprocess
 import sys
 
@@ -27,12 +28,33 @@ def stale() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def register_shortages(log: str, source: str | None = None) -> list[str]:
+    """Kernels that move registers between their roles (setmaxnreg) can only be launched with the registers that they were
+    written for: kv_prefill_tc_kernel with LAUNCH_REGS a thread. `log` is what ptxas -v said; returns what falls short."""
+    if source is None:
+        with open(os.path.join(CSRC, "kv_prefill_tc.cu")) as f:
+            source = f.read()
+    want = int(re.search(r"LAUNCH_REGS = (\d+)", source).group(1))
+    used = re.findall(r"Compiling entry function '([^']*kv_prefill_tc_kernel[^']*)'.*?Used (\d+) registers", log, re.S)
+    if not used:
+        return ["kv_prefill_tc_kernel: not found"]
+    return [f"{name}: {n} registers, {want} needed" for name, n in used if int(n) < want]
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not stale():
         return LIB
     extra = os.environ.get("SQAP_NVCC_FLAGS", "").split()
-    cmd = [NVCC] + FLAGS + extra + (["-Xptxas", "-v"] if verbose else []) + ["-o", LIB + ".tmp"] + sources()
-    subprocess.run(cmd, check=True)
+    cmd = [NVCC] + FLAGS + extra + ["-Xptxas", "-v", "-o", LIB + ".tmp"] + sources()
+    run = subprocess.run(cmd, stderr=subprocess.PIPE, text=True)
+    if verbose or run.returncode:
+        sys.stderr.write(run.stderr)
+    else:
+        sys.stderr.writelines(line + "\n" for line in run.stderr.splitlines() if "warning" in line)
+    run.check_returncode()
+    short = register_shortages(run.stderr)
+    if short:
+        raise RuntimeError("the compiler gave a kernel too few registers to be launched: " + "; ".join(short))
     os.replace(LIB + ".tmp", LIB)
     return LIB
 
