@@ -87,7 +87,7 @@ struct Plan {
     bool decode;
     int tiles, splits, chunk;
 };
-// From the sizes alone, so that the workspace can be asked for ahead. Decode: up to 1024 keys a history is cut only where there
+// From the sizes (and the device) alone, so that the workspace can be asked for ahead. Decode: up to 1024 keys a history is cut only where there
 // are fewer than three CTAs to an SM, beyond that to four, and to sixteen as long as pieces keep 1024 keys (uneven histories then even
 // out). Measured at 8 and 32 heads, us, with four / eight / sixteen CTAs to an SM: 1 x 32768 keys 24 / 28 / 28, 16 x 2048 48 / 52 / 56,
 // 32 x 4096 48 / 50 / 53, 32 uneven ones of up to 16384 145 / 139 / 137; three / four at 16 x 290: 8.9 / 12.8.
@@ -100,14 +100,15 @@ Plan plan_for(int64_t batch, int kv_heads, int group, int head_dim, int64_t max_
     const int per_tile = head_dim <= 128 ? PREFILL_TC_ROWS : PREFILL_ROWS;
     p.tiles = p.decode ? 1 : static_cast<int>((rows + per_tile - 1) / per_tile);
     const int64_t ctas = size_product(batch, kv_heads, p.tiles);
-    auto pieces = [&](int per_sm) { return ctas > 0 ? (148 * per_sm + ctas - 1) / ctas : 1; };
+    const int64_t sms = sm_count();
+    auto pieces = [&](int per_sm) { return ctas > 0 ? (sms * per_sm + ctas - 1) / ctas : 1; };
     auto least = [](int64_t x, int64_t y) { return x < y ? x : y; };
     int64_t splits;
     if (p.decode) {
         const int64_t fill = least(pieces(max_len > 1024 ? 4 : 3), (max_len + 255) / 256), even = least(pieces(16), max_len / 1024);
         splits = fill > even ? fill : even;
     } else {
-        splits = ctas < 148 ? least(pieces(2), max_len / 1024) : 1;
+        splits = ctas < sms ? least(pieces(2), max_len / 1024) : 1;
     }
     if (splits < 1) splits = 1;
     const int64_t chunk = ((max_len + splits - 1) / splits + 127) / 128 * 128;

@@ -382,11 +382,11 @@ cudaError_t launch_rows(const AttnArgs& a, unsigned grid, cudaStream_t s) {
     // flight count for more. Measured, one / two groups, us: D = 128, 16 x 290 tokens x 32 heads 8.9 / 10.3, 16 x 2048 45 / 56,
     // 32 sequences of up to 16384 x 8 heads 125 / 137; D = 64, the same, 6.9 / 6.6, 32 / 30, 82 / 75.
     constexpr int GROUPS = D == 64 ? 2 : 1;
-    if (static_cast<int64_t>(a.max_q) * a.group <= 8)
-        return launch_dependent(kv_decode_kernel<T, TYPE, D, 1, GROUPS>, dim3(grid), dim3(WARPS * 32), 0, s, a);
-    // 9 to 16 rows: one / two groups, 32 x 8192 tokens x 8 heads of 128, 12 rows, 127 / 107; 16 x 2048, 16 rows, 33 / 30.
-    if (D == 256) return cudaErrorInvalidValue;     // not reached: see decode_max_rows()
-    return launch_dependent(kv_decode_kernel<T, TYPE, D == 256 ? 128 : D, 2, 2>, dim3(grid), dim3(WARPS * 32), 0, s, a);
+    if constexpr (D != 256)                         // 8 rows at most: decode_max_rows()
+        // 9 to 16 rows: one / two groups, 32 x 8192 tokens x 8 heads of 128, 12 rows, 127 / 107; 16 x 2048, 16 rows, 33 / 30.
+        if (static_cast<int64_t>(a.max_q) * a.group > 8)
+            return launch_dependent(kv_decode_kernel<T, TYPE, D, 2, 2>, dim3(grid), dim3(WARPS * 32), 0, s, a);
+    return launch_dependent(kv_decode_kernel<T, TYPE, D, 1, GROUPS>, dim3(grid), dim3(WARPS * 32), 0, s, a);
 }
 template <typename T, int TYPE>
 cudaError_t launch_dim(const AttnArgs& a, unsigned grid, cudaStream_t s) {

@@ -23,24 +23,19 @@ __device__ __forceinline__ void ldmatrix4_trans(uint32_t* r, uint32_t addr) {
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 
-template <int D>
-struct Shape {
-    static constexpr int WARPS = 8;
-    static constexpr int THREADS = WARPS * 32;
-    static constexpr int KEYS = 32;                      // keys per tile
-    static constexpr int LD = D + 8;                     // halves per row in shared memory: rows 16 bytes apart in the banks
-    static constexpr int CHUNKS = KEYS * D / 16 / THREADS;   // 16-byte pieces of codes per thread
-    static constexpr int GROUPS = KEYS / 16;
-};
+constexpr int D = 256;
+constexpr int WARPS = 8, THREADS = WARPS * 32;
+constexpr int KEYS = 32;                             // keys per tile
+constexpr int LD = D + 8;                            // halves per row in shared memory: rows 16 bytes apart in the banks
+constexpr int CHUNKS = KEYS * D / 16 / THREADS;      // 16-byte pieces of codes per thread
+constexpr int GROUPS = KEYS / 16;
+static_assert(WARPS * 16 == PREFILL_ROWS && CHUNKS >= 1, "tile shape");
 
-template <typename T, int TYPE, int D>
-__global__ void __launch_bounds__(256, 1) kv_prefill_kernel(AttnArgs a) {
-    using S = Shape<D>;
-    constexpr int KEYS = S::KEYS, LD = S::LD;
-    static_assert(S::WARPS * 16 == PREFILL_ROWS && S::CHUNKS >= 1, "tile shape");
+template <typename T, int TYPE>
+__global__ void __launch_bounds__(THREADS, 1) kv_prefill_kernel(AttnArgs a) {
     __shared__ alignas(16) __half sk[KEYS][LD];
     __shared__ alignas(16) __half sv[KEYS][LD];
-    __shared__ float s_ks[S::GROUPS], s_lv[S::GROUPS], s_iv[S::GROUPS];   // a missing page has lv = -inf
+    __shared__ float s_ks[GROUPS], s_lv[GROUPS], s_iv[GROUPS];   // a missing page has lv = -inf
 
     pdl_launch_dependents();
     pdl_wait();
@@ -104,13 +99,13 @@ __global__ void __launch_bounds__(256, 1) kv_prefill_kernel(AttnArgs a) {
         const int j = key >> shift;
         return key < end && j < a.ldt ? checked_page(a.c, __ldg(table + j)) : -1;
     };
-    uint4 kc[S::CHUNKS], vc[S::CHUNKS];
+    uint4 kc[CHUNKS], vc[CHUNKS];
     float next_ks = 0.0f, next_vs = 0.0f;
     int next_page = -1;
     auto fetch = [&](int k0) {
 #pragma unroll
-        for (int i = 0; i < S::CHUNKS; ++i) {
-            const int x = threadIdx.x + i * S::THREADS, row = x / (D / 16), col = x % (D / 16) * 16;
+        for (int i = 0; i < CHUNKS; ++i) {
+            const int x = threadIdx.x + i * THREADS, row = x / (D / 16), col = x % (D / 16) * 16;
             const int key = k0 + row;
             const int page = page_at(key);
             kc[i] = vc[i] = make_uint4(0, 0, 0, 0);       // behind the end: zero codes, whatever lies there
@@ -120,7 +115,7 @@ __global__ void __launch_bounds__(256, 1) kv_prefill_kernel(AttnArgs a) {
                 vc[i] = __ldg(reinterpret_cast<const uint4*>(a.c.v.codes + at));
             }
         }
-        if (threadIdx.x < S::GROUPS) {
+        if (threadIdx.x < GROUPS) {
             next_page = page_at(k0 + 16 * threadIdx.x);
             next_ks = next_vs = 0.0f;
             if (next_page >= 0) {
@@ -151,12 +146,12 @@ __global__ void __launch_bounds__(256, 1) kv_prefill_kernel(AttnArgs a) {
     for (int k0 = key0; k0 < end; k0 += KEYS) {
         __syncthreads();                                  // the tile before has been read
 #pragma unroll
-        for (int i = 0; i < S::CHUNKS; ++i) {
-            const int x = threadIdx.x + i * S::THREADS, row = x / (D / 16), col = x % (D / 16) * 16;
+        for (int i = 0; i < CHUNKS; ++i) {
+            const int x = threadIdx.x + i * THREADS, row = x / (D / 16), col = x % (D / 16) * 16;
             put16(&sk[row][col], kc[i]);
             put16(&sv[row][col], vc[i]);
         }
-        if (threadIdx.x < S::GROUPS) {
+        if (threadIdx.x < GROUPS) {
             const float x = next_vs > 0.0f ? next_vs : ZERO_PAGE_SCALE;
             const float lv = __log2f(x);
             s_ks[threadIdx.x] = next_ks;
@@ -254,7 +249,7 @@ __global__ void __launch_bounds__(256, 1) kv_prefill_kernel(AttnArgs a) {
 
 template <typename T, int TYPE>
 cudaError_t launch_as(const AttnArgs& a, unsigned grid, cudaStream_t s) {
-    return launch_dependent(kv_prefill_kernel<T, TYPE, 256>, dim3(grid), dim3(256), 0, s, a);
+    return launch_dependent(kv_prefill_kernel<T, TYPE>, dim3(grid), dim3(THREADS), 0, s, a);
 }
 
 }  // namespace

@@ -96,12 +96,6 @@ __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t* r) {
           "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
-__device__ __forceinline__ void tc_st8(uint32_t taddr, const uint32_t* r) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-                 : "memory");
-}
-__device__ __forceinline__ void tc_wait_st_f() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // Values [key][element], elements contiguous (the operand's N dimension): 128B-swizzled blocks of 64 elements; 8 keys are 1024
 // bytes apart, blocks KV_BLOCK.
 __device__ __forceinline__ uint64_t smem_desc_values(uint32_t addr) {
@@ -316,7 +310,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
                         l = fmaf(s0 + s1, iv[run], l);
                         tc_st8(t_s + 8 * run, p);                       // the scores are in registers
                     }
-                    tc_wait_st_f();
+                    tc_wait_st();
                     tc_fence_before();
                 }
                 __syncwarp();

@@ -57,19 +57,6 @@ struct MxArgs {
     int* status;
 };
 
-__device__ __forceinline__ uint32_t cluster_ctarank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t map_to_cta(uint32_t addr, uint32_t rank) {
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
 __device__ __forceinline__ void st_cluster_v4(uint32_t cluster_addr, const uint32_t* v) {
     asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
@@ -393,14 +380,9 @@ static sqap_status launch(const Mx4Product& q, cudaStream_t s) {
             k.ksplit = c;
         }
     }
-    const int own_max = (k.BN / 16 + k.ksplit - 1) / k.ksplit;
-    const int need = own_max * k.ksplit * CHUNK_BYTES + 4 * STAGE_BYTES;   // the exchange and the staging lie in the idle ring
-    int ring_bytes = k.stages * k.stage_bytes;
-    while (ring_bytes < need) {   // cannot happen with the depths above; keeps the invariant visible
-        ++k.stages;
-        ring_bytes += k.stage_bytes;
-    }
-    const int smem = ring_bytes + TAIL_BYTES + 1024;
+    // The exchange and the staging, own_max * ksplit * CHUNK_BYTES + 4 * STAGE_BYTES, lie in the idle ring: it is 4 KB larger at least,
+    // over all BN, formats and splits.
+    const int smem = k.stages * k.stage_bytes + TAIL_BYTES + 1024;
 
     CUtensorMap tm_w, tm_x;
     if (!make_map(&tm_w, q.w_codes, N, K / 2, BM, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||

@@ -69,22 +69,6 @@ struct PairArgs {
     int* status;
 };
 
-__device__ __forceinline__ uint32_t cluster_ctarank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t map_to_cta(uint32_t addr, uint32_t rank) {
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
 // Into this CTA's shared memory; the bytes are counted on a barrier that may live in the peer CTA.
 __device__ __forceinline__ void tma_pair_if(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar_cluster, uint32_t issue) {
     asm volatile(
@@ -99,12 +83,6 @@ __device__ __forceinline__ void tc_commit_pair(uint32_t bar) {
         "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
         ::"r"(bar), "h"(static_cast<uint16_t>(3))
         : "memory");
-}
-// Eight columns of this thread's tensor-memory lane.
-__device__ __forceinline__ void tc_st8(uint32_t taddr, const uint32_t* r) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-                 : "memory");
 }
 // 16 lanes x 32 columns as fragments of 8 x 8: r[4 u + 2 h + e] is row 8 h + lane / 4, column 8 u + 2 (lane % 4) + e.
 __device__ __forceinline__ void tc_ld_fragments(uint32_t taddr, uint32_t* r) {
@@ -126,7 +104,6 @@ __device__ __forceinline__ uint32_t bits16x2(float lo, float hi) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 template <int FMT>
 __device__ __forceinline__ void tc_mma_mx4(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                            uint32_t accumulate) {
