@@ -172,7 +172,8 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
             }
             const int64_t s = static_cast<int64_t>(max(page[u], 0)) * a.c.kv_heads + w.h;
             ks[u] = __ldg(a.c.k.scales + s);
-            vs[u] = __ldg(a.c.v.scales + s);
+            vs[u] = 0.0f;                          // not page 0's: its reciprocal times a weight of 0 need not be 0
+            if (page[u] >= 0) vs[u] = __ldg(a.c.v.scales + s);
         }
     };
     auto load_values = [&](int k0) {
@@ -230,8 +231,7 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
         for (int u = 0; u < GROUPS; ++u) {
             there[u] = page[u] >= 0;
             this_ks[u] = ks[u];
-            // (a place without a page has page 0's scales here: its weight is 0, but 0 times the reciprocal of what may stand there is not)
-            lv[u] = __log2f(there[u] && vs[u] > 0.0f ? vs[u] : ZERO_PAGE_SCALE);
+            lv[u] = __log2f(vs[u] > 0.0f ? vs[u] : ZERO_PAGE_SCALE);
             iv[u] = fast_exp2(-lv[u]);             // the reciprocal of what lv stands for: the weights use lv
         }
         if (more) load_keys(k0 + WARPS * STEP);
