@@ -52,17 +52,17 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(AppendArgs a) {
     id /= c.kv_heads;
     const int slot = static_cast<int>(id % a.slots), b = static_cast<int>(id / a.slots);
     const int first_row = a.cu[b];
-    const int n = a.cu[b + 1] - first_row;
-    const int64_t start = static_cast<int64_t>(a.lens[b]) - max(n, 0);     // position of the first new token; negative positions do not exist
-    const int64_t stop = start + min(n, a.max_new);         // behind the last one that is read
+    const int n = max(a.cu[b + 1] - first_row, 0), len = a.lens[b];
+    const int start = max(len, 0) - n;                      // position of the first new token; negative positions do not exist
+    const int stop = start + min(n, a.max_new);             // behind the last one that is read
     if (stop <= 0) return;
-    const int from = start < 0 ? 0 : static_cast<int>(start);
+    const int from = max(start, 0);
     const int j = (from >> c.page_shift) + slot;            // page of the sequence
     if (static_cast<int64_t>(j) << c.page_shift >= stop) return;
     const int lo = j << c.page_shift;
     // new tokens of this page
     const int t0 = from > lo ? from : lo;
-    const int t1 = static_cast<int>(min(stop, static_cast<int64_t>(lo) + (1 << c.page_shift)));
+    const int t1 = static_cast<int>(min(static_cast<int64_t>(stop), static_cast<int64_t>(lo) + (1 << c.page_shift)));
     if (t0 >= t1 || j >= a.ldt) return;
     const int page = checked_page(c, a.table[b * a.ldt + j]);
     if (page < 0) return;
