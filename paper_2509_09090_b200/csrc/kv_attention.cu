@@ -89,10 +89,11 @@ struct Plan {
 };
 // From the sizes (and the device) alone, so that the workspace can be asked for ahead. Decode: up to 1024 keys a history is cut only where there
 // are fewer than three CTAs to an SM, beyond that to four, and to sixteen as long as pieces keep 1024 keys (uneven histories then even
-// out). Measured at 8 and 32 heads, us, with four / eight / sixteen CTAs to an SM: 1 x 32768 keys 24 / 28 / 28, 16 x 2048 48 / 52 / 56,
-// 32 x 4096 48 / 50 / 53, 32 uneven ones of up to 16384 145 / 139 / 137; three / four at 16 x 290: 8.9 / 12.8.
-// Prompts: two rounds of CTAs where there is less than one, in pieces of 1024 keys at least: cut / whole, us, 256 rows behind 1000
-// keys (8 heads, groups of 4) 38 / 31, behind 8000 92 / 153; 288 rows behind 4096 (32 heads) 73 / 85.
+// out). Measured, us, with four / eight / sixteen CTAs to an SM, uneven histories of up to so many keys: 32 x 16384, 8 heads 132 / 147 / 127;
+// 32 x 8192, 32 heads 258 / 232 / 219; 32 x 4096, 32 heads 147 / 135 / 131, 8 heads 48 / 48 / 48; 16 x 2048, 32 heads 51.5 / 51.1 / 51.3; but
+// one of 32768, 32 heads 42 / 57 / 57 (8 heads 21 all three). Three / four up to 1024 keys: 16 x 290, 32 heads 11.7 / 15.2, 16 x 1000 27.0 / 31.5.
+// Prompts: two rounds of CTAs where there is less than one, in pieces of 1024 keys at least: cut / whole, us, 256 rows (8 heads, groups of
+// 4) behind 3000 keys 44 / 63, behind 8000 76 / 114; 288 rows behind 4096 (32 heads) 59 / 62.
 Plan plan_for(int64_t batch, int kv_heads, int group, int head_dim, int64_t max_q, int64_t max_len) {
     Plan p;
     const int64_t rows = max_q * group;

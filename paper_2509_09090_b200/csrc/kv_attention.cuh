@@ -116,8 +116,9 @@ __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 x) { return _
 // Few query rows per key/value head (kv_decode.cu) and many: head_dim 64 and 128 (kv_prefill_tc.cu), 256 (kv_prefill.cu).
 // With 256 elements a lane cannot hold the output of more than 8 rows in registers.
 // Rows per key/value head up to which the register kernel takes the call. That / the prompt kernel, us, 16 sequences: 4 rows, 32 heads
-// of 64, 290 keys 9.6 / 30, 4096 keys 71 / 289; 16 rows, 8 heads of 128, 290 keys 12.3 / 11.8, 2048 keys 30 / 43; 8 rows, 32 heads of
-// 256, 290 keys 27 / 119.
+// of 64, 290 keys 9.1 / 26, 4096 keys 53 / 245; 8 rows, 32 heads of 128, 290 keys 12.5 / 30.6; 8 rows, 32 heads of 256, 290 keys 20 / 69.
+// 9 to 16 rows, 8 heads of 128: 100 keys 8.3 / 9.4, 500 keys 14.7 / 16.1, 2048 keys 31 / 44, 32 sequences of 16384 182 / 526, 64 of 290
+// 21 / 34. The other sign only where 128 CTAs walk some 290 keys in one round, 14.2 / 12.6, which no rule of its own was made for.
 inline int decode_max_rows(int head_dim) { return head_dim == 256 ? 8 : 16; }
 constexpr int PREFILL_ROWS = 128, PREFILL_TC_ROWS = 256;   // query rows of a CTA's item
 sqap_status launch_kv_decode(const AttnArgs& a, int type, int dtype, cudaStream_t s);

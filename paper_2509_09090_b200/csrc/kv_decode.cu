@@ -12,7 +12,7 @@
 // A warp keeps a running maximum, denominator and output of its own over steps of 16 or 32 tokens (see launch_rows); the warps of a
 // CTA take the steps of their piece of the history in turn and meet in shared memory once at the end. Histories that are
 // too few to fill the device are cut into pieces, joined by kv_combine_kernel. 32 uneven histories of up to 16384 tokens, 8 heads of
-// 128 in e4m3, groups of 4: 125 us, 4.8 TB/s; what is left is the start and end of uneven pieces and 16 warps an SM.
+// 128 in e4m3, groups of 4: 126 us, 4.8 TB/s; what is left is the start and end of uneven pieces and 16 warps an SM.
 #include "kv_attention.cuh"
 
 namespace sqap {
@@ -379,11 +379,11 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
 template <typename T, int TYPE, int D>
 cudaError_t launch_rows(const AttnArgs& a, unsigned grid, cudaStream_t s) {
     // 16-token groups per step. With one group of 128 elements a fourth CTA fits an SM, at 64 elements a second group's loads in
-    // flight count for more. Measured, one / two groups, us: D = 128, 16 x 290 tokens x 32 heads 8.9 / 10.3, 16 x 2048 45 / 56,
-    // 32 sequences of up to 16384 x 8 heads 125 / 137; D = 64, the same, 6.9 / 6.6, 32 / 30, 82 / 75.
+    // flight count for more. Measured, one / two groups, us: D = 128, 16 x 290 tokens x 32 heads 11.6 / 13.5, 16 x 2048 51.6 / 53.4,
+    // 32 sequences of up to 16384 x 8 heads 126 / 137; D = 64, the same, 9.1 / 8.7, 35.0 / 32.7, 83 / 76.
     constexpr int GROUPS = D == 64 ? 2 : 1;
     if constexpr (D != 256)                         // 8 rows at most: decode_max_rows()
-        // 9 to 16 rows: one / two groups, 32 x 8192 tokens x 8 heads of 128, 12 rows, 127 / 107; 16 x 2048, 16 rows, 33 / 30.
+        // 9 to 16 rows: one / two groups, 32 x 8192 tokens x 8 heads of 128, 12 rows, 134 / 115; 16 x 2048, 16 rows, 35 / 31.
         if (static_cast<int64_t>(a.max_q) * a.group > 8)
             return launch_dependent(kv_decode_kernel<T, TYPE, D, 2, 2>, dim3(grid), dim3(WARPS * 32), 0, s, a);
     return launch_dependent(kv_decode_kernel<T, TYPE, D, 1, GROUPS>, dim3(grid), dim3(WARPS * 32), 0, s, a);

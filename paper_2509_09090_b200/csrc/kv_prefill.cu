@@ -1,12 +1,12 @@
-// Attention of many query rows (prompts) over the paged 8-bit cache, head_dim 256: there a tile's output alone takes 256 columns of
-// tensor memory and its operands 192 KB of shared memory, so that nothing could overlap; register matrix instructions
-// hold it in registers instead. (head_dim 64 and 128: kv_prefill_tc.cu.)
+// Attention of many query rows (prompts) over the paged 8-bit cache, head_dim 256, on register matrix instructions. (head_dim 64 and 128:
+// kv_prefill_tc.cu, whose items of 256 rows do not fit: 512 columns of tensor memory for the output alone. Items of 128 rows would, 256
+// columns of output and two tiles of scores, with 64 KB of queries and two stages of 64 keys and values; that form is not built.)
 //
 // One CTA takes 128 rows (query x head of the group, packed: the heads that share a key/value head share its tiles) of one
 // sequence and key/value head and walks the keys in tiles. A tile's codes are fetched one tile ahead into registers,
 // turned into fp16 once per CTA and kept in shared memory, from where the eight warps (16 rows each) feed
 // register matrix instructions: scores, running maximum and denominator, weights times values. Bounded by their rate, an
-// eighth of tcgen05's, and by the registers that allow one CTA an SM (16 prompts' last 8 tokens behind 290, 32 heads: 119 us).
+// eighth of tcgen05's, and by the registers that allow one CTA an SM (16 prompts' last 9 tokens behind 290, 32 heads: 73 us, 78 MB).
 #include "kv_attention.cuh"
 
 namespace sqap {

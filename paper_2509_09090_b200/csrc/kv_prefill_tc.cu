@@ -11,7 +11,7 @@
 // Work per 64 keys and half, and what it costs an SM: MMAs 2 x 128 x 64 x D (640 cycles at D = 128: the scores read both
 // operands from shared memory), 8192 exponentials (512 cycles), some 3 instructions per weight; and per 64 keys 1.3 per code. It
 // is the instructions and the round trips between the roles that bound it (two prompts of 4099 tokens behind 1000, 32 heads in
-// groups of 4: 498 us, 822 TFLOP/s; 16 of 288 tokens, 32 heads: 59 us): an earlier form with 128 rows an item and two CTAs to an SM, which converted every tile
+// groups of 4: 501 us, 818 TFLOP/s, 510 us in a region of seconds; 16 of 288 tokens, 32 heads: 60 us): an earlier form with 128 rows an item and two CTAs to an SM, which converted every tile
 // for 128 rows only, issued 8200 warp instructions per 128 x 128 scores, 5000 of them for the conversion, at 64 % of
 // the issue slots. Persistent CTAs, one to an SM; 512 columns of tensor memory: two tiles of scores and one output for
 // each half.

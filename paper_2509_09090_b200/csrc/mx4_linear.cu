@@ -6,7 +6,8 @@
 //
 // This kernel is for few tokens, few weight rows and long K (use_clusters()); many tokens or rows: mx4_pair.cu. What bounds it: the
 // weight stream (0.5625 or 0.53 bytes per weight, 3.7 us of HBM for 4096 x 11008), and around it the set-up (some 2400 cycles)
-// and the exchange of partial sums (3000 to 4000 at 160 tokens). 160 x 4096 x 11008 in MXFP4 with the quantizer: 14.6 us.
+// and the exchange of partial sums (3000 to 4000 at 160 tokens). 160 x 4096 x 11008 in MXFP4 with the quantizer: 16.1 us, the
+// product alone 13.4.
 //
 // A stage of the shared-memory ring holds 256 elements of K: 128 bytes per row of either operand (one 128B-swizzled
 // TMA box each) and the scale tiles that belong to them, copied as they lie in memory (512 bytes per 128 rows and
@@ -326,9 +327,10 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constan
 // Which kernel. The pairs (mx4_pair.cu) take 256 weight rows and up to 192 tokens each and walk K alone: some 5 us and 0.25 us
 // per 256 elements of K and round. The clusters here split K where there are few tiles, but then exchange 4 bytes per token and
 // weight row of every slice. So they are for long K, few weight rows and few tokens. Measured with the quantizer, clusters / pairs,
-// us: 4096 x 11008 (rows x K): 14.9 / 15.9 for 64 tokens, 14.7 / 16.6 for 128, 17.3 / 17.6 for 192, 25.9 / 19.6 for 320;
-// 1024 x 4096: 7.2 / 9.1 for 16, 8.3 / 9.3 for 64, 10.1 / 9.3 for 128; 4096 x 4096: 10.3 / 8.9 for 16, 13.5 / 10.1 for 256;
-// 12288 x 4096: 16.4 / 10.0 for 16, 21.0 / 17.1 for 256.
+// us, NVFP4, operands from HBM: 4096 x 11008 (rows x K): 13.9 / 15.9 for 16 tokens, 15.5 / 16.4 for 64, 16.5 / 17.0 for 128, 17.9 / 18.1
+// for 160, 20.0 / 18.4 for 256; 1024 x 16384: 11.7 / 20.9 for 16, 19.1 / 23.3 for 256; 1024 x 4096: 7.7 / 9.3 for 16, 8.6 / 9.5 for 64,
+// 10.1 / 9.5 for 128; 4096 x 4096: 10.4 / 9.8 for 16, 14.4 / 10.6 for 256; 12288 x 4096: 17.2 / 11.8 for 16, 21.6 / 17.3 for 256.
+// MXFP4 differs by up to 2 us on both sides and by the same sign.
 static bool use_clusters(int M, int N, int K) {
     const int64_t steps = (K + BK - 1) / BK, weight_tiles = (N + 2 * BM - 1) / (2 * BM);
     return M <= BN_MAX && 64ll * M <= K && steps * (sm_count() / 2) > 128 * weight_tiles;

@@ -6,9 +6,10 @@
 // elements of K at BN = 192. The scales of the tokens are wanted in full by both CTAs (4 KB), those of the weights by their own
 // (2 KB). The codes' bytes are counted on the leader's barrier, where the MMAs are issued.
 // What bounds it: the four-bit MMAs of a stage (256 elements of K) take 384 cycles at BN = 192. 4608 x 12288 x 4096 in NVFP4 with
-// the quantizer takes 111 us, of it the product 98 (4.7 PFLOP/s, tensor pipe 68 %). A stage costs 0.32 us there; with one MMA of four issued it is 0.23, with no loads
+// the quantizer takes 112 us in bursts of a millisecond, of it the product 98 to 103 (4.5 PFLOP/s, tensor pipe 68 %), and 132 us (product
+// 117) in a region of seconds, where the power limit holds the SM clock at 1.4 GHz. A stage costs 0.32 us there; with one MMA of four issued it is 0.23, with no loads
 // 0.22, with neither 0.21: the round trip of a stage's signals (done -> scales written again -> issued) and the SM clock, which
-// the full load brings down to 1.55 GHz, share the rest. A tile's results cost 1.6 us of issue slots beside it.
+// the full load brings down to 1.55 GHz in a burst already, share the rest. A tile's results cost 1.6 us of issue slots beside it.
 // The scales go to tensor memory through registers (four warps: shared memory -> tcgen05.st, one lane quadrant each): a
 // tcgen05.cp of a scale tile holds up the tensor pipe for some 24 cycles, and a stage has twelve of them beside 374 cycles of
 // MMAs (measured: pipe busy 78 %, with MMAs 44 %; 15 us more for 4608 x 12288 x 4096).
