@@ -272,3 +272,77 @@ def test_calls_from_two_host_threads():
         t.join()
     torch.cuda.synchronize()
     assert not failed and all(torch.equal(sets[i][4], ref[i]) for i in (0, 1))
+
+
+# ------------------------------------------------------------------------------------------------- the ends of the sizes
+
+@pytest.mark.parametrize("D,heads,H,new,max_q", [(64, 4, 2, [5, 2], 3), (128, 12, 2, [9, 1], 4), (128, 4, 2, [40, 20], 33), (256, 2, 2, [7, 3], 5), (256, 2, 2, [60, 9], 40)])
+def test_queries_beyond_max_q_are_left_out(D, heads, H, new, max_q):
+    lens = [200, 70]
+    s = Setup(lens, H, D, 16, R.E4M3, 5)
+    cu = np.concatenate([[0], np.cumsum(new)])
+    q = dev(np.random.default_rng(1).standard_normal((sum(new), heads * D)), torch.float16)
+    got = []
+    for m in (max(new), max_q):
+        out = torch.full((sum(new), heads * D), 7.0, dtype=torch.float16, device=DEV)
+        lse = torch.full((sum(new), heads), 7.0, device=DEV)
+        size = B.sqap_kv_attention_workspace_bytes(s.cache, 2, m, 200, heads)
+        work = torch.empty(size + 16, dtype=torch.uint8, device=DEV)
+        B.sqap_kv_attention(s.cache, s.dtable, s.width, 2, ints(lens), ints(cu), m, 200, q, heads * D, heads, 0.1, 1, out, heads * D, lse, 0, work, size)
+        torch.cuda.synchronize()
+        got.append((out.double().cpu().numpy(), lse.cpu().numpy()))
+    for b in range(2):
+        m = min(new[b], max_q)
+        mine, rest = slice(cu[b], cu[b] + m), slice(cu[b] + m, cu[b + 1])
+        # (another kernel may have taken the shorter call: two roundings of the weights and of the output apart)
+        assert (np.abs(got[0][0][mine] - got[1][0][mine]) <= 2.0 ** -9 * np.abs(s.codes("v")).max() * s.scale["v"].max()).all()
+        assert np.allclose(got[0][1][mine], got[1][1][mine], rtol=0, atol=1e-3)
+        assert (got[1][0][rest] == 7).all() and (got[1][1][rest] == 7).all()
+
+
+@pytest.mark.parametrize("pages,free_every", [(16385, 1), (40000, 3), (100003, 17)])
+def test_pool_of_many_pages(pages, free_every):
+    """More pages than one step of the reserving kernels looks at."""
+    g = np.random.default_rng(pages)
+    refs_n = np.ones(pages, np.int32)
+    refs_n[::free_every] = 0
+    free = np.flatnonzero(refs_n == 0)
+    rows, width, P = 300, 40, 16
+    refs, lens = dev(refs_n), torch.zeros(rows, dtype=torch.int32, device=DEV)
+    table = torch.full((rows, width), -1, dtype=torch.int32, device=DEV)
+    args = (refs, pages, P, table, width, rows, lens)
+    need = g.integers(1, width, rows)
+    add = need * P - g.integers(0, P, rows)
+    granted = torch.empty(rows, dtype=torch.int32, device=DEV)
+    B.sqap_kv_alloc(*args, ints(range(rows)), ints(add), rows, granted)
+    torch.cuda.synchronize()
+    upto = np.cumsum(need)
+    ok = upto <= len(free)
+    assert granted.cpu().numpy().tolist() == ok.astype(int).tolist() and ok.any()
+    t = table.cpu().numpy()
+    for r in range(rows):
+        want = free[upto[r] - need[r]:upto[r]].tolist() if ok[r] else []
+        assert t[r].tolist() == want + [-1] * (width - len(want))
+    refs_n[free[:upto[ok][-1]]] = 1
+    assert np.array_equal(refs.cpu().numpy(), refs_n) and np.array_equal(lens.cpu().numpy(), np.where(ok, add, 0))
+
+
+def test_pool_of_as_many_rows_as_there_may_be():
+    rows, width, P, pages = 16384, 3, 16, 20000
+    refs, lens = torch.zeros(pages, dtype=torch.int32, device=DEV), torch.zeros(rows, dtype=torch.int32, device=DEV)
+    table = torch.full((rows, width), -1, dtype=torch.int32, device=DEV)
+    args = (refs, pages, P, table, width, rows, lens)
+    half = rows // 2
+    granted = torch.empty(rows, dtype=torch.int32, device=DEV)
+    B.sqap_kv_alloc(*args, ints(range(rows)), ints([17 if r < half else 0 for r in range(rows)]), rows, granted)
+    assert (granted == 1).all() and (lens[:half] == 17).all() and (lens[half:] == 0).all()
+    assert torch.equal(table[:half, :2].flatten().cpu(), torch.arange(rows, dtype=torch.int32)) and (refs[:rows] == 1).all() and (refs[rows:] == 0).all()
+    pairs = torch.empty((half, 2), dtype=torch.int32, device=DEV)
+    B.sqap_kv_fork(*args, ints(range(half)), ints(range(half, rows)), half, pairs, granted)
+    ok = pages - rows                                       # so many last pages are left to be copied
+    assert granted[:half].tolist() == [1] * ok + [0] * (half - ok)
+    assert pairs[:ok].tolist() == [[2 * i + 1, rows + i] for i in range(ok)] and (pairs[ok:] == -2).all()
+    assert table[half:half + ok].tolist() == [[2 * i, rows + i, -1] for i in range(ok)]
+    B.sqap_kv_free(*args, ints(range(rows)), rows)
+    torch.cuda.synchronize()
+    assert (refs == 0).all() and (lens == 0).all() and (table == -1).all()

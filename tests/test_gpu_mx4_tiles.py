@@ -124,3 +124,32 @@ def test_one_and_two_tokens_on_either_side_of_the_rule(M, N, K, fmt):
     o = out.double().cpu().numpy()
     assert (o[M] == 7).all()
     check_product(o[:M], x, w, "fp32", K)
+
+
+@pytest.mark.parametrize("fmt", [R.NVFP4, R.MXFP4])
+@pytest.mark.parametrize("M,N,K", [(1, 1, 32), (4, 1, 32), (5, 1, 32), (64, 3, 16384), (300, 1, 64), (70001, 20, 64)])
+def test_products_of_the_smallest_and_tallest_sizes(M, N, K, fmt):
+    xc, xs, wc, ws, x, w = product_case(M, N, K, fmt, seed=M + N + K)
+    out = torch.full((M + 1, 24), 7.0, dtype=torch.float32, device=DEV)
+    B.sqap_mx4_linear(dev(xc), dev(xs), None, M, dev(wc), dev(ws), None, N, K, fmt, out, 24, B.SQAP_FP32)
+    torch.cuda.synchronize()
+    assert B.sqap_device_status() == B.SQAP_OK
+    o = out.double().cpu().numpy()
+    assert (o[M] == 7).all() and (o[:, N:] == 7).all()
+    check_product(o[:M, :N], x, w, "fp32", K)
+
+
+@pytest.mark.parametrize("fmt", [R.NVFP4, R.MXFP4])
+def test_quantizer_and_inverse_of_more_rows_than_a_grid_is_high(fmt):
+    M, K = 70001, 96
+    x = torch.randn(M, K, device=DEV)
+    codes = torch.empty(M, K // 2, dtype=torch.uint8, device=DEV)
+    sc = torch.full((B.sqap_mx4_scale_bytes(M, K, fmt),), 0x7F, dtype=torch.uint8, device=DEV)
+    out = torch.empty_like(x)
+    B.sqap_mx4_quantize(x, B.SQAP_FP32, M, K, K, None, fmt, None, codes, sc)
+    B.sqap_mx4_dequantize(codes, sc, M, K, fmt, None, out, K, B.SQAP_FP32)
+    torch.cuda.synchronize()
+    v, scale = R.mx4_quantize(x.double().cpu().numpy(), fmt)
+    assert np.array_equal(R.E2M1[R.nibbles(codes.cpu().numpy())], v)
+    want = (v.reshape(M, -1, R.block(fmt)) * scale[..., None]).reshape(M, K)
+    assert np.array_equal(out.double().cpu().numpy(), want)
