@@ -126,8 +126,8 @@ def lib() -> ctypes.CDLL:
 
 def _ptr(t):
     """Address of a torch tensor / numpy array / int / None."""
-    if t is None:
-        return None
+    if t is None or type(t) is int:
+        return t
     try:
         return t.data_ptr()
     except AttributeError:
