@@ -346,6 +346,22 @@ sqap_status sqap_attention_scores(const void* qkv, int64_t ldq, int batch, int r
                                   void* stream);
 
 /*
+ * Rotary positions: the first rot_dim elements of every head are turned in pairs,
+ *   (y_i, y_j) = (x_i cos f - x_j sin f, x_j cos f + x_i sin f),   f = positions[axis * ldp + row] * freq[pair]
+ * pair n < rot_dim / 2 being elements (n, n + rot_dim / 2), with SQAP_ROTARY_NEIGHBOURS (2 n, 2 n + 1). The other elements are copied.
+ * axis_of: HOST bytes [rot_dim / 2], the axis whose position turns each pair (time, row and column of visual tokens, in runs or in turn),
+ * all < axes; NULL: axis 0. positions: device int32 [axes rows, ldp apart], any sign. freq: device fp32 [rot_dim / 2], radians per
+ * position. x: device FP16 or BF16 (dtype), rows ldx elements apart, heads side by side from x on (the queries and keys of a fused QKV
+ * output are heads + kv_heads of them); out the same way, ldo apart; out may be x (then ldo = ldx), and overlaps it in no other
+ * way. The angle is formed in 64 bits, sines and products in fp32, rounded once. head_dim % 8 == 0, head_dim <= 256, rot_dim % 8 == 0,
+ * axes <= 8; x, out 16-byte aligned; ldx, ldo % 8 == 0. rows = 0 is a no-op.
+ */
+#define SQAP_ROTARY_NEIGHBOURS 1u
+sqap_status sqap_rotary(const void* x, int64_t ldx, int rows, int heads, int head_dim, int rot_dim, const int32_t* positions, int64_t ldp,
+                        int axes, const uint8_t* axis_of, const float* freq, uint32_t flags, void* out, int64_t ldo, int dtype,
+                        void* stream);
+
+/*
  * Paged key/value cache in 8 bits. One layer's cache is
  *   k, v              device codes [pages][kv_heads][page_tokens][head_dim], int8 or e4m3, 16-byte aligned
  *   k_scale, v_scale  device fp32 [pages][kv_heads]: the scale of that page's codes of that head
@@ -403,6 +419,64 @@ sqap_status sqap_kv_attention(const sqap_kv_cache* cache, const int32_t* table, 
                               const int32_t* cu_q, int max_q, int max_len, const void* q, int64_t ldq, int heads, float scale,
                               uint32_t flags, void* out, int64_t ldo, float* lse, int dtype, void* workspace,
                               size_t workspace_bytes, void* stream);
+
+/*
+ * The same attention within a window: the query at position p of its sequence (the i-th of n_q: p = lens[b] - n_q + i) sees token t <= p
+ * if t > p - window, or if t < sinks (the first tokens stay visible). window >= 1, sinks >= 0; a window that reaches every token gives
+ * the causal attention. Everything else is as in sqap_kv_attention with SQAP_KV_CAUSAL. Only the pages of tokens that some query of the
+ * sequence sees, and their neighbours (up to 63 tokens on either side), are read: other entries of the table may be no pages.
+ */
+size_t sqap_kv_attention_window_workspace_bytes(const sqap_kv_cache* cache, int batch, int max_q, int max_len, int heads, int window,
+                                                int sinks);
+sqap_status sqap_kv_attention_window(const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int batch, const int32_t* lens,
+                                     const int32_t* cu_q, int max_q, int max_len, const void* q, int64_t ldq, int heads, float scale,
+                                     int window, int sinks, void* out, int64_t ldo, float* lse, int dtype, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/*
+ * The same attention for sequences that begin alike (copies made by sqap_kv_fork, requests behind one instruction): the sequences
+ * cu_group[g] .. cu_group[g+1]-1 are a group, whose first prefix[g] tokens are the same, and are read once for the group, from the
+ * pages of its first sequence. Results are those of sqap_kv_attention on tables that agree in these tokens, up to the order
+ * of the sums. cu_group: device int32 [groups + 1], not decreasing; prefix: device int32 [groups], < 0 counts as 0; a prefix need not
+ * end with a page and may be longer than a sequence. max_group, max_prefix: no group has more sequences, no prefix is longer (the rest of a
+ * group's sequences is not computed; tokens beyond max_prefix are read for each sequence). They size the launch, like max_q and
+ * max_len. Rows of sequences that are in no group are left as they are.
+ */
+size_t sqap_kv_attention_shared_workspace_bytes(const sqap_kv_cache* cache, int batch, int max_q, int max_len, int groups, int max_group,
+                                                int max_prefix, int heads);
+sqap_status sqap_kv_attention_shared(const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int batch, const int32_t* lens,
+                                     const int32_t* cu_q, int max_q, int max_len, const int32_t* cu_group, int groups, int max_group,
+                                     const int32_t* prefix, int max_prefix, const void* q, int64_t ldq, int heads, float scale,
+                                     uint32_t flags, void* out, int64_t ldo, float* lse, int dtype, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/*
+ * The same attention, and what each token received of it:
+ *   mass[b*ldm + t] = (t < lens[b] - n_q and past given ? past[b*ldm + t] : 0) + sum over i, h of p_t(i, h)
+ * for t < lens[b] (and < ldm, max_len), p_t the softmax weight of token t, i the last last_q of the sequence's n_q query rows, h all
+ * heads. Tokens that are new in the call have no past. past: device fp32 [batch rows, ldm apart], NULL for zeros; may be the same array
+ * as mass, and overlaps it in no other way. Query rows without a finite log-sum-exp add nothing. Sums in fp32 in an order that depends
+ * on the sizes alone. Other places of mass stay as they are.
+ */
+size_t sqap_kv_attention_mass_workspace_bytes(const sqap_kv_cache* cache, int batch, int max_q, int max_len, int heads, int last_q);
+sqap_status sqap_kv_attention_mass(const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int batch, const int32_t* lens,
+                                   const int32_t* cu_q, int max_q, int max_len, const void* q, int64_t ldq, int heads, float scale,
+                                   uint32_t flags, int last_q, void* out, int64_t ldo, float* lse, const float* past, float* mass,
+                                   int64_t ldm, int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Eviction: which tokens of row src_rows[i] of the table (lens[row] tokens, at most max_len and ldm) stay if keep[i] may. In this order:
+ * the `recent` last tokens (the last one first), the `first` first ones, and the others by mass[row*ldm + t] (as sqap_kv_attention_mass
+ * sums it), the largest first, equal ones in the order of their tokens; what is not a number comes last.
+ * kept: device int32 [n rows, ldkept apart], the tokens that stay, ascending, then -1 up to ldkept; n_kept: device int32 [n]. At most
+ * ldkept tokens stay. That is the list that sqap_kv_compact takes. dst_rows (may be NULL): the weights of the tokens that stay become
+ * the first n_kept[i] of row dst_rows[i] of mass; no row may be the destination of two entries, or of one and the source of another. A source
+ * that is no row has no tokens; a destination that is no row gets nothing. `rows` rows of mass and lens exist. max_len only sizes the
+ * launch beyond that.
+ */
+sqap_status sqap_kv_evict(float* mass, int64_t ldm, int rows, const int32_t* lens, const int32_t* src_rows, const int32_t* dst_rows,
+                          int n, const int32_t* keep, int first, int recent, int max_len, int32_t* kept, int64_t ldkept,
+                          int32_t* n_kept, void* stream);
 
 /* Reads back: tokens first[b] + i (first NULL: i) of sequence b, i < cu_rows[b+1] - cu_rows[b] (at most max_rows), become rows
  * cu_rows[b] + i of k and v (either may be NULL), rounded once to dtype (FP16, BF16). Token positions are not compared

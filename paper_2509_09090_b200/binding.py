@@ -18,6 +18,7 @@ SQAP_FP16, SQAP_BF16, SQAP_I32, SQAP_FP32 = 0, 1, 2, 3
 SQAP_MX_NVFP4, SQAP_MX_MXFP4 = 0, 1
 SQAP_KV_INT8, SQAP_KV_E4M3 = 0, 1
 SQAP_KV_CAUSAL = 1
+SQAP_ROTARY_NEIGHBOURS = 1
 SQAP_Q_ROTATE = 1
 SQAP_Q_PER_TENSOR = 2
 SQAP_W_ROTATED = 1
@@ -34,6 +35,8 @@ EXPORTS = ("sqap_pack_weights", "sqap_quantize_weights", "sqap_free_weights", "s
            "sqap_quantize_linear", "sqap_quantize_linear_workspace_bytes",
            "sqap_mx4_scale_bytes", "sqap_mx4_quantize", "sqap_mx4_dequantize", "sqap_mx4_linear", "sqap_mx4_workspace_bytes",
            "sqap_mx4_quantize_linear",
+           "sqap_rotary", "sqap_kv_attention_window", "sqap_kv_attention_window_workspace_bytes", "sqap_kv_attention_shared",
+           "sqap_kv_attention_shared_workspace_bytes", "sqap_kv_attention_mass", "sqap_kv_attention_mass_workspace_bytes", "sqap_kv_evict",
            "sqap_kv_append", "sqap_kv_attention", "sqap_kv_attention_workspace_bytes", "sqap_kv_read", "sqap_kv_alloc",
            "sqap_kv_fork", "sqap_kv_free", "sqap_kv_copy_pages", "sqap_kv_compact",
            "sqap_prune_tokens", "sqap_prune_select", "sqap_attention_scores",
@@ -100,6 +103,20 @@ def lib() -> ctypes.CDLL:
     L.sqap_kv_attention_workspace_bytes.argtypes = [cache, i32, i32, i32, i32]
     L.sqap_kv_attention_workspace_bytes.restype = sz
     L.sqap_kv_attention.argtypes = [cache, vp, i64, i32, vp, vp, i32, i32, vp, i64, i32, ctypes.c_float, u32, vp, i64, vp, i32, vp, sz, vp]
+    L.sqap_kv_attention_window_workspace_bytes.argtypes = [cache, i32, i32, i32, i32, i32, i32]
+    L.sqap_kv_attention_window_workspace_bytes.restype = sz
+    L.sqap_kv_attention_window.argtypes = [cache, vp, i64, i32, vp, vp, i32, i32, vp, i64, i32, ctypes.c_float, i32, i32, vp, i64, vp, i32,
+                                           vp, sz, vp]
+    L.sqap_kv_attention_shared_workspace_bytes.argtypes = [cache, i32, i32, i32, i32, i32, i32, i32]
+    L.sqap_kv_attention_shared_workspace_bytes.restype = sz
+    L.sqap_kv_attention_shared.argtypes = [cache, vp, i64, i32, vp, vp, i32, i32, vp, i32, i32, vp, i32, vp, i64, i32, ctypes.c_float, u32,
+                                           vp, i64, vp, i32, vp, sz, vp]
+    L.sqap_kv_attention_mass_workspace_bytes.argtypes = [cache, i32, i32, i32, i32, i32]
+    L.sqap_kv_attention_mass_workspace_bytes.restype = sz
+    L.sqap_kv_attention_mass.argtypes = [cache, vp, i64, i32, vp, vp, i32, i32, vp, i64, i32, ctypes.c_float, u32, i32, vp, i64, vp, vp, vp,
+                                         i64, i32, vp, sz, vp]
+    L.sqap_kv_evict.argtypes = [vp, i64, i32, vp, vp, vp, i32, vp, i32, i32, i32, vp, i64, vp, vp]
+    L.sqap_rotary.argtypes = [vp, i64, i32, i32, i32, i32, vp, i64, i32, vp, vp, u32, vp, i64, i32, vp]
     L.sqap_kv_read.argtypes = [cache, vp, i64, i32, vp, vp, i32, vp, i64, vp, i64, i32, vp]
     L.sqap_kv_alloc.argtypes = [vp, i32, i32, vp, i64, i32, vp, vp, vp, i32, vp, vp]
     L.sqap_kv_fork.argtypes = [vp, i32, i32, vp, i64, i32, vp, vp, vp, i32, vp, vp, vp]
@@ -315,6 +332,60 @@ def sqap_kv_attention(cache: KvCache, table, ldt: int, batch: int, lens, cu_q, m
     _check(lib().sqap_kv_attention(cache.ref, _ptr(table), ldt, batch, _ptr(lens), _ptr(cu_q), max_q, max_len, _ptr(q), ldq, heads,
                                    scale, flags, _ptr(out), ldo, _ptr(lse), dtype, _ptr(workspace), workspace_bytes,
                                    _stream(stream)), "sqap_kv_attention")
+
+
+def sqap_kv_attention_window_workspace_bytes(cache: KvCache, batch: int, max_q: int, max_len: int, heads: int, window: int, sinks: int) -> int:
+    return int(lib().sqap_kv_attention_window_workspace_bytes(cache.ref, batch, max_q, max_len, heads, window, sinks))
+
+
+def sqap_kv_attention_window(cache: KvCache, table, ldt: int, batch: int, lens, cu_q, max_q: int, max_len: int, q, ldq: int, heads: int,
+                             scale: float, window: int, sinks: int, out, ldo: int, lse, dtype: int, workspace, workspace_bytes: int,
+                             stream=None):
+    """Attention over the last tokens and a few first ones, see include/sqap.h."""
+    _check(lib().sqap_kv_attention_window(cache.ref, _ptr(table), ldt, batch, _ptr(lens), _ptr(cu_q), max_q, max_len, _ptr(q), ldq, heads,
+                                          scale, window, sinks, _ptr(out), ldo, _ptr(lse), dtype, _ptr(workspace), workspace_bytes,
+                                          _stream(stream)), "sqap_kv_attention_window")
+
+
+def sqap_kv_attention_shared_workspace_bytes(cache: KvCache, batch: int, max_q: int, max_len: int, groups: int, max_group: int,
+                                             max_prefix: int, heads: int) -> int:
+    return int(lib().sqap_kv_attention_shared_workspace_bytes(cache.ref, batch, max_q, max_len, groups, max_group, max_prefix, heads))
+
+
+def sqap_kv_attention_shared(cache: KvCache, table, ldt: int, batch: int, lens, cu_q, max_q: int, max_len: int, cu_group, groups: int,
+                             max_group: int, prefix, max_prefix: int, q, ldq: int, heads: int, scale: float, flags: int, out, ldo: int, lse,
+                             dtype: int, workspace, workspace_bytes: int, stream=None):
+    """Attention of sequences that share their first tokens, see include/sqap.h."""
+    _check(lib().sqap_kv_attention_shared(cache.ref, _ptr(table), ldt, batch, _ptr(lens), _ptr(cu_q), max_q, max_len, _ptr(cu_group), groups,
+                                          max_group, _ptr(prefix), max_prefix, _ptr(q), ldq, heads, scale, flags, _ptr(out), ldo, _ptr(lse),
+                                          dtype, _ptr(workspace), workspace_bytes, _stream(stream)), "sqap_kv_attention_shared")
+
+
+def sqap_kv_attention_mass_workspace_bytes(cache: KvCache, batch: int, max_q: int, max_len: int, heads: int, last_q: int) -> int:
+    return int(lib().sqap_kv_attention_mass_workspace_bytes(cache.ref, batch, max_q, max_len, heads, last_q))
+
+
+def sqap_kv_attention_mass(cache: KvCache, table, ldt: int, batch: int, lens, cu_q, max_q: int, max_len: int, q, ldq: int, heads: int,
+                           scale: float, flags: int, last_q: int, out, ldo: int, lse, past, mass, ldm: int, dtype: int, workspace,
+                           workspace_bytes: int, stream=None):
+    """Attention, and the sum of the weights that each token received, see include/sqap.h."""
+    _check(lib().sqap_kv_attention_mass(cache.ref, _ptr(table), ldt, batch, _ptr(lens), _ptr(cu_q), max_q, max_len, _ptr(q), ldq, heads,
+                                        scale, flags, last_q, _ptr(out), ldo, _ptr(lse), _ptr(past), _ptr(mass), ldm, dtype,
+                                        _ptr(workspace), workspace_bytes, _stream(stream)), "sqap_kv_attention_mass")
+
+
+def sqap_kv_evict(mass, ldm: int, rows: int, lens, src_rows, dst_rows, n: int, keep, first: int, recent: int, max_len: int, kept,
+                  ldkept: int, n_kept, stream=None):
+    """The tokens that stay in the cache, by the weight that attention gave them, see include/sqap.h."""
+    _check(lib().sqap_kv_evict(_ptr(mass), ldm, rows, _ptr(lens), _ptr(src_rows), _ptr(dst_rows), n, _ptr(keep), first, recent, max_len,
+                               _ptr(kept), ldkept, _ptr(n_kept), _stream(stream)), "sqap_kv_evict")
+
+
+def sqap_rotary(x, ldx: int, rows: int, heads: int, head_dim: int, rot_dim: int, positions, ldp: int, axes: int, axis_of, freq, flags: int,
+                out, ldo: int, dtype: int, stream=None):
+    """Rotary positions with one or several axes; axis_of: host bytes (or None), see include/sqap.h."""
+    _check(lib().sqap_rotary(_ptr(x), ldx, rows, heads, head_dim, rot_dim, _ptr(positions), ldp, axes, axis_of, _ptr(freq), flags, _ptr(out),
+                             ldo, dtype, _stream(stream)), "sqap_rotary")
 
 
 def sqap_kv_read(cache: KvCache, table, ldt: int, batch: int, first, cu_rows, max_rows: int, k, ldk: int, v, ldv: int, dtype: int,

@@ -21,19 +21,26 @@ __global__ void __launch_bounds__(128) kv_combine_kernel(AttnArgs a) {
     const int i = static_cast<int>(id % a.max_q);
     const int64_t bh = id / a.max_q;
     const int head = static_cast<int>(bh % a.heads);
-    const int64_t b = bh / a.heads;
+    int64_t b = bh / a.heads;
+    if (a.cu_group) {                                            // place of a sequence in a group
+        const int64_t group = b / a.max_group;
+        if (group >= a.groups) return;
+        const int first = a.cu_group[group];
+        b = first + b % a.max_group;
+        if (first < 0 || b >= a.cu_group[group + 1]) return;
+    }
     if (b >= a.batch) return;                                    // WARPS == 4: the whole CTA
     const int row0 = a.cu[b];
     if (i >= a.cu[b + 1] - row0) return;
     const int64_t at = part_index(a, static_cast<int>(b), head, i, 0);
     float m = -INFINITY;
-    for (int s = lane; s < a.splits; s += 32) m = fmaxf(m, a.part_ml[at + s].x);
+    for (int s = lane; s < a.parts; s += 32) m = fmaxf(m, a.part_ml[at + s].x);
 #pragma unroll
     for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     const float ref = m == -INFINITY ? 0.0f : m;
     float l = 0.0f, y[D / 32] = {};
 #pragma unroll 4
-    for (int s = part; s < a.splits; s += WARPS) {
+    for (int s = part; s < a.parts; s += WARPS) {
         const float2 ml = a.part_ml[at + s];
         const float f = fast_exp2(ml.x - ref);                   // 0 for a piece without keys, whose output and denominator are 0
         l = fmaf(ml.y, f, l);
@@ -71,36 +78,39 @@ __global__ void __launch_bounds__(128) kv_combine_kernel(AttnArgs a) {
 }
 
 template <typename T, int D>
-cudaError_t combine_dim(const AttnArgs& a, cudaStream_t s) {
-    const int64_t rows = static_cast<int64_t>(a.batch) * a.heads * a.max_q;
-    if (a.splits >= COMBINE_SPLITS && rows <= 0x7FFFFFFF) return launch_dependent(kv_combine_kernel<T, D, 4>, dim3(static_cast<unsigned>(rows)), dim3(128), 0, s, a);
+cudaError_t combine_dim(const AttnArgs& a, int64_t units, cudaStream_t s) {
+    const int64_t rows = units * a.heads * a.max_q;
+    if (a.parts >= COMBINE_SPLITS && rows <= 0x7FFFFFFF) return launch_dependent(kv_combine_kernel<T, D, 4>, dim3(static_cast<unsigned>(rows)), dim3(128), 0, s, a);
     return launch_dependent(kv_combine_kernel<T, D, 1>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(128), 0, s, a);
 }
 template <typename T>
-cudaError_t combine_as(const AttnArgs& a, cudaStream_t s) {
-    if (a.c.head_dim == 64) return combine_dim<T, 64>(a, s);
-    if (a.c.head_dim == 128) return combine_dim<T, 128>(a, s);
-    return combine_dim<T, 256>(a, s);
+cudaError_t combine_as(const AttnArgs& a, int64_t units, cudaStream_t s) {
+    if (a.c.head_dim == 64) return combine_dim<T, 64>(a, units, s);
+    if (a.c.head_dim == 128) return combine_dim<T, 128>(a, units, s);
+    return combine_dim<T, 256>(a, units, s);
+}
+sqap_status combine(const AttnArgs& a, int64_t units, int dtype, cudaStream_t s) {
+    return finish_launch(dtype == SQAP_FP16 ? combine_as<__half>(a, units, s) : combine_as<__nv_bfloat16>(a, units, s));
 }
 
 struct Plan {
     bool decode;
     int tiles, splits, chunk;
 };
-// From the sizes (and the device) alone, so that the workspace can be asked for ahead. Decode: up to 1024 keys a history is cut only where there
+// From the sizes (and the device) alone, so that the workspace can be asked for ahead: `units` sequences (or groups) of `rows` rows that look
+// at up to max_len keys each. Decode: up to 1024 keys a history is cut only where there
 // are fewer than three CTAs to an SM, beyond that to four, and to sixteen as long as pieces keep 1024 keys (uneven histories then even
 // out). Measured, us, with four / eight / sixteen CTAs to an SM, uneven histories of up to so many keys: 32 x 16384, 8 heads 132 / 147 / 127;
 // 32 x 8192, 32 heads 258 / 232 / 219; 32 x 4096, 32 heads 147 / 135 / 131, 8 heads 48 / 48 / 48; 16 x 2048, 32 heads 51.5 / 51.1 / 51.3; but
 // one of 32768, 32 heads 42 / 57 / 57 (8 heads 21 all three). Three / four up to 1024 keys: 16 x 290, 32 heads 11.7 / 15.2, 16 x 1000 27.0 / 31.5.
 // Prompts: two rounds of CTAs where there is less than one, in pieces of 1024 keys at least: cut / whole, us, 256 rows (8 heads, groups of
 // 4) behind 3000 keys 44 / 63, behind 8000 76 / 114; 288 rows behind 4096 (32 heads) 59 / 62.
-Plan plan_for(int64_t batch, int kv_heads, int group, int head_dim, int64_t max_q, int64_t max_len) {
+Plan plan_rows(int64_t units, int kv_heads, int head_dim, int64_t rows, int64_t max_len, bool decode) {
     Plan p;
-    const int64_t rows = max_q * group;
-    p.decode = rows <= decode_max_rows(head_dim);
-    const int per_tile = head_dim <= 128 ? PREFILL_TC_ROWS : PREFILL_ROWS;
-    p.tiles = p.decode ? 1 : static_cast<int>((rows + per_tile - 1) / per_tile);
-    const int64_t ctas = size_product(batch, kv_heads, p.tiles);
+    p.decode = decode;
+    const int per_tile = p.decode ? decode_max_rows(head_dim) : head_dim <= 128 ? PREFILL_TC_ROWS : PREFILL_ROWS;
+    p.tiles = static_cast<int>((rows + per_tile - 1) / per_tile);
+    const int64_t ctas = size_product(units, kv_heads, p.tiles);
     const int64_t sms = sm_count();
     auto pieces = [&](int per_sm) { return ctas > 0 ? (sms * per_sm + ctas - 1) / ctas : 1; };
     auto least = [](int64_t x, int64_t y) { return x < y ? x : y; };
@@ -118,36 +128,85 @@ Plan plan_for(int64_t batch, int kv_heads, int group, int head_dim, int64_t max_
     if (p.splits < 1) p.splits = 1;
     return p;
 }
+Plan plan_for(int64_t batch, int kv_heads, int group, int head_dim, int64_t max_q, int64_t max_len) {
+    const int64_t rows = max_q * group;
+    return plan_rows(batch, kv_heads, head_dim, rows, max_len, rows <= decode_max_rows(head_dim));
+}
 // What the kernels' 32-bit indexes hold.
 bool sizes_fit(int batch, int kv_heads, int heads, int max_q, int max_len) {
     return size_product(max_q, heads / kv_heads) <= 1 << 30 && max_len <= 1 << 30 && size_product(batch, heads, max_q) <= 4ll * 0x7FFFFFFF;
 }
-bool grid_fits(int batch, int kv_heads, const Plan& p) { return size_product(batch, kv_heads, p.splits, p.tiles) <= 0x7FFFFFFF; }
-size_t part_bytes(int64_t batch, int heads, int64_t max_q, int head_dim, const Plan& p) {
-    if (p.splits <= 1) return 0;
-    const size_t parts = static_cast<size_t>(batch) * heads * max_q * p.splits;
-    return parts * (static_cast<size_t>(head_dim) * 4 + 8);
+bool grid_fits(int64_t units, int kv_heads, const Plan& p) { return size_product(units, kv_heads, p.splits, p.tiles) <= 0x7FFFFFFF; }
+size_t part_bytes(int64_t batch, int heads, int64_t max_q, int head_dim, int parts) {
+    if (parts <= 1) return 0;
+    return static_cast<size_t>(batch) * heads * max_q * parts * (static_cast<size_t>(head_dim) * 4 + 8);
+}
+
+// Keys that the rows of a CTA look at, at most: a window for the first of its queries, on to the last, the sinks, and both rounded to tiles.
+int64_t window_keys(int64_t max_q, int64_t max_len, int group, int head_dim, int64_t window, int64_t sinks) {
+    const int64_t rows = max_q * group, tile = head_dim <= 128 ? PREFILL_TC_ROWS : PREFILL_ROWS;
+    const int64_t queries = rows <= decode_max_rows(head_dim) || max_q < tile / group + 2 ? max_q : tile / group + 2;
+    const int64_t keys = window + queries + sinks + 128;
+    return keys < max_len ? keys : max_len;
+}
+Plan plan_window(int64_t batch, int kv_heads, int group, int head_dim, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks) {
+    const int64_t rows = max_q * group;
+    return plan_rows(batch, kv_heads, head_dim, rows, window_keys(max_q, max_len, group, head_dim, window, sinks), rows <= decode_max_rows(head_dim));
+}
+
+// Shared prefixes: the rows of a group over its prefix, then those of each sequence over its own tokens. The pieces of both are cut on
+// the device, from the lengths that it finds; the plan only says how many there are.
+struct SharedPlan {
+    Plan prefix, own;
+    int prefix_parts;      // 0: there is no prefix
+    int parts;
+};
+// Row tiles of a group up to which the register kernel takes the prefix.
+constexpr int PREFIX_DECODE_TILES = 3;
+SharedPlan plan_shared(int kv_heads, int group, int head_dim, int64_t max_q, int64_t max_len, int64_t groups, int64_t max_group,
+                       int64_t max_prefix) {
+    SharedPlan p;
+    const int64_t rows = max_q * group, together = rows * max_group;
+    const int64_t own = max_len > max_prefix ? max_len - max_prefix : 1;
+    p.own = plan_rows(size_product(groups, max_group), kv_heads, head_dim, rows, own, rows <= decode_max_rows(head_dim));
+    p.prefix = plan_rows(groups, kv_heads, head_dim, together, max_prefix, together <= PREFIX_DECODE_TILES * decode_max_rows(head_dim));
+    p.prefix_parts = max_prefix > 0 ? p.prefix.splits : 0;
+    p.parts = p.prefix_parts + p.own.splits;
+    return p;
+}
+bool shared_fits(const sqap_kv_cache* c, int groups, int max_group, int max_q, int heads, const SharedPlan& p) {
+    return size_product(max_group, max_q, heads / c->kv_heads) <= 1 << 30 && grid_fits(groups, c->kv_heads, p.prefix) &&
+           grid_fits(size_product(groups, max_group), c->kv_heads, p.own) && size_product(groups, max_group, heads, max_q) <= 4ll * 0x7FFFFFFF;
+}
+
+sqap_status take_workspace(AttnArgs& a, int parts, void* workspace, size_t workspace_bytes) {
+    a.parts = parts;
+    const size_t need = part_bytes(a.batch, a.heads, a.max_q, a.c.head_dim, parts);
+    if (need == 0) return SQAP_OK;
+    if (!workspace) return SQAP_ERR_INVALID;
+    if (!aligned16(workspace)) return SQAP_ERR_ALIGN;
+    if (workspace_bytes < need) return SQAP_ERR_NOMEM;
+    a.part_o = static_cast<float*>(workspace);
+    a.part_ml = reinterpret_cast<float2*>(a.part_o + static_cast<int64_t>(a.batch) * a.heads * a.max_q * parts * a.c.head_dim);
+    return SQAP_OK;
+}
+sqap_status launch(AttnArgs a, const Plan& p, View view, int64_t units, int type, int dtype, cudaStream_t s) {
+    a.splits = p.splits;
+    a.chunk = p.chunk;
+    a.tiles = p.tiles;
+    if (p.decode) return launch_kv_decode(a, view, units, type, dtype, s);
+    if (a.c.head_dim <= 128) return launch_kv_prefill_tc(a, view, units, type, dtype, s);
+    return launch_kv_prefill(a, view, units, type, dtype, s);
 }
 
 }  // namespace
-}  // namespace kv
-}  // namespace sqap
 
-extern "C" size_t sqap_kv_attention_workspace_bytes(const sqap_kv_cache* cache, int batch, int max_q, int max_len, int heads) {
-    using namespace sqap::kv;
-    if (check_cache(cache) != SQAP_OK || batch <= 0 || max_q <= 0 || max_len < 0 || heads <= 0 || heads % cache->kv_heads != 0) return 0;
-    if (!sizes_fit(batch, cache->kv_heads, heads, max_q, max_len)) return 0;
-    const Plan p = plan_for(batch, cache->kv_heads, heads / cache->kv_heads, cache->head_dim, max_q, max_len);
-    return grid_fits(batch, cache->kv_heads, p) ? part_bytes(batch, heads, max_q, cache->head_dim, p) : 0;
-}
-
-extern "C" sqap_status sqap_kv_attention(const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int batch, const int32_t* lens,
-                                         const int32_t* cu_q, int max_q, int max_len, const void* q, int64_t ldq, int heads, float scale,
-                                         uint32_t flags, void* out, int64_t ldo, float* lse, int dtype, void* workspace,
-                                         size_t workspace_bytes, void* stream) {
-    using namespace sqap;
-    using namespace sqap::kv;
-    sqap_status st = check_cache(cache);
+// What the attention calls have in common: checks, and the arguments of the kernels but for the plan. `work`: there is something to do.
+sqap_status begin_attention(AttnArgs& a, bool& work, const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int batch, const int32_t* lens,
+                       const int32_t* cu_q, int max_q, int max_len, const void* q, int64_t ldq, int heads, float scale, uint32_t flags,
+                       void* out, int64_t ldo, float* lse, int dtype) {
+    work = false;
+    const sqap_status st = check_cache(cache);
     if (st != SQAP_OK) return st;
     if (batch < 0 || max_q < 0 || max_len < 0 || ldt < 0 || ldt > 0x7FFFFFFF || heads <= 0 || !row_type(dtype)) return SQAP_ERR_INVALID;
     if (flags & ~SQAP_KV_CAUSAL) return SQAP_ERR_INVALID;
@@ -158,18 +217,10 @@ extern "C" sqap_status sqap_kv_attention(const sqap_kv_cache* cache, const int32
     if (batch == 0 || max_q == 0) return SQAP_OK;
     if (!lens || !cu_q || !q || !out || (ldt > 0 && !table)) return SQAP_ERR_INVALID;
     if (!aligned16(q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return SQAP_ERR_ALIGN;
-    AttnArgs a;
+    if (!sizes_fit(batch, cache->kv_heads, heads, max_q, max_len)) return SQAP_ERR_UNSUPPORTED;
+    a = {};
     a.c = device_view(cache);
     a.group = heads / cache->kv_heads;
-    if (!sizes_fit(batch, cache->kv_heads, heads, max_q, max_len)) return SQAP_ERR_UNSUPPORTED;
-    const Plan p = plan_for(batch, cache->kv_heads, a.group, cache->head_dim, max_q, max_len);
-    if (!grid_fits(batch, cache->kv_heads, p)) return SQAP_ERR_UNSUPPORTED;
-    const size_t need = part_bytes(batch, heads, max_q, cache->head_dim, p);
-    if (need > 0) {
-        if (!workspace) return SQAP_ERR_INVALID;
-        if (!aligned16(workspace)) return SQAP_ERR_ALIGN;
-        if (workspace_bytes < need) return SQAP_ERR_NOMEM;
-    }
     a.table = table;
     a.ldt = ldt;
     a.batch = batch;
@@ -185,16 +236,122 @@ extern "C" sqap_status sqap_kv_attention(const sqap_kv_cache* cache, const int32
     a.out = out;
     a.ldo = ldo;
     a.lse = lse;
-    a.splits = p.splits;
-    a.chunk = p.chunk;
-    a.tiles = p.tiles;
-    const int64_t parts = static_cast<int64_t>(batch) * heads * max_q * p.splits;
-    a.part_o = static_cast<float*>(workspace);
-    a.part_ml = p.splits > 1 ? reinterpret_cast<float2*>(a.part_o + parts * cache->head_dim) : nullptr;
+    work = true;
+    return SQAP_OK;
+}
+sqap_status run_attention(const AttnArgs& args, int type, int dtype, void* workspace, size_t workspace_bytes, cudaStream_t s) {
+    AttnArgs a = args;
+    const Plan p = plan_for(a.batch, a.c.kv_heads, a.group, a.c.head_dim, a.max_q, a.max_len);
+    if (!grid_fits(a.batch, a.c.kv_heads, p)) return SQAP_ERR_UNSUPPORTED;
+    sqap_status st = take_workspace(a, p.splits, workspace, workspace_bytes);
+    if (st != SQAP_OK) return st;
+    st = launch(a, p, VIEW_ALL, a.batch, type, dtype, s);
+    if (st != SQAP_OK || a.parts <= 1) return st;
+    return combine(a, a.batch, dtype, s);
+}
+}  // namespace kv
+}  // namespace sqap
+
+extern "C" size_t sqap_kv_attention_workspace_bytes(const sqap_kv_cache* cache, int batch, int max_q, int max_len, int heads) {
+    using namespace sqap::kv;
+    if (check_cache(cache) != SQAP_OK || batch <= 0 || max_q <= 0 || max_len < 0 || heads <= 0 || heads % cache->kv_heads != 0) return 0;
+    if (!sizes_fit(batch, cache->kv_heads, heads, max_q, max_len)) return 0;
+    const Plan p = plan_for(batch, cache->kv_heads, heads / cache->kv_heads, cache->head_dim, max_q, max_len);
+    return grid_fits(batch, cache->kv_heads, p) ? part_bytes(batch, heads, max_q, cache->head_dim, p.splits) : 0;
+}
+
+extern "C" sqap_status sqap_kv_attention(const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int batch, const int32_t* lens,
+                                         const int32_t* cu_q, int max_q, int max_len, const void* q, int64_t ldq, int heads, float scale,
+                                         uint32_t flags, void* out, int64_t ldo, float* lse, int dtype, void* workspace,
+                                         size_t workspace_bytes, void* stream) {
+    using namespace sqap;
+    using namespace sqap::kv;
+    AttnArgs a;
+    bool work;
+    const sqap_status st = begin_attention(a, work, cache, table, ldt, batch, lens, cu_q, max_q, max_len, q, ldq, heads, scale, flags, out, ldo, lse, dtype);
+    if (st != SQAP_OK || !work) return st;
+    return run_attention(a, cache->type, dtype, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" size_t sqap_kv_attention_window_workspace_bytes(const sqap_kv_cache* cache, int batch, int max_q, int max_len, int heads,
+                                                           int window, int sinks) {
+    using namespace sqap::kv;
+    if (check_cache(cache) != SQAP_OK || batch <= 0 || max_q <= 0 || max_len < 0 || heads <= 0 || heads % cache->kv_heads != 0) return 0;
+    if (window <= 0 || sinks < 0 || !sizes_fit(batch, cache->kv_heads, heads, max_q, max_len)) return 0;
+    const Plan p = plan_window(batch, cache->kv_heads, heads / cache->kv_heads, cache->head_dim, max_q, max_len, window, sinks);
+    return grid_fits(batch, cache->kv_heads, p) ? part_bytes(batch, heads, max_q, cache->head_dim, p.splits) : 0;
+}
+
+extern "C" sqap_status sqap_kv_attention_window(const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int batch, const int32_t* lens,
+                                                const int32_t* cu_q, int max_q, int max_len, const void* q, int64_t ldq, int heads,
+                                                float scale, int window, int sinks, void* out, int64_t ldo, float* lse, int dtype,
+                                                void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace sqap;
+    using namespace sqap::kv;
+    AttnArgs a;
+    bool work;
+    sqap_status st = begin_attention(a, work, cache, table, ldt, batch, lens, cu_q, max_q, max_len, q, ldq, heads, scale, SQAP_KV_CAUSAL, out, ldo, lse, dtype);
+    if (st != SQAP_OK) return st;
+    if (window <= 0 || sinks < 0) return SQAP_ERR_INVALID;
+    if (!work) return SQAP_OK;
+    const Plan p = plan_window(batch, cache->kv_heads, a.group, cache->head_dim, max_q, max_len, window, sinks);
+    if (!grid_fits(batch, cache->kv_heads, p)) return SQAP_ERR_UNSUPPORTED;
+    st = take_workspace(a, p.splits, workspace, workspace_bytes);
+    if (st != SQAP_OK) return st;
+    a.window = window;
+    a.sinks = sinks < max_len ? sinks : max_len;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (p.decode) st = launch_kv_decode(a, cache->type, dtype, s);
-    else if (cache->head_dim <= 128) st = launch_kv_prefill_tc(a, cache->type, dtype, s);
-    else st = launch_kv_prefill(a, cache->type, dtype, s);
-    if (st != SQAP_OK || p.splits <= 1) return st;
-    return finish_launch(dtype == SQAP_FP16 ? combine_as<__half>(a, s) : combine_as<__nv_bfloat16>(a, s));
+    st = launch(a, p, VIEW_WINDOW, batch, cache->type, dtype, s);
+    if (st != SQAP_OK || a.parts <= 1) return st;
+    return combine(a, batch, dtype, s);
+}
+
+extern "C" size_t sqap_kv_attention_shared_workspace_bytes(const sqap_kv_cache* cache, int batch, int max_q, int max_len, int groups,
+                                                           int max_group, int max_prefix, int heads) {
+    using namespace sqap::kv;
+    if (check_cache(cache) != SQAP_OK || batch <= 0 || max_q <= 0 || max_len < 0 || heads <= 0 || heads % cache->kv_heads != 0) return 0;
+    if (groups <= 0 || max_group <= 0 || max_prefix < 0 || !sizes_fit(batch, cache->kv_heads, heads, max_q, max_len)) return 0;
+    if (size_product(max_group, max_q, heads / cache->kv_heads) > 1 << 30) return 0;
+    const SharedPlan p = plan_shared(cache->kv_heads, heads / cache->kv_heads, cache->head_dim, max_q, max_len, groups, max_group,
+                                     max_prefix < max_len ? max_prefix : max_len);
+    return shared_fits(cache, groups, max_group, max_q, heads, p) ? part_bytes(batch, heads, max_q, cache->head_dim, p.parts) : 0;
+}
+
+extern "C" sqap_status sqap_kv_attention_shared(const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int batch, const int32_t* lens,
+                                                const int32_t* cu_q, int max_q, int max_len, const int32_t* cu_group, int groups,
+                                                int max_group, const int32_t* prefix, int max_prefix, const void* q, int64_t ldq, int heads,
+                                                float scale, uint32_t flags, void* out, int64_t ldo, float* lse, int dtype,
+                                                void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace sqap;
+    using namespace sqap::kv;
+    AttnArgs a;
+    bool work;
+    sqap_status st = begin_attention(a, work, cache, table, ldt, batch, lens, cu_q, max_q, max_len, q, ldq, heads, scale, flags, out, ldo, lse, dtype);
+    if (st != SQAP_OK) return st;
+    if (groups < 0 || max_group < 0 || max_prefix < 0) return SQAP_ERR_INVALID;
+    if (!work || groups == 0 || max_group == 0) return SQAP_OK;
+    if (!cu_group || !prefix) return SQAP_ERR_INVALID;
+    if ((reinterpret_cast<uintptr_t>(cu_group) & 3u) || (reinterpret_cast<uintptr_t>(prefix) & 3u)) return SQAP_ERR_ALIGN;
+    if (size_product(max_group, max_q, a.group) > 1 << 30) return SQAP_ERR_UNSUPPORTED;
+    max_prefix = max_prefix < max_len ? max_prefix : max_len;
+    const SharedPlan p = plan_shared(cache->kv_heads, a.group, cache->head_dim, max_q, max_len, groups, max_group, max_prefix);
+    if (!shared_fits(cache, groups, max_group, max_q, heads, p)) return SQAP_ERR_UNSUPPORTED;
+    st = take_workspace(a, p.parts, workspace, workspace_bytes);
+    if (st != SQAP_OK) return st;
+    a.cu_group = cu_group;
+    a.prefix = prefix;
+    a.groups = groups;
+    a.max_group = max_group;
+    a.max_prefix = max_prefix;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int64_t places = static_cast<int64_t>(groups) * max_group;
+    if (p.prefix_parts > 0) {
+        st = launch(a, p.prefix, VIEW_PREFIX, groups, cache->type, dtype, s);
+        if (st != SQAP_OK) return st;
+    }
+    a.part0 = p.prefix_parts;
+    st = launch(a, p.own, VIEW_OWN, places, cache->type, dtype, s);
+    if (st != SQAP_OK || a.parts <= 1) return st;
+    a.part0 = 0;
+    return combine(a, places, dtype, s);
 }

@@ -33,16 +33,28 @@ struct AttnArgs {
     int64_t ldo;
     float* lse;            // [rows][heads] or null
     int splits, chunk;     // a history is cut into `splits` pieces of `chunk` keys, or one
-    float* part_o;         // [batch][heads][max_q][splits][D]
+    float* part_o;         // [batch][heads][max_q][parts][D]
     float2* part_ml;       // the same without D: maximum and denominator
     int tiles;             // row tiles per (sequence, key/value head)
+    int parts, part0;      // pieces of a row that are joined (1: the kernel writes the output itself), and the first of this launch
+    // views other than VIEW_ALL
+    int window, sinks;     // VIEW_WINDOW
+    const int32_t* cu_group;   // VIEW_PREFIX, VIEW_OWN: sequences of the groups
+    const int32_t* prefix;
+    int groups, max_group, max_prefix;
 };
+
+// What the rows of a launch look at: all (causal or not); the tokens of a window and the first ones; the prefix that the
+// sequences of a group share, rows of all of them together; the tokens of a sequence behind its group's prefix.
+enum View { VIEW_ALL, VIEW_WINDOW, VIEW_PREFIX, VIEW_OWN };
 
 // Work of a CTA, from its index.
 struct Where {
     int b, h, split, tile;
     int row0, n_q;         // first row of the sequence, its query rows
     int tokens, len;       // its tokens, and how many of them are looked at (max_len at most)
+    int prefix;            // VIEW_PREFIX, VIEW_OWN: shared tokens
+    int members;           // VIEW_PREFIX: sequences of the group, from b on
 };
 __device__ __forceinline__ Where locate(const AttnArgs& a, unsigned id, int tiles) {
     Where w;
@@ -71,8 +83,120 @@ __device__ __forceinline__ int visible(const AttnArgs& a, const Where& w, int i)
     const int64_t n = static_cast<int64_t>(w.tokens) - w.n_q + i + 1;
     return n < 0 ? 0 : static_cast<int>(min(n, static_cast<int64_t>(w.len)));
 }
+// The same for the views that go by groups. `tiles` row tiles innermost, then pieces, heads, and (VIEW_OWN) the sequences of a group.
+// A sequence or group that is not there has no rows.
+template <int VIEW>
+__device__ __forceinline__ Where locate_view(const AttnArgs& a, unsigned id, int tiles) {
+    if constexpr (VIEW != VIEW_PREFIX && VIEW != VIEW_OWN) return locate(a, id, tiles);
+    Where w = {};
+    if (tiles > 1) {
+        w.tile = static_cast<int>(id % tiles);
+        id /= tiles;
+    }
+    if (a.splits > 1) {
+        w.split = static_cast<int>(id % a.splits);
+        id /= a.splits;
+    }
+    w.h = static_cast<int>(id % a.c.kv_heads);
+    id /= a.c.kv_heads;
+    int member = 0;
+    if (VIEW == VIEW_OWN) {
+        member = static_cast<int>(id % a.max_group);
+        id /= a.max_group;
+    }
+    const int first = a.cu_group[id], last = min(a.cu_group[id + 1], a.batch);
+    w.b = first + member;
+    w.prefix = max(0, min(a.prefix[id], min(a.max_prefix, a.max_len)));
+    if (first < 0 || w.b >= last) return w;
+    w.members = min(last - first, a.max_group);
+    if (VIEW == VIEW_PREFIX) return w;
+    w.row0 = a.cu[w.b];
+    w.n_q = max(a.cu[w.b + 1] - w.row0, 0);
+    w.tokens = max(a.lens[w.b], 0);
+    w.len = min(w.tokens, a.max_len);
+    return w;
+}
+// Query rows (query x head of the group of heads) of a CTA's sequence, or of its group's sequences, max_q queries for each.
+template <int VIEW>
+__device__ __forceinline__ int rows_of(const AttnArgs& a, const Where& w) {
+    if constexpr (VIEW == VIEW_PREFIX) return w.members * a.max_q * a.group;
+    return (w.n_q < a.max_q ? w.n_q : a.max_q) * a.group;
+}
+// Row r of them.
+struct Row {
+    int b, i, head;        // sequence, query, head
+    int64_t at;            // row of q and out
+    int sees;              // keys that it may look at, 0 for a row that is not there
+    bool real;
+};
+template <int VIEW>
+__device__ __forceinline__ Row row_at(const AttnArgs& a, const Where& w, int rows, int r) {
+    Row x;
+    x.real = r < rows;
+    if (!x.real) r = 0;
+    x.b = w.b;
+    if constexpr (VIEW == VIEW_PREFIX) {
+        const int per = a.max_q * a.group, member = r / per;
+        r -= member * per;
+        x.b += member;
+    }
+    x.i = r / a.group;
+    x.head = w.h * a.group + r - x.i * a.group;
+    if constexpr (VIEW == VIEW_PREFIX) {
+        x.at = 0;
+        x.sees = 0;
+        if (x.real) {
+            const int row0 = a.cu[x.b], n = a.cu[x.b + 1] - row0;
+            x.real = x.i < n;
+            x.at = static_cast<int64_t>(row0) + (x.real ? x.i : 0);
+            Where own = w;
+            own.n_q = n;
+            own.tokens = max(a.lens[x.b], 0);
+            own.len = min(own.tokens, w.prefix);
+            x.sees = x.real ? visible(a, own, x.i) : 0;
+        }
+    } else {
+        x.at = static_cast<int64_t>(w.row0) + x.i;
+        x.sees = x.real ? visible(a, w, x.i) : 0;
+    }
+    return x;
+}
+// First token that query i sees, the sinks apart.
+template <int VIEW>
+__device__ __forceinline__ int first_seen(const AttnArgs& a, const Where& w, int i) {
+    if constexpr (VIEW == VIEW_OWN) return w.prefix;
+    if constexpr (VIEW == VIEW_WINDOW) {
+        const int behind = w.tokens - w.n_q + i + 1;         // the place behind the query's; negative where there are more queries than tokens
+        return behind > a.window ? behind - a.window : 0;
+    }
+    return 0;
+}
+// The keys that rows from query i0 on look at, without those between the sinks and the first that i0 sees: key u of them is token
+// u where u < stop, else u + gap. Both are multiples of ALIGN.
+struct Span {
+    int stop, gap;
+    __device__ __forceinline__ int token(int u) const { return u < stop ? u : u + gap; }
+};
+template <int VIEW, int ALIGN>
+__device__ __forceinline__ Span span_of(const AttnArgs& a, const Where& w, int i0) {
+    Span s = {0, 0};
+    if constexpr (VIEW == VIEW_WINDOW || VIEW == VIEW_OWN) {
+        const int low = first_seen<VIEW>(a, w, i0);
+        if (VIEW == VIEW_WINDOW) s.stop = (min(a.sinks, low) + ALIGN - 1) / ALIGN * ALIGN;
+        s.gap = max(0, low / ALIGN * ALIGN - s.stop);
+    }
+    return s;
+}
+
+// Keys of a piece of a history of `len` keys: of the same size for all, or (by groups) as even as tiles of 64 allow.
+template <int VIEW>
+__device__ __forceinline__ int chunk_of(const AttnArgs& a, int len) {
+    if constexpr (VIEW == VIEW_PREFIX || VIEW == VIEW_OWN) return a.splits > 1 && len > 0 ? ((len - 1) / a.splits / 64 + 1) * 64 : 64;
+    return a.chunk;
+}
+
 __device__ __forceinline__ int64_t part_index(const AttnArgs& a, int b, int head, int i, int split) {
-    return ((static_cast<int64_t>(b) * a.heads + head) * a.max_q + i) * a.splits + split;
+    return ((static_cast<int64_t>(b) * a.heads + head) * a.max_q + i) * a.parts + a.part0 + split;
 }
 // Largest power of two not above 2^9 / amax, so that amax lands in [2^8, 2^9): rows of bf16 then fit fp16 with 22 binary
 // orders below their largest element, more than an fp32 sum resolves.
@@ -120,10 +244,22 @@ __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 x) { return _
 // 9 to 16 rows, 8 heads of 128: 100 keys 8.3 / 9.4, 500 keys 14.7 / 16.1, 2048 keys 31 / 44, 32 sequences of 16384 182 / 526, 64 of 290
 // 21 / 34. The other sign only where 128 CTAs walk some 290 keys in one round, 14.2 / 12.6, which no rule of its own was made for.
 inline int decode_max_rows(int head_dim) { return head_dim == 256 ? 8 : 16; }
+// Rows of a CTA of the register kernel: all of its sequence, or a tile of its group's.
+inline int decode_row_tile(const AttnArgs& a, int view, int head_dim) {
+    const int64_t rows = static_cast<int64_t>(a.max_q) * a.group * (view == VIEW_PREFIX ? a.max_group : 1);
+    return rows > 8 && head_dim != 256 ? 16 : 8;
+}
 constexpr int PREFILL_ROWS = 128, PREFILL_TC_ROWS = 256;   // query rows of a CTA's item
-sqap_status launch_kv_decode(const AttnArgs& a, int type, int dtype, cudaStream_t s);
-sqap_status launch_kv_prefill_tc(const AttnArgs& a, int type, int dtype, cudaStream_t s);
-sqap_status launch_kv_prefill(const AttnArgs& a, int type, int dtype, cudaStream_t s);
+// `units`: what a launch goes over, sequences, groups (VIEW_PREFIX) or places of sequences in groups (VIEW_OWN).
+sqap_status launch_kv_decode(const AttnArgs& a, View view, int64_t units, int type, int dtype, cudaStream_t s);
+sqap_status launch_kv_prefill_tc(const AttnArgs& a, View view, int64_t units, int type, int dtype, cudaStream_t s);
+sqap_status launch_kv_prefill(const AttnArgs& a, View view, int64_t units, int type, int dtype, cudaStream_t s);
+
+// The checks and arguments of sqap_kv_attention (kv_attention.cu), `work`: there is something to compute; and the rest of it.
+sqap_status begin_attention(AttnArgs& a, bool& work, const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int batch,
+                            const int32_t* lens, const int32_t* cu_q, int max_q, int max_len, const void* q, int64_t ldq, int heads,
+                            float scale, uint32_t flags, void* out, int64_t ldo, float* lse, int dtype);
+sqap_status run_attention(const AttnArgs& args, int type, int dtype, void* workspace, size_t workspace_bytes, cudaStream_t s);
 
 }  // namespace kv
 }  // namespace sqap

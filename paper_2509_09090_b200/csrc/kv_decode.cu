@@ -64,7 +64,7 @@ __device__ __forceinline__ void word_to_half2x2(uint32_t w, uint32_t* lo, uint32
     }
 }
 
-template <typename T, int TYPE, int D, int NT, int GROUPS>
+template <typename T, int TYPE, int D, int NT, int GROUPS, int VIEW>
 __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1 ? 4 : 1) kv_decode_kernel(AttnArgs a) {
     constexpr int STEP = 16 * GROUPS;
     constexpr int KC = D / 64;                     // 16-byte chunks of a key row per lane
@@ -75,32 +75,37 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
 
     pdl_launch_dependents();
     pdl_wait();
-    const Where w = locate(a, blockIdx.x, 1);
+    const Where w = locate_view<VIEW>(a, blockIdx.x, VIEW == VIEW_PREFIX ? a.tiles : 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int G = a.group;
-    const int nq = w.n_q < a.max_q ? w.n_q : a.max_q;
-    const int rows = nq * G;                       // row r: query r / G, head h G + r % G
-    if (rows == 0) return;
-    const int key0 = w.split * a.chunk;
-    const int key1 = a.splits > 1 ? min(key0 + a.chunk, w.len) : w.len;
+    const int rows_all = rows_of<VIEW>(a, w);      // row r: query r / G, head h G + r % G
+    const int r_first = VIEW == VIEW_PREFIX ? w.tile * 8 * NT : 0;
+    const int rows = VIEW == VIEW_PREFIX ? min(rows_all - r_first, 8 * NT) : rows_all;
+    if (rows <= 0) return;
+    const Span span = span_of<VIEW, STEP>(a, w, 0);
+    const int len = (VIEW == VIEW_PREFIX ? w.prefix : w.len) - span.gap;
+    const int chunk = chunk_of<VIEW>(a, len);
+    const int key0 = w.split * chunk;              // keys: tokens without the gap
+    const int key1 = a.splits > 1 ? min(key0 + chunk, len) : len;
 
     // the queries as B operands, scaled row by row to fit fp16
     uint32_t qf[NT][KC][4][2];
     float fac[NT][2];                              // back-scaling of the rows of this lane's columns (2t, 2t + 1)
-    int lim[NT][2];                                // keys that those rows may see
+    int lim[NT][2], low[NT][2];                    // tokens that those rows may see: below lim, and from low on or below a.sinks
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int r = 8 * n + g;
-        const bool real = r < rows;
-        const T* src = static_cast<const T*>(a.q) + (static_cast<int64_t>(w.row0) + (real ? r / G : 0)) * a.ldq +
-                       static_cast<int64_t>(w.h * G + (real ? r % G : 0)) * D;
+        const Row row = row_at<VIEW>(a, w, rows_all, r_first + 8 * n + g);
+        const bool real = row.real;
+        const T* src = static_cast<const T*>(a.q) + row.at * a.ldq + static_cast<int64_t>(row.head) * D;
         float v[KC][16];
         float amax = 0.0f;
 #pragma unroll
         for (int c = 0; c < KC; ++c) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                unpack8<T>(__ldg(reinterpret_cast<const uint4*>(src + 64 * c + 16 * t) + i), v[c] + 8 * i);
+                uint4 u = make_uint4(0, 0, 0, 0);
+                if (VIEW != VIEW_PREFIX || real) u = __ldg(reinterpret_cast<const uint4*>(src + 64 * c + 16 * t) + i);
+                unpack8<T>(u, v[c] + 8 * i);
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -123,11 +128,13 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             fac[n][e] = __shfl_sync(0xffffffffu, back, (2 * t + e) * 4) * a.scale_log2;
-            const int rr = 8 * n + 2 * t + e;
-            lim[n][e] = rr < rows ? visible(a, w, rr / G) : 0;
+            const Row seen_by = row_at<VIEW>(a, w, rows_all, r_first + 8 * n + 2 * t + e);
+            lim[n][e] = seen_by.sees;
+            low[n][e] = first_seen<VIEW>(a, w, seen_by.i);
         }
     }
-    const int lim_max = visible(a, w, nq - 1);     // the last row sees the most
+    // the last row sees the most
+    const int lim_max = VIEW == VIEW_PREFIX ? len : visible(a, w, rows / G - 1) - span.gap;
     const int end = a.c.pages > 0 ? min(key1, lim_max) : 0;
 
     float o[NT][MT][4];
@@ -153,13 +160,13 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
     auto entries = [&](int k0) {
 #pragma unroll
         for (int u = 0; u < GROUPS; ++u) {
-            const int key = k0 + 16 * u, j = key >> shift;
+            const int key = k0 + 16 * u, j = span.token(key) >> shift;
             entry[u] = -1;
             if (key < end && j < a.ldt) entry[u] = __ldg(table + j);
         }
     };
     // a page that does not exist is read as page 0 and masked
-    auto token_at = [&](int k0, int u) { return page_codes(a.c, max(page[u], 0), w.h) + ((k0 + 16 * u) & mask); };
+    auto token_at = [&](int k0, int u) { return page_codes(a.c, max(page[u], 0), w.h) + (span.token(k0 + 16 * u) & mask); };
     auto load_keys = [&](int k0) {
 #pragma unroll
         for (int u = 0; u < GROUPS; ++u) {
@@ -250,7 +257,14 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int key = base + g + (e >> 1) * 8;
-                    const bool seen = there[u] && key < min(lim[n][e & 1], end);
+                    bool seen;
+                    if (VIEW == VIEW_ALL) {
+                        seen = there[u] && key < min(lim[n][e & 1], end);
+                    } else {
+                        const int token = span.token(base) + g + (e >> 1) * 8;
+                        seen = there[u] && key < end && token < lim[n][e & 1];
+                        if (VIEW != VIEW_PREFIX) seen = seen && (token >= low[n][e & 1] || (VIEW == VIEW_WINDOW && token < a.sinks));
+                    }
                     sc[u][n][e] = seen ? fmaf(sc[u][n][e], fac[n][e & 1] * this_ks[u], lv[u]) : -INFINITY;
                     top[n][e & 1] = fmaxf(top[n][e & 1], sc[u][n][e]);
                 }
@@ -358,9 +372,10 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = fmaf(red_o[i][r][d + e], f, y[e]);
         }
-        const int i = r / G, head = w.h * G + r % G;
-        if (a.splits > 1) {
-            const int64_t at = part_index(a, w.b, head, i, w.split);
+        const Row row = row_at<VIEW>(a, w, rows_all, r_first + r);
+        if (VIEW == VIEW_PREFIX && !row.real) continue;
+        if (a.parts > 1) {
+            const int64_t at = part_index(a, row.b, row.head, row.i, w.split);
             if (d == 0) a.part_ml[at] = make_float2(mm, ll);
             float4* po = reinterpret_cast<float4*>(a.part_o + at * D + d);
             po[0] = make_float4(y[0], y[1], y[2], y[3]);
@@ -369,14 +384,13 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
             const float inv = ll != 0.0f ? 1.0f / ll : 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] *= inv;
-            const int64_t row = static_cast<int64_t>(w.row0) + i;
-            *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + row * a.ldo + static_cast<int64_t>(head) * D + d) = pack8<T>(y);
-            if (d == 0 && a.lse) a.lse[row * a.heads + head] = ll != 0.0f ? log_sum(mm, ll) : -INFINITY;
+            *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + row.at * a.ldo + static_cast<int64_t>(row.head) * D + d) = pack8<T>(y);
+            if (d == 0 && a.lse) a.lse[row.at * a.heads + row.head] = ll != 0.0f ? log_sum(mm, ll) : -INFINITY;
         }
     }
 }
 
-template <typename T, int TYPE, int D>
+template <typename T, int TYPE, int D, int VIEW>
 cudaError_t launch_rows(const AttnArgs& a, unsigned grid, cudaStream_t s) {
     // 16-token groups per step. With one group of 128 elements a fourth CTA fits an SM, at 64 elements a second group's loads in
     // flight count for more. Measured, one / two groups, us: D = 128, 16 x 290 tokens x 32 heads 11.6 / 13.5, 16 x 2048 51.6 / 53.4,
@@ -384,25 +398,34 @@ cudaError_t launch_rows(const AttnArgs& a, unsigned grid, cudaStream_t s) {
     constexpr int GROUPS = D == 64 ? 2 : 1;
     if constexpr (D != 256)                         // 8 rows at most: decode_max_rows()
         // 9 to 16 rows: one / two groups, 32 x 8192 tokens x 8 heads of 128, 12 rows, 134 / 115; 16 x 2048, 16 rows, 35 / 31.
-        if (static_cast<int64_t>(a.max_q) * a.group > 8)
-            return launch_dependent(kv_decode_kernel<T, TYPE, D, 2, 2>, dim3(grid), dim3(WARPS * 32), 0, s, a);
-    return launch_dependent(kv_decode_kernel<T, TYPE, D, 1, GROUPS>, dim3(grid), dim3(WARPS * 32), 0, s, a);
+        if (decode_row_tile(a, VIEW, D) > 8)
+            return launch_dependent(kv_decode_kernel<T, TYPE, D, 2, 2, VIEW>, dim3(grid), dim3(WARPS * 32), 0, s, a);
+    return launch_dependent(kv_decode_kernel<T, TYPE, D, 1, GROUPS, VIEW>, dim3(grid), dim3(WARPS * 32), 0, s, a);
 }
-template <typename T, int TYPE>
+template <typename T, int TYPE, int VIEW>
 cudaError_t launch_dim(const AttnArgs& a, unsigned grid, cudaStream_t s) {
-    if (a.c.head_dim == 64) return launch_rows<T, TYPE, 64>(a, grid, s);
-    if (a.c.head_dim == 128) return launch_rows<T, TYPE, 128>(a, grid, s);
-    return launch_rows<T, TYPE, 256>(a, grid, s);
+    if (a.c.head_dim == 64) return launch_rows<T, TYPE, 64, VIEW>(a, grid, s);
+    if (a.c.head_dim == 128) return launch_rows<T, TYPE, 128, VIEW>(a, grid, s);
+    return launch_rows<T, TYPE, 256, VIEW>(a, grid, s);
+}
+template <int VIEW>
+cudaError_t launch_view(const AttnArgs& a, int type, int dtype, unsigned grid, cudaStream_t s) {
+    if (dtype == SQAP_FP16)
+        return type == SQAP_KV_INT8 ? launch_dim<__half, SQAP_KV_INT8, VIEW>(a, grid, s) : launch_dim<__half, SQAP_KV_E4M3, VIEW>(a, grid, s);
+    return type == SQAP_KV_INT8 ? launch_dim<__nv_bfloat16, SQAP_KV_INT8, VIEW>(a, grid, s)
+                                : launch_dim<__nv_bfloat16, SQAP_KV_E4M3, VIEW>(a, grid, s);
 }
 
 }  // namespace
 
-sqap_status launch_kv_decode(const AttnArgs& a, int type, int dtype, cudaStream_t s) {
-    const unsigned grid = static_cast<unsigned>(static_cast<int64_t>(a.batch) * a.c.kv_heads * a.splits);
-    if (dtype == SQAP_FP16)
-        return finish_launch(type == SQAP_KV_INT8 ? launch_dim<__half, SQAP_KV_INT8>(a, grid, s) : launch_dim<__half, SQAP_KV_E4M3>(a, grid, s));
-    return finish_launch(type == SQAP_KV_INT8 ? launch_dim<__nv_bfloat16, SQAP_KV_INT8>(a, grid, s)
-                                              : launch_dim<__nv_bfloat16, SQAP_KV_E4M3>(a, grid, s));
+sqap_status launch_kv_decode(const AttnArgs& a, View view, int64_t units, int type, int dtype, cudaStream_t s) {
+    const unsigned grid = static_cast<unsigned>(units * a.c.kv_heads * a.splits * (view == VIEW_PREFIX ? a.tiles : 1));
+    switch (view) {
+        case VIEW_WINDOW: return finish_launch(launch_view<VIEW_WINDOW>(a, type, dtype, grid, s));
+        case VIEW_PREFIX: return finish_launch(launch_view<VIEW_PREFIX>(a, type, dtype, grid, s));
+        case VIEW_OWN: return finish_launch(launch_view<VIEW_OWN>(a, type, dtype, grid, s));
+        default: return finish_launch(launch_view<VIEW_ALL>(a, type, dtype, grid, s));
+    }
 }
 
 }  // namespace kv

@@ -1,0 +1,230 @@
+// Attention with the weight that each token received: the attention itself, then the scores of the rows that count once more, now with
+// their log-sum-exp, so that a weight is known as soon as its score is.
+//
+// A warp holds 16 tokens' keys of a head as the A operand (from codes in registers, as in kv_decode.cu) and goes over the
+// query rows, eight at a time, as the B operand: S[token][row], p = 2^(s scale log2 e - lse log2 e), summed over the row in the lane that
+// holds it. Codes are exact in fp16 and in bf16, so the queries enter in the type that they have. A CTA's four warps
+// take neighbouring tokens and find each other's query rows in L1; heads are shared out over CTAs where tokens are few,
+// and their sums added by a second kernel, in the order of the heads.
+#include "kv_attention.cuh"
+
+namespace sqap {
+namespace kv {
+namespace {
+
+constexpr int WARPS = 4, TOKENS = 16 * WARPS;
+
+struct MassArgs {
+    AttnArgs a;
+    int last_q;
+    const float* past;
+    float* mass;
+    int64_t ldm;
+    int tiles, parts;          // token tiles of a sequence; pieces that its heads are cut into
+    float* sums;               // [parts][batch][tiles * TOKENS], where there are several
+};
+
+template <typename T>
+__device__ __forceinline__ void mma_rows(float* d, const uint32_t* a, uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma_rows<__half>(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) { mma_16816(d, a, b0, b1); }
+template <>
+__device__ __forceinline__ void mma_rows<__nv_bfloat16>(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Four codes as two pairs of T; exact.
+template <typename T, int TYPE>
+__device__ __forceinline__ void word_to_pairs(uint32_t w, uint32_t* lo, uint32_t* hi) {
+    if (TYPE == SQAP_KV_INT8) {
+        w ^= 0x80808080u;
+        *lo = biased_to_half2<0>(w);
+        *hi = biased_to_half2<1>(w);
+    } else {
+        *lo = e4m3x2_to_half2(w & 0xFFFFu);
+        *hi = e4m3x2_to_half2(w >> 16);
+    }
+    if (!std::is_same<T, __half>::value) {
+        const float2 x = __half22float2(*reinterpret_cast<const __half2*>(lo)), y = __half22float2(*reinterpret_cast<const __half2*>(hi));
+        *lo = pack2<T>(x.x, x.y);
+        *hi = pack2<T>(y.x, y.y);
+    }
+}
+
+// The sum of a token's weights joins what it had.
+__device__ __forceinline__ void add_to_past(const MassArgs& m, int b, int token, int tokens, int n_q, float sum) {
+    const int64_t at = b * m.ldm + token;
+    if (token >= m.ldm) return;
+    m.mass[at] = (m.past && token < tokens - n_q ? m.past[at] : 0.0f) + sum;
+}
+
+template <typename T, int TYPE, int D>
+__global__ void __launch_bounds__(WARPS * 32) kv_mass_kernel(MassArgs m) {
+    constexpr int KC = D / 64;
+    pdl_launch_dependents();
+    pdl_wait();
+    const AttnArgs& a = m.a;
+    unsigned id = blockIdx.x;
+    Where w = {};
+    w.tile = static_cast<int>(id % m.tiles);
+    id /= m.tiles;
+    const int part = static_cast<int>(id % m.parts);
+    w.b = static_cast<int>(id / m.parts);
+    w.row0 = a.cu[w.b];
+    w.n_q = max(a.cu[w.b + 1] - w.row0, 0);
+    w.tokens = max(a.lens[w.b], 0);
+    w.len = min(w.tokens, a.max_len);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, G = a.group;
+    const int t0 = w.tile * TOKENS + 16 * warp;
+    if (t0 >= w.len) return;
+    const int h0 = static_cast<int>(static_cast<int64_t>(a.c.kv_heads) * part / m.parts);
+    const int h1 = static_cast<int>(static_cast<int64_t>(a.c.kv_heads) * (part + 1) / m.parts);
+    const int i0 = max(0, w.n_q - m.last_q), rows = (min(w.n_q, a.max_q) - i0) * G;
+    const int j = t0 >> a.c.page_shift;
+    const int page = a.c.pages > 0 && j < a.ldt ? checked_page(a.c, a.table[w.b * a.ldt + j]) : -1;
+    float sum[2] = {0.0f, 0.0f};
+    if (page >= 0) {
+        for (int h = h0; h < h1; ++h) {
+            const uint8_t* kp = a.c.k.codes + (page_codes(a.c, page, h) + (t0 & ((1 << a.c.page_shift) - 1)) + g) * D + 16 * t;
+            uint32_t kf[KC][4][4];
+#pragma unroll
+            for (int c = 0; c < KC; ++c) {
+                const uint4 x = __ldg(reinterpret_cast<const uint4*>(kp + 64 * c)), y = __ldg(reinterpret_cast<const uint4*>(kp + 8 * D + 64 * c));
+                const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    word_to_pairs<T, TYPE>(xs[q], &kf[c][q][0], &kf[c][q][2]);
+                    word_to_pairs<T, TYPE>(ys[q], &kf[c][q][1], &kf[c][q][3]);
+                }
+            }
+            const float fac = __ldg(a.c.k.scales + static_cast<int64_t>(page) * a.c.kv_heads + h) * a.scale_log2;
+            for (int r0 = 0; r0 < rows; r0 += 8) {
+                float sc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                const int r = r0 + g;
+                const bool real = r < rows;
+                const int i = real ? i0 + r / G : i0;
+                const T* src = static_cast<const T*>(a.q) + (static_cast<int64_t>(w.row0) + i) * a.ldq + (h * G + (real ? r % G : 0)) * D + 16 * t;
+#pragma unroll
+                for (int c = 0; c < KC; ++c)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const uint4 u = real ? __ldg(reinterpret_cast<const uint4*>(src + 64 * c) + half) : make_uint4(0, 0, 0, 0);
+                        mma_rows<T>(sc, kf[c][2 * half], u.x, u.y);
+                        mma_rows<T>(sc, kf[c][2 * half + 1], u.z, u.w);
+                    }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int rr = r0 + 2 * t + e;
+                    if (rr >= rows) continue;
+                    const int ii = i0 + rr / G;
+                    const float lse = __ldg(a.lse + (static_cast<int64_t>(w.row0) + ii) * a.heads + h * G + rr % G) * 1.4426950408889634f;
+                    if (!(fabsf(lse) < INFINITY)) continue;
+                    const int sees = visible(a, w, ii);
+                    if (t0 + g < sees) sum[0] += fast_exp2(fmaf(sc[e], fac, -lse));
+                    if (t0 + g + 8 < sees) sum[1] += fast_exp2(fmaf(sc[e + 2], fac, -lse));
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 1);
+        sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 2);
+        const int token = t0 + g + 8 * e;
+        if (t != 0 || token >= w.len) continue;
+        if (m.parts > 1) m.sums[(static_cast<int64_t>(part) * a.batch + w.b) * (static_cast<int64_t>(m.tiles) * TOKENS) + token] = sum[e];
+        else add_to_past(m, w.b, token, w.tokens, w.n_q, sum[e]);
+    }
+}
+
+constexpr int SUM_THREADS = 128;
+__global__ void __launch_bounds__(SUM_THREADS) kv_mass_sum_kernel(MassArgs m, unsigned blocks) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const AttnArgs& a = m.a;
+    const int b = static_cast<int>(blockIdx.x / blocks), token = static_cast<int>(blockIdx.x % blocks) * SUM_THREADS + threadIdx.x;
+    const int tokens = max(a.lens[b], 0);
+    if (token >= min(tokens, a.max_len)) return;
+    const int64_t width = static_cast<int64_t>(m.tiles) * TOKENS;
+    const float* p = m.sums + b * width + token;
+    float sum = 0.0f;
+    for (int i = 0; i < m.parts; ++i) sum += p[i * a.batch * width];
+    add_to_past(m, b, token, tokens, max(a.cu[b + 1] - a.cu[b], 0), sum);
+}
+
+template <typename T, int TYPE>
+cudaError_t mass_dim(const MassArgs& m, unsigned grid, cudaStream_t s) {
+    if (m.a.c.head_dim == 64) return launch_dependent(kv_mass_kernel<T, TYPE, 64>, dim3(grid), dim3(WARPS * 32), 0, s, m);
+    if (m.a.c.head_dim == 128) return launch_dependent(kv_mass_kernel<T, TYPE, 128>, dim3(grid), dim3(WARPS * 32), 0, s, m);
+    return launch_dependent(kv_mass_kernel<T, TYPE, 256>, dim3(grid), dim3(WARPS * 32), 0, s, m);
+}
+cudaError_t mass_as(const MassArgs& m, int type, int dtype, unsigned grid, cudaStream_t s) {
+    if (dtype == SQAP_FP16) return type == SQAP_KV_INT8 ? mass_dim<__half, SQAP_KV_INT8>(m, grid, s) : mass_dim<__half, SQAP_KV_E4M3>(m, grid, s);
+    return type == SQAP_KV_INT8 ? mass_dim<__nv_bfloat16, SQAP_KV_INT8>(m, grid, s) : mass_dim<__nv_bfloat16, SQAP_KV_E4M3>(m, grid, s);
+}
+
+struct MassPlan {
+    int tiles, parts;
+    size_t attention, bytes;       // of the workspace: the attention's part in front, and all
+    bool fits;
+};
+MassPlan plan_mass(const sqap_kv_cache* c, int batch, int max_q, int max_len, int heads) {
+    MassPlan p;
+    p.tiles = max_len > 0 ? (max_len - 1) / TOKENS + 1 : 0;
+    const int64_t ctas = size_product(batch, p.tiles), want = ctas > 0 ? (2ll * sm_count() + ctas - 1) / ctas : 1;
+    p.parts = static_cast<int>(want < c->kv_heads ? want : c->kv_heads);
+    p.fits = size_product(ctas, p.parts) <= 0x7FFFFFFF;
+    p.attention = (sqap_kv_attention_workspace_bytes(c, batch, max_q, max_len, heads) + 15) / 16 * 16;
+    p.bytes = p.attention + (p.parts > 1 ? static_cast<size_t>(p.parts) * batch * p.tiles * TOKENS * 4 : 0);
+    return p;
+}
+
+}  // namespace
+}  // namespace kv
+}  // namespace sqap
+
+extern "C" size_t sqap_kv_attention_mass_workspace_bytes(const sqap_kv_cache* cache, int batch, int max_q, int max_len, int heads, int last_q) {
+    using namespace sqap::kv;
+    if (check_cache(cache) != SQAP_OK || batch <= 0 || max_q <= 0 || max_len < 0 || max_len > 1 << 30 || heads <= 0 || heads % cache->kv_heads != 0 || last_q < 0)
+        return 0;
+    const MassPlan p = plan_mass(cache, batch, max_q, max_len, heads);
+    return p.fits ? p.bytes : 0;
+}
+
+extern "C" sqap_status sqap_kv_attention_mass(const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int batch, const int32_t* lens,
+                                              const int32_t* cu_q, int max_q, int max_len, const void* q, int64_t ldq, int heads, float scale,
+                                              uint32_t flags, int last_q, void* out, int64_t ldo, float* lse, const float* past, float* mass,
+                                              int64_t ldm, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace sqap;
+    using namespace sqap::kv;
+    MassArgs m;
+    bool work;
+    sqap_status st = begin_attention(m.a, work, cache, table, ldt, batch, lens, cu_q, max_q, max_len, q, ldq, heads, scale, flags, out, ldo, lse, dtype);
+    if (st != SQAP_OK) return st;
+    if (last_q < 0 || ldm < 0) return SQAP_ERR_INVALID;
+    if (!work) return SQAP_OK;
+    if (!lse || (ldm > 0 && !mass)) return SQAP_ERR_INVALID;
+    if ((reinterpret_cast<uintptr_t>(past) & 3u) || (reinterpret_cast<uintptr_t>(mass) & 3u)) return SQAP_ERR_ALIGN;
+    const MassPlan p = plan_mass(cache, batch, max_q, max_len, heads);
+    if (!p.fits) return SQAP_ERR_UNSUPPORTED;
+    if (p.bytes > 0) {
+        if (!workspace) return SQAP_ERR_INVALID;
+        if (!aligned16(workspace)) return SQAP_ERR_ALIGN;
+        if (workspace_bytes < p.bytes) return SQAP_ERR_NOMEM;
+    }
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    st = run_attention(m.a, cache->type, dtype, workspace, p.attention, s);
+    if (st != SQAP_OK || ldm == 0 || p.tiles == 0) return st;
+    m.last_q = last_q;
+    m.past = past;
+    m.mass = mass;
+    m.ldm = ldm;
+    m.tiles = p.tiles;
+    m.parts = p.parts;
+    m.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.attention);
+    st = finish_launch(mass_as(m, cache->type, dtype, static_cast<unsigned>(static_cast<int64_t>(batch) * p.tiles * p.parts), s));
+    if (st != SQAP_OK || p.parts <= 1) return st;
+    const unsigned blocks = static_cast<unsigned>((static_cast<int64_t>(p.tiles) * TOKENS + SUM_THREADS - 1) / SUM_THREADS);
+    return finish_launch(launch_dependent(kv_mass_sum_kernel, dim3(blocks * static_cast<unsigned>(batch)), dim3(SUM_THREADS), 0, s, m, blocks));
+}

@@ -31,7 +31,7 @@ constexpr int CHUNKS = KEYS * D / 16 / THREADS;      // 16-byte pieces of codes 
 constexpr int GROUPS = KEYS / 16;
 static_assert(WARPS * 16 == PREFILL_ROWS && CHUNKS >= 1, "tile shape");
 
-template <typename T, int TYPE>
+template <typename T, int TYPE, int VIEW>
 __global__ void __launch_bounds__(THREADS, 1) kv_prefill_kernel(AttnArgs a) {
     __shared__ alignas(16) __half sk[KEYS][LD];
     __shared__ alignas(16) __half sv[KEYS][LD];
@@ -39,30 +39,31 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_kernel(AttnArgs a) {
 
     pdl_launch_dependents();
     pdl_wait();
-    Where w = locate(a, blockIdx.x, a.tiles);
+    Where w = locate_view<VIEW>(a, blockIdx.x, a.tiles);
     w.tile = a.tiles - 1 - w.tile;                       // the rows that see the most first
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int G = a.group;
-    const int nq = w.n_q < a.max_q ? w.n_q : a.max_q;
-    const int rows = nq * G;
+    const int rows = rows_of<VIEW>(a, w);
     const int r_first = w.tile * PREFILL_ROWS;
     if (r_first >= rows) return;
-    const int key0 = w.split * a.chunk;
-    const int key1 = a.splits > 1 ? min(key0 + a.chunk, w.len) : w.len;
+    const Span span = span_of<VIEW, KEYS>(a, w, r_first / G);
+    const int len = (VIEW == VIEW_PREFIX ? w.prefix : w.len) - span.gap;
+    const int chunk = chunk_of<VIEW>(a, len);
+    const int key0 = w.split * chunk;                    // keys: tokens without the gap
+    const int key1 = a.splits > 1 ? min(key0 + chunk, len) : len;
     const int last_row = min(rows, r_first + PREFILL_ROWS) - 1;
-    const int end = a.c.pages > 0 ? min(key1, visible(a, w, last_row / G)) : 0;
+    const int end = a.c.pages > 0 ? min(key1, VIEW == VIEW_PREFIX ? len : visible(a, w, last_row / G) - span.gap) : 0;
 
     // queries: A operands of the warp's 16 rows, scaled row by row to fit fp16
     const int r_warp = r_first + warp * 16;
     uint32_t qf[D / 16][4];
     float fac[2];
-    int lim[2];
+    int lim[2], low[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        const int r = r_warp + g + 8 * e;
-        const bool real = r < rows;
-        const T* src = static_cast<const T*>(a.q) + (static_cast<int64_t>(w.row0) + (real ? r / G : 0)) * a.ldq +
-                       static_cast<int64_t>(w.h * G + (real ? r % G : 0)) * D;
+        const Row row = row_at<VIEW>(a, w, rows, r_warp + g + 8 * e);
+        const bool real = row.real;
+        const T* src = static_cast<const T*>(a.q) + row.at * a.ldq + static_cast<int64_t>(row.head) * D;
         // lane (g, t) holds elements 2t, 2t+1, 2t+8, 2t+9 of every sixteen
         float amax = 0.0f;
 #pragma unroll
@@ -83,7 +84,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_kernel(AttnArgs a) {
             qf[k >> 1][(k & 1) * 2 + e] = half2_of(to_f<T>(x[0]) * up, to_f<T>(x[1]) * up);
         }
         fac[e] = back * a.scale_log2;
-        lim[e] = real ? min(visible(a, w, r / G), end) : 0;
+        lim[e] = VIEW == VIEW_ALL ? min(row.sees, end) : row.sees;
+        low[e] = first_seen<VIEW>(a, w, row.i);
     }
 
     float o[D / 8][4];
@@ -96,7 +98,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_kernel(AttnArgs a) {
     const int32_t* table = a.table + w.b * a.ldt;
     const int shift = a.c.page_shift, mask = (1 << shift) - 1;
     auto page_at = [&](int key) {
-        const int j = key >> shift;
+        const int j = span.token(key) >> shift;
         return key < end && j < a.ldt ? checked_page(a.c, __ldg(table + j)) : -1;
     };
     uint4 kc[CHUNKS], vc[CHUNKS];
@@ -110,7 +112,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_kernel(AttnArgs a) {
             const int page = page_at(key);
             kc[i] = vc[i] = make_uint4(0, 0, 0, 0);       // behind the end: zero codes, whatever lies there
             if (page >= 0) {
-                const int64_t at = (page_codes(a.c, page, w.h) + (key & mask)) * D + col;
+                const int64_t at = (page_codes(a.c, page, w.h) + (span.token(key) & mask)) * D + col;
                 kc[i] = __ldg(reinterpret_cast<const uint4*>(a.c.k.codes + at));
                 vc[i] = __ldg(reinterpret_cast<const uint4*>(a.c.v.codes + at));
             }
@@ -183,8 +185,16 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_kernel(AttnArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int key = k0 + 8 * j + 2 * t + (e & 1);
+                bool seen;
+                if (VIEW == VIEW_ALL) {
+                    seen = key < lim[e >> 1];
+                } else {
+                    const int token = span.token(k0) + 8 * j + 2 * t + (e & 1);
+                    seen = key < end && token < lim[e >> 1];
+                    if (VIEW != VIEW_PREFIX) seen = seen && (token >= low[e >> 1] || (VIEW == VIEW_WINDOW && token < a.sinks));
+                }
                 // lv = -inf for a missing page: its scores (of zero codes) become -inf as well
-                sc[j][e] = key < lim[e >> 1] ? fmaf(sc[j][e], fac[e >> 1] * ks, lv) : -INFINITY;
+                sc[j][e] = seen ? fmaf(sc[j][e], fac[e >> 1] * ks, lv) : -INFINITY;
                 top[e >> 1] = fmaxf(top[e >> 1], sc[j][e]);
             }
         }
@@ -227,39 +237,43 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_kernel(AttnArgs a) {
     for (int e = 0; e < 2; ++e) {
         l[e] += __shfl_xor_sync(0xffffffffu, l[e], 1);
         l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
-        const int r = r_warp + g + 8 * e;
-        if (r >= rows) continue;
-        const int i = r / G, head = w.h * G + r % G;
-        if (a.splits > 1) {
-            const int64_t at = part_index(a, w.b, head, i, w.split);
+        const Row row = row_at<VIEW>(a, w, rows, r_warp + g + 8 * e);
+        if (!row.real) continue;
+        if (a.parts > 1) {
+            const int64_t at = part_index(a, row.b, row.head, row.i, w.split);
             if (t == 0) a.part_ml[at] = make_float2(m[e], l[e]);
             float* po = a.part_o + at * D + 2 * t;
 #pragma unroll
             for (int x = 0; x < D / 8; ++x) *reinterpret_cast<float2*>(po + 8 * x) = make_float2(o[x][2 * e], o[x][2 * e + 1]);
         } else {
             const float inv = l[e] != 0.0f ? 1.0f / l[e] : 0.0f;
-            const int64_t row = static_cast<int64_t>(w.row0) + i;
-            T* out = static_cast<T*>(a.out) + row * a.ldo + static_cast<int64_t>(head) * D + 2 * t;
+            T* out = static_cast<T*>(a.out) + row.at * a.ldo + static_cast<int64_t>(row.head) * D + 2 * t;
 #pragma unroll
             for (int x = 0; x < D / 8; ++x) *reinterpret_cast<uint32_t*>(out + 8 * x) = pack2<T>(o[x][2 * e] * inv, o[x][2 * e + 1] * inv);
-            if (t == 0 && a.lse) a.lse[row * a.heads + head] = l[e] != 0.0f ? log_sum(m[e], l[e]) : -INFINITY;
+            if (t == 0 && a.lse) a.lse[row.at * a.heads + row.head] = l[e] != 0.0f ? log_sum(m[e], l[e]) : -INFINITY;
         }
     }
 }
 
-template <typename T, int TYPE>
-cudaError_t launch_as(const AttnArgs& a, unsigned grid, cudaStream_t s) {
-    return launch_dependent(kv_prefill_kernel<T, TYPE>, dim3(grid), dim3(THREADS), 0, s, a);
+template <int VIEW>
+cudaError_t launch_view(const AttnArgs& a, int type, int dtype, unsigned grid, cudaStream_t s) {
+    if (dtype == SQAP_FP16)
+        return type == SQAP_KV_INT8 ? launch_dependent(kv_prefill_kernel<__half, SQAP_KV_INT8, VIEW>, dim3(grid), dim3(THREADS), 0, s, a)
+                                    : launch_dependent(kv_prefill_kernel<__half, SQAP_KV_E4M3, VIEW>, dim3(grid), dim3(THREADS), 0, s, a);
+    return type == SQAP_KV_INT8 ? launch_dependent(kv_prefill_kernel<__nv_bfloat16, SQAP_KV_INT8, VIEW>, dim3(grid), dim3(THREADS), 0, s, a)
+                                : launch_dependent(kv_prefill_kernel<__nv_bfloat16, SQAP_KV_E4M3, VIEW>, dim3(grid), dim3(THREADS), 0, s, a);
 }
 
 }  // namespace
 
-sqap_status launch_kv_prefill(const AttnArgs& a, int type, int dtype, cudaStream_t s) {
-    const unsigned grid = static_cast<unsigned>(static_cast<int64_t>(a.batch) * a.c.kv_heads * a.splits * a.tiles);
-    if (dtype == SQAP_FP16)
-        return finish_launch(type == SQAP_KV_INT8 ? launch_as<__half, SQAP_KV_INT8>(a, grid, s) : launch_as<__half, SQAP_KV_E4M3>(a, grid, s));
-    return finish_launch(type == SQAP_KV_INT8 ? launch_as<__nv_bfloat16, SQAP_KV_INT8>(a, grid, s)
-                                              : launch_as<__nv_bfloat16, SQAP_KV_E4M3>(a, grid, s));
+sqap_status launch_kv_prefill(const AttnArgs& a, View view, int64_t units, int type, int dtype, cudaStream_t s) {
+    const unsigned grid = static_cast<unsigned>(units * a.c.kv_heads * a.splits * a.tiles);
+    switch (view) {
+        case VIEW_WINDOW: return finish_launch(launch_view<VIEW_WINDOW>(a, type, dtype, grid, s));
+        case VIEW_PREFIX: return finish_launch(launch_view<VIEW_PREFIX>(a, type, dtype, grid, s));
+        case VIEW_OWN: return finish_launch(launch_view<VIEW_OWN>(a, type, dtype, grid, s));
+        default: return finish_launch(launch_view<VIEW_ALL>(a, type, dtype, grid, s));
+    }
 }
 
 }  // namespace kv

@@ -130,26 +130,31 @@ __device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
 // One item: 256 rows of a sequence and key/value head (and one piece of its history, where those are cut).
 struct Item {
     Where w;
-    int rows, r_first, key0, end, steps;
+    int rows, r_first, key0, end, steps;      // keys: tokens without the gap
     int steps_lo;     // tiles that the lower half of the rows looks at (the upper half: all, or there is no upper half)
+    Span span;
 };
-__device__ __forceinline__ Item item_of(const AttnArgs& a, unsigned id) {
+template <int VIEW>
+__device__ __forceinline__ Item item_of(const AttnArgs& a, unsigned id, unsigned per_tile) {
     Item x;
     // tiles outermost, the rows that see the most first
-    const unsigned per_tile = static_cast<unsigned>(a.batch) * a.c.kv_heads * a.splits;
     const unsigned tile = id / per_tile;
-    x.w = locate(a, id - tile * per_tile, 1);
+    x.w = locate_view<VIEW>(a, id - tile * per_tile, 1);
     x.w.tile = a.tiles - 1 - static_cast<int>(tile);
-    x.rows = (x.w.n_q < a.max_q ? x.w.n_q : a.max_q) * a.group;
+    x.rows = rows_of<VIEW>(a, x.w);
     x.r_first = x.w.tile * ROWS;
-    x.key0 = x.w.split * a.chunk;
-    x.end = 0;
+    x.key0 = x.end = 0;
     x.steps = x.steps_lo = 0;
+    x.span = {0, 0};
     if (x.r_first < x.rows && a.c.pages > 0) {
-        const int key1 = a.splits > 1 ? min(x.key0 + a.chunk, x.w.len) : x.w.len;
+        x.span = span_of<VIEW, KEYS>(a, x.w, x.r_first / a.group);
+        const int len = (VIEW == VIEW_PREFIX ? x.w.prefix : x.w.len) - x.span.gap;
+        const int chunk = chunk_of<VIEW>(a, len);
+        x.key0 = x.w.split * chunk;
+        const int key1 = a.splits > 1 ? min(x.key0 + chunk, len) : len;
         const int last = min(x.rows, x.r_first + ROWS) - 1, last_lo = min(x.rows, x.r_first + ROWS / 2) - 1;
-        x.end = min(key1, visible(a, x.w, last / a.group));
-        const int end_lo = min(key1, visible(a, x.w, last_lo / a.group));
+        x.end = VIEW == VIEW_PREFIX ? key1 : min(key1, visible(a, x.w, last / a.group) - x.span.gap);
+        const int end_lo = VIEW == VIEW_PREFIX ? key1 : min(key1, visible(a, x.w, last_lo / a.group) - x.span.gap);
         x.steps = x.end > x.key0 ? (x.end - x.key0 + KEYS - 1) / KEYS : 0;
         x.steps_lo = end_lo > x.key0 ? (end_lo - x.key0 + KEYS - 1) / KEYS : 0;
     }
@@ -161,8 +166,8 @@ __device__ __forceinline__ int half_steps(const Item& x, int g) {
     return x.r_first + ROWS / 2 < x.rows ? x.steps : 0;
 }
 
-template <typename T, int TYPE, int D>
-__global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, unsigned items, int* status) {
+template <typename T, int TYPE, int D, int VIEW>
+__global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, unsigned items, unsigned per_tile, int* status) {
     using S = Smem<D>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -226,13 +231,13 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
         const uint32_t t_lane = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + 128 * half, t_o = t_lane + O_COL;
         uint32_t n = 0;             // tiles of this half so far
         uint32_t full_items = 0;
-        Item next = item_of(a, blockIdx.x);
+        Item next = item_of<VIEW>(a, blockIdx.x, per_tile);
         for (unsigned id = blockIdx.x; id < items; id += gridDim.x) {
             const Item x = next;
-            const int r = x.r_first + static_cast<int>(threadIdx.x);
-            const bool real = r < x.rows;
-            const int qi = real ? r / G : 0, head = x.w.h * G + (real ? r - qi * G : 0);
-            const int lim = real ? min(visible(a, x.w, qi), x.end) : 0;
+            const Row row = row_at<VIEW>(a, x.w, x.rows, x.r_first + static_cast<int>(threadIdx.x));
+            const bool real = row.real;
+            const int lim = VIEW == VIEW_ALL ? min(row.sees, x.end) : min(row.sees, x.end > 0 ? x.span.token(x.end - 1) + 1 : 0);
+            const int low = first_seen<VIEW>(a, x.w, row.i);
             const bool idle = x.r_first + warp * 32 >= x.rows;          // no rows: whatever these lanes hold goes nowhere
             const int steps = half_steps(x, half);
             float m = -INFINITY, l = 0.0f, fac = 0.0f;
@@ -245,7 +250,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
                     const float* ks = scales->ks[slot];
                     const float* lv = scales->lv[slot];
                     const float* iv = scales->iv[slot];
-                    const int seen = lim - (x.key0 + j * KEYS);         // this row sees the first `seen` keys of the tile
+                    const int token0 = x.span.token(x.key0 + j * KEYS);
+                    const int seen = lim - token0;                      // this row sees the first `seen` keys of the tile
+                    const int from = VIEW == VIEW_WINDOW || VIEW == VIEW_OWN ? low - token0 : 0;     // but for those in front of `from`
+                    const int sink = VIEW == VIEW_WINDOW ? a.sinks - token0 : 0;                     // that are not in front of `sink`
                     const uint32_t t_s = t_lane + KEYS * (n & 1);
                     uint32_t v[KEYS];
                     tc_ld32(t_s, v);
@@ -255,6 +263,13 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
 #pragma unroll
                         for (int i = 0; i < KEYS; ++i)
                             if (i >= seen) v[i] = 0xFF800000u;
+                    }
+                    if (VIEW == VIEW_WINDOW || VIEW == VIEW_OWN) {
+                        if (!__all_sync(0xffffffffu, from <= 0 || sink >= KEYS)) {
+#pragma unroll
+                            for (int i = 0; i < KEYS; ++i)
+                                if (i < from && i >= sink) v[i] = 0xFF800000u;
+                        }
                     }
                     // of a run's scores; never 0, so that what is masked stays at -inf
                     auto factor = [&](int run) { return fmaxf(fac * ks[run], 1e-37f); };
@@ -317,7 +332,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
                 if (lane == 0) mbar_arrive(p_full(half, n));
             }
             if (failed) break;
-            if (id + gridDim.x < items) next = item_of(a, id + gridDim.x);      // while the last output product runs
+            if (id + gridDim.x < items) next = item_of<VIEW>(a, id + gridDim.x, per_tile);      // while the last output product runs
             for (int j = steps; j < x.steps; ++j) next_slot();          // tiles that the other half alone looks at
             if (x.steps > 0) ++full_items;
             if (steps > 0) {
@@ -326,9 +341,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
             }
             if (idle) continue;
             const float inv = l != 0.0f ? 1.0f / l : 0.0f;
-            const int64_t row = static_cast<int64_t>(x.w.row0) + qi;
-            const int64_t at = a.splits > 1 && real ? part_index(a, x.w.b, head, qi, x.w.split) : 0;
-            T* out = static_cast<T*>(a.out) + row * a.ldo + static_cast<int64_t>(head) * D;
+            const int64_t at = a.parts > 1 && real ? part_index(a, row.b, row.head, row.i, x.w.split) : 0;
+            T* out = static_cast<T*>(a.out) + row.at * a.ldo + static_cast<int64_t>(row.head) * D;
             float* po = a.part_o + at * D;
 #pragma unroll
             for (int c = 0; c < D / 64; ++c) {
@@ -342,7 +356,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
                     for (int i = 0; i < 64; ++i) v[i] = 0;
                 }
                 if (!real) continue;
-                if (a.splits > 1) {
+                if (a.parts > 1) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) reinterpret_cast<uint4*>(po + 64 * c)[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
                 } else {
@@ -356,8 +370,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
                 }
             }
             if (real) {
-                if (a.splits > 1) a.part_ml[at] = make_float2(m, l);
-                else if (a.lse) a.lse[row * a.heads + head] = l != 0.0f ? log_sum(m, l) : -INFINITY;
+                if (a.parts > 1) a.part_ml[at] = make_float2(m, l);
+                else if (a.lse) a.lse[row.at * a.heads + row.head] = l != 0.0f ? log_sum(m, l) : -INFINITY;
             }
             tc_fence_before();
         }
@@ -374,22 +388,26 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
         // The tiles of this CTA's items, one after another.
         struct Tile {
             const int32_t* table;
-            int h, k0, end;            // keys k0 .. of a sequence of `end` keys that count; end = 0: no more tiles
+            int h, k0, end;            // tokens k0 .. of a sequence of `end` tokens that count; end = 0: no more tiles
             int row0, r_first, rows;   // rows > 0: the first tile of an item, whose queries are wanted
+            int b;                     // its sequence (the group's first, VIEW_PREFIX)
         };
         unsigned id = blockIdx.x;
         Tile then = {};
         int left = 0;                  // tiles of the item behind `then`
+        Span span = {0, 0};            // of the item
         auto open_item = [&]() {
             then.end = 0;
             while (id < items) {
-                const Item x = item_of(a, id);
+                const Item x = item_of<VIEW>(a, id, per_tile);
                 id += gridDim.x;
                 if (x.steps == 0) continue;
                 then.table = a.table + x.w.b * a.ldt;
                 then.h = x.w.h;
-                then.k0 = x.key0;
-                then.end = x.end;
+                span = x.span;
+                then.k0 = span.token(x.key0);
+                then.end = span.token(x.end - 1) + 1;
+                then.b = x.w.b;
                 then.row0 = x.w.row0;
                 then.r_first = x.r_first;
                 then.rows = x.rows;
@@ -401,6 +419,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
             if (left > 0) {
                 --left;
                 then.k0 += KEYS;
+                if (VIEW == VIEW_WINDOW && then.k0 == span.stop) then.k0 += span.gap;
                 then.rows = 0;
             } else {
                 open_item();
@@ -470,7 +489,17 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
         auto begin_queries = [&](const Tile& t) {
             const int first = t.r_first + q_row0;
             const T* q = static_cast<const T*>(a.q) + static_cast<int64_t>(t.row0) * a.ldq + static_cast<int64_t>(t.h) * G * D + 8 * qc;
-            if (G == 1) {
+            if constexpr (VIEW == VIEW_PREFIX) {
+                Where w = {};
+                w.b = t.b;
+                w.h = t.h;
+#pragma unroll 4
+                for (int i = 0; i < Q_STEPS; ++i) {
+                    const Row x = row_at<VIEW>(a, w, t.rows, first + i * RPI);
+                    const T* p = static_cast<const T*>(a.q) + x.at * a.ldq + static_cast<int64_t>(x.head) * D + 8 * qc;
+                    cp_async_16(base + q_at(i), x.real ? p : a.q, x.real);
+                }
+            } else if (G == 1) {
                 const T* p = q + first * a.ldq;
 #pragma unroll
                 for (int i = 0; i < Q_STEPS; ++i, p += RPI * a.ldq) {
@@ -600,7 +629,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
             return true;
         };
         for (unsigned id = blockIdx.x; id < items && !failed; id += gridDim.x) {
-            const Item x = item_of(a, id);
+            const Item x = item_of<VIEW>(a, id, per_tile);
             if (x.steps == 0) continue;
             const int steps[2] = {half_steps(x, 0), half_steps(x, 1)};
             if (!wait_phase(q_full, full_items)) { failed = true; break; }
@@ -638,41 +667,52 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
     if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(TMEM_COLS) : "memory");
 }
 
-template <typename T, int TYPE, int D>
-sqap_status launch_as(const AttnArgs& a, unsigned items, int* status, cudaStream_t s) {
+template <typename T, int TYPE, int D, int VIEW>
+sqap_status launch_as(const AttnArgs& a, unsigned per_tile, int* status, cudaStream_t s) {
     static PerDevice<int> setup;
     const sqap_status st = setup.run([](int*) {
         // the softmax's registers come out of those that the kernel is launched with: with fewer, it would wait for them for ever
         cudaFuncAttributes f;
-        const cudaError_t e = cudaFuncGetAttributes(&f, kv_prefill_tc_kernel<T, TYPE, D>);
+        const cudaError_t e = cudaFuncGetAttributes(&f, kv_prefill_tc_kernel<T, TYPE, D, VIEW>);
         if (e != cudaSuccess) {
             note_cuda_error(e);
             cudaGetLastError();
             return SQAP_ERR_CUDA;
         }
         if (f.numRegs < LAUNCH_REGS) return SQAP_ERR_UNSUPPORTED;
-        return set_max_dynamic_smem(kv_prefill_tc_kernel<T, TYPE, D>, Smem<D>::BYTES);
+        return set_max_dynamic_smem(kv_prefill_tc_kernel<T, TYPE, D, VIEW>, Smem<D>::BYTES);
     });
     if (st != SQAP_OK) return st;
-    const unsigned slots = static_cast<unsigned>(sm_count());
-    return finish_launch(launch_dependent(kv_prefill_tc_kernel<T, TYPE, D>, dim3(items < slots ? items : slots), dim3(THREADS),
-                                          Smem<D>::BYTES, s, a, items, status));
+    const unsigned slots = static_cast<unsigned>(sm_count()), items = per_tile * a.tiles;
+    return finish_launch(launch_dependent(kv_prefill_tc_kernel<T, TYPE, D, VIEW>, dim3(items < slots ? items : slots), dim3(THREADS),
+                                          Smem<D>::BYTES, s, a, items, per_tile, status));
 }
-template <typename T>
-sqap_status launch_type(const AttnArgs& a, int type, unsigned items, int* status, cudaStream_t s) {
+template <typename T, int VIEW>
+sqap_status launch_type(const AttnArgs& a, int type, unsigned per_tile, int* status, cudaStream_t s) {
     if (a.c.head_dim == 64)
-        return type == SQAP_KV_INT8 ? launch_as<T, SQAP_KV_INT8, 64>(a, items, status, s) : launch_as<T, SQAP_KV_E4M3, 64>(a, items, status, s);
-    return type == SQAP_KV_INT8 ? launch_as<T, SQAP_KV_INT8, 128>(a, items, status, s) : launch_as<T, SQAP_KV_E4M3, 128>(a, items, status, s);
+        return type == SQAP_KV_INT8 ? launch_as<T, SQAP_KV_INT8, 64, VIEW>(a, per_tile, status, s)
+                                    : launch_as<T, SQAP_KV_E4M3, 64, VIEW>(a, per_tile, status, s);
+    return type == SQAP_KV_INT8 ? launch_as<T, SQAP_KV_INT8, 128, VIEW>(a, per_tile, status, s)
+                                : launch_as<T, SQAP_KV_E4M3, 128, VIEW>(a, per_tile, status, s);
+}
+template <int VIEW>
+sqap_status launch_view(const AttnArgs& a, int type, int dtype, unsigned per_tile, int* status, cudaStream_t s) {
+    return dtype == SQAP_FP16 ? launch_type<__half, VIEW>(a, type, per_tile, status, s) : launch_type<__nv_bfloat16, VIEW>(a, type, per_tile, status, s);
 }
 
 }  // namespace
 
-sqap_status launch_kv_prefill_tc(const AttnArgs& a, int type, int dtype, cudaStream_t s) {
+sqap_status launch_kv_prefill_tc(const AttnArgs& a, View view, int64_t units, int type, int dtype, cudaStream_t s) {
     int* status = device_status_word();
     if (!status) return SQAP_ERR_CUDA;
     if (!device_is_sm100()) return SQAP_ERR_UNSUPPORTED;
-    const unsigned items = static_cast<unsigned>(static_cast<int64_t>(a.batch) * a.c.kv_heads * a.splits * a.tiles);
-    return dtype == SQAP_FP16 ? launch_type<__half>(a, type, items, status, s) : launch_type<__nv_bfloat16>(a, type, items, status, s);
+    const unsigned per_tile = static_cast<unsigned>(units * a.c.kv_heads * a.splits);
+    switch (view) {
+        case VIEW_WINDOW: return launch_view<VIEW_WINDOW>(a, type, dtype, per_tile, status, s);
+        case VIEW_PREFIX: return launch_view<VIEW_PREFIX>(a, type, dtype, per_tile, status, s);
+        case VIEW_OWN: return launch_view<VIEW_OWN>(a, type, dtype, per_tile, status, s);
+        default: return launch_view<VIEW_ALL>(a, type, dtype, per_tile, status, s);
+    }
 }
 
 }  // namespace kv
