@@ -239,13 +239,14 @@ sqap_status begin_attention(AttnArgs& a, bool& work, const sqap_kv_cache* cache,
     work = true;
     return SQAP_OK;
 }
-sqap_status run_attention(const AttnArgs& args, int type, int dtype, void* workspace, size_t workspace_bytes, cudaStream_t s) {
+bool few_rows(int max_q, int group, int head_dim) { return static_cast<int64_t>(max_q) * group <= decode_max_rows(head_dim); }
+sqap_status run_attention(const AttnArgs& args, bool scores, int type, int dtype, void* workspace, size_t workspace_bytes, cudaStream_t s) {
     AttnArgs a = args;
     const Plan p = plan_for(a.batch, a.c.kv_heads, a.group, a.c.head_dim, a.max_q, a.max_len);
     if (!grid_fits(a.batch, a.c.kv_heads, p)) return SQAP_ERR_UNSUPPORTED;
     sqap_status st = take_workspace(a, p.splits, workspace, workspace_bytes);
     if (st != SQAP_OK) return st;
-    st = launch(a, p, VIEW_ALL, a.batch, type, dtype, s);
+    st = launch(a, p, scores ? VIEW_SCORES : VIEW_ALL, a.batch, type, dtype, s);
     if (st != SQAP_OK || a.parts <= 1) return st;
     return combine(a, a.batch, dtype, s);
 }
@@ -270,7 +271,7 @@ extern "C" sqap_status sqap_kv_attention(const sqap_kv_cache* cache, const int32
     bool work;
     const sqap_status st = begin_attention(a, work, cache, table, ldt, batch, lens, cu_q, max_q, max_len, q, ldq, heads, scale, flags, out, ldo, lse, dtype);
     if (st != SQAP_OK || !work) return st;
-    return run_attention(a, cache->type, dtype, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
+    return run_attention(a, false, cache->type, dtype, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" size_t sqap_kv_attention_window_workspace_bytes(const sqap_kv_cache* cache, int batch, int max_q, int max_len, int heads,

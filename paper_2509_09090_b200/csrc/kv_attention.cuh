@@ -42,11 +42,13 @@ struct AttnArgs {
     const int32_t* cu_group;   // VIEW_PREFIX, VIEW_OWN: sequences of the groups
     const int32_t* prefix;
     int groups, max_group, max_prefix;
+    float* scores;             // VIEW_SCORES: [batch][kv_heads][max_len][max_q x group], (q . k_t) scale log2 e, -inf where t is not seen
 };
 
 // What the rows of a launch look at: all (causal or not); the tokens of a window and the first ones; the prefix that the
-// sequences of a group share, rows of all of them together; the tokens of a sequence behind its group's prefix.
-enum View { VIEW_ALL, VIEW_WINDOW, VIEW_PREFIX, VIEW_OWN };
+// sequences of a group share, rows of all of them together; the tokens of a sequence behind its group's prefix; all, and the
+// scores are kept (register kernel only).
+enum View { VIEW_ALL, VIEW_WINDOW, VIEW_PREFIX, VIEW_OWN, VIEW_SCORES };
 
 // Work of a CTA, from its index.
 struct Where {
@@ -259,7 +261,9 @@ sqap_status launch_kv_prefill(const AttnArgs& a, View view, int64_t units, int t
 sqap_status begin_attention(AttnArgs& a, bool& work, const sqap_kv_cache* cache, const int32_t* table, int64_t ldt, int batch,
                             const int32_t* lens, const int32_t* cu_q, int max_q, int max_len, const void* q, int64_t ldq, int heads,
                             float scale, uint32_t flags, void* out, int64_t ldo, float* lse, int dtype);
-sqap_status run_attention(const AttnArgs& args, int type, int dtype, void* workspace, size_t workspace_bytes, cudaStream_t s);
+// `scores`: keep them (VIEW_SCORES), where few_rows().
+bool few_rows(int max_q, int group, int head_dim);
+sqap_status run_attention(const AttnArgs& args, bool scores, int type, int dtype, void* workspace, size_t workspace_bytes, cudaStream_t s);
 
 }  // namespace kv
 }  // namespace sqap

@@ -67,6 +67,7 @@ __device__ __forceinline__ void word_to_half2x2(uint32_t w, uint32_t* lo, uint32
 template <typename T, int TYPE, int D, int NT, int GROUPS, int VIEW>
 __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1 ? 4 : 1) kv_decode_kernel(AttnArgs a) {
     constexpr int STEP = 16 * GROUPS;
+    constexpr bool WHOLE = VIEW == VIEW_ALL || VIEW == VIEW_SCORES;
     constexpr int KC = D / 64;                     // 16-byte chunks of a key row per lane
     constexpr int VB = D / 8;                      // bytes of a value row per lane
     constexpr int MT = D / 16;                     // MMA rows of 16 elements of the output
@@ -148,6 +149,8 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
         m[n][0] = m[n][1] = -INFINITY;
         l[n][0] = l[n][1] = 0.0f;
     }
+    const int per_token = a.max_q * G;
+    float* scores = VIEW == VIEW_SCORES ? a.scores + (static_cast<int64_t>(w.b) * a.c.kv_heads + w.h) * a.max_len * per_token : nullptr;
     const int32_t* table = a.table + w.b * a.ldt;
     const int shift = a.c.page_shift, mask = (1 << shift) - 1;
 
@@ -258,14 +261,20 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
                 for (int e = 0; e < 4; ++e) {
                     const int key = base + g + (e >> 1) * 8;
                     bool seen;
-                    if (VIEW == VIEW_ALL) {
+                    if (WHOLE) {
                         seen = there[u] && key < min(lim[n][e & 1], end);
                     } else {
                         const int token = span.token(base) + g + (e >> 1) * 8;
                         seen = there[u] && key < end && token < lim[n][e & 1];
                         if (VIEW != VIEW_PREFIX) seen = seen && (token >= low[n][e & 1] || (VIEW == VIEW_WINDOW && token < a.sinks));
                     }
-                    sc[u][n][e] = seen ? fmaf(sc[u][n][e], fac[n][e & 1] * this_ks[u], lv[u]) : -INFINITY;
+                    if (VIEW == VIEW_SCORES) {
+                        sc[u][n][e] = seen ? sc[u][n][e] * (fac[n][e & 1] * this_ks[u]) : -INFINITY;
+                        if (key < end && 8 * n + 2 * t + (e & 1) < rows) scores[static_cast<int64_t>(key) * per_token + 8 * n + 2 * t + (e & 1)] = sc[u][n][e];
+                        if (seen) sc[u][n][e] += lv[u];
+                    } else {
+                        sc[u][n][e] = seen ? fmaf(sc[u][n][e], fac[n][e & 1] * this_ks[u], lv[u]) : -INFINITY;
+                    }
                     top[n][e & 1] = fmaxf(top[n][e & 1], sc[u][n][e]);
                 }
             if (!there[u] || base + 16 > end) {
@@ -424,6 +433,7 @@ sqap_status launch_kv_decode(const AttnArgs& a, View view, int64_t units, int ty
         case VIEW_WINDOW: return finish_launch(launch_view<VIEW_WINDOW>(a, type, dtype, grid, s));
         case VIEW_PREFIX: return finish_launch(launch_view<VIEW_PREFIX>(a, type, dtype, grid, s));
         case VIEW_OWN: return finish_launch(launch_view<VIEW_OWN>(a, type, dtype, grid, s));
+        case VIEW_SCORES: return finish_launch(launch_view<VIEW_SCORES>(a, type, dtype, grid, s));
         default: return finish_launch(launch_view<VIEW_ALL>(a, type, dtype, grid, s));
     }
 }

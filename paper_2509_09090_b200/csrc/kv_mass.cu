@@ -1,5 +1,6 @@
-// Attention with the weight that each token received: the attention itself, then the scores of the rows that count once more, now with
-// their log-sum-exp, so that a weight is known as soon as its score is.
+// Attention with the weight that each token received. Few rows (decoding): the register kernel keeps its scores, 4 bytes for each
+// row beside the 2 D bytes of the keys and values that it reads, and a second kernel turns them into weights once the
+// log-sum-exps are there. Many rows: their scores would be more than the keys; those of the rows that count are computed once more.
 //
 // A warp holds 16 tokens' keys of a head as the A operand (from codes in registers, as in kv_decode.cu) and goes over the
 // query rows, eight at a time, as the B operand: S[token][row], p = 2^(s scale log2 e - lse log2 e), summed over the row in the lane that
@@ -59,6 +60,20 @@ __device__ __forceinline__ void add_to_past(const MassArgs& m, int b, int token,
     m.mass[at] = (m.past && token < tokens - n_q ? m.past[at] : 0.0f) + sum;
 }
 
+// Row r of a key/value head: query i, head `head` of the group; without a division per step.
+struct Walk {
+    int i, head, group;
+    __device__ __forceinline__ Walk(int G, int r) : i(r / G), head(r % G), group(G) {}
+    __device__ __forceinline__ void next(const Walk& by) {
+        i += by.i;
+        head += by.head;
+        if (head >= group) {
+            head -= group;
+            ++i;
+        }
+    }
+};
+
 template <typename T, int TYPE, int D>
 __global__ void __launch_bounds__(WARPS * 32) kv_mass_kernel(MassArgs m) {
     constexpr int KC = D / 64;
@@ -83,8 +98,11 @@ __global__ void __launch_bounds__(WARPS * 32) kv_mass_kernel(MassArgs m) {
     const int i0 = max(0, w.n_q - m.last_q), rows = (min(w.n_q, a.max_q) - i0) * G;
     const int j = t0 >> a.c.page_shift;
     const int page = a.c.pages > 0 && j < a.ldt ? checked_page(a.c, a.table[w.b * a.ldt + j]) : -1;
+    const T* q0 = static_cast<const T*>(a.q) + (static_cast<int64_t>(w.row0) + i0) * a.ldq + 16 * t;
+    const float* lse0 = a.lse + (static_cast<int64_t>(w.row0) + i0) * a.heads;
+    const Walk by(G, 8);
     float sum[2] = {0.0f, 0.0f};
-    if (page >= 0) {
+    if (page >= 0 && rows > 0) {
         for (int h = h0; h < h1; ++h) {
             const uint8_t* kp = a.c.k.codes + (page_codes(a.c, page, h) + (t0 & ((1 << a.c.page_shift) - 1)) + g) * D + 16 * t;
             uint32_t kf[KC][4][4];
@@ -99,30 +117,52 @@ __global__ void __launch_bounds__(WARPS * 32) kv_mass_kernel(MassArgs m) {
                 }
             }
             const float fac = __ldg(a.c.k.scales + static_cast<int64_t>(page) * a.c.kv_heads + h) * a.scale_log2;
+            // The rows eight by eight; the queries and log-sum-exps of the next eight are fetched while these are computed with.
+            Walk mine(G, g), col[2] = {Walk(G, 2 * t), Walk(G, 2 * t + 1)};
+            uint4 next_q[KC][2];
+            float next_lse[2];
+            auto fetch = [&](int r0) {
+                const bool real = r0 + g < rows;
+                const T* src = q0 + static_cast<int64_t>(mine.i) * a.ldq + (h * G + mine.head) * D;
+#pragma unroll
+                for (int c = 0; c < KC; ++c)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+                        next_q[c][half] = real ? __ldg(reinterpret_cast<const uint4*>(src + 64 * c) + half) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    next_lse[e] = r0 + 2 * t + e < rows ? __ldg(lse0 + static_cast<int64_t>(col[e].i) * a.heads + h * G + col[e].head) : INFINITY;
+            };
+            fetch(0);
             for (int r0 = 0; r0 < rows; r0 += 8) {
-                float sc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                const int r = r0 + g;
-                const bool real = r < rows;
-                const int i = real ? i0 + r / G : i0;
-                const T* src = static_cast<const T*>(a.q) + (static_cast<int64_t>(w.row0) + i) * a.ldq + (h * G + (real ? r % G : 0)) * D + 16 * t;
+                uint4 q[KC][2];
+                float lse[2];
+                int sees[2];
+#pragma unroll
+                for (int c = 0; c < KC; ++c) {
+                    q[c][0] = next_q[c][0];
+                    q[c][1] = next_q[c][1];
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    lse[e] = next_lse[e] * 1.4426950408889634f;
+                    sees[e] = fabsf(lse[e]) < INFINITY ? visible(a, w, i0 + col[e].i) - t0 : 0;       // rows that saw nothing, or are not numbers
+                    col[e].next(by);
+                }
+                mine.next(by);
+                if (r0 + 8 < rows) fetch(r0 + 8);
+                float sc[4] = {0.0f, 0.0f, 0.0f, 0.0f}, sd[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int c = 0; c < KC; ++c)
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        const uint4 u = real ? __ldg(reinterpret_cast<const uint4*>(src + 64 * c) + half) : make_uint4(0, 0, 0, 0);
-                        mma_rows<T>(sc, kf[c][2 * half], u.x, u.y);
-                        mma_rows<T>(sc, kf[c][2 * half + 1], u.z, u.w);
+                        mma_rows<T>(sc, kf[c][2 * half], q[c][half].x, q[c][half].y);
+                        mma_rows<T>(sd, kf[c][2 * half + 1], q[c][half].z, q[c][half].w);
                     }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int rr = r0 + 2 * t + e;
-                    if (rr >= rows) continue;
-                    const int ii = i0 + rr / G;
-                    const float lse = __ldg(a.lse + (static_cast<int64_t>(w.row0) + ii) * a.heads + h * G + rr % G) * 1.4426950408889634f;
-                    if (!(fabsf(lse) < INFINITY)) continue;
-                    const int sees = visible(a, w, ii);
-                    if (t0 + g < sees) sum[0] += fast_exp2(fmaf(sc[e], fac, -lse));
-                    if (t0 + g + 8 < sees) sum[1] += fast_exp2(fmaf(sc[e + 2], fac, -lse));
+                    if (g < sees[e]) sum[0] += fast_exp2(fmaf(sc[e] + sd[e], fac, -lse[e]));
+                    if (g + 8 < sees[e]) sum[1] += fast_exp2(fmaf(sc[e + 2] + sd[e + 2], fac, -lse[e]));
                 }
             }
         }
@@ -138,6 +178,92 @@ __global__ void __launch_bounds__(WARPS * 32) kv_mass_kernel(MassArgs m) {
     }
 }
 
+// Scores to weights, summed over heads and rows: a lane takes BLOCKS tokens, 32 apart, the warps of a CTA take the heads in turn and meet
+// in shared memory. ROWS rows of a key/value head, 0: any number.
+constexpr int FOLD_WARPS = 8;
+template <int ROWS, int BLOCKS>
+__global__ void __launch_bounds__(FOLD_WARPS * 32) kv_mass_fold_kernel(MassArgs m) {
+    __shared__ float red[FOLD_WARPS][32 * BLOCKS];
+    pdl_launch_dependents();
+    pdl_wait();
+    const AttnArgs& a = m.a;
+    const int b = static_cast<int>(blockIdx.x / m.tiles), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int token0 = static_cast<int>(blockIdx.x % m.tiles) * 32 * BLOCKS;
+    Where w = {};
+    w.b = b;
+    w.row0 = a.cu[b];
+    w.n_q = max(a.cu[b + 1] - w.row0, 0);
+    w.tokens = max(a.lens[b], 0);
+    w.len = min(w.tokens, a.max_len);
+    if (token0 >= w.len) return;
+    const int nq = min(w.n_q, a.max_q), per_token = ROWS ? ROWS : a.max_q * a.group, first = max(0, w.n_q - m.last_q) * a.group;
+    const int rows = nq * a.group;                                 // of the head; `first` and behind count
+    const int limit = nq > 0 && a.c.pages > 0 ? visible(a, w, nq - 1) : 0;      // scores of tokens in front of it are there
+    float sum[BLOCKS] = {};
+    if (first < rows) {
+#pragma unroll 2
+        for (int h = warp; h < a.c.kv_heads; h += FOLD_WARPS) {
+            const float* s = a.scores + ((static_cast<int64_t>(b) * a.c.kv_heads + h) * a.max_len + token0 + lane) * per_token;
+            const float* lse = a.lse + static_cast<int64_t>(w.row0) * a.heads + h * a.group;
+            // weights of rows r .. r + N - 1 of this head, N consecutive numbers of a token
+            auto add = [&](auto n, int r) {
+                constexpr int N = decltype(n)::value;
+                float x[BLOCKS][N], minus[N];
+#pragma unroll
+                for (int k = 0; k < BLOCKS; ++k) {
+                    const bool there = token0 + 32 * k + lane < limit;
+                    if constexpr (N == 4) {
+                        const float4 v = there ? __ldg(reinterpret_cast<const float4*>(s + 32 * k * per_token + r)) : make_float4(0, 0, 0, 0);
+                        x[k][0] = v.x;
+                        x[k][1] = v.y;
+                        x[k][2] = v.z;
+                        x[k][3] = v.w;
+                    } else {
+                        x[k][0] = there ? __ldg(s + 32 * k * per_token + r) : 0.0f;
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const int i = (r + e) / a.group;
+                    const float l = r + e >= first && r + e < rows ? -1.4426950408889634f * __ldg(lse + static_cast<int64_t>(i) * a.heads + r + e - i * a.group) : -INFINITY;
+                    minus[e] = fabsf(l) < INFINITY ? l : -INFINITY;
+                }
+#pragma unroll
+                for (int k = 0; k < BLOCKS; ++k)
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        if (minus[e] > -INFINITY && token0 + 32 * k + lane < limit) sum[k] += fast_exp2(x[k][e] + minus[e]);
+            };
+            if constexpr (ROWS % 4 == 0 && ROWS > 0) {
+#pragma unroll
+                for (int r = 0; r < ROWS; r += 4) add(std::integral_constant<int, 4>(), r);
+            } else if constexpr (ROWS == 1) {
+                add(std::integral_constant<int, 1>(), 0);
+            } else {
+                for (int r = 0; r < per_token; ++r) add(std::integral_constant<int, 1>(), r);
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < BLOCKS; ++k) red[warp][32 * k + lane] = sum[k];
+    __syncthreads();
+    for (int x = threadIdx.x; x < 32 * BLOCKS && token0 + x < w.len; x += FOLD_WARPS * 32) {
+        float total = red[0][x];
+#pragma unroll
+        for (int i = 1; i < FOLD_WARPS; ++i) total += red[i][x];
+        add_to_past(m, b, token0 + x, w.tokens, w.n_q, total);
+    }
+}
+template <int BLOCKS>
+cudaError_t launch_fold(const MassArgs& m, unsigned grid, cudaStream_t s) {
+    const int rows = m.a.max_q * m.a.group;
+    const dim3 g(grid), t(FOLD_WARPS * 32);
+    if (rows == 1) return launch_dependent(kv_mass_fold_kernel<1, BLOCKS>, g, t, 0, s, m);
+    if (rows == 4) return launch_dependent(kv_mass_fold_kernel<4, BLOCKS>, g, t, 0, s, m);
+    if (rows == 8) return launch_dependent(kv_mass_fold_kernel<8, BLOCKS>, g, t, 0, s, m);
+    return launch_dependent(kv_mass_fold_kernel<0, BLOCKS>, g, t, 0, s, m);
+}
+
 constexpr int SUM_THREADS = 128;
 __global__ void __launch_bounds__(SUM_THREADS) kv_mass_sum_kernel(MassArgs m, unsigned blocks) {
     pdl_launch_dependents();
@@ -149,6 +275,7 @@ __global__ void __launch_bounds__(SUM_THREADS) kv_mass_sum_kernel(MassArgs m, un
     const int64_t width = static_cast<int64_t>(m.tiles) * TOKENS;
     const float* p = m.sums + b * width + token;
     float sum = 0.0f;
+#pragma unroll 8
     for (int i = 0; i < m.parts; ++i) sum += p[i * a.batch * width];
     add_to_past(m, b, token, tokens, max(a.cu[b + 1] - a.cu[b], 0), sum);
 }
@@ -165,17 +292,30 @@ cudaError_t mass_as(const MassArgs& m, int type, int dtype, unsigned grid, cudaS
 }
 
 struct MassPlan {
+    bool keep;                     // the scores are kept
+    int blocks;                    // then: runs of 32 tokens that a lane of the second kernel takes
     int tiles, parts;
     size_t attention, bytes;       // of the workspace: the attention's part in front, and all
     bool fits;
 };
 MassPlan plan_mass(const sqap_kv_cache* c, int batch, int max_q, int max_len, int heads) {
     MassPlan p;
+    p.keep = few_rows(max_q, heads / c->kv_heads, c->head_dim);
+    p.attention = (sqap_kv_attention_workspace_bytes(c, batch, max_q, max_len, heads) + 15) / 16 * 16;
+    if (p.keep) {
+        const int64_t runs = max_len > 0 ? (max_len - 1) / 32 + 1 : 0;
+        p.blocks = size_product(batch, runs) > 8ll * sm_count() ? 4 : 1;
+        p.tiles = static_cast<int>((runs + p.blocks - 1) / p.blocks);
+        p.parts = 1;
+        const int64_t scores = size_product(batch, heads, max_len, max_q);
+        p.fits = size_product(batch, p.tiles) <= 0x7FFFFFFF && scores < int64_t{1} << 60;
+        p.bytes = p.attention + static_cast<size_t>(scores) * 4;
+        return p;
+    }
     p.tiles = max_len > 0 ? (max_len - 1) / TOKENS + 1 : 0;
-    const int64_t ctas = size_product(batch, p.tiles), want = ctas > 0 ? (2ll * sm_count() + ctas - 1) / ctas : 1;
+    const int64_t ctas = size_product(batch, p.tiles), want = ctas > 0 ? (16ll * sm_count() + ctas - 1) / ctas : 1;
     p.parts = static_cast<int>(want < c->kv_heads ? want : c->kv_heads);
     p.fits = size_product(ctas, p.parts) <= 0x7FFFFFFF;
-    p.attention = (sqap_kv_attention_workspace_bytes(c, batch, max_q, max_len, heads) + 15) / 16 * 16;
     p.bytes = p.attention + (p.parts > 1 ? static_cast<size_t>(p.parts) * batch * p.tiles * TOKENS * 4 : 0);
     return p;
 }
@@ -214,15 +354,21 @@ extern "C" sqap_status sqap_kv_attention_mass(const sqap_kv_cache* cache, const 
         if (workspace_bytes < p.bytes) return SQAP_ERR_NOMEM;
     }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    st = run_attention(m.a, cache->type, dtype, workspace, p.attention, s);
-    if (st != SQAP_OK || ldm == 0 || p.tiles == 0) return st;
+    const bool weigh = ldm > 0 && p.tiles > 0;
+    m.a.scores = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.attention);
+    st = run_attention(m.a, p.keep && weigh, cache->type, dtype, workspace, p.attention, s);
+    if (st != SQAP_OK || !weigh) return st;
     m.last_q = last_q;
     m.past = past;
     m.mass = mass;
     m.ldm = ldm;
     m.tiles = p.tiles;
     m.parts = p.parts;
-    m.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.attention);
+    if (p.keep) {
+        const unsigned grid = static_cast<unsigned>(static_cast<int64_t>(batch) * p.tiles);
+        return finish_launch(p.blocks > 1 ? launch_fold<4>(m, grid, s) : launch_fold<1>(m, grid, s));
+    }
+    m.sums = m.a.scores;
     st = finish_launch(mass_as(m, cache->type, dtype, static_cast<unsigned>(static_cast<int64_t>(batch) * p.tiles * p.parts), s));
     if (st != SQAP_OK || p.parts <= 1) return st;
     const unsigned blocks = static_cast<unsigned>((static_cast<int64_t>(p.tiles) * TOKENS + SUM_THREADS - 1) / SUM_THREADS);
