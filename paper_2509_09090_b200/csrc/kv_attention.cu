@@ -105,6 +105,7 @@ struct Plan {
 // one of 32768, 32 heads 42 / 57 / 57 (8 heads 21 all three). Three / four up to 1024 keys: 16 x 290, 32 heads 11.7 / 15.2, 16 x 1000 27.0 / 31.5.
 // Prompts: two rounds of CTAs where there is less than one, in pieces of 1024 keys at least: cut / whole, us, 256 rows (8 heads, groups of
 // 4) behind 3000 keys 44 / 63, behind 8000 76 / 114; 288 rows behind 4096 (32 heads) 59 / 62.
+int64_t least(int64_t x, int64_t y) { return x < y ? x : y; }
 Plan plan_rows(int64_t units, int kv_heads, int head_dim, int64_t rows, int64_t max_len, bool decode) {
     Plan p;
     p.decode = decode;
@@ -113,7 +114,6 @@ Plan plan_rows(int64_t units, int kv_heads, int head_dim, int64_t rows, int64_t 
     const int64_t ctas = size_product(units, kv_heads, p.tiles);
     const int64_t sms = sm_count();
     auto pieces = [&](int per_sm) { return ctas > 0 ? (sms * per_sm + ctas - 1) / ctas : 1; };
-    auto least = [](int64_t x, int64_t y) { return x < y ? x : y; };
     int64_t splits;
     if (p.decode) {
         const int64_t fill = least(pieces(max_len > 1024 ? 4 : 3), (max_len + 255) / 256), even = least(pieces(16), max_len / 1024);
@@ -157,21 +157,35 @@ Plan plan_window(int64_t batch, int kv_heads, int group, int head_dim, int64_t m
 // Shared prefixes: the rows of a group over its prefix, then those of each sequence over its own tokens. The pieces of both are cut on
 // the device, from the lengths that it finds; the plan only says how many there are.
 struct SharedPlan {
-    Plan prefix, own;
+    bool together;         // one launch of the register kernel over the prefix and the own tokens of a group's sequences
+    Plan prefix, own;      // `together`: prefix is its plan
     int prefix_parts;      // 0: there is no prefix
-    int parts;
+    bool join;             // the kernel of the own tokens joins the pieces of the prefix
+    int parts;             // pieces in the workspace
 };
-// Row tiles of a group up to which the register kernel takes the prefix.
-constexpr int PREFIX_DECODE_TILES = 3;
+// Tiles of a group's rows up to which the register kernel takes the group.
+constexpr int SHARED_TILES = 3;
 SharedPlan plan_shared(int kv_heads, int group, int head_dim, int64_t max_q, int64_t max_len, int64_t groups, int64_t max_group,
                        int64_t max_prefix) {
     SharedPlan p;
     const int64_t rows = max_q * group, together = rows * max_group;
     const int64_t own = max_len > max_prefix ? max_len - max_prefix : 1;
-    p.own = plan_rows(size_product(groups, max_group), kv_heads, head_dim, rows, own, rows <= decode_max_rows(head_dim));
-    p.prefix = plan_rows(groups, kv_heads, head_dim, together, max_prefix, together <= PREFIX_DECODE_TILES * decode_max_rows(head_dim));
+    const int64_t tile = decode_max_rows(head_dim);
+    p.together = together <= SHARED_TILES * tile;
+    if (p.together) {
+        const int64_t members = least(max_group, (together < tile ? together : tile) / rows + 1);
+        p.prefix = p.own = plan_rows(groups, kv_heads, head_dim, together, least(size_product(own, members) + max_prefix, 1 << 30), true);
+        p.prefix_parts = 0;
+        p.join = false;
+        p.parts = p.prefix.splits;
+        return p;
+    }
+    p.own = plan_rows(size_product(groups, max_group), kv_heads, head_dim, rows, own, rows <= tile);
+    p.prefix = plan_rows(groups, kv_heads, head_dim, together, max_prefix, false);
     p.prefix_parts = max_prefix > 0 ? p.prefix.splits : 0;
-    p.parts = p.prefix_parts + p.own.splits;
+    p.join = p.own.decode && p.own.splits == 1 && p.prefix_parts > 0;
+    p.parts = p.prefix_parts + (p.join ? 0 : p.own.splits);
+    if (p.join && p.parts < 2) p.parts = 2;      // a single one goes through the workspace too
     return p;
 }
 bool shared_fits(const sqap_kv_cache* c, int groups, int max_group, int max_q, int heads, const SharedPlan& p) {
@@ -346,13 +360,19 @@ extern "C" sqap_status sqap_kv_attention_shared(const sqap_kv_cache* cache, cons
     a.max_prefix = max_prefix;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int64_t places = static_cast<int64_t>(groups) * max_group;
+    if (p.together) {
+        st = launch(a, p.prefix, VIEW_SHARED, groups, cache->type, dtype, s);
+        if (st != SQAP_OK || a.parts <= 1) return st;
+        return combine(a, places, dtype, s);
+    }
     if (p.prefix_parts > 0) {
         st = launch(a, p.prefix, VIEW_PREFIX, groups, cache->type, dtype, s);
         if (st != SQAP_OK) return st;
     }
-    a.part0 = p.prefix_parts;
+    a.part0 = p.join ? 0 : p.prefix_parts;
+    a.join = p.join ? p.prefix_parts : 0;
     st = launch(a, p.own, VIEW_OWN, places, cache->type, dtype, s);
-    if (st != SQAP_OK || a.parts <= 1) return st;
+    if (st != SQAP_OK || a.parts <= 1 || p.join) return st;
     a.part0 = 0;
     return combine(a, places, dtype, s);
 }

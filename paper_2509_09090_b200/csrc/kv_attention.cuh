@@ -37,6 +37,7 @@ struct AttnArgs {
     float2* part_ml;       // the same without D: maximum and denominator
     int tiles;             // row tiles per (sequence, key/value head)
     int parts, part0;      // pieces of a row that are joined (1: the kernel writes the output itself), and the first of this launch
+    int join;              // VIEW_OWN: pieces of the prefix that the kernel joins with its rows' own tokens, and writes the output
     // views other than VIEW_ALL
     int window, sinks;     // VIEW_WINDOW
     const int32_t* cu_group;   // VIEW_PREFIX, VIEW_OWN: sequences of the groups
@@ -46,17 +47,20 @@ struct AttnArgs {
 };
 
 // What the rows of a launch look at: all (causal or not); the tokens of a window and the first ones; the prefix that the
-// sequences of a group share, rows of all of them together; the tokens of a sequence behind its group's prefix; all, and the
-// scores are kept (register kernel only).
-enum View { VIEW_ALL, VIEW_WINDOW, VIEW_PREFIX, VIEW_OWN, VIEW_SCORES };
+// sequences of a group share, rows of all of them together; the tokens of a sequence behind its group's prefix; both, rows of the
+// group together (register kernel only); all, and the scores are kept (register kernel only).
+enum View { VIEW_ALL, VIEW_WINDOW, VIEW_PREFIX, VIEW_OWN, VIEW_SHARED, VIEW_SCORES };
+// Rows of all sequences of a group together.
+template <int VIEW>
+constexpr bool by_group = VIEW == VIEW_PREFIX || VIEW == VIEW_SHARED;
 
 // Work of a CTA, from its index.
 struct Where {
     int b, h, split, tile;
     int row0, n_q;         // first row of the sequence, its query rows
     int tokens, len;       // its tokens, and how many of them are looked at (max_len at most)
-    int prefix;            // VIEW_PREFIX, VIEW_OWN: shared tokens
-    int members;           // VIEW_PREFIX: sequences of the group, from b on
+    int prefix;            // views that go by groups: shared tokens
+    int members;           // sequences of the group, from b on
 };
 __device__ __forceinline__ Where locate(const AttnArgs& a, unsigned id, int tiles) {
     Where w;
@@ -89,7 +93,7 @@ __device__ __forceinline__ int visible(const AttnArgs& a, const Where& w, int i)
 // A sequence or group that is not there has no rows.
 template <int VIEW>
 __device__ __forceinline__ Where locate_view(const AttnArgs& a, unsigned id, int tiles) {
-    if constexpr (VIEW != VIEW_PREFIX && VIEW != VIEW_OWN) return locate(a, id, tiles);
+    if constexpr (!by_group<VIEW> && VIEW != VIEW_OWN) return locate(a, id, tiles);
     Where w = {};
     if (tiles > 1) {
         w.tile = static_cast<int>(id % tiles);
@@ -111,7 +115,7 @@ __device__ __forceinline__ Where locate_view(const AttnArgs& a, unsigned id, int
     w.prefix = max(0, min(a.prefix[id], min(a.max_prefix, a.max_len)));
     if (first < 0 || w.b >= last) return w;
     w.members = min(last - first, a.max_group);
-    if (VIEW == VIEW_PREFIX) return w;
+    if (by_group<VIEW>) return w;
     w.row0 = a.cu[w.b];
     w.n_q = max(a.cu[w.b + 1] - w.row0, 0);
     w.tokens = max(a.lens[w.b], 0);
@@ -121,7 +125,7 @@ __device__ __forceinline__ Where locate_view(const AttnArgs& a, unsigned id, int
 // Query rows (query x head of the group of heads) of a CTA's sequence, or of its group's sequences, max_q queries for each.
 template <int VIEW>
 __device__ __forceinline__ int rows_of(const AttnArgs& a, const Where& w) {
-    if constexpr (VIEW == VIEW_PREFIX) return w.members * a.max_q * a.group;
+    if constexpr (by_group<VIEW>) return w.members * a.max_q * a.group;
     return (w.n_q < a.max_q ? w.n_q : a.max_q) * a.group;
 }
 // Row r of them.
@@ -137,14 +141,14 @@ __device__ __forceinline__ Row row_at(const AttnArgs& a, const Where& w, int row
     x.real = r < rows;
     if (!x.real) r = 0;
     x.b = w.b;
-    if constexpr (VIEW == VIEW_PREFIX) {
+    if constexpr (by_group<VIEW>) {
         const int per = a.max_q * a.group, member = r / per;
         r -= member * per;
         x.b += member;
     }
     x.i = r / a.group;
     x.head = w.h * a.group + r - x.i * a.group;
-    if constexpr (VIEW == VIEW_PREFIX) {
+    if constexpr (by_group<VIEW>) {
         x.at = 0;
         x.sees = 0;
         if (x.real) {
@@ -154,7 +158,7 @@ __device__ __forceinline__ Row row_at(const AttnArgs& a, const Where& w, int row
             Where own = w;
             own.n_q = n;
             own.tokens = max(a.lens[x.b], 0);
-            own.len = min(own.tokens, w.prefix);
+            own.len = min(own.tokens, VIEW == VIEW_PREFIX ? w.prefix : a.max_len);
             x.sees = x.real ? visible(a, own, x.i) : 0;
         }
     } else {
@@ -193,8 +197,17 @@ __device__ __forceinline__ Span span_of(const AttnArgs& a, const Where& w, int i
 // Keys of a piece of a history of `len` keys: of the same size for all, or (by groups) as even as tiles of 64 allow.
 template <int VIEW>
 __device__ __forceinline__ int chunk_of(const AttnArgs& a, int len) {
-    if constexpr (VIEW == VIEW_PREFIX || VIEW == VIEW_OWN) return a.splits > 1 && len > 0 ? ((len - 1) / a.splits / 64 + 1) * 64 : 64;
+    if constexpr (by_group<VIEW> || VIEW == VIEW_OWN) return a.splits > 1 && len > 0 ? ((len - 1) / a.splits / 64 + 1) * 64 : 64;
     return a.chunk;
+}
+
+// Whether the 16 tokens from `run` on hold one that some row sees, given the first token that its first row sees (sinks apart): the page of
+// others may no longer be the sequence's.
+template <int VIEW>
+__device__ __forceinline__ bool run_counts(const AttnArgs& a, int run, int from) {
+    if constexpr (VIEW == VIEW_WINDOW) return run + 15 >= from || run < a.sinks;
+    if constexpr (VIEW == VIEW_OWN) return run + 15 >= from;
+    return true;
 }
 
 __device__ __forceinline__ int64_t part_index(const AttnArgs& a, int b, int head, int i, int split) {
@@ -248,7 +261,7 @@ __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 x) { return _
 inline int decode_max_rows(int head_dim) { return head_dim == 256 ? 8 : 16; }
 // Rows of a CTA of the register kernel: all of its sequence, or a tile of its group's.
 inline int decode_row_tile(const AttnArgs& a, int view, int head_dim) {
-    const int64_t rows = static_cast<int64_t>(a.max_q) * a.group * (view == VIEW_PREFIX ? a.max_group : 1);
+    const int64_t rows = static_cast<int64_t>(a.max_q) * a.group * (view == VIEW_SHARED ? a.max_group : 1);
     return rows > 8 && head_dim != 256 ? 16 : 8;
 }
 constexpr int PREFILL_ROWS = 128, PREFILL_TC_ROWS = 256;   // query rows of a CTA's item

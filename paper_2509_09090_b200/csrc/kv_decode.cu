@@ -76,15 +76,43 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
 
     pdl_launch_dependents();
     pdl_wait();
-    const Where w = locate_view<VIEW>(a, blockIdx.x, VIEW == VIEW_PREFIX ? a.tiles : 1);
+    const Where w = locate_view<VIEW>(a, blockIdx.x, VIEW == VIEW_SHARED ? a.tiles : 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int G = a.group;
     const int rows_all = rows_of<VIEW>(a, w);      // row r: query r / G, head h G + r % G
-    const int r_first = VIEW == VIEW_PREFIX ? w.tile * 8 * NT : 0;
-    const int rows = VIEW == VIEW_PREFIX ? min(rows_all - r_first, 8 * NT) : rows_all;
+    const int r_first = VIEW == VIEW_SHARED ? w.tile * 8 * NT : 0;
+    const int rows = VIEW == VIEW_SHARED ? min(rows_all - r_first, 8 * NT) : rows_all;
     if (rows <= 0) return;
     const Span span = span_of<VIEW, STEP>(a, w, 0);
-    const int len = (VIEW == VIEW_PREFIX ? w.prefix : w.len) - span.gap;
+    // VIEW_SHARED: the keys are the prefix, then the own tokens of each sequence that has rows here, in runs of 16; lane 0 knows the
+    // prefix, lane s the s-th of the sequences: the run it begins with, its first token less 16 times that, and its last
+    int seg_run = 0x7FFFFFFF, seg_base = 0, seg_end = 0, seg0 = 0, runs = 0;
+    if constexpr (VIEW == VIEW_SHARED) {
+        const int per = a.max_q * G;
+        seg0 = r_first / per;
+        const int segments = (r_first + rows - 1) / per - seg0 + 2;
+        int mine = 0, first = 0;
+        if (lane == 0) {
+            seg_end = w.prefix;
+            mine = (w.prefix + 15) >> 4;
+        } else if (lane < segments) {
+            seg_end = min(max(a.lens[w.b + seg0 + lane - 1], 0), a.max_len);
+            first = w.prefix & ~15;
+            mine = seg_end > w.prefix ? (seg_end - first + 15) >> 4 : 0;
+        }
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
+        }
+        runs = __shfl_sync(0xffffffffu, upto, 31);
+        if (lane < segments) seg_run = upto - mine;
+        seg_base = first - 16 * (upto - mine);
+    }
+    auto segment_of = [&](int k) { return VIEW == VIEW_SHARED ? __popc(__ballot_sync(0xffffffffu, seg_run <= k >> 4)) - 1 : 0; };
+    auto token_of = [&](int k, int seg) { return VIEW == VIEW_SHARED ? __shfl_sync(0xffffffffu, seg_base, seg) + k : span.token(k); };
+    const int len = VIEW == VIEW_SHARED ? 16 * runs : w.len - span.gap;
     const int chunk = chunk_of<VIEW>(a, len);
     const int key0 = w.split * chunk;              // keys: tokens without the gap
     const int key1 = a.splits > 1 ? min(key0 + chunk, len) : len;
@@ -93,6 +121,7 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
     uint32_t qf[NT][KC][4][2];
     float fac[NT][2];                              // back-scaling of the rows of this lane's columns (2t, 2t + 1)
     int lim[NT][2], low[NT][2];                    // tokens that those rows may see: below lim, and from low on or below a.sinks
+                                                   // (VIEW_SHARED: low is the segment of the row's own tokens)
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const Row row = row_at<VIEW>(a, w, rows_all, r_first + 8 * n + g);
@@ -105,7 +134,7 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 uint4 u = make_uint4(0, 0, 0, 0);
-                if (VIEW != VIEW_PREFIX || real) u = __ldg(reinterpret_cast<const uint4*>(src + 64 * c + 16 * t) + i);
+                if (VIEW != VIEW_SHARED || real) u = __ldg(reinterpret_cast<const uint4*>(src + 64 * c + 16 * t) + i);
                 unpack8<T>(u, v[c] + 8 * i);
             }
 #pragma unroll
@@ -131,11 +160,11 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
             fac[n][e] = __shfl_sync(0xffffffffu, back, (2 * t + e) * 4) * a.scale_log2;
             const Row seen_by = row_at<VIEW>(a, w, rows_all, r_first + 8 * n + 2 * t + e);
             lim[n][e] = seen_by.sees;
-            low[n][e] = first_seen<VIEW>(a, w, seen_by.i);
+            low[n][e] = VIEW == VIEW_SHARED ? seen_by.b - w.b - seg0 + 1 : first_seen<VIEW>(a, w, seen_by.i);
         }
     }
     // the last row sees the most
-    const int lim_max = VIEW == VIEW_PREFIX ? len : visible(a, w, rows / G - 1) - span.gap;
+    const int lim_max = VIEW == VIEW_SHARED ? len : visible(a, w, rows / G - 1) - span.gap;
     const int end = a.c.pages > 0 ? min(key1, lim_max) : 0;
 
     float o[NT][MT][4];
@@ -152,6 +181,7 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
     const int per_token = a.max_q * G;
     float* scores = VIEW == VIEW_SCORES ? a.scores + (static_cast<int64_t>(w.b) * a.c.kv_heads + w.h) * a.max_len * per_token : nullptr;
     const int32_t* table = a.table + w.b * a.ldt;
+    const int from = first_seen<VIEW>(a, w, 0);
     const int shift = a.c.page_shift, mask = (1 << shift) - 1;
 
     // A step's loads are issued as soon as their registers are free: the next keys during this step's softmax, the next values
@@ -163,13 +193,15 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
     auto entries = [&](int k0) {
 #pragma unroll
         for (int u = 0; u < GROUPS; ++u) {
-            const int key = k0 + 16 * u, j = span.token(key) >> shift;
+            const int key = k0 + 16 * u, seg = segment_of(key), token = token_of(key, seg), j = token >> shift;
             entry[u] = -1;
-            if (key < end && j < a.ldt) entry[u] = __ldg(table + j);
+            if (key < end && j < a.ldt && run_counts<VIEW>(a, token, from)) entry[u] = __ldg(table + (VIEW == VIEW_SHARED && seg > 0 ? (seg0 + seg - 1) * a.ldt : 0) + j);
         }
     };
     // a page that does not exist is read as page 0 and masked
-    auto token_at = [&](int k0, int u) { return page_codes(a.c, max(page[u], 0), w.h) + (span.token(k0 + 16 * u) & mask); };
+    auto token_at = [&](int k0, int u) {
+        return page_codes(a.c, max(page[u], 0), w.h) + (token_of(k0 + 16 * u, segment_of(k0 + 16 * u)) & mask);
+    };
     auto load_keys = [&](int k0) {
 #pragma unroll
         for (int u = 0; u < GROUPS; ++u) {
@@ -255,33 +287,33 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
 #pragma unroll
         for (int u = 0; u < GROUPS; ++u) {
             const int base = k0 + 16 * u;
+            // the run's first token, and those of it that are the segment's: from .. until - 1
+            const int seg = segment_of(base), token0 = WHOLE ? base : token_of(base, seg);
+            const int begin = VIEW == VIEW_OWN || (VIEW == VIEW_SHARED && seg > 0) ? w.prefix : 0;
+            const int until = VIEW == VIEW_SHARED ? (base < end ? __shfl_sync(0xffffffffu, seg_end, seg) : 0) : end - base + token0;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int key = base + g + (e >> 1) * 8;
-                    bool seen;
-                    if (WHOLE) {
-                        seen = there[u] && key < min(lim[n][e & 1], end);
-                    } else {
-                        const int token = span.token(base) + g + (e >> 1) * 8;
-                        seen = there[u] && key < end && token < lim[n][e & 1];
-                        if (VIEW != VIEW_PREFIX) seen = seen && (token >= low[n][e & 1] || (VIEW == VIEW_WINDOW && token < a.sinks));
-                    }
+                    const int token = token0 + g + (e >> 1) * 8;
+                    bool seen = there[u] && token < min(lim[n][e & 1], until);
+                    if (VIEW == VIEW_SHARED) seen = seen && token >= begin && (seg == 0 || seg == low[n][e & 1]);
+                    if (VIEW == VIEW_OWN) seen = seen && token >= begin;
+                    if (VIEW == VIEW_WINDOW) seen = seen && (token >= low[n][e & 1] || token < a.sinks);
                     if (VIEW == VIEW_SCORES) {
                         sc[u][n][e] = seen ? sc[u][n][e] * (fac[n][e & 1] * this_ks[u]) : -INFINITY;
-                        if (key < end && 8 * n + 2 * t + (e & 1) < rows) scores[static_cast<int64_t>(key) * per_token + 8 * n + 2 * t + (e & 1)] = sc[u][n][e];
+                        if (token < end && 8 * n + 2 * t + (e & 1) < rows) scores[static_cast<int64_t>(token) * per_token + 8 * n + 2 * t + (e & 1)] = sc[u][n][e];
                         if (seen) sc[u][n][e] += lv[u];
                     } else {
                         sc[u][n][e] = seen ? fmaf(sc[u][n][e], fac[n][e & 1] * this_ks[u], lv[u]) : -INFINITY;
                     }
                     top[n][e & 1] = fmaxf(top[n][e & 1], sc[u][n][e]);
                 }
-            if (!there[u] || base + 16 > end) {
+            if (!there[u] || token0 + 16 > until || token0 < begin) {
                 // what lies behind the end of a history may be anything, not-a-numbers included: weight 0 is not enough
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (!there[u] || base + 2 * t + (i & 1) + (i >> 1) * 8 >= end)
+                    if (!there[u] || token0 + 2 * t + (i & 1) + (i >> 1) * 8 >= until || token0 + 2 * t + (i & 1) + (i >> 1) * 8 < begin)
 #pragma unroll
                         for (int q = 0; q < VB / 4; ++q) vw[u][i].w[q] = 0;
             }
@@ -382,8 +414,35 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
             for (int e = 0; e < 8; ++e) y[e] = fmaf(red_o[i][r][d + e], f, y[e]);
         }
         const Row row = row_at<VIEW>(a, w, rows_all, r_first + r);
-        if (VIEW == VIEW_PREFIX && !row.real) continue;
-        if (a.parts > 1) {
+        if (VIEW == VIEW_SHARED && !row.real) continue;
+        if (VIEW == VIEW_OWN && a.join > 0) {
+            // the pieces of the prefix are there: joined here
+            const int64_t at = part_index(a, row.b, row.head, row.i, 0);
+            float top = mm;
+            for (int s = 0; s < a.join; ++s) top = fmaxf(top, a.part_ml[at + s].x);
+            const float base = top == -INFINITY ? 0.0f : top, f = fast_exp2(mm - base);
+            ll *= f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] *= f;
+#pragma unroll 4
+            for (int s = 0; s < a.join; ++s) {
+                const float2 ml = a.part_ml[at + s];
+                const float c = fast_exp2(ml.x - base);
+                const float4* p = reinterpret_cast<const float4*>(a.part_o + (at + s) * D + d);
+                const float4 p0 = p[0], p1 = p[1];
+                ll = fmaf(ml.y, c, ll);
+                y[0] = fmaf(p0.x, c, y[0]);
+                y[1] = fmaf(p0.y, c, y[1]);
+                y[2] = fmaf(p0.z, c, y[2]);
+                y[3] = fmaf(p0.w, c, y[3]);
+                y[4] = fmaf(p1.x, c, y[4]);
+                y[5] = fmaf(p1.y, c, y[5]);
+                y[6] = fmaf(p1.z, c, y[6]);
+                y[7] = fmaf(p1.w, c, y[7]);
+            }
+            mm = top;
+        }
+        if (a.parts > 1 && !(VIEW == VIEW_OWN && a.join > 0)) {
             const int64_t at = part_index(a, row.b, row.head, row.i, w.split);
             if (d == 0) a.part_ml[at] = make_float2(mm, ll);
             float4* po = reinterpret_cast<float4*>(a.part_o + at * D + d);
@@ -428,10 +487,10 @@ cudaError_t launch_view(const AttnArgs& a, int type, int dtype, unsigned grid, c
 }  // namespace
 
 sqap_status launch_kv_decode(const AttnArgs& a, View view, int64_t units, int type, int dtype, cudaStream_t s) {
-    const unsigned grid = static_cast<unsigned>(units * a.c.kv_heads * a.splits * (view == VIEW_PREFIX ? a.tiles : 1));
+    const unsigned grid = static_cast<unsigned>(units * a.c.kv_heads * a.splits * (view == VIEW_SHARED ? a.tiles : 1));
     switch (view) {
         case VIEW_WINDOW: return finish_launch(launch_view<VIEW_WINDOW>(a, type, dtype, grid, s));
-        case VIEW_PREFIX: return finish_launch(launch_view<VIEW_PREFIX>(a, type, dtype, grid, s));
+        case VIEW_SHARED: return finish_launch(launch_view<VIEW_SHARED>(a, type, dtype, grid, s));
         case VIEW_OWN: return finish_launch(launch_view<VIEW_OWN>(a, type, dtype, grid, s));
         case VIEW_SCORES: return finish_launch(launch_view<VIEW_SCORES>(a, type, dtype, grid, s));
         default: return finish_launch(launch_view<VIEW_ALL>(a, type, dtype, grid, s));

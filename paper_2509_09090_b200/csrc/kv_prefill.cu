@@ -96,10 +96,11 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_kernel(AttnArgs a) {
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
 
     const int32_t* table = a.table + w.b * a.ldt;
+    const int from = first_seen<VIEW>(a, w, r_first / G);
     const int shift = a.c.page_shift, mask = (1 << shift) - 1;
     auto page_at = [&](int key) {
-        const int j = span.token(key) >> shift;
-        return key < end && j < a.ldt ? checked_page(a.c, __ldg(table + j)) : -1;
+        const int token = span.token(key), j = token >> shift;
+        return key < end && j < a.ldt && run_counts<VIEW>(a, token & ~15, from) ? checked_page(a.c, __ldg(table + j)) : -1;
     };
     uint4 kc[CHUNKS], vc[CHUNKS];
     float next_ks = 0.0f, next_vs = 0.0f;
@@ -111,7 +112,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_kernel(AttnArgs a) {
             const int key = k0 + row;
             const int page = page_at(key);
             kc[i] = vc[i] = make_uint4(0, 0, 0, 0);       // behind the end: zero codes, whatever lies there
-            if (page >= 0) {
+            // (VIEW_OWN: what the sequence's own page holds in front of its own tokens may be anything)
+            if (page >= 0 && (VIEW != VIEW_OWN || span.token(key) >= from)) {
                 const int64_t at = (page_codes(a.c, page, w.h) + (span.token(key) & mask)) * D + col;
                 kc[i] = __ldg(reinterpret_cast<const uint4*>(a.c.k.codes + at));
                 vc[i] = __ldg(reinterpret_cast<const uint4*>(a.c.v.codes + at));

@@ -391,6 +391,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
             int h, k0, end;            // tokens k0 .. of a sequence of `end` tokens that count; end = 0: no more tiles
             int row0, r_first, rows;   // rows > 0: the first tile of an item, whose queries are wanted
             int b;                     // its sequence (the group's first, VIEW_PREFIX)
+            int from;                  // first token that the item's first row sees
         };
         unsigned id = blockIdx.x;
         Tile then = {};
@@ -408,6 +409,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
                 then.k0 = span.token(x.key0);
                 then.end = span.token(x.end - 1) + 1;
                 then.b = x.w.b;
+                then.from = first_seen<VIEW>(a, x.w, x.r_first / G);
                 then.row0 = x.w.row0;
                 then.r_first = x.r_first;
                 then.rows = x.rows;
@@ -428,14 +430,15 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
         // The table entry as it is; checked when it is used, so that nothing waits for it here.
         auto entry_of = [&](const Tile& t) {
             const int key = t.k0 + row, j = key >> shift;
-            return key < t.end && j < a.ldt ? __ldg(t.table + j) : -1;
+            return key < t.end && j < a.ldt && run_counts<VIEW>(a, key & ~15, t.from) ? __ldg(t.table + j) : -1;
         };
         // Place of this thread's codes in the cache; -1 behind the end or where there is no page.
         const uint32_t page_bytes = static_cast<uint32_t>(a.c.kv_heads * D) << shift;      // 2^31 at most
         auto place_of = [&](const Tile& t, int entry) {
             const int64_t at = static_cast<int64_t>(static_cast<uint64_t>(static_cast<uint32_t>(entry)) * page_bytes) +
                                (((static_cast<uint32_t>(t.h) << shift) + ((t.k0 + row) & mask)) * D + (tid & 3) * 16);
-            return checked_page(a.c, entry) < 0 ? -1 : at;
+            // (VIEW_OWN: what the sequence's own page holds in front of its own tokens may be anything)
+            return checked_page(a.c, entry) < 0 || (VIEW == VIEW_OWN && t.k0 + row < t.from) ? -1 : at;
         };
         auto fetch = [&](const uint8_t* codes, int64_t place, uint4 (&to)[BLOCKS]) {
 #pragma unroll

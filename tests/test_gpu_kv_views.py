@@ -144,17 +144,20 @@ def test_window_more_queries_than_tokens(D, new):
     check_window(s, [new, new, new], 4, "fp16", 7, 2)
 
 
-@pytest.mark.parametrize("D,new", [(64, 1), (128, 1), (128, 70), (256, 1), (256, 20)])
-def test_window_does_not_need_the_pages_outside(D, new):
-    """Pages that hold neither the window's tokens nor the sinks' may have been given up: same bits, whatever their numbers are now."""
-    n, window, sinks, P = 1500, 200, 20, 16
+@pytest.mark.parametrize("D,new,P", [(64, 1, 16), (128, 1, 16), (128, 3, 64), (128, 70, 16), (64, 200, 32), (256, 1, 32), (256, 20, 16)])
+@pytest.mark.parametrize("window,sinks", [(200, 20), (37, 0), (64, 16)])
+def test_window_does_not_need_the_pages_outside(D, new, P, window, sinks):
+    """Pages that hold neither the window's tokens nor the sinks' may have been given up: same bits, whatever their numbers are now,
+    pages of not-a-numbers among them."""
+    n = 1501
     s = Setup([n], 2, D, P, R.E4M3, seed=D + new, nan_behind=True)
+    spare = next(i for i in range(s.pages) if i not in s.table)
     got = []
-    for hole in (None, -1, s.pages + 5):
+    for hole in (None, -1, s.pages + 5, spare):
         qs = Queries(s, [new], 4, "bf16")
         table = s.table.copy()
         if hole is not None:
-            table[0, (sinks + 63) // 64 * 64 // P:(n - new - window) // 64 * 64 // P] = hole
+            table[0, -(-sinks // P):(n - new + 1 - window) // P] = hole
         run_window(s, qs, [new], window, sinks, [n], table=ints(table))
         got.append(qs.results([(qs.cu[0], qs.cu[-1])]))
     for o, l in got[1:]:
@@ -190,7 +193,7 @@ def test_window_without_lse_and_without_work():
 
 class Group:
     """Sequences of groups (sizes, prefixes); own[b] tokens behind the prefix of sequence b. The pages of the prefix are missing from all
-    rows of the table but the first of each group."""
+    rows of the table but the first of each group, and what the page in which a prefix ends holds of it is no number in theirs."""
 
     def __init__(self, sizes, prefixes, own, H, D, P, kind, seed=0, lens=None):
         self.first = np.concatenate([[0], np.cumsum(sizes)])
@@ -200,6 +203,12 @@ class Group:
         self.table = self.s.table.copy()
         for g, n in enumerate(sizes):
             self.table[self.first[g] + 1:self.first[g] + n, :prefixes[g] // P] = -1
+            for b in range(self.first[g] + 1, self.first[g] + n):
+                page = self.table[b, prefixes[g] // P]
+                if page >= 0:
+                    for a in "kv":
+                        self.s.raw[a][page, :, :prefixes[g] % P] = 0x7F
+        self.s.to_device()
 
     def tokens(self, b, max_prefix):
         """What sequence b is made of: the group's first tokens, then its own."""
@@ -278,6 +287,9 @@ def test_shared_limits_drop_work_and_move_nothing(D, copies):
     gr.table = gr.s.table.copy()
     shared = [gr.s.table[1, :2]]
     gr.table[2:copies + 1, :2] = shared[0]                  # beyond max_prefix every sequence reads its own entries
+    for a in "kv":
+        gr.s.raw[a][gr.s.raw[a] == 0x7F] = 0x31
+    gr.s.to_device()
     check_shared(gr, new, 2, "fp16", max_prefix=100)
     check_shared(gr, new, 2, "fp16", max_prefix=0)
     gr.prefix = gr.prefix[1:2]
