@@ -1,12 +1,12 @@
 // Which tokens of a sequence stay in the cache: the last ones, the first ones, and of the rest those with the largest weight.
 //
 // One CTA takes one sequence. The weights are ordered as whole numbers; the m-th largest is found by narrowing the interval
-// that holds it: a histogram of BINS equal parts of the interval (at first from the smallest to the largest weight, so that neither
-// zeros nor a narrow spread crowd a bin), the bin that holds the m-th, and again within it: two or three rounds for
-// 32 bits. Equal weights are told apart by their place. A thread owns consecutive tokens, so that one sum over the CTA in the
-// order of the threads gives the places in the list.
+// that holds it: a histogram of BINS equal parts of the interval (at first from the smallest to the largest weight), the bin that
+// holds the m-th, and again within it: two or three rounds for 32 bits. Equal weights are told apart by their place. A
+// warp owns runs of 32 consecutive tokens, a lane one of each: its votes give a token's place within the run, one sum over
+// the runs in front of it the rest, and the lanes that write the list write side by side.
 // Bounded by latency: 4 bytes a token are read once (up to 16384 tokens are kept in registers, longer ones read again each
-// round), and some eight sums over the CTA follow one another.
+// round), and some seven steps of the whole CTA follow one another.
 #include "kv.cuh"
 
 namespace sqap {
@@ -27,48 +27,25 @@ struct EvictArgs {
     int32_t* n_kept;
 };
 
-// Order of the numbers as whole numbers from 1 on; -0 = 0; what is not a number comes in front of all.
+// Order of the numbers as whole numbers; -0 = 0; 1 for what is not a number, in front of all.
 __device__ __forceinline__ uint32_t order_of(float f) {
-    if (!(f == f)) return 0;
+    if (!(f == f)) return 1;
     const uint32_t b = __float_as_uint(f + 0.0f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// Sum of x over the threads in front of this one, and over all; a call uses the other half of `part` than the one before.
-template <int THREADS>
-__device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t (&part)[2][THREADS / 32], int& turn, uint32_t* all) {
-    constexpr int WARPS = THREADS / 32;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    uint32_t y = x;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t z = __shfl_up_sync(0xffffffffu, y, o);
-        if (lane >= o) y += z;
-    }
-    if (lane == 31) part[turn][warp] = y;
-    __syncthreads();
-    uint32_t w = lane < WARPS ? part[turn][lane] : 0;
-    turn ^= 1;
-#pragma unroll
-    for (int o = 1; o < WARPS; o <<= 1) {
-        const uint32_t z = __shfl_up_sync(0xffffffffu, w, o);
-        if (lane >= o) w += z;
-    }
-    *all = __shfl_sync(0xffffffffu, w, WARPS - 1);
-    const uint32_t front = __shfl_sync(0xffffffffu, w, warp > 0 ? warp - 1 : 0);
-    return y - x + (warp > 0 ? front : 0);
-}
-
-// EACH consecutive tokens a thread and round; longer sequences than THREADS x EACH take several rounds.
+// EACH tokens a thread and round; longer sequences than THREADS x EACH take several rounds.
 template <int THREADS, int EACH>
 __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
-    constexpr int BINS = 2 * THREADS, WARPS = THREADS / 32;
+    constexpr int BINS = 2 * THREADS, WARPS = THREADS / 32, RUNS = EACH * WARPS;
+    static_assert(THREADS * EACH < 65536 && RUNS % 32 == 0, "two counts to a word, runs shared out to a warp");
     __shared__ uint32_t bins[BINS];
-    __shared__ uint32_t part[2][WARPS], least[WARPS], most[WARPS];
+    __shared__ uint32_t part[WARPS], least[WARPS], most[WARPS];
     __shared__ uint32_t found[3];        // the bin, how many are above it, how many in it
+    __shared__ uint32_t front[RUNS + 1]; // of each run of 32 tokens: those in front of it that stay, and (upper half) that are at the border
     pdl_launch_dependents();
     pdl_wait();
-    const int i = blockIdx.x, row = a.src[i], tid = threadIdx.x, lane = tid & 31;
+    const int i = blockIdx.x, row = a.src[i], tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const bool there = row >= 0 && row < a.rows;
     const int64_t held = a.ldm < a.max_len ? a.ldm : a.max_len;
     int len = there ? a.lens[row] : 0;
@@ -82,71 +59,62 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
     const uint32_t wanted = static_cast<uint32_t>(keep - recent - first);
     const float* mass = a.mass + (there ? row : 0) * a.ldm;
     const int rounds = (len + THREADS * EACH - 1) / (THREADS * EACH);
-    float x[EACH];
+    auto token_of = [&](int r, int e) { return (r * EACH + e) * THREADS + tid; };
+    uint32_t order[EACH];                // 0: not chosen from
     auto load = [&](int r) {
-        const int t0 = (r * THREADS + tid) * EACH;
+        float x[EACH];
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) x[e] = t0 + e < len ? mass[t0 + e] : 0.0f;
+        for (int e = 0; e < EACH; ++e) x[e] = token_of(r, e) < len ? mass[token_of(r, e)] : 0.0f;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) order[e] = token_of(r, e) >= first && token_of(r, e) < to ? order_of(x[e]) : 0;
     };
-    // f(token, order) for the tokens that are chosen from
     auto each = [&](auto f) {
         for (int r = 0; r < rounds; ++r) {
             if (rounds > 1) load(r);
-            const int t0 = (r * THREADS + tid) * EACH;
 #pragma unroll
-            for (int e = 0; e < EACH; ++e)
-                if (t0 + e >= first && t0 + e < to) f(t0 + e, order_of(x[e]));
+            for (int e = 0; e < EACH; ++e) f(order[e]);
         }
     };
     if (rounds == 1) load(0);
 
     // border: orders above it stay, of those equal to it the first `ties` in their places
-    uint32_t border = 0, ties = 0;
-    if (wanted == static_cast<uint32_t>(to - first)) {
-        ties = wanted;                   // all of them: no order is below 0
-    } else if (wanted == 0) {
-        border = 0xFFFFFFFFu;
-    } else {
+    uint32_t border = 0xFFFFFFFFu, ties = 0;
+    if (wanted > 0) {
         uint32_t lo = 0xFFFFFFFFu, hi = 0;
-        each([&](int, uint32_t k) {
-            lo = min(lo, k);
+        each([&](uint32_t k) {
+            lo = min(lo, k - 1);         // 0 comes out on top
             hi = max(hi, k);
         });
         lo = __reduce_min_sync(0xffffffffu, lo);
         hi = __reduce_max_sync(0xffffffffu, hi);
         if (lane == 0) {
-            least[tid >> 5] = lo;
-            most[tid >> 5] = hi;
+            least[warp] = lo;
+            most[warp] = hi;
         }
         __syncthreads();
-        lo = least[lane < WARPS ? lane : 0];
-        hi = most[lane < WARPS ? lane : 0];
-        lo = __reduce_min_sync(0xffffffffu, lo);
-        hi = __reduce_max_sync(0xffffffffu, hi);
+        lo = __reduce_min_sync(0xffffffffu, least[lane < WARPS ? lane : 0]) + 1;
+        hi = __reduce_max_sync(0xffffffffu, most[lane < WARPS ? lane : 0]);
         uint32_t left = wanted;          // of the orders in lo .. hi, the left-th largest is the border
         for (;;) {
-            // parts of 2^shift orders, fewer than BINS of them (shift 0 once the interval is that short)
+            // parts of 2^shift orders, at most BINS of them (shift 0 once the interval is that short)
             const int width = 32 - __clz(hi - lo), shift = max(0, width - (31 - __clz(BINS)));
             for (int b = tid; b < BINS; b += THREADS) bins[b] = 0;
             __syncthreads();
-            each([&](int, uint32_t k) {
+            each([&](uint32_t k) {
                 if (k >= lo && k <= hi) atomicAdd(&bins[(k - lo) >> shift], 1u);
             });
             __syncthreads();
             // thread t looks at bins BINS - 1 - 2t and the one below it: the sums run from the largest orders down
             const uint32_t up = bins[BINS - 1 - 2 * tid], down = bins[BINS - 2 - 2 * tid];
-            const int lane_warp = tid >> 5;
             uint32_t y = up + down;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const uint32_t z = __shfl_up_sync(0xffffffffu, y, o);
                 if (lane >= o) y += z;
             }
-            if (lane == 31) part[0][lane_warp] = y;
+            if (lane == 31) part[warp] = y;
             __syncthreads();
-            uint32_t w = lane < WARPS ? part[0][lane] : 0;
-            w = __reduce_add_sync(0xffffffffu, lane < lane_warp ? w : 0u);
-            const uint32_t above = w + y - up - down;
+            const uint32_t above = __reduce_add_sync(0xffffffffu, lane < warp ? part[lane] : 0u) + y - up - down;
             if (above < left && left <= above + up) {
                 found[0] = BINS - 1 - 2 * tid;
                 found[1] = above;
@@ -161,9 +129,8 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
             left -= found[1];
             lo += found[0] << shift;
             hi = min(hi, lo + ((1u << shift) - 1u));
-            if (left == in_bin) {        // all of the bin stay
-                border = lo;
-                ties = 0xFFFFFFFFu;
+            if (left == in_bin) {        // all of the bin stay: from lo >= 1 on
+                border = lo - 1;
                 break;
             }
             if (shift == 0) {
@@ -172,52 +139,59 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
                 break;
             }
         }
-        if (ties == 0xFFFFFFFFu) {       // from `border` on: everything above border - 1 (orders of numbers that are chosen from start at 0)
-            if (border > 0) {
-                --border;
-                ties = 0;
-            }
-        }
     }
 
     int32_t* kept = a.kept + i * a.ldkept;
     const int dst = a.dst ? a.dst[i] : -1;
     float* carry = dst >= 0 && dst < a.rows ? a.mass + dst * a.ldm : nullptr;
-    uint32_t ties_before = 0, kept_before = 0;
-    int turn = 1;                        // part[0] was read last
+    uint32_t kept_before = 0, ties_before = 0;
     for (int r = 0; r < rounds; ++r) {
         if (rounds > 1) load(r);
-        const int t0 = (r * THREADS + tid) * EACH;
-        uint32_t equal = 0, stays = 0;   // bits
+        uint32_t stays[EACH], equal[EACH];       // votes of the run
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
-            const int t = t0 + e;
-            if (t >= len) continue;
-            if (t < first || t >= to) {
-                stays |= 1u << e;
-                continue;
+            const int t = token_of(r, e);
+            stays[e] = __ballot_sync(0xffffffffu, t < len && (t < first || t >= to || order[e] > border));
+            equal[e] = __ballot_sync(0xffffffffu, ties > 0 && order[e] == border);
+            if (lane == 0) front[e * WARPS + warp] = __popc(stays[e]) | __popc(equal[e]) << 16;
+        }
+        __syncthreads();
+        if (warp == 0) {
+            uint32_t mine[RUNS / 32], sum = 0;
+#pragma unroll
+            for (int x = 0; x < RUNS / 32; ++x) {
+                mine[x] = front[lane * (RUNS / 32) + x];
+                sum += mine[x];
             }
-            const uint32_t k = order_of(x[e]);
-            if (k > border) stays |= 1u << e;
-            if (k == border) equal |= 1u << e;
-        }
-        uint32_t all;
-        if (ties > 0) {
-            uint32_t place = ties_before + sum_before<THREADS>(__popc(equal), part, turn, &all);
-            ties_before += all;
+            uint32_t y = sum;
 #pragma unroll
-            for (int e = 0; e < EACH; ++e)
-                if (equal >> e & 1u && place++ < ties) stays |= 1u << e;
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t z = __shfl_up_sync(0xffffffffu, y, o);
+                if (lane >= o) y += z;
+            }
+            uint32_t at = y - sum;
+#pragma unroll
+            for (int x = 0; x < RUNS / 32; ++x) {
+                front[lane * (RUNS / 32) + x] = at;
+                at += mine[x];
+            }
+            if (lane == 31) front[RUNS] = y;
         }
-        uint32_t place = kept_before + sum_before<THREADS>(__popc(stays), part, turn, &all);
-        kept_before += all;
+        __syncthreads();
+        const uint32_t under = (1u << lane) - 1u;
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
-            if (!(stays >> e & 1u)) continue;
-            kept[place] = t0 + e;
-            if (carry) carry[place] = x[e];
-            ++place;
+            const uint32_t f = front[e * WARPS + warp];
+            const uint32_t ties_here = ties_before + (f >> 16), ties_mine = ties_here + __popc(equal[e] & under);
+            const bool stay = (stays[e] >> lane & 1u) || ((equal[e] >> lane & 1u) && ties_mine < ties);
+            if (!stay) continue;
+            const uint32_t place = kept_before + (f & 0xFFFFu) + __popc(stays[e] & under) + min(ties_mine, ties);
+            kept[place] = token_of(r, e);
+            if (carry) carry[place] = mass[token_of(r, e)];
         }
+        kept_before += front[RUNS] & 0xFFFFu;
+        ties_before += front[RUNS] >> 16;
+        __syncthreads();                         // `front` is written again
     }
     if (tid == 0) a.n_kept[i] = keep;
     for (int64_t p = keep + tid; p < a.ldkept; p += THREADS) kept[p] = -1;
