@@ -38,14 +38,15 @@ __device__ __forceinline__ uint32_t order_of(float f) {
 template <int THREADS, int EACH>
 __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
     constexpr int BINS = 2 * THREADS, WARPS = THREADS / 32, RUNS = EACH * WARPS;
-    static_assert(THREADS * EACH < 65536 && RUNS % 32 == 0, "two counts to a word, runs shared out to a warp");
+    static_assert(THREADS * EACH < 65536 && RUNS % 32 == 0, "two counts to a word, runs shared out to whole warps");
     __shared__ uint32_t bins[BINS];
     __shared__ uint32_t part[WARPS], least[WARPS], most[WARPS];
     __shared__ uint32_t found[3];        // the bin, how many are above it, how many in it
-    __shared__ uint32_t front[RUNS + 1]; // of each run of 32 tokens: those in front of it that stay, and (upper half) that are at the border
+    __shared__ uint32_t front[RUNS];     // of each run of 32 tokens: those in front of it that stay, and (upper half) that are at the border
+    __shared__ uint16_t list[THREADS * EACH];
     pdl_launch_dependents();
     pdl_wait();
-    const int i = blockIdx.x, row = a.src[i], tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int i = blockIdx.x, row = a.src[i], dst = a.dst ? a.dst[i] : -1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const bool there = row >= 0 && row < a.rows;
     const int64_t held = a.ldm < a.max_len ? a.ldm : a.max_len;
     int len = there ? a.lens[row] : 0;
@@ -142,56 +143,78 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
     }
 
     int32_t* kept = a.kept + i * a.ldkept;
-    const int dst = a.dst ? a.dst[i] : -1;
     float* carry = dst >= 0 && dst < a.rows ? a.mass + dst * a.ldm : nullptr;
-    uint32_t kept_before = 0, ties_before = 0;
+    uint32_t placed = 0, ties_before = 0;
     for (int r = 0; r < rounds; ++r) {
         if (rounds > 1) load(r);
-        uint32_t stays[EACH], equal[EACH];       // votes of the run
+        uint32_t votes[EACH];                    // of the run: who stays, ties apart
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
             const int t = token_of(r, e);
-            stays[e] = __ballot_sync(0xffffffffu, t < len && (t < first || t >= to || order[e] > border));
-            equal[e] = __ballot_sync(0xffffffffu, ties > 0 && order[e] == border);
-            if (lane == 0) front[e * WARPS + warp] = __popc(stays[e]) | __popc(equal[e]) << 16;
+            votes[e] = __ballot_sync(0xffffffffu, t < len && (t < first || t >= to || order[e] > border));
+            if (lane == 0) front[e * WARPS + warp] = __popc(votes[e]);
+        }
+        if (ties > 0) {
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                const uint32_t equal = __ballot_sync(0xffffffffu, order[e] == border);
+                if (lane == 0) front[e * WARPS + warp] += __popc(equal) << 16;
+            }
         }
         __syncthreads();
-        if (warp == 0) {
-            uint32_t mine[RUNS / 32], sum = 0;
+        // sums in front of each run: RUNS / THREADS of them a thread, or one for some of the threads
+        constexpr int SUMMING = RUNS < THREADS ? RUNS : THREADS, MINE = RUNS / SUMMING;
+        uint32_t mine[MINE], sum = 0, y = 0;
+        if (tid < SUMMING) {
 #pragma unroll
-            for (int x = 0; x < RUNS / 32; ++x) {
-                mine[x] = front[lane * (RUNS / 32) + x];
+            for (int x = 0; x < MINE; ++x) {
+                mine[x] = front[tid * MINE + x];
                 sum += mine[x];
             }
-            uint32_t y = sum;
+            y = sum;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const uint32_t z = __shfl_up_sync(0xffffffffu, y, o);
                 if (lane >= o) y += z;
             }
-            uint32_t at = y - sum;
+            if (lane == 31) part[warp] = y;
+        }
+        __syncthreads();
+        const uint32_t in_part = lane < SUMMING / 32 ? part[lane] : 0u;
+        const uint32_t all = __reduce_add_sync(0xffffffffu, in_part);
+        uint32_t at = __reduce_add_sync(0xffffffffu, lane < warp ? in_part : 0u) + y - sum;
+        if (tid < SUMMING) {
 #pragma unroll
-            for (int x = 0; x < RUNS / 32; ++x) {
-                front[lane * (RUNS / 32) + x] = at;
+            for (int x = 0; x < MINE; ++x) {
+                front[tid * MINE + x] = at;
                 at += mine[x];
             }
-            if (lane == 31) front[RUNS] = y;
         }
         __syncthreads();
         const uint32_t under = (1u << lane) - 1u;
+        const uint32_t ties_left = ties - min(ties_before, ties);
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
             const uint32_t f = front[e * WARPS + warp];
-            const uint32_t ties_here = ties_before + (f >> 16), ties_mine = ties_here + __popc(equal[e] & under);
-            const bool stay = (stays[e] >> lane & 1u) || ((equal[e] >> lane & 1u) && ties_mine < ties);
-            if (!stay) continue;
-            const uint32_t place = kept_before + (f & 0xFFFFu) + __popc(stays[e] & under) + min(ties_mine, ties);
-            kept[place] = token_of(r, e);
-            if (carry) carry[place] = mass[token_of(r, e)];
+            bool stay = votes[e] >> lane & 1u;
+            uint32_t ties_mine = 0;
+            if (ties > 0) {
+                const uint32_t equal = __ballot_sync(0xffffffffu, order[e] == border);
+                ties_mine = min((f >> 16) + __popc(equal & under), ties_left);
+                stay = stay || (order[e] == border && ties_mine < ties_left);
+            }
+            if (stay) list[(f & 0xFFFFu) + __popc(votes[e] & under) + ties_mine] = static_cast<uint16_t>(e * THREADS + tid);
         }
-        kept_before += front[RUNS] & 0xFFFFu;
-        ties_before += front[RUNS] >> 16;
-        __syncthreads();                         // `front` is written again
+        __syncthreads();
+        const int n = static_cast<int>((all & 0xFFFFu) + min(all >> 16, ties_left));
+        for (int p = tid; p < n; p += THREADS) {
+            const int t = r * THREADS * EACH + list[p];
+            kept[placed + p] = t;
+            if (carry) carry[placed + p] = __ldg(mass + t);      // no row is both read and written
+        }
+        placed += n;
+        ties_before += all >> 16;
+        __syncthreads();                         // `front` and `list` are written again
     }
     if (tid == 0) a.n_kept[i] = keep;
     for (int64_t p = keep + tid; p < a.ldkept; p += THREADS) kept[p] = -1;
