@@ -122,6 +122,7 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
     float fac[NT][2];                              // back-scaling of the rows of this lane's columns (2t, 2t + 1)
     int lim[NT][2], low[NT][2];                    // tokens that those rows may see: below lim, and from low on or below a.sinks
                                                    // (VIEW_SHARED: low is the segment of the row's own tokens)
+    int lim_all = 0x7FFFFFFF, low_all = 0;         // tokens that all rows see: below lim_all, from low_all on
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const Row row = row_at<VIEW>(a, w, rows_all, r_first + 8 * n + g);
@@ -161,8 +162,14 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
             const Row seen_by = row_at<VIEW>(a, w, rows_all, r_first + 8 * n + 2 * t + e);
             lim[n][e] = seen_by.sees;
             low[n][e] = VIEW == VIEW_SHARED ? seen_by.b - w.b - seg0 + 1 : first_seen<VIEW>(a, w, seen_by.i);
+            if (seen_by.real) {
+                lim_all = min(lim_all, lim[n][e]);
+                low_all = max(low_all, low[n][e]);
+            }
         }
     }
+    lim_all = __reduce_min_sync(0xffffffffu, lim_all);
+    low_all = __reduce_max_sync(0xffffffffu, low_all);
     // the last row sees the most
     const int lim_max = VIEW == VIEW_SHARED ? len : visible(a, w, rows / G - 1) - span.gap;
     const int end = a.c.pages > 0 ? min(key1, lim_max) : 0;
@@ -277,13 +284,10 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
             iv[u] = fast_exp2(-lv[u]);             // the reciprocal of what lv stands for: the weights use lv
         }
         if (more) load_keys(k0 + WARPS * STEP);
-        // scale, mask, maximum
+        // scale, mask, maximum of what this lane holds
         float top[NT][2];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            top[n][0] = m[n][0];
-            top[n][1] = m[n][1];
-        }
+        for (int n = 0; n < NT; ++n) top[n][0] = top[n][1] = -INFINITY;
 #pragma unroll
         for (int u = 0; u < GROUPS; ++u) {
             const int base = k0 + 16 * u;
@@ -291,24 +295,44 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
             const int seg = segment_of(base), token0 = WHOLE ? base : token_of(base, seg);
             const int begin = VIEW == VIEW_OWN || (VIEW == VIEW_SHARED && seg > 0) ? w.prefix : 0;
             const int until = VIEW == VIEW_SHARED ? (base < end ? __shfl_sync(0xffffffffu, seg_end, seg) : 0) : end - base + token0;
+            // most runs are seen by all rows as they are
+            const bool plain = there[u] && token0 + 16 <= min(until, lim_all) && (VIEW != VIEW_OWN || token0 >= begin) && (VIEW != VIEW_SHARED || seg == 0) &&
+                               (VIEW != VIEW_WINDOW || token0 >= low_all);
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n) {
+                const float f[2] = {fac[n][0] * this_ks[u], fac[n][1] * this_ks[u]};
+                if (VIEW == VIEW_SCORES) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int token = token0 + g + (e >> 1) * 8;
-                    bool seen = there[u] && token < min(lim[n][e & 1], until);
-                    if (VIEW == VIEW_SHARED) seen = seen && token >= begin && (seg == 0 || seg == low[n][e & 1]);
-                    if (VIEW == VIEW_OWN) seen = seen && token >= begin;
-                    if (VIEW == VIEW_WINDOW) seen = seen && (token >= low[n][e & 1] || token < a.sinks);
-                    if (VIEW == VIEW_SCORES) {
-                        sc[u][n][e] = seen ? sc[u][n][e] * (fac[n][e & 1] * this_ks[u]) : -INFINITY;
-                        if (token < end && 8 * n + 2 * t + (e & 1) < rows) scores[static_cast<int64_t>(token) * per_token + 8 * n + 2 * t + (e & 1)] = sc[u][n][e];
-                        if (seen) sc[u][n][e] += lv[u];
-                    } else {
-                        sc[u][n][e] = seen ? fmaf(sc[u][n][e], fac[n][e & 1] * this_ks[u], lv[u]) : -INFINITY;
+                    for (int e = 0; e < 4; ++e) sc[u][n][e] *= f[e & 1];
+                    if (!plain) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!there[u] || token0 + g + (e >> 1) * 8 >= min(lim[n][e & 1], until)) sc[u][n][e] = -INFINITY;
                     }
-                    top[n][e & 1] = fmaxf(top[n][e & 1], sc[u][n][e]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int token = token0 + g + (e >> 1) * 8, r = 8 * n + 2 * t + (e & 1);
+                        if (token < end && r < rows) scores[static_cast<int64_t>(token) * per_token + r] = sc[u][n][e];
+                        sc[u][n][e] += lv[u];
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sc[u][n][e] = fmaf(sc[u][n][e], f[e & 1], lv[u]);
+                    if (!plain) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int token = token0 + g + (e >> 1) * 8;
+                            bool seen = there[u] && token < min(lim[n][e & 1], until);
+                            if (VIEW == VIEW_SHARED) seen = seen && token >= begin && (seg == 0 || seg == low[n][e & 1]);
+                            if (VIEW == VIEW_OWN) seen = seen && token >= begin;
+                            if (VIEW == VIEW_WINDOW) seen = seen && (token >= low[n][e & 1] || token < a.sinks);
+                            if (!seen) sc[u][n][e] = -INFINITY;
+                        }
+                    }
                 }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top[n][e & 1] = fmaxf(top[n][e & 1], sc[u][n][e]);
+            }
             if (!there[u] || token0 + 16 > until || token0 < begin) {
                 // what lies behind the end of a history may be anything, not-a-numbers included: weight 0 is not enough
 #pragma unroll
@@ -318,23 +342,35 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
                         for (int q = 0; q < VB / 4; ++q) vw[u][i].w[q] = 0;
             }
         }
+        // where a maximum grows, the rows are brought down to the new one
+        bool raise = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) raise = raise || top[n][0] > m[n][0] || top[n][1] > m[n][1];
+        if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float x = fmaxf(m[n][e], top[n][e]);
+#pragma unroll
+                    for (int y = 4; y < 32; y <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, y));
+                    const float fade = fast_exp2(m[n][e] - (x == -INFINITY ? 0.0f : x));   // m = -inf gives 0
+                    m[n][e] = x;
+                    l[n][e] *= fade;
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        o[n][i][e] *= fade;
+                        o[n][i][e + 2] *= fade;
+                    }
+                }
+        }
         // weights
         uint32_t pf[GROUPS][NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                for (int x = 4; x < 32; x <<= 1) top[n][e] = fmaxf(top[n][e], __shfl_xor_sync(0xffffffffu, top[n][e], x));
-                const float ref = top[n][e] == -INFINITY ? 0.0f : top[n][e];
-                const float fade = fast_exp2(m[n][e] - ref);   // m = -inf gives 0
-                m[n][e] = top[n][e];
-                l[n][e] *= fade;
-#pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    o[n][i][e] *= fade;
-                    o[n][i][e + 2] *= fade;
-                }
+                const float ref = m[n][e] == -INFINITY ? 0.0f : m[n][e];
 #pragma unroll
                 for (int u = 0; u < GROUPS; ++u) {
                     sc[u][n][e] = fast_exp2(sc[u][n][e] - ref);
