@@ -93,8 +93,7 @@ __global__ void __launch_bounds__(WARPS * 32) kv_mass_kernel(MassArgs m) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, G = a.group;
     const int t0 = w.tile * TOKENS + 16 * warp;
     if (t0 >= w.len) return;
-    const int h0 = static_cast<int>(static_cast<int64_t>(a.c.kv_heads) * part / m.parts);
-    const int h1 = static_cast<int>(static_cast<int64_t>(a.c.kv_heads) * (part + 1) / m.parts);
+    const int heads_each = (a.c.kv_heads + m.parts - 1) / m.parts, h0 = part * heads_each, h1 = min(h0 + heads_each, a.c.kv_heads);
     const int i0 = max(0, w.n_q - m.last_q), rows = (min(w.n_q, a.max_q) - i0) * G;
     const int j = t0 >> a.c.page_shift;
     const int page = a.c.pages > 0 && j < a.ldt ? checked_page(a.c, a.table[w.b * a.ldt + j]) : -1;
@@ -103,12 +102,24 @@ __global__ void __launch_bounds__(WARPS * 32) kv_mass_kernel(MassArgs m) {
     const Walk by(G, 8);
     float sum[2] = {0.0f, 0.0f};
     if (page >= 0 && rows > 0) {
-        for (int h = h0; h < h1; ++h) {
+        // codes and scale of a head's keys, fetched a head ahead
+        uint4 codes[KC][2];
+        float scale;
+        auto fetch_keys = [&](int h) {
             const uint8_t* kp = a.c.k.codes + (page_codes(a.c, page, h) + (t0 & ((1 << a.c.page_shift) - 1)) + g) * D + 16 * t;
+#pragma unroll
+            for (int c = 0; c < KC; ++c) {
+                codes[c][0] = __ldg(reinterpret_cast<const uint4*>(kp + 64 * c));
+                codes[c][1] = __ldg(reinterpret_cast<const uint4*>(kp + 8 * D + 64 * c));
+            }
+            scale = __ldg(a.c.k.scales + static_cast<int64_t>(page) * a.c.kv_heads + h);
+        };
+        fetch_keys(h0);
+        for (int h = h0; h < h1; ++h) {
             uint32_t kf[KC][4][4];
 #pragma unroll
             for (int c = 0; c < KC; ++c) {
-                const uint4 x = __ldg(reinterpret_cast<const uint4*>(kp + 64 * c)), y = __ldg(reinterpret_cast<const uint4*>(kp + 8 * D + 64 * c));
+                const uint4 x = codes[c][0], y = codes[c][1];
                 const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
@@ -116,7 +127,8 @@ __global__ void __launch_bounds__(WARPS * 32) kv_mass_kernel(MassArgs m) {
                     word_to_pairs<T, TYPE>(ys[q], &kf[c][q][1], &kf[c][q][3]);
                 }
             }
-            const float fac = __ldg(a.c.k.scales + static_cast<int64_t>(page) * a.c.kv_heads + h) * a.scale_log2;
+            const float fac = scale * a.scale_log2;
+            if (h + 1 < h1) fetch_keys(h + 1);
             // The rows eight by eight; the queries and log-sum-exps of the next eight are fetched while these are computed with.
             Walk mine(G, g), col[2] = {Walk(G, 2 * t), Walk(G, 2 * t + 1)};
             uint4 next_q[KC][2];
@@ -313,8 +325,10 @@ MassPlan plan_mass(const sqap_kv_cache* c, int batch, int max_q, int max_len, in
         return p;
     }
     p.tiles = max_len > 0 ? (max_len - 1) / TOKENS + 1 : 0;
-    const int64_t ctas = size_product(batch, p.tiles), want = ctas > 0 ? (16ll * sm_count() + ctas - 1) / ctas : 1;
-    p.parts = static_cast<int>(want < c->kv_heads ? want : c->kv_heads);
+    const int64_t ctas = size_product(batch, p.tiles), want = ctas > 0 ? 4ll * sm_count() / ctas : 1;
+    // as many as run at once, each with the same number of heads but the last
+    const int64_t heads_each = want > 0 ? (c->kv_heads + want - 1) / want : c->kv_heads;
+    p.parts = static_cast<int>((c->kv_heads + heads_each - 1) / heads_each);
     p.fits = size_product(ctas, p.parts) <= 0x7FFFFFFF;
     p.bytes = p.attention + (p.parts > 1 ? static_cast<size_t>(p.parts) * batch * p.tiles * TOKENS * 4 : 0);
     return p;
