@@ -60,23 +60,21 @@ __device__ __forceinline__ void add_to_past(const MassArgs& m, int b, int token,
     m.mass[at] = (m.past && token < tokens - n_q ? m.past[at] : 0.0f) + sum;
 }
 
-// Row r of a key/value head: query i, head `head` of the group; without a division per step.
-struct Walk {
-    int i, head, group;
-    __device__ __forceinline__ Walk(int G, int r) : i(r / G), head(r % G), group(G) {}
-    __device__ __forceinline__ void next(const Walk& by) {
-        i += by.i;
-        head += by.head;
-        if (head >= group) {
-            head -= group;
-            ++i;
-        }
-    }
-};
+__device__ __forceinline__ void copy_async_16(void* to, const void* from, bool real) {      // zeros where there is nothing to copy
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(to))), "l"(from), "r"(real ? 16 : 0)
+                 : "memory");
+}
+__device__ __forceinline__ void copy_async_4(void* to, const void* from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(to))), "l"(from) : "memory");
+}
 
+constexpr int ROWS = 32;               // query rows of a stage
 template <typename T, int TYPE, int D>
-__global__ void __launch_bounds__(WARPS * 32) kv_mass_kernel(MassArgs m) {
-    constexpr int KC = D / 64;
+__global__ void __launch_bounds__(WARPS * 32, D <= 128 ? 5 : 2) kv_mass_kernel(MassArgs m) {
+    constexpr int KC = D / 64, LD = D + 8;           // halves of a row in shared memory: 16 bytes on in the banks from row to row
+    __shared__ alignas(16) T s_q[2][ROWS][LD];
+    __shared__ float s_lse[2][ROWS];
+    __shared__ int s_sees[2][ROWS];    // tokens that the row sees, 0 for no row
     pdl_launch_dependents();
     pdl_wait();
     const AttnArgs& a = m.a;
@@ -91,21 +89,38 @@ __global__ void __launch_bounds__(WARPS * 32) kv_mass_kernel(MassArgs m) {
     w.tokens = max(a.lens[w.b], 0);
     w.len = min(w.tokens, a.max_len);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, G = a.group;
+    if (w.tile * TOKENS >= w.len) return;
     const int t0 = w.tile * TOKENS + 16 * warp;
-    if (t0 >= w.len) return;
     const int heads_each = (a.c.kv_heads + m.parts - 1) / m.parts, h0 = part * heads_each, h1 = min(h0 + heads_each, a.c.kv_heads);
     const int i0 = max(0, w.n_q - m.last_q), rows = (min(w.n_q, a.max_q) - i0) * G;
     const int j = t0 >> a.c.page_shift;
-    const int page = a.c.pages > 0 && j < a.ldt ? checked_page(a.c, a.table[w.b * a.ldt + j]) : -1;
-    const T* q0 = static_cast<const T*>(a.q) + (static_cast<int64_t>(w.row0) + i0) * a.ldq + 16 * t;
-    const float* lse0 = a.lse + (static_cast<int64_t>(w.row0) + i0) * a.heads;
-    const Walk by(G, 8);
+    const int page = a.c.pages > 0 && t0 < w.len && j < a.ldt ? checked_page(a.c, a.table[w.b * a.ldt + j]) : -1;
     float sum[2] = {0.0f, 0.0f};
-    if (page >= 0 && rows > 0) {
+    if (rows > 0) {
+        // A stage: ROWS rows of a head, with their log-sum-exps.
+        const int stages = (rows + ROWS - 1) / ROWS;
+        auto fetch = [&](int h, int stage, int buffer) {
+            constexpr int PIECES = D / 8;
+#pragma unroll
+            for (int x = threadIdx.x; x < ROWS * PIECES; x += WARPS * 32) {
+                const int k = x / PIECES, piece = x % PIECES, r = stage * ROWS + k, i = r / G;
+                const bool real = r < rows;
+                const T* src = static_cast<const T*>(a.q) + (static_cast<int64_t>(w.row0) + i0 + i) * a.ldq + (h * G + r - i * G) * D + 8 * piece;
+                copy_async_16(&s_q[buffer][k][8 * piece], real ? src : a.q, real);
+            }
+            if (threadIdx.x < ROWS) {
+                const int k = threadIdx.x, r = stage * ROWS + k, i = r / G;
+                s_sees[buffer][k] = r < rows ? visible(a, w, i0 + i) : 0;
+                if (r < rows) copy_async_4(&s_lse[buffer][k], a.lse + (static_cast<int64_t>(w.row0) + i0 + i) * a.heads + h * G + r - i * G);
+                else s_lse[buffer][k] = INFINITY;
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
         // codes and scale of a head's keys, fetched a head ahead
-        uint4 codes[KC][2];
-        float scale;
+        uint4 codes[KC][2] = {};
+        float scale = 0.0f;
         auto fetch_keys = [&](int h) {
+            if (page < 0) return;
             const uint8_t* kp = a.c.k.codes + (page_codes(a.c, page, h) + (t0 & ((1 << a.c.page_shift) - 1)) + g) * D + 16 * t;
 #pragma unroll
             for (int c = 0; c < KC; ++c) {
@@ -114,7 +129,9 @@ __global__ void __launch_bounds__(WARPS * 32) kv_mass_kernel(MassArgs m) {
             }
             scale = __ldg(a.c.k.scales + static_cast<int64_t>(page) * a.c.kv_heads + h);
         };
+        fetch(h0, 0, 0);
         fetch_keys(h0);
+        int buffer = 0;
         for (int h = h0; h < h1; ++h) {
             uint32_t kf[KC][4][4];
 #pragma unroll
@@ -129,53 +146,37 @@ __global__ void __launch_bounds__(WARPS * 32) kv_mass_kernel(MassArgs m) {
             }
             const float fac = scale * a.scale_log2;
             if (h + 1 < h1) fetch_keys(h + 1);
-            // The rows eight by eight; the queries and log-sum-exps of the next eight are fetched while these are computed with.
-            Walk mine(G, g), col[2] = {Walk(G, 2 * t), Walk(G, 2 * t + 1)};
-            uint4 next_q[KC][2];
-            float next_lse[2];
-            auto fetch = [&](int r0) {
-                const bool real = r0 + g < rows;
-                const T* src = q0 + static_cast<int64_t>(mine.i) * a.ldq + (h * G + mine.head) * D;
+            for (int stage = 0; stage < stages; ++stage, buffer ^= 1) {
+                const bool last = stage + 1 == stages;
+                if (!last) fetch(h, stage + 1, buffer ^ 1);
+                else if (h + 1 < h1) fetch(h + 1, 0, buffer ^ 1);
+                else asm volatile("cp.async.commit_group;" ::: "memory");
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+                __syncthreads();
+                if (page >= 0) {
+                    const int blocks = min(ROWS, rows - stage * ROWS + 7) / 8;
+                    for (int n = 0; n < blocks; ++n) {
+                        float sc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int c = 0; c < KC; ++c)
+                        for (int c = 0; c < KC; ++c)
 #pragma unroll
-                    for (int half = 0; half < 2; ++half)
-                        next_q[c][half] = real ? __ldg(reinterpret_cast<const uint4*>(src + 64 * c) + half) : make_uint4(0, 0, 0, 0);
+                            for (int half = 0; half < 2; ++half) {
+                                const uint4 q = *reinterpret_cast<const uint4*>(&s_q[buffer][8 * n + g][64 * c + 16 * t + 8 * half]);
+                                mma_rows<T>(sc, kf[c][2 * half], q.x, q.y);
+                                mma_rows<T>(sc, kf[c][2 * half + 1], q.z, q.w);
+                            }
+                        const float2 lse = *reinterpret_cast<const float2*>(&s_lse[buffer][8 * n + 2 * t]);
+                        const int2 sees = *reinterpret_cast<const int2*>(&s_sees[buffer][8 * n + 2 * t]);
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    next_lse[e] = r0 + 2 * t + e < rows ? __ldg(lse0 + static_cast<int64_t>(col[e].i) * a.heads + h * G + col[e].head) : INFINITY;
-            };
-            fetch(0);
-            for (int r0 = 0; r0 < rows; r0 += 8) {
-                uint4 q[KC][2];
-                float lse[2];
-                int sees[2];
-#pragma unroll
-                for (int c = 0; c < KC; ++c) {
-                    q[c][0] = next_q[c][0];
-                    q[c][1] = next_q[c][1];
-                }
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    lse[e] = next_lse[e] * 1.4426950408889634f;
-                    sees[e] = fabsf(lse[e]) < INFINITY ? visible(a, w, i0 + col[e].i) - t0 : 0;       // rows that saw nothing, or are not numbers
-                    col[e].next(by);
-                }
-                mine.next(by);
-                if (r0 + 8 < rows) fetch(r0 + 8);
-                float sc[4] = {0.0f, 0.0f, 0.0f, 0.0f}, sd[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int c = 0; c < KC; ++c)
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        mma_rows<T>(sc, kf[c][2 * half], q[c][half].x, q[c][half].y);
-                        mma_rows<T>(sd, kf[c][2 * half + 1], q[c][half].z, q[c][half].w);
+                        for (int e = 0; e < 2; ++e) {
+                            const float l = (e ? lse.y : lse.x) * 1.4426950408889634f;
+                            const int n_seen = (fabsf(l) < INFINITY ? (e ? sees.y : sees.x) : 0) - t0;      // rows that saw nothing, or are not numbers
+                            if (g < n_seen) sum[0] += fast_exp2(fmaf(sc[e], fac, -l));
+                            if (g + 8 < n_seen) sum[1] += fast_exp2(fmaf(sc[e + 2], fac, -l));
+                        }
                     }
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    if (g < sees[e]) sum[0] += fast_exp2(fmaf(sc[e] + sd[e], fac, -lse[e]));
-                    if (g + 8 < sees[e]) sum[1] += fast_exp2(fmaf(sc[e + 2] + sd[e + 2], fac, -lse[e]));
                 }
+                __syncthreads();
             }
         }
     }
@@ -325,7 +326,7 @@ MassPlan plan_mass(const sqap_kv_cache* c, int batch, int max_q, int max_len, in
         return p;
     }
     p.tiles = max_len > 0 ? (max_len - 1) / TOKENS + 1 : 0;
-    const int64_t ctas = size_product(batch, p.tiles), want = ctas > 0 ? 4ll * sm_count() / ctas : 1;
+    const int64_t ctas = size_product(batch, p.tiles), want = ctas > 0 ? static_cast<int64_t>(c->head_dim <= 128 ? 5 : 2) * sm_count() / ctas : 1;
     // as many as run at once, each with the same number of heads but the last
     const int64_t heads_each = want > 0 ? (c->kv_heads + want - 1) / want : c->kv_heads;
     p.parts = static_cast<int>((c->kv_heads + heads_each - 1) / heads_each);
