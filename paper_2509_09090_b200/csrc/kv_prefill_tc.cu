@@ -266,9 +266,13 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
                     }
                     if (VIEW == VIEW_WINDOW || VIEW == VIEW_OWN) {
                         if (!__all_sync(0xffffffffu, from <= 0 || sink >= KEYS)) {
+                            // bits of the keys that are not seen: sink .. from - 1
+                            const uint64_t hidden = (from >= KEYS ? ~0ull : from > 0 ? (1ull << from) - 1 : 0ull) &
+                                                    ~(sink >= KEYS ? ~0ull : sink > 0 ? (1ull << sink) - 1 : 0ull);
+                            const uint32_t lo = static_cast<uint32_t>(hidden), hi = static_cast<uint32_t>(hidden >> 32);
 #pragma unroll
                             for (int i = 0; i < KEYS; ++i)
-                                if (i < from && i >= sink) v[i] = 0xFF800000u;
+                                if ((i < 32 ? lo : hi) & (1u << (i & 31))) v[i] = 0xFF800000u;
                         }
                     }
                     // of a run's scores; never 0, so that what is masked stays at -inf
@@ -510,15 +514,20 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
                     cp_async_16(base + q_at(i), there ? p : q, there);
                 }
             } else {
-                int qi = first / G, g = first - qi * G;
-#pragma unroll 4
+                // RPI rows on: so many queries and heads of the group, and a query more where the heads pass the group
+                const int by = RPI % G;
+                const int64_t step = (RPI / G) * a.ldq + by * D, carry = a.ldq - static_cast<int64_t>(G) * D;
+                int g = first % G;
+                const T* p = q + (first / G) * a.ldq + g * D;
+#pragma unroll
                 for (int i = 0; i < Q_STEPS; ++i) {
                     const bool there = first + i * RPI < t.rows;
-                    cp_async_16(base + q_at(i), there ? q + qi * a.ldq + g * D : q, there);
-                    g += RPI;
-                    while (g >= G) {
+                    cp_async_16(base + q_at(i), there ? p : q, there);
+                    p += step;
+                    g += by;
+                    if (g >= G) {
                         g -= G;
-                        ++qi;
+                        p += carry;
                     }
                 }
             }
@@ -534,23 +543,25 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
                     }
                 fac[tid] = fabsf(a.scale_log2);
             } else {
+                // a lane takes a row of the 32 that its warp has brought
+                __syncwarp();
+                uint8_t* row_of = sm + S::Q + (tid >> 7) * S::HALF_Q + (tid & 127) * 128;
+                auto piece = [&](int c) { return reinterpret_cast<uint4*>(row_of + (c >> 3) * Q_BLOCK + (((c & 7) ^ (tid & 7)) << 4)); };
+                uint32_t top = 0;
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) widen8<T>(*piece(c), &top);
+                float back;
+                float up = fit_exponent(fold_pair<T>(top), &back);
+                if (a.scale_log2 < 0.0f) up = -up;
 #pragma unroll 4
-                for (int i = 0; i < Q_STEPS; ++i) {
-                    uint4* u = reinterpret_cast<uint4*>(sm + q_at(i));
+                for (int c = 0; c < D / 8; ++c) {
                     float v[8];
-                    unpack8<T>(*u, v);
-                    float amax = 0.0f, back;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(v[e]));
-#pragma unroll
-                    for (int o = 1; o < LPR; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-                    float up = fit_exponent(amax, &back);
-                    if (a.scale_log2 < 0.0f) up = -up;
+                    unpack8<T>(*piece(c), v);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] *= up;
-                    *u = pack8<__half>(v);
-                    if (qc == 0) fac[q_row0 + i * RPI] = back * fabsf(a.scale_log2);
+                    *piece(c) = pack8<__half>(v);
                 }
+                fac[tid] = back * fabsf(a.scale_log2);
             }
         };
 
