@@ -231,6 +231,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
         const uint32_t t_lane = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + 128 * half, t_o = t_lane + O_COL;
         uint32_t n = 0;             // tiles of this half so far
         uint32_t full_items = 0;
+        const bool wide = ((reinterpret_cast<uintptr_t>(a.out) | static_cast<uintptr_t>(a.ldo * sizeof(T))) & 31) == 0;
         Item next = item_of<VIEW>(a, blockIdx.x, per_tile);
         for (unsigned id = blockIdx.x; id < items; id += gridDim.x) {
             const Item x = next;
@@ -364,12 +365,25 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
 #pragma unroll
                     for (int i = 0; i < 16; ++i) reinterpret_cast<uint4*>(po + 64 * c)[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
                 } else {
+                    // 32 bytes at a time where rows allow it: a warp's store takes a step for each line, and every lane has its own
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        float z[8];
+                    for (int i = 0; i < 8; i += 2) {
+                        uint4 y[2];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) z[e] = __uint_as_float(v[8 * i + e]) * inv;
-                        reinterpret_cast<uint4*>(out + 64 * c)[i] = pack8<T>(z);
+                        for (int k = 0; k < 2; ++k) {
+                            float z[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) z[e] = __uint_as_float(v[8 * (i + k) + e]) * inv;
+                            y[k] = pack8<T>(z);
+                        }
+                        uint4* to = reinterpret_cast<uint4*>(out + 64 * c) + i;
+                        if (wide) {
+                            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(y[0].x), "r"(y[0].y), "r"(y[0].z),
+                                         "r"(y[0].w), "r"(y[1].x), "r"(y[1].y), "r"(y[1].z), "r"(y[1].w) : "memory");
+                        } else {
+                            to[0] = y[0];
+                            to[1] = y[1];
+                        }
                     }
                 }
             }
@@ -553,13 +567,19 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
                 float back;
                 float up = fit_exponent(fold_pair<T>(top), &back);
                 if (a.scale_log2 < 0.0f) up = -up;
-#pragma unroll 4
-                for (int c = 0; c < D / 8; ++c) {
-                    float v[8];
-                    unpack8<T>(*piece(c), v);
+#pragma unroll 1
+                for (int c0 = 0; c0 < D / 8; c0 += 4) {
+                    uint4 u[4];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] *= up;
-                    *piece(c) = pack8<__half>(v);
+                    for (int c = 0; c < 4; ++c) u[c] = *piece(c0 + c);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        float v[8];
+                        unpack8<T>(u[c], v);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] *= up;
+                        *piece(c0 + c) = pack8<__half>(v);
+                    }
                 }
                 fac[tid] = back * fabsf(a.scale_log2);
             }
