@@ -103,12 +103,14 @@ struct Plan {
 // out). Measured, us, with four / eight / sixteen CTAs to an SM, uneven histories of up to so many keys: 32 x 16384, 8 heads 132 / 147 / 127;
 // 32 x 8192, 32 heads 258 / 232 / 219; 32 x 4096, 32 heads 147 / 135 / 131, 8 heads 48 / 48 / 48; 16 x 2048, 32 heads 51.5 / 51.1 / 51.3; but
 // one of 32768, 32 heads 42 / 57 / 57 (8 heads 21 all three). Three / four up to 1024 keys: 16 x 290, 32 heads 11.7 / 15.2, 16 x 1000 27.0 / 31.5.
-// `alike`: all rows look at about as many keys (a window): as many pieces as all run at once. 32 windows of 2048, 8 heads, us: 1 piece 46, 2 33,
+// ALIKE: all rows look at about as many keys (a window): as many pieces as all run at once. 32 windows of 2048, 8 heads, us: 1 piece 46, 2 33,
 // 3 39, 5 37, 9 40.
 // Prompts: two rounds of CTAs where there is less than one, in pieces of 1024 keys at least: cut / whole, us, 256 rows (8 heads, groups of
 // 4) behind 3000 keys 44 / 63, behind 8000 76 / 114; 288 rows behind 4096 (32 heads) 59 / 62.
 int64_t least(int64_t x, int64_t y) { return x < y ? x : y; }
-Plan plan_rows(int64_t units, int kv_heads, int head_dim, int64_t rows, int64_t max_len, bool decode, bool alike = false) {
+// Histories of uneven lengths, as a rule; of about the same (windows); cut on the device, each into the same number of pieces.
+enum Cut { UNEVEN, ALIKE, EVENLY };
+Plan plan_rows(int64_t units, int kv_heads, int head_dim, int64_t rows, int64_t max_len, bool decode, Cut cut = UNEVEN) {
     Plan p;
     p.decode = decode;
     const int per_tile = p.decode ? decode_max_rows(head_dim) : head_dim <= 128 ? PREFILL_TC_ROWS : PREFILL_ROWS;
@@ -119,12 +121,15 @@ Plan plan_rows(int64_t units, int kv_heads, int head_dim, int64_t rows, int64_t 
     int64_t splits;
     if (p.decode) {
         const int64_t at_once = sms * (rows <= 8 && head_dim <= 128 ? 4 : 2);
-        const int64_t fill = least(alike ? at_once / (ctas > 0 ? ctas : 1) : pieces(max_len > 1024 ? 4 : 3), (max_len + 255) / 256), even = least(pieces(16), max_len / 1024);
+        const int64_t fill = least(cut == ALIKE ? at_once / (ctas > 0 ? ctas : 1) : pieces(max_len > 1024 ? 4 : 3), (max_len + 255) / 256), even = least(pieces(16), max_len / 1024);
         splits = fill > even ? fill : even;
     } else {
-        splits = ctas < sms ? least(pieces(2), max_len / 1024) : 1;
+        splits = ctas >= sms ? 1 : cut != UNEVEN ? least(sms / (ctas > 0 ? ctas : 1), max_len / 512) : least(pieces(2), max_len / 1024);
     }
     if (splits < 1) splits = 1;
+    p.splits = static_cast<int>(splits);
+    p.chunk = 0;
+    if (cut == EVENLY) return p;
     const int64_t chunk = ((max_len + splits - 1) / splits + 127) / 128 * 128;
     p.chunk = static_cast<int>(chunk < 128 ? 128 : chunk);
     p.splits = static_cast<int>((max_len + p.chunk - 1) / p.chunk);
@@ -154,7 +159,7 @@ int64_t window_keys(int64_t max_q, int64_t max_len, int group, int head_dim, int
 }
 Plan plan_window(int64_t batch, int kv_heads, int group, int head_dim, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks) {
     const int64_t rows = max_q * group;
-    return plan_rows(batch, kv_heads, head_dim, rows, window_keys(max_q, max_len, group, head_dim, window, sinks), rows <= decode_max_rows(head_dim), true);
+    return plan_rows(batch, kv_heads, head_dim, rows, window_keys(max_q, max_len, group, head_dim, window, sinks), rows <= decode_max_rows(head_dim), ALIKE);
 }
 
 // Shared prefixes: the rows of a group over its prefix, then those of each sequence over its own tokens. The pieces of both are cut on
@@ -177,14 +182,14 @@ SharedPlan plan_shared(int kv_heads, int group, int head_dim, int64_t max_q, int
     p.together = together <= SHARED_TILES * tile;
     if (p.together) {
         const int64_t members = least(max_group, (together < tile ? together : tile) / rows + 1);
-        p.prefix = p.own = plan_rows(groups, kv_heads, head_dim, together, least(size_product(own, members) + max_prefix, 1 << 30), true);
+        p.prefix = p.own = plan_rows(groups, kv_heads, head_dim, together, least(size_product(own, members) + max_prefix, 1 << 30), true, EVENLY);
         p.prefix_parts = 0;
         p.join = false;
         p.parts = p.prefix.splits;
         return p;
     }
-    p.own = plan_rows(size_product(groups, max_group), kv_heads, head_dim, rows, own, rows <= tile);
-    p.prefix = plan_rows(groups, kv_heads, head_dim, together, max_prefix, false);
+    p.own = plan_rows(size_product(groups, max_group), kv_heads, head_dim, rows, own, rows <= tile, EVENLY);
+    p.prefix = plan_rows(groups, kv_heads, head_dim, together, max_prefix, false, EVENLY);
     p.prefix_parts = max_prefix > 0 ? p.prefix.splits : 0;
     p.join = p.own.decode && p.own.splits == 1 && p.prefix_parts > 0;
     p.parts = p.prefix_parts + (p.join ? 0 : p.own.splits);

@@ -455,12 +455,13 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
             // the pieces of the prefix are there: joined here
             const int64_t at = part_index(a, row.b, row.head, row.i, 0);
             float top = mm;
+#pragma unroll 8
             for (int s = 0; s < a.join; ++s) top = fmaxf(top, a.part_ml[at + s].x);
             const float base = top == -INFINITY ? 0.0f : top, f = fast_exp2(mm - base);
             ll *= f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] *= f;
-#pragma unroll 4
+#pragma unroll 8
             for (int s = 0; s < a.join; ++s) {
                 const float2 ml = a.part_ml[at + s];
                 const float c = fast_exp2(ml.x - base);

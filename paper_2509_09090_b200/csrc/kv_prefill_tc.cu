@@ -103,6 +103,16 @@ __device__ __forceinline__ uint64_t smem_desc_values(uint32_t addr) {
            (2ull << 61);
 }
 
+// 32 bytes of a row, at once where its address allows it: a warp's store takes a step for each line that it meets, and every lane has its own.
+__device__ __forceinline__ void store_32(void* to, bool wide, const uint32_t* v) {
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]),
+                     "r"(v[6]), "r"(v[7]) : "memory");
+    } else {
+        reinterpret_cast<uint4*>(to)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<uint4*>(to)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+    }
+}
 __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src, bool real) {   // zeros where there is nothing to copy
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
 }
@@ -231,6 +241,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
         const uint32_t t_lane = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + 128 * half, t_o = t_lane + O_COL;
         uint32_t n = 0;             // tiles of this half so far
         uint32_t full_items = 0;
+        const bool wide_parts = (reinterpret_cast<uintptr_t>(a.part_o) & 31) == 0;
         const bool wide = ((reinterpret_cast<uintptr_t>(a.out) | static_cast<uintptr_t>(a.ldo * sizeof(T))) & 31) == 0;
         Item next = item_of<VIEW>(a, blockIdx.x, per_tile);
         for (unsigned id = blockIdx.x; id < items; id += gridDim.x) {
@@ -363,27 +374,14 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
                 if (!real) continue;
                 if (a.parts > 1) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) reinterpret_cast<uint4*>(po + 64 * c)[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                    for (int i = 0; i < 64; i += 8) store_32(po + 64 * c + i, wide_parts, v + i);
                 } else {
-                    // 32 bytes at a time where rows allow it: a warp's store takes a step for each line, and every lane has its own
 #pragma unroll
-                    for (int i = 0; i < 8; i += 2) {
-                        uint4 y[2];
+                    for (int i = 0; i < 64; i += 16) {
+                        uint32_t y[8];
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            float z[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) z[e] = __uint_as_float(v[8 * (i + k) + e]) * inv;
-                            y[k] = pack8<T>(z);
-                        }
-                        uint4* to = reinterpret_cast<uint4*>(out + 64 * c) + i;
-                        if (wide) {
-                            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(y[0].x), "r"(y[0].y), "r"(y[0].z),
-                                         "r"(y[0].w), "r"(y[1].x), "r"(y[1].y), "r"(y[1].z), "r"(y[1].w) : "memory");
-                        } else {
-                            to[0] = y[0];
-                            to[1] = y[1];
-                        }
+                        for (int e = 0; e < 8; ++e) y[e] = pack2<T>(__uint_as_float(v[i + 2 * e]) * inv, __uint_as_float(v[i + 2 * e + 1]) * inv);
+                        store_32(out + 64 * c + i, wide, y);
                     }
                 }
             }
@@ -514,11 +512,13 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
                 Where w = {};
                 w.b = t.b;
                 w.h = t.h;
-#pragma unroll 4
+                // a lane looks up one of the warp's 32 rows, for all
+                const Row mine = row_at<VIEW>(a, w, t.rows, t.r_first + tid);
+                const int64_t at = mine.real ? mine.at * a.ldq + static_cast<int64_t>(mine.head) * D : -1;
+#pragma unroll
                 for (int i = 0; i < Q_STEPS; ++i) {
-                    const Row x = row_at<VIEW>(a, w, t.rows, first + i * RPI);
-                    const T* p = static_cast<const T*>(a.q) + x.at * a.ldq + static_cast<int64_t>(x.head) * D + 8 * qc;
-                    cp_async_16(base + q_at(i), x.real ? p : a.q, x.real);
+                    const int64_t x = __shfl_sync(0xffffffffu, at, lane / LPR + i * RPI);
+                    cp_async_16(base + q_at(i), x >= 0 ? static_cast<const T*>(a.q) + x + 8 * qc : a.q, x >= 0);
                 }
             } else if (G == 1) {
                 const T* p = q + first * a.ldq;
