@@ -27,7 +27,8 @@ struct EvictArgs {
     int32_t* n_kept;
 };
 
-// Order of the numbers as whole numbers; -0 = 0; 1 for what is not a number, in front of all.
+// Order of the numbers as whole numbers; -0 = 0; 1 for what is not a number, in front of all. None of them is 0 or ALWAYS.
+constexpr uint32_t ALWAYS = 0xFFFFFFFFu;
 __device__ __forceinline__ uint32_t order_of(float f) {
     if (!(f == f)) return 1;
     const uint32_t b = __float_as_uint(f + 0.0f);
@@ -61,13 +62,16 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
     const float* mass = a.mass + (there ? row : 0) * a.ldm;
     const int rounds = (len + THREADS * EACH - 1) / (THREADS * EACH);
     auto token_of = [&](int r, int e) { return (r * EACH + e) * THREADS + tid; };
-    uint32_t order[EACH];                // 0: not chosen from
+    uint32_t order[EACH];                // 0: no token; ALWAYS: stays whatever its weight is
     auto load = [&](int r) {
         float x[EACH];
 #pragma unroll
         for (int e = 0; e < EACH; ++e) x[e] = token_of(r, e) < len ? mass[token_of(r, e)] : 0.0f;
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) order[e] = token_of(r, e) >= first && token_of(r, e) < to ? order_of(x[e]) : 0;
+        for (int e = 0; e < EACH; ++e) {
+            const int t = token_of(r, e);
+            order[e] = t >= first && t < to ? order_of(x[e]) : t < len ? ALWAYS : 0;
+        }
     };
     auto each = [&](auto f) {
         for (int r = 0; r < rounds; ++r) {
@@ -79,12 +83,12 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
     if (rounds == 1) load(0);
 
     // border: orders above it stay, of those equal to it the first `ties` in their places
-    uint32_t border = 0xFFFFFFFFu, ties = 0;
+    uint32_t border = ALWAYS - 1, ties = 0;
     if (wanted > 0) {
         uint32_t lo = 0xFFFFFFFFu, hi = 0;
         each([&](uint32_t k) {
             lo = min(lo, k - 1);         // 0 comes out on top
-            hi = max(hi, k);
+            hi = max(hi, k + 1);         // and ALWAYS at the bottom
         });
         lo = __reduce_min_sync(0xffffffffu, lo);
         hi = __reduce_max_sync(0xffffffffu, hi);
@@ -94,7 +98,7 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
         }
         __syncthreads();
         lo = __reduce_min_sync(0xffffffffu, least[lane < WARPS ? lane : 0]) + 1;
-        hi = __reduce_max_sync(0xffffffffu, most[lane < WARPS ? lane : 0]);
+        hi = __reduce_max_sync(0xffffffffu, most[lane < WARPS ? lane : 0]) - 1;
         uint32_t left = wanted;          // of the orders in lo .. hi, the left-th largest is the border
         for (;;) {
             // parts of 2^shift orders, at most BINS of them (shift 0 once the interval is that short)
@@ -102,7 +106,7 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
             for (int b = tid; b < BINS; b += THREADS) bins[b] = 0;
             __syncthreads();
             each([&](uint32_t k) {
-                if (k >= lo && k <= hi) atomicAdd(&bins[(k - lo) >> shift], 1u);
+                if (k - lo <= hi - lo) atomicAdd(&bins[(k - lo) >> shift], 1u);
             });
             __syncthreads();
             // thread t looks at bins BINS - 1 - 2t and the one below it: the sums run from the largest orders down
@@ -150,8 +154,7 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
         uint32_t votes[EACH];                    // of the run: who stays, ties apart
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
-            const int t = token_of(r, e);
-            votes[e] = __ballot_sync(0xffffffffu, t < len && (t < first || t >= to || order[e] > border));
+            votes[e] = __ballot_sync(0xffffffffu, order[e] > border);
             if (lane == 0) front[e * WARPS + warp] = __popc(votes[e]);
         }
         if (ties > 0) {
