@@ -1,12 +1,13 @@
 // Which tokens of a sequence stay in the cache: the last ones, the first ones, and of the rest those with the largest weight.
 //
-// One CTA takes one sequence. The weights are ordered as whole numbers; the m-th largest is found by narrowing the interval
+// A CTA, or a cluster of up to eight, takes one sequence. The weights are ordered as whole numbers; the m-th largest is found by narrowing the interval
 // that holds it: a histogram of BINS equal parts of the interval (at first from the smallest to the largest weight), the bin that
 // holds the m-th, and again within it: two or three rounds for 32 bits. Equal weights are told apart by their place. A
 // warp owns runs of 32 consecutive tokens, a lane one of each: its votes give a token's place within the run, one sum over
 // the runs in front of it the rest, and the lanes that write the list write side by side.
-// Bounded by latency: 4 bytes a token are read once (up to 16384 tokens are kept in registers, longer ones read again each
-// round), and some seven steps of the whole CTA follow one another.
+// Bounded by latency: 4 bytes a token are read once (up to 16384 tokens a CTA are kept in registers, longer ones read again each
+// round), and some seven steps of the whole CTA follow one another, four of them with a cluster's barrier: 16 x 288 tokens 4.5 us,
+// 32 uneven sequences of up to 16384 11.4 us, one of 131072 17.6 us.
 #include "kv.cuh"
 
 namespace sqap {
@@ -35,19 +36,43 @@ __device__ __forceinline__ uint32_t order_of(float f) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// EACH tokens a thread and round; longer sequences than THREADS x EACH take several rounds.
-template <int THREADS, int EACH>
+// Shared memory of another CTA of the cluster: the place of `p` there.
+__device__ __forceinline__ uint32_t remote_address(const void* p, int rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(p))), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ uint2 remote_load(uint32_t at) {
+    uint2 v;
+    asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void remote_store(uint32_t at, uint32_t x, uint32_t y) {
+    asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(at), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+
+// CTAS CTAs, a cluster, take a sequence; EACH tokens a thread and round, a CTA's side by side; longer sequences take several rounds. Every
+// CTA knows what it needs to find the same border: the histograms of all, and how many stay in front of it.
+template <int THREADS, int EACH, int CTAS>
 __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
     constexpr int BINS = 2 * THREADS, WARPS = THREADS / 32, RUNS = EACH * WARPS;
     static_assert(THREADS * EACH < 65536 && RUNS % 32 == 0, "two counts to a word, runs shared out to whole warps");
-    __shared__ uint32_t bins[BINS];
+    constexpr int BUFFERS = CTAS > 1 ? 2 : 1;    // another CTA may still be reading the bins of the round before
+    // the bins; once the border is known, places of the tokens that stay within the CTA's share of the round
+    constexpr int SHARED = BUFFERS * BINS * 4 > THREADS * EACH * 2 ? BUFFERS * BINS * 4 : THREADS * EACH * 2;
+    __shared__ alignas(8) uint8_t bins_or_list[SHARED];
+    uint32_t (*bins)[BINS] = reinterpret_cast<uint32_t (*)[BINS]>(bins_or_list);
+    uint16_t* list = reinterpret_cast<uint16_t*>(bins_or_list);
+    __shared__ alignas(8) uint32_t of_all[3][CTAS][2];      // of each CTA: smallest and largest order; places and ties, by parity of the round
     __shared__ uint32_t part[WARPS], least[WARPS], most[WARPS];
     __shared__ uint32_t found[3];        // the bin, how many are above it, how many in it
     __shared__ uint32_t front[RUNS];     // of each run of 32 tokens: those in front of it that stay, and (upper half) that are at the border
-    __shared__ uint16_t list[THREADS * EACH];
     pdl_launch_dependents();
     pdl_wait();
-    const int i = blockIdx.x, row = a.src[i], dst = a.dst ? a.dst[i] : -1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int i = blockIdx.x / CTAS, rank = blockIdx.x % CTAS, row = a.src[i], dst = a.dst ? a.dst[i] : -1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const bool there = row >= 0 && row < a.rows;
     const int64_t held = a.ldm < a.max_len ? a.ldm : a.max_len;
     int len = there ? a.lens[row] : 0;
@@ -60,8 +85,8 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
     const int to = len - recent;         // tokens first .. to - 1 are chosen from
     const uint32_t wanted = static_cast<uint32_t>(keep - recent - first);
     const float* mass = a.mass + (there ? row : 0) * a.ldm;
-    const int rounds = (len + THREADS * EACH - 1) / (THREADS * EACH);
-    auto token_of = [&](int r, int e) { return (r * EACH + e) * THREADS + tid; };
+    const int rounds = (len + CTAS * THREADS * EACH - 1) / (CTAS * THREADS * EACH);
+    auto token_of = [&](int r, int e) { return ((r * CTAS + rank) * EACH + e) * THREADS + tid; };
     uint32_t order[EACH];                // 0: no token; ALWAYS: stays whatever its weight is
     auto load = [&](int r) {
         float x[EACH];
@@ -99,18 +124,44 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
         __syncthreads();
         lo = __reduce_min_sync(0xffffffffu, least[lane < WARPS ? lane : 0]) + 1;
         hi = __reduce_max_sync(0xffffffffu, most[lane < WARPS ? lane : 0]) - 1;
+        if (CTAS > 1) {
+            if (tid < CTAS) remote_store(remote_address(&of_all[2][rank], tid), lo, hi);
+            cluster_sync();
+#pragma unroll
+            for (int q = 0; q < CTAS; ++q) {
+                lo = min(lo, of_all[2][q][0]);
+                hi = max(hi, of_all[2][q][1]);
+            }
+        }
+        int buffer = 0;
         uint32_t left = wanted;          // of the orders in lo .. hi, the left-th largest is the border
         for (;;) {
             // parts of 2^shift orders, at most BINS of them (shift 0 once the interval is that short)
             const int width = 32 - __clz(hi - lo), shift = max(0, width - (31 - __clz(BINS)));
-            for (int b = tid; b < BINS; b += THREADS) bins[b] = 0;
+            for (int b = tid; b < BINS; b += THREADS) bins[buffer][b] = 0;
             __syncthreads();
             each([&](uint32_t k) {
-                if (k - lo <= hi - lo) atomicAdd(&bins[(k - lo) >> shift], 1u);
+                if (k - lo <= hi - lo) atomicAdd(&bins[buffer][(k - lo) >> shift], 1u);
             });
-            __syncthreads();
             // thread t looks at bins BINS - 1 - 2t and the one below it: the sums run from the largest orders down
-            const uint32_t up = bins[BINS - 1 - 2 * tid], down = bins[BINS - 2 - 2 * tid];
+            uint32_t up, down;
+            if (CTAS > 1) {
+                cluster_sync();
+                uint2 two[CTAS];
+#pragma unroll
+                for (int q = 0; q < CTAS; ++q) two[q] = remote_load(remote_address(&bins[buffer][BINS - 2 - 2 * tid], q));
+                up = down = 0;
+#pragma unroll
+                for (int q = 0; q < CTAS; ++q) {
+                    up += two[q].y;
+                    down += two[q].x;
+                }
+                buffer ^= 1;
+            } else {
+                __syncthreads();
+                up = bins[0][BINS - 1 - 2 * tid];
+                down = bins[0][BINS - 2 - 2 * tid];
+            }
             uint32_t y = up + down;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -148,7 +199,7 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
 
     int32_t* kept = a.kept + i * a.ldkept;
     float* carry = dst >= 0 && dst < a.rows ? a.mass + dst * a.ldm : nullptr;
-    uint32_t placed = 0, ties_before = 0;
+    uint32_t sure_before = 0, ties_before = 0;               // of earlier rounds, and of CTAs in front
     for (int r = 0; r < rounds; ++r) {
         if (rounds > 1) load(r);
         uint32_t votes[EACH];                    // of the run: who stays, ties apart
@@ -194,8 +245,24 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
             }
         }
         __syncthreads();
+        uint32_t sure_all = all & 0xFFFFu, ties_all = all >> 16;
+        if (CTAS > 1) {
+            if (tid < CTAS) remote_store(remote_address(&of_all[r & 1][rank], tid), sure_all, ties_all);
+            cluster_sync();
+            sure_all = ties_all = 0;
+#pragma unroll
+            for (int q = 0; q < CTAS; ++q) {
+                if (q == rank) {
+                    sure_before += sure_all;
+                    ties_before += ties_all;
+                    sure_all = ties_all = 0;
+                }
+                sure_all += of_all[r & 1][q][0];
+                ties_all += of_all[r & 1][q][1];
+            }
+        }
         const uint32_t under = (1u << lane) - 1u;
-        const uint32_t ties_left = ties - min(ties_before, ties);
+        const uint32_t ties_left = ties - min(ties_before, ties), placed = sure_before + min(ties_before, ties);
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
             const uint32_t f = front[e * WARPS + warp];
@@ -211,16 +278,34 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
         __syncthreads();
         const int n = static_cast<int>((all & 0xFFFFu) + min(all >> 16, ties_left));
         for (int p = tid; p < n; p += THREADS) {
-            const int t = r * THREADS * EACH + list[p];
+            const int t = (r * CTAS + rank) * THREADS * EACH + list[p];
             kept[placed + p] = t;
             if (carry) carry[placed + p] = __ldg(mass + t);      // no row is both read and written
         }
-        placed += n;
-        ties_before += all >> 16;
+        sure_before += sure_all;
+        ties_before += ties_all;
         __syncthreads();                         // `front` and `list` are written again
     }
-    if (tid == 0) a.n_kept[i] = keep;
-    for (int64_t p = keep + tid; p < a.ldkept; p += THREADS) kept[p] = -1;
+    if (tid == 0 && rank == 0) a.n_kept[i] = keep;
+    for (int64_t p = keep + rank * THREADS + tid; p < a.ldkept; p += CTAS * THREADS) kept[p] = -1;
+}
+
+template <int THREADS, int EACH, int CTAS>
+cudaError_t launch_evict(const EvictArgs& a, int n, cudaStream_t s) {
+    if (CTAS == 1) return launch_dependent(kv_evict_kernel<THREADS, EACH, CTAS>, dim3(static_cast<unsigned>(n)), dim3(THREADS), 0, s, a);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(n) * CTAS);
+    cfg.blockDim = dim3(THREADS);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = CTAS;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kv_evict_kernel<THREADS, EACH, CTAS>, a);
 }
 
 }  // namespace
@@ -242,8 +327,15 @@ extern "C" sqap_status sqap_kv_evict(float* mass, int64_t ldm, int rows, const i
     if (ldkept > 0x7FFFFFFF || max_len > 1 << 30) return SQAP_ERR_UNSUPPORTED;
     const EvictArgs a = {mass, ldm, rows, lens, src_rows, dst_rows, keep, first, recent, max_len, kept, ldkept, n_kept};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const dim3 grid(static_cast<unsigned>(n));
-    if (max_len <= 1024) return finish_launch(launch_dependent(kv_evict_kernel<256, 4>, grid, dim3(256), 0, s, a));
-    if (max_len <= 4096) return finish_launch(launch_dependent(kv_evict_kernel<1024, 4>, grid, dim3(1024), 0, s, a));
-    return finish_launch(launch_dependent(kv_evict_kernel<1024, 16>, grid, dim3(1024), 0, s, a));
+    if (max_len <= 1024) return finish_launch(launch_evict<256, 4, 1>(a, n, s));
+    if (max_len <= 4096) return finish_launch(launch_evict<1024, 4, 1>(a, n, s));
+    // As many CTAs to a sequence as the device has SMs for, as long as each has 4096 tokens or more, and two only where they save a round (us,
+    // one CTA / as many as here: 32 x 16384 13.0 / 11.4; one / two: 64 x 16384 13.5 / 16.7). Up to 16 tokens a thread rather than
+    // a second round (131072 tokens in eight CTAs, 4 / 16: 31.9 / 17.6).
+    const int64_t ctas = sm_count() / (n < sm_count() ? n : sm_count());
+    if (ctas >= 8 && max_len > 16384) return finish_launch(max_len <= 32768 ? launch_evict<1024, 4, 8>(a, n, s) : launch_evict<1024, 16, 8>(a, n, s));
+    if (ctas >= 4 && max_len > 8192) return finish_launch(max_len <= 16384 ? launch_evict<1024, 4, 4>(a, n, s) : launch_evict<1024, 16, 4>(a, n, s));
+    if (ctas >= 2 && max_len <= 8192) return finish_launch(launch_evict<1024, 4, 2>(a, n, s));
+    if (ctas >= 2 && max_len > 16384) return finish_launch(launch_evict<1024, 16, 2>(a, n, s));
+    return finish_launch(launch_evict<1024, 16, 1>(a, n, s));
 }
