@@ -40,10 +40,12 @@ def evict(mass, lens, src, keep, first, recent, max_len, room):
         n = max(0, min(lens[a], max_len, ldm)) if 0 <= a < rows else 0
         k = max(0, min(k, room, n))
         order = list(range(n - 1, max(n - recent, 0) - 1, -1)) + [t for t in range(min(first, n)) if t < n - recent]
-        rest = [t for t in range(n) if t not in set(order)]
-        m = mass[a].astype(np.float64) if n else None
-        rest.sort(key=lambda t: (np.isnan(m[t]), 0.0 if np.isnan(m[t]) else -m[t], t))
-        got.append(sorted((order + rest)[:k]))
+        free = np.ones(n, bool)
+        free[order] = False
+        rest = np.flatnonzero(free)
+        m = mass[a, rest].astype(np.float64) if n else np.zeros(0)
+        rest = rest[np.lexsort((rest, np.where(np.isnan(m), 0, -m), np.isnan(m)))]
+        got.append(sorted((order + rest.tolist())[:k]))
     return got
 
 

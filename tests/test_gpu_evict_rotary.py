@@ -54,6 +54,16 @@ def test_evict_lengths(n):
         check_evict(m, lens, [0, 1, 2, 3], [keep] * 4, first, recent, dst=[4, 5, 6, 7])
 
 
+@pytest.mark.parametrize("n,top", [(20, 9000), (30, 20000), (37, 16384), (38, 16385), (64, 5000), (74, 20001), (75, 9000), (150, 33000)])
+def test_evict_many_sequences(n, top):
+    """As many CTAs to a sequence as the number of sequences leaves room for: eight, four, two, one; in one round and in several."""
+    g = np.random.default_rng(n)
+    m = weights(g, 2 * n, top)
+    lens = [int(x) for x in g.integers(0, top + 1, n)] + [0] * n
+    lens[0] = top
+    check_evict(m, lens, list(range(n)), [int(x) for x in g.integers(0, top // 2, n)], 3, 70, dst=list(range(n, 2 * n)), max_len=top)
+
+
 @pytest.mark.parametrize("keep,first,recent", [(0, 5, 5), (3, 5, 5), (7, 5, 5), (10, 5, 5), (11, 5, 5), (100, 0, 200), (100, 200, 0), (150, 3, 0), (2, 0, 0)])
 def test_evict_what_is_always_kept(keep, first, recent):
     g = np.random.default_rng(keep)
