@@ -96,9 +96,10 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 ? 5 : 2) kv_mass_kernel(M
     const int j = t0 >> a.c.page_shift;
     const int page = a.c.pages > 0 && t0 < w.len && j < a.ldt ? checked_page(a.c, a.table[w.b * a.ldt + j]) : -1;
     float sum[2] = {0.0f, 0.0f};
-    if (rows > 0) {
-        // A stage: ROWS rows of a head, with their log-sum-exps.
-        const int stages = (rows + ROWS - 1) / ROWS;
+    // A stage: ROWS rows of a head, with their log-sum-exps. Rows in front of those that see the CTA's first token give nothing.
+    const int64_t blind = a.causal ? static_cast<int64_t>(w.tile) * TOKENS - (static_cast<int64_t>(w.tokens) - w.n_q + i0) : 0;
+    const int stages = (rows + ROWS - 1) / ROWS, stage0 = blind <= 0 ? 0 : blind * G / ROWS < stages ? static_cast<int>(blind * G / ROWS) : stages;
+    if (stage0 < stages) {
         auto fetch = [&](int h, int stage, int buffer) {
             constexpr int PIECES = D / 8;
 #pragma unroll
@@ -129,7 +130,7 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 ? 5 : 2) kv_mass_kernel(M
             }
             scale = __ldg(a.c.k.scales + static_cast<int64_t>(page) * a.c.kv_heads + h);
         };
-        fetch(h0, 0, 0);
+        fetch(h0, stage0, 0);
         fetch_keys(h0);
         int buffer = 0;
         for (int h = h0; h < h1; ++h) {
@@ -146,10 +147,10 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 ? 5 : 2) kv_mass_kernel(M
             }
             const float fac = scale * a.scale_log2;
             if (h + 1 < h1) fetch_keys(h + 1);
-            for (int stage = 0; stage < stages; ++stage, buffer ^= 1) {
+            for (int stage = stage0; stage < stages; ++stage, buffer ^= 1) {
                 const bool last = stage + 1 == stages;
                 if (!last) fetch(h, stage + 1, buffer ^ 1);
-                else if (h + 1 < h1) fetch(h + 1, 0, buffer ^ 1);
+                else if (h + 1 < h1) fetch(h + 1, stage0, buffer ^ 1);
                 else asm volatile("cp.async.commit_group;" ::: "memory");
                 asm volatile("cp.async.wait_group 1;" ::: "memory");
                 __syncthreads();
