@@ -423,8 +423,8 @@ sqap_status sqap_kv_attention(const sqap_kv_cache* cache, const int32_t* table, 
 /*
  * The same attention within a window: the query at position p of its sequence (the i-th of n_q: p = lens[b] - n_q + i) sees token t <= p
  * if t > p - window, or if t < sinks (the first tokens stay visible). window >= 1, sinks >= 0; a window that reaches every token gives
- * the causal attention. Everything else is as in sqap_kv_attention with SQAP_KV_CAUSAL. Only the pages of tokens that some query of the
- * sequence sees, and their neighbours (up to 63 tokens on either side), are read: other entries of the table may be no pages.
+ * the causal attention. Everything else is as in sqap_kv_attention with SQAP_KV_CAUSAL. Only pages that hold a token which some query
+ * of the sequence sees are read: the others may have been given up, whatever their entries in the table are now.
  */
 size_t sqap_kv_attention_window_workspace_bytes(const sqap_kv_cache* cache, int batch, int max_q, int max_len, int heads, int window,
                                                 int sinks);

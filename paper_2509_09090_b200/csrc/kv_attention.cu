@@ -95,6 +95,7 @@ sqap_status combine(const AttnArgs& a, int64_t units, int dtype, cudaStream_t s)
 
 struct Plan {
     bool decode;
+    int row_tile;          // of the register kernel
     int tiles, splits, chunk;
 };
 // From the sizes (and the device) alone, so that the workspace can be asked for ahead: `units` sequences (or groups) of `rows` rows that look
@@ -110,17 +111,18 @@ struct Plan {
 int64_t least(int64_t x, int64_t y) { return x < y ? x : y; }
 // Histories of uneven lengths, as a rule; of about the same (windows); cut on the device, each into the same number of pieces.
 enum Cut { UNEVEN, ALIKE, EVENLY };
-Plan plan_rows(int64_t units, int kv_heads, int head_dim, int64_t rows, int64_t max_len, bool decode, Cut cut = UNEVEN) {
+Plan plan_rows(int64_t units, int kv_heads, int head_dim, int64_t rows, int64_t max_len, bool decode, Cut cut = UNEVEN, int row_tile = 0) {
     Plan p;
     p.decode = decode;
-    const int per_tile = p.decode ? decode_max_rows(head_dim) : head_dim <= 128 ? PREFILL_TC_ROWS : PREFILL_ROWS;
+    p.row_tile = row_tile > 0 ? row_tile : rows <= 8 ? 8 : decode_max_rows(head_dim);
+    const int per_tile = p.decode ? p.row_tile : head_dim <= 128 ? PREFILL_TC_ROWS : PREFILL_ROWS;
     p.tiles = static_cast<int>((rows + per_tile - 1) / per_tile);
     const int64_t ctas = size_product(units, kv_heads, p.tiles);
     const int64_t sms = sm_count();
     auto pieces = [&](int per_sm) { return ctas > 0 ? (sms * per_sm + ctas - 1) / ctas : 1; };
     int64_t splits;
     if (p.decode) {
-        const int64_t at_once = sms * (rows <= 8 && head_dim <= 128 ? 4 : 2);
+        const int64_t at_once = sms * (p.row_tile <= 8 && head_dim <= 128 ? 4 : 2);
         const int64_t fill = least(cut == ALIKE ? at_once / (ctas > 0 ? ctas : 1) : pieces(max_len > 1024 ? 4 : 3), (max_len + 255) / 256), even = least(pieces(16), max_len / 1024);
         splits = fill > even ? fill : even;
     } else {
@@ -167,28 +169,46 @@ Plan plan_window(int64_t batch, int kv_heads, int group, int head_dim, int64_t m
 struct SharedPlan {
     bool together;         // one launch of the register kernel over the prefix and the own tokens of a group's sequences
     Plan prefix, own;      // `together`: prefix is its plan
+    View own_view;         // the own tokens: a CTA takes a sequence, or a tile of the group's rows
+    int64_t own_units;
     int prefix_parts;      // 0: there is no prefix
     bool join;             // the kernel of the own tokens joins the pieces of the prefix
     int parts;             // pieces in the workspace
 };
-// Tiles of a group's rows up to which the register kernel takes the group.
-constexpr int SHARED_TILES = 3;
+// The register kernel takes a group in tiles of 8 rows, each of which reads the prefix (from L2, but for one) and its own sequences' tokens;
+// the kernels for many rows read a prefix once for 256 (128) rows, and then the own tokens want a launch of their own. us, tiles / the
+// others, 40 to 100 own tokens: 32 heads, prefix 256, 16 groups of 10, 32, 64 rows 40 / 71, 80 / 107, 143 / 165; 8 heads, prefix 16384,
+// 16 and 32 rows 23 / 34, 40 / 32; prefix 1000, 16 groups of 16, 32, 64 rows 31 / 34, 43 / 37, 63 / 49; head_dim 256, prefix 4096, 32
+// rows 43 / 63. (Tiles of 16 rows: 45, 108, 188; 28, 37; 39, 53, 82.)
+bool in_row_tiles(int head_dim, int64_t rows, int64_t max_group, int64_t max_prefix) {
+    if (max_prefix == 0 || rows > decode_max_rows(head_dim)) return false;
+    const int64_t tiles = (rows * max_group + 7) / 8;
+    return tiles <= (head_dim <= 128 ? 3 : 6) || size_product(tiles - 1, max_prefix) <= (head_dim <= 128 ? 2048 : 8192);
+}
 SharedPlan plan_shared(int kv_heads, int group, int head_dim, int64_t max_q, int64_t max_len, int64_t groups, int64_t max_group,
                        int64_t max_prefix) {
     SharedPlan p;
     const int64_t rows = max_q * group, together = rows * max_group;
     const int64_t own = max_len > max_prefix ? max_len - max_prefix : 1;
-    const int64_t tile = decode_max_rows(head_dim);
-    p.together = together <= SHARED_TILES * tile;
+    const int tile = decode_max_rows(head_dim);
+    const int64_t met = size_product(own, least(max_group, 8 / rows + 1));      // own tokens of the sequences that a row tile meets
+    p.together = in_row_tiles(head_dim, rows, max_group, max_prefix);
     if (p.together) {
-        const int64_t members = least(max_group, (together < tile ? together : tile) / rows + 1);
-        p.prefix = p.own = plan_rows(groups, kv_heads, head_dim, together, least(size_product(own, members) + max_prefix, 1 << 30), true, EVENLY);
+        p.prefix = p.own = plan_rows(groups, kv_heads, head_dim, together, least(met + max_prefix, 1 << 30), true, EVENLY, 8);
+        p.own_view = VIEW_SHARED;
+        p.own_units = groups;
         p.prefix_parts = 0;
         p.join = false;
         p.parts = p.prefix.splits;
         return p;
     }
-    p.own = plan_rows(size_product(groups, max_group), kv_heads, head_dim, rows, own, rows <= tile, EVENLY);
+    const int64_t places = size_product(groups, max_group);
+    // Short tokens of many sequences: a tile of rows to a CTA (16 x 16 sequences of 4 rows, 8 heads, 64 own tokens: 49 us, a sequence to a CTA 53;
+    // 16 x 64 of one row, 32 heads, 40 own tokens: 165 / 311; but 4 x 64 of one row, 8 heads, 1000 own tokens: 157 / 143).
+    p.own_view = rows <= 4 && own <= 512 && size_product(places, kv_heads) > 8ll * sm_count() ? VIEW_OWN_ROWS : VIEW_OWN;
+    p.own_units = p.own_view == VIEW_OWN ? places : groups;
+    p.own = p.own_view == VIEW_OWN ? plan_rows(places, kv_heads, head_dim, rows, own, rows <= tile, EVENLY)
+                                   : plan_rows(groups, kv_heads, head_dim, together, least(met, 1 << 30), true, EVENLY, 8);
     p.prefix = plan_rows(groups, kv_heads, head_dim, together, max_prefix, false, EVENLY);
     p.prefix_parts = max_prefix > 0 ? p.prefix.splits : 0;
     p.join = p.own.decode && p.own.splits == 1 && p.prefix_parts > 0;
@@ -198,7 +218,7 @@ SharedPlan plan_shared(int kv_heads, int group, int head_dim, int64_t max_q, int
 }
 bool shared_fits(const sqap_kv_cache* c, int groups, int max_group, int max_q, int heads, const SharedPlan& p) {
     return size_product(max_group, max_q, heads / c->kv_heads) <= 1 << 30 && grid_fits(groups, c->kv_heads, p.prefix) &&
-           grid_fits(size_product(groups, max_group), c->kv_heads, p.own) && size_product(groups, max_group, heads, max_q) <= 4ll * 0x7FFFFFFF;
+           grid_fits(p.own_units, c->kv_heads, p.own) && size_product(groups, max_group, heads, max_q) <= 4ll * 0x7FFFFFFF;
 }
 
 sqap_status take_workspace(AttnArgs& a, int parts, void* workspace, size_t workspace_bytes) {
@@ -216,6 +236,7 @@ sqap_status launch(AttnArgs a, const Plan& p, View view, int64_t units, int type
     a.splits = p.splits;
     a.chunk = p.chunk;
     a.tiles = p.tiles;
+    a.row_tile = p.row_tile;
     if (p.decode) return launch_kv_decode(a, view, units, type, dtype, s);
     if (a.c.head_dim <= 128) return launch_kv_prefill_tc(a, view, units, type, dtype, s);
     return launch_kv_prefill(a, view, units, type, dtype, s);
@@ -379,7 +400,7 @@ extern "C" sqap_status sqap_kv_attention_shared(const sqap_kv_cache* cache, cons
     }
     a.part0 = p.join ? 0 : p.prefix_parts;
     a.join = p.join ? p.prefix_parts : 0;
-    st = launch(a, p.own, VIEW_OWN, places, cache->type, dtype, s);
+    st = launch(a, p.own, p.own_view, p.own_units, cache->type, dtype, s);
     if (st != SQAP_OK || a.parts <= 1 || p.join) return st;
     a.part0 = 0;
     return combine(a, places, dtype, s);

@@ -35,9 +35,9 @@ struct AttnArgs {
     int splits, chunk;     // a history is cut into `splits` pieces of `chunk` keys, or one
     float* part_o;         // [batch][heads][max_q][parts][D]
     float2* part_ml;       // the same without D: maximum and denominator
-    int tiles;             // row tiles per (sequence, key/value head)
+    int tiles, row_tile;   // row tiles per (sequence, key/value head); rows of one (register kernel)
     int parts, part0;      // pieces of a row that are joined (1: the kernel writes the output itself), and the first of this launch
-    int join;              // VIEW_OWN: pieces of the prefix that the kernel joins with its rows' own tokens, and writes the output
+    int join;              // VIEW_OWN, VIEW_OWN_ROWS: pieces of the prefix that the kernel joins with its rows' own tokens, and writes the output
     // views other than VIEW_ALL
     int window, sinks;     // VIEW_WINDOW
     const int32_t* cu_group;   // VIEW_PREFIX, VIEW_OWN: sequences of the groups
@@ -48,11 +48,13 @@ struct AttnArgs {
 
 // What the rows of a launch look at: all (causal or not); the tokens of a window and the first ones; the prefix that the
 // sequences of a group share, rows of all of them together; the tokens of a sequence behind its group's prefix; both, rows of the
-// group together (register kernel only); all, and the scores are kept (register kernel only).
-enum View { VIEW_ALL, VIEW_WINDOW, VIEW_PREFIX, VIEW_OWN, VIEW_SHARED, VIEW_SCORES };
-// Rows of all sequences of a group together.
+// group together; the own tokens alone, rows of the group together; all, and the scores are kept (the last three: register kernel only).
+enum View { VIEW_ALL, VIEW_WINDOW, VIEW_PREFIX, VIEW_OWN, VIEW_SHARED, VIEW_OWN_ROWS, VIEW_SCORES };
+// Rows of all sequences of a group together; those of which look at the tokens of several sequences.
 template <int VIEW>
-constexpr bool by_group = VIEW == VIEW_PREFIX || VIEW == VIEW_SHARED;
+constexpr bool by_group = VIEW == VIEW_PREFIX || VIEW == VIEW_SHARED || VIEW == VIEW_OWN_ROWS;
+template <int VIEW>
+constexpr bool of_several = VIEW == VIEW_SHARED || VIEW == VIEW_OWN_ROWS;
 
 // Work of a CTA, from its index.
 struct Where {
@@ -259,11 +261,6 @@ __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 x) { return _
 // 9 to 16 rows, 8 heads of 128: 100 keys 8.3 / 9.4, 500 keys 14.7 / 16.1, 2048 keys 31 / 44, 32 sequences of 16384 182 / 526, 64 of 290
 // 21 / 34. The other sign only where 128 CTAs walk some 290 keys in one round, 14.2 / 12.6, which no rule of its own was made for.
 inline int decode_max_rows(int head_dim) { return head_dim == 256 ? 8 : 16; }
-// Rows of a CTA of the register kernel: all of its sequence, or a tile of its group's.
-inline int decode_row_tile(const AttnArgs& a, int view, int head_dim) {
-    const int64_t rows = static_cast<int64_t>(a.max_q) * a.group * (view == VIEW_SHARED ? a.max_group : 1);
-    return rows > 8 && head_dim != 256 ? 16 : 8;
-}
 constexpr int PREFILL_ROWS = 128, PREFILL_TC_ROWS = 256;   // query rows of a CTA's item
 // `units`: what a launch goes over, sequences, groups (VIEW_PREFIX) or places of sequences in groups (VIEW_OWN).
 sqap_status launch_kv_decode(const AttnArgs& a, View view, int64_t units, int type, int dtype, cudaStream_t s);

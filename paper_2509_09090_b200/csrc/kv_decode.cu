@@ -76,25 +76,25 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
 
     pdl_launch_dependents();
     pdl_wait();
-    const Where w = locate_view<VIEW>(a, blockIdx.x, VIEW == VIEW_SHARED ? a.tiles : 1);
+    const Where w = locate_view<VIEW>(a, blockIdx.x, of_several<VIEW> ? a.tiles : 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int G = a.group;
     const int rows_all = rows_of<VIEW>(a, w);      // row r: query r / G, head h G + r % G
-    const int r_first = VIEW == VIEW_SHARED ? w.tile * 8 * NT : 0;
-    const int rows = VIEW == VIEW_SHARED ? min(rows_all - r_first, 8 * NT) : rows_all;
+    const int r_first = of_several<VIEW> ? w.tile * 8 * NT : 0;
+    const int rows = min(rows_all - r_first, 8 * NT);
     if (rows <= 0) return;
     const Span span = span_of<VIEW, STEP>(a, w, 0);
     // VIEW_SHARED: the keys are the prefix, then the own tokens of each sequence that has rows here, in runs of 16; lane 0 knows the
     // prefix, lane s the s-th of the sequences: the run it begins with, its first token less 16 times that, and its last
     int seg_run = 0x7FFFFFFF, seg_base = 0, seg_end = 0, seg0 = 0, runs = 0;
-    if constexpr (VIEW == VIEW_SHARED) {
+    if constexpr (of_several<VIEW>) {
         const int per = a.max_q * G;
         seg0 = r_first / per;
         const int segments = (r_first + rows - 1) / per - seg0 + 2;
         int mine = 0, first = 0;
         if (lane == 0) {
             seg_end = w.prefix;
-            mine = (w.prefix + 15) >> 4;
+            mine = VIEW == VIEW_SHARED ? (w.prefix + 15) >> 4 : 0;
         } else if (lane < segments) {
             seg_end = min(max(a.lens[w.b + seg0 + lane - 1], 0), a.max_len);
             first = w.prefix & ~15;
@@ -110,9 +110,9 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
         if (lane < segments) seg_run = upto - mine;
         seg_base = first - 16 * (upto - mine);
     }
-    auto segment_of = [&](int k) { return VIEW == VIEW_SHARED ? __popc(__ballot_sync(0xffffffffu, seg_run <= k >> 4)) - 1 : 0; };
-    auto token_of = [&](int k, int seg) { return VIEW == VIEW_SHARED ? __shfl_sync(0xffffffffu, seg_base, seg) + k : span.token(k); };
-    const int len = VIEW == VIEW_SHARED ? 16 * runs : w.len - span.gap;
+    auto segment_of = [&](int k) { return of_several<VIEW> ? __popc(__ballot_sync(0xffffffffu, seg_run <= k >> 4)) - 1 : 0; };
+    auto token_of = [&](int k, int seg) { return of_several<VIEW> ? __shfl_sync(0xffffffffu, seg_base, seg) + k : span.token(k); };
+    const int len = of_several<VIEW> ? 16 * runs : w.len - span.gap;
     const int chunk = chunk_of<VIEW>(a, len);
     const int key0 = w.split * chunk;              // keys: tokens without the gap
     const int key1 = a.splits > 1 ? min(key0 + chunk, len) : len;
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 uint4 u = make_uint4(0, 0, 0, 0);
-                if (VIEW != VIEW_SHARED || real) u = __ldg(reinterpret_cast<const uint4*>(src + 64 * c + 16 * t) + i);
+                if (!of_several<VIEW> || real) u = __ldg(reinterpret_cast<const uint4*>(src + 64 * c + 16 * t) + i);
                 unpack8<T>(u, v[c] + 8 * i);
             }
 #pragma unroll
@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
             fac[n][e] = __shfl_sync(0xffffffffu, back, (2 * t + e) * 4) * a.scale_log2;
             const Row seen_by = row_at<VIEW>(a, w, rows_all, r_first + 8 * n + 2 * t + e);
             lim[n][e] = seen_by.sees;
-            low[n][e] = VIEW == VIEW_SHARED ? seen_by.b - w.b - seg0 + 1 : first_seen<VIEW>(a, w, seen_by.i);
+            low[n][e] = of_several<VIEW> ? seen_by.b - w.b - seg0 + 1 : first_seen<VIEW>(a, w, seen_by.i);
             if (seen_by.real) {
                 lim_all = min(lim_all, lim[n][e]);
                 low_all = max(low_all, low[n][e]);
@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
     lim_all = __reduce_min_sync(0xffffffffu, lim_all);
     low_all = __reduce_max_sync(0xffffffffu, low_all);
     // the last row sees the most
-    const int lim_max = VIEW == VIEW_SHARED ? len : visible(a, w, rows / G - 1) - span.gap;
+    const int lim_max = of_several<VIEW> ? len : visible(a, w, rows / G - 1) - span.gap;
     const int end = a.c.pages > 0 ? min(key1, lim_max) : 0;
 
     float o[NT][MT][4];
@@ -202,7 +202,7 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
         for (int u = 0; u < GROUPS; ++u) {
             const int key = k0 + 16 * u, seg = segment_of(key), token = token_of(key, seg), j = token >> shift;
             entry[u] = -1;
-            if (key < end && j < a.ldt && run_counts<VIEW>(a, token, from)) entry[u] = __ldg(table + (VIEW == VIEW_SHARED && seg > 0 ? (seg0 + seg - 1) * a.ldt : 0) + j);
+            if (key < end && j < a.ldt && run_counts<VIEW>(a, token, from)) entry[u] = __ldg(table + (of_several<VIEW> && seg > 0 ? (seg0 + seg - 1) * a.ldt : 0) + j);
         }
     };
     // a page that does not exist is read as page 0 and masked
@@ -293,10 +293,10 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
             const int base = k0 + 16 * u;
             // the run's first token, and those of it that are the segment's: from .. until - 1
             const int seg = segment_of(base), token0 = WHOLE ? base : token_of(base, seg);
-            const int begin = VIEW == VIEW_OWN || (VIEW == VIEW_SHARED && seg > 0) ? w.prefix : 0;
-            const int until = VIEW == VIEW_SHARED ? (base < end ? __shfl_sync(0xffffffffu, seg_end, seg) : 0) : end - base + token0;
+            const int begin = VIEW == VIEW_OWN || (of_several<VIEW> && seg > 0) ? w.prefix : 0;
+            const int until = of_several<VIEW> ? (base < end ? __shfl_sync(0xffffffffu, seg_end, seg) : 0) : end - base + token0;
             // most runs are seen by all rows as they are
-            const bool plain = there[u] && token0 + 16 <= min(until, lim_all) && (VIEW != VIEW_OWN || token0 >= begin) && (VIEW != VIEW_SHARED || seg == 0) &&
+            const bool plain = there[u] && token0 + 16 <= min(until, lim_all) && (VIEW != VIEW_OWN || token0 >= begin) && (!of_several<VIEW> || seg == 0) &&
                                (VIEW != VIEW_WINDOW || token0 >= low_all);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -323,7 +323,7 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
                         for (int e = 0; e < 4; ++e) {
                             const int token = token0 + g + (e >> 1) * 8;
                             bool seen = there[u] && token < min(lim[n][e & 1], until);
-                            if (VIEW == VIEW_SHARED) seen = seen && token >= begin && (seg == 0 || seg == low[n][e & 1]);
+                            if (of_several<VIEW>) seen = seen && token >= begin && (seg == 0 || seg == low[n][e & 1]);
                             if (VIEW == VIEW_OWN) seen = seen && token >= begin;
                             if (VIEW == VIEW_WINDOW) seen = seen && (token >= low[n][e & 1] || token < a.sinks);
                             if (!seen) sc[u][n][e] = -INFINITY;
@@ -450,8 +450,8 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
             for (int e = 0; e < 8; ++e) y[e] = fmaf(red_o[i][r][d + e], f, y[e]);
         }
         const Row row = row_at<VIEW>(a, w, rows_all, r_first + r);
-        if (VIEW == VIEW_SHARED && !row.real) continue;
-        if (VIEW == VIEW_OWN && a.join > 0) {
+        if (of_several<VIEW> && !row.real) continue;
+        if ((VIEW == VIEW_OWN || VIEW == VIEW_OWN_ROWS) && a.join > 0) {
             // the pieces of the prefix are there: joined here
             const int64_t at = part_index(a, row.b, row.head, row.i, 0);
             float top = mm;
@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
             }
             mm = top;
         }
-        if (a.parts > 1 && !(VIEW == VIEW_OWN && a.join > 0)) {
+        if (a.parts > 1 && !((VIEW == VIEW_OWN || VIEW == VIEW_OWN_ROWS) && a.join > 0)) {
             const int64_t at = part_index(a, row.b, row.head, row.i, w.split);
             if (d == 0) a.part_ml[at] = make_float2(mm, ll);
             float4* po = reinterpret_cast<float4*>(a.part_o + at * D + d);
@@ -503,7 +503,7 @@ cudaError_t launch_rows(const AttnArgs& a, unsigned grid, cudaStream_t s) {
     constexpr int GROUPS = D == 64 ? 2 : 1;
     if constexpr (D != 256)                         // 8 rows at most: decode_max_rows()
         // 9 to 16 rows: one / two groups, 32 x 8192 tokens x 8 heads of 128, 12 rows, 134 / 115; 16 x 2048, 16 rows, 35 / 31.
-        if (decode_row_tile(a, VIEW, D) > 8)
+        if (a.row_tile > 8)
             return launch_dependent(kv_decode_kernel<T, TYPE, D, 2, 2, VIEW>, dim3(grid), dim3(WARPS * 32), 0, s, a);
     return launch_dependent(kv_decode_kernel<T, TYPE, D, 1, GROUPS, VIEW>, dim3(grid), dim3(WARPS * 32), 0, s, a);
 }
@@ -524,10 +524,11 @@ cudaError_t launch_view(const AttnArgs& a, int type, int dtype, unsigned grid, c
 }  // namespace
 
 sqap_status launch_kv_decode(const AttnArgs& a, View view, int64_t units, int type, int dtype, cudaStream_t s) {
-    const unsigned grid = static_cast<unsigned>(units * a.c.kv_heads * a.splits * (view == VIEW_SHARED ? a.tiles : 1));
+    const unsigned grid = static_cast<unsigned>(units * a.c.kv_heads * a.splits * a.tiles);
     switch (view) {
         case VIEW_WINDOW: return finish_launch(launch_view<VIEW_WINDOW>(a, type, dtype, grid, s));
         case VIEW_SHARED: return finish_launch(launch_view<VIEW_SHARED>(a, type, dtype, grid, s));
+        case VIEW_OWN_ROWS: return finish_launch(launch_view<VIEW_OWN_ROWS>(a, type, dtype, grid, s));
         case VIEW_OWN: return finish_launch(launch_view<VIEW_OWN>(a, type, dtype, grid, s));
         case VIEW_SCORES: return finish_launch(launch_view<VIEW_SCORES>(a, type, dtype, grid, s));
         default: return finish_launch(launch_view<VIEW_ALL>(a, type, dtype, grid, s));

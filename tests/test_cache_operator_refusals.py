@@ -9,7 +9,7 @@ HISTORY = dict(table=16, ldt=4, batch=2, lens=16, cu=16, max_q=3, max_len=64)
 Q = dict(q=16, ldq=256, heads=4, scale=0.1)
 REST = dict(out=16, ldo=256, lse=None, dt=0, work=None, bytes=0, stream=None)
 WINDOW = {**HISTORY, **Q, **dict(window=8, sinks=1), **REST}
-SHARED = {**HISTORY, **dict(cu_group=16, groups=1, max_group=64, prefix=16, max_prefix=32), **Q, **dict(flags=1), **REST}
+SHARED = {**HISTORY, **dict(cu_group=16, groups=1, max_group=64, prefix=16, max_prefix=64), **Q, **dict(flags=1), **REST}
 MASS = {**HISTORY, **Q, **dict(flags=1, last_q=1, out=16, ldo=256, lse=16, past=None, mass=16, ldm=64, dt=0, work=16, bytes=1 << 20, stream=None)}
 SHARED_BYTES = 2 * 4 * 3 * 2 * (64 * 4 + 8)        # rows x pieces
 
@@ -81,7 +81,7 @@ def test_workspace_bytes():
     window, shared, mass = L.sqap_kv_attention_window_workspace_bytes, L.sqap_kv_attention_shared_workspace_bytes, L.sqap_kv_attention_mass_workspace_bytes
     assert window(cache(), 4, 1, 1 << 20, 2, 100, 4) == 0                       # a short window is not cut, however long the history
     assert window(cache(), 1, 1, 16384, 2, 16384, 0) > 0 and window(cache(), 1, 1, 16384, 2, 0, 0) == window(cache(), 1, 1, 16384, 2, 5, -1) == 0
-    assert shared(cache(), 2, 3, 64, 1, 64, 32, 4) == SHARED_BYTES and shared(cache(), 2, 3, 64, 1, 2, 32, 4) == 0     # few rows: one launch, one piece
+    assert shared(cache(), 2, 3, 64, 1, 64, 64, 4) == SHARED_BYTES and shared(cache(), 2, 3, 64, 1, 2, 64, 4) == 0     # few rows: one launch, one piece
     assert shared(cache(), 2, 3, 64, 1, 64, 0, 4) == 0 == shared(cache(), 2, 3, 64, 0, 2, 32, 4) == shared(cache(), 2, 3, 64, 1, 2, -1, 4)
     assert mass(cache(), 0, 1, 64, 2, 1) == mass(cache(), 1, 1, 64, 3, 1) == mass(cache(), 1, 1, 64, 2, -1) == 0
     for f, args in ((window, (5, 5)), (mass, (1,))):

@@ -255,6 +255,7 @@ def check_shared(gr, new, heads, dtype, causal=True, seed=0, max_prefix=None, ma
     ("fp16", 2, 1, 64, 16, [70, 2], [90, 17], [3] * 72, [1] * 72),
     ("bf16", 2, 1, 256, 16, [9, 20], [200, 65], [17] * 29, [1] * 29),
     ("fp16", 6, 3, 128, 64, [3, 4], [130, 128], [5, 6, 7, 300, 6, 5, 9], [5, 0, 3, 2, 4, 5, 1]),
+    ("fp16", 128, 32, 64, 16, [20, 19], [120, 110], [1 + b % 13 for b in range(39)], [1 - b % 5 // 4 for b in range(39)]),   # tiles over own tokens
     ("bf16", 4, 2, 128, 16, [2, 3], [70, 300], [90, 60, 100, 40, 33], [90, 31, 64, 40, 1])])
 def test_shared_prefix(dtype, heads, H, D, P, sizes, prefixes, own, new, kind):
     gr = Group(sizes, prefixes, own, H, D, P, kind, seed=len(own))
@@ -277,36 +278,34 @@ def test_shared_queries_inside_the_prefix(D, heads):
     check_shared(gr, [40, 30, 60, 0, 20, 40, 33], heads, "bf16")
 
 
-@pytest.mark.parametrize("D,copies", [(128, 3), (128, 60), (256, 30)])
-def test_shared_limits_drop_work_and_move_nothing(D, copies):
+@pytest.mark.parametrize("D,copies,heads", [(128, 3, 2), (128, 24, 2), (128, 24, 8), (256, 30, 2), (256, 40, 16)])
+def test_shared_limits_drop_work_and_move_nothing(D, copies, heads):
     """More sequences than max_group, prefixes beyond max_prefix, sequences outside of all groups, tokens beyond max_len."""
     own = [7 + b for b in range(copies + 3)]
     gr = Group([1, copies, 2], [64, 130, 0], own, 1, D, 64, R.INT8, seed=5)
     new = [1] * (copies + 3)
-    check_shared(gr, new, 2, "fp16", max_group=copies - 1)
+    check_shared(gr, new, heads, "fp16", max_group=copies - 1)
     gr.table = gr.s.table.copy()
     shared = [gr.s.table[1, :2]]
     gr.table[2:copies + 1, :2] = shared[0]                  # beyond max_prefix every sequence reads its own entries
     for a in "kv":
         gr.s.raw[a][gr.s.raw[a] == 0x7F] = 0x31
     gr.s.to_device()
-    check_shared(gr, new, 2, "fp16", max_prefix=100)
-    check_shared(gr, new, 2, "fp16", max_prefix=0)
+    check_shared(gr, new, heads, "fp16", max_prefix=100)
+    check_shared(gr, new, heads, "fp16", max_prefix=0)
     gr.prefix = gr.prefix[1:2]
     some = np.array([1, copies + 1])
-    base = gr.first
     gr.first, gr.sizes = np.array([0, 1, copies + 1, copies + 3]), [1, copies, 2]
     gr.prefix = [0, 130, 0]
-    qs = Queries(gr.s, new, 2, "fp16")
+    qs = Queries(gr.s, new, heads, "fp16")
     s, table = gr.s, ints(gr.table)
-    n = B.sqap_kv_attention_shared_workspace_bytes(s.cache, copies + 3, 1, max(gr.lens), 1, copies, 130, 2)
+    n = B.sqap_kv_attention_shared_workspace_bytes(s.cache, copies + 3, 1, max(gr.lens), 1, copies, 130, heads)
     B.sqap_kv_attention_shared(s.cache, table, table.stride(0), copies + 3, ints(gr.lens), qs.dcu, 1, max(gr.lens), ints(some), 1, copies,
-                               ints([130]), 130, qs.q, qs.q.stride(0), 2, 1 / math.sqrt(D), 1, qs.out, qs.out.stride(0), qs.lse, 0, scratch(n), n)
+                               ints([130]), 130, qs.q, qs.q.stride(0), heads, 1 / math.sqrt(D), 1, qs.out, qs.out.stride(0), qs.lse, 0, scratch(n), n)
     o, l = qs.results([(qs.cu[1], qs.cu[copies + 1])])
     for b in range(1, copies + 1):
         r, n = slice(qs.cu[b], qs.cu[b + 1]), gr.lens[b]
         check_rows(s, o[r], l[r], qs.qn[r], *gr.tokens(b, 130), C.causal(n, 1), "fp16", 1 / math.sqrt(D))
-    assert base is not None
 
 
 def test_shared_groups_out_of_order_or_beyond_the_batch_touch_nothing():
