@@ -309,11 +309,21 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
                         for (int e = 0; e < 4; ++e)
                             if (!there[u] || token0 + g + (e >> 1) * 8 >= min(lim[n][e & 1], until)) sc[u][n][e] = -INFINITY;
                     }
+                    const int r = 8 * n + 2 * t;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int token = token0 + g + (e >> 1) * 8, r = 8 * n + 2 * t + (e & 1);
-                        if (token < end && r < rows) scores[static_cast<int64_t>(token) * per_token + r] = sc[u][n][e];
-                        sc[u][n][e] += lv[u];
+                    for (int half = 0; half < 2; ++half) {
+                        const int token = token0 + g + half * 8;
+                        float* to = scores + static_cast<int64_t>(token) * per_token + r;
+                        if (token < end && r < rows) {
+                            if ((per_token & 1) == 0) {
+                                *reinterpret_cast<float2*>(to) = make_float2(sc[u][n][2 * half], sc[u][n][2 * half + 1]);
+                            } else {
+                                to[0] = sc[u][n][2 * half];
+                                if (r + 1 < rows) to[1] = sc[u][n][2 * half + 1];
+                            }
+                        }
+                        sc[u][n][2 * half] += lv[u];
+                        sc[u][n][2 * half + 1] += lv[u];
                     }
                 } else {
 #pragma unroll
