@@ -329,14 +329,26 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 && NT == 1 && GROUPS == 1
 #pragma unroll
                     for (int e = 0; e < 4; ++e) sc[u][n][e] = fmaf(sc[u][n][e], f[e & 1], lv[u]);
                     if (!plain) {
+                        int limit[2];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int token = token0 + g + (e >> 1) * 8;
-                            bool seen = there[u] && token < min(lim[n][e & 1], until);
-                            if (of_several<VIEW>) seen = seen && token >= begin && (seg == 0 || seg == low[n][e & 1]);
-                            if (VIEW == VIEW_OWN) seen = seen && token >= begin;
-                            if (VIEW == VIEW_WINDOW) seen = seen && (token >= low[n][e & 1] || token < a.sinks);
-                            if (!seen) sc[u][n][e] = -INFINITY;
+                        for (int e = 0; e < 2; ++e) {
+                            limit[e] = there[u] ? min(lim[n][e], until) : 0;
+                            if (of_several<VIEW> && seg > 0 && seg != low[n][e]) limit[e] = 0;       // another sequence's tokens
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (token0 + g + (e >> 1) * 8 >= limit[e & 1]) sc[u][n][e] = -INFINITY;
+                        if ((VIEW == VIEW_OWN || of_several<VIEW>) && token0 < begin) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (token0 + g + (e >> 1) * 8 < begin) sc[u][n][e] = -INFINITY;
+                        }
+                        if (VIEW == VIEW_WINDOW && token0 < low_all) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int token = token0 + g + (e >> 1) * 8;
+                                if (token < low[n][e & 1] && token >= a.sinks) sc[u][n][e] = -INFINITY;
+                            }
                         }
                     }
                 }
