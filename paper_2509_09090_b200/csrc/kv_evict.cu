@@ -50,8 +50,11 @@ __device__ __forceinline__ uint2 remote_load(uint32_t at) {
 __device__ __forceinline__ void remote_store(uint32_t at, uint32_t x, uint32_t y) {
     asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(at), "r"(x), "r"(y) : "memory");
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+    cluster_arrive();
+    cluster_wait();
 }
 
 // CTAS CTAs, a cluster, take a sequence; EACH tokens a thread and round, a CTA's side by side; longer sequences take several rounds. Every
@@ -71,6 +74,7 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
     __shared__ uint32_t found[3];        // the bin, how many are above it, how many in it
     __shared__ uint32_t front[RUNS];     // of each run of 32 tokens: those in front of it that stay, and (upper half) that are at the border
     pdl_launch_dependents();
+    if (CTAS > 1) cluster_arrive();
     pdl_wait();
     const int i = blockIdx.x / CTAS, rank = blockIdx.x % CTAS, row = a.src[i], dst = a.dst ? a.dst[i] : -1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const bool there = row >= 0 && row < a.rows;
@@ -106,6 +110,7 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
         }
     };
     if (rounds == 1) load(0);
+    if (CTAS > 1) cluster_wait();        // all CTAs have started: their shared memory may be written
 
     // border: orders above it stay, of those equal to it the first `ties` in their places
     uint32_t border = ALWAYS - 1, ties = 0;
