@@ -13,7 +13,7 @@ constexpr int COMBINE_SPLITS = 8;
 // shared memory; four rows / WARPS to a CTA.
 template <typename T, int D, int WARPS>
 __global__ void __launch_bounds__(128) kv_combine_kernel(AttnArgs a) {
-    __shared__ float red[WARPS > 1 ? WARPS : 1][WARPS > 1 ? D : 1], red_l[4];
+    __shared__ alignas(8) float red[WARPS > 1 ? WARPS : 1][WARPS > 1 ? D : 1], red_l[4];
     pdl_launch_dependents();
     pdl_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % WARPS;

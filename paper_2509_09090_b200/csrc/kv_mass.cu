@@ -75,8 +75,8 @@ template <typename T, int TYPE, int D>
 __global__ void __launch_bounds__(WARPS * 32, D <= 128 ? 5 : 2) kv_mass_kernel(MassArgs m) {
     constexpr int KC = D / 64, LD = D + 8;           // halves of a row in shared memory: 16 bytes on in the banks from row to row
     __shared__ alignas(16) T s_q[2][ROWS][LD];
-    __shared__ float s_lse[2][ROWS];
-    __shared__ int s_sees[2][ROWS];    // tokens that the row sees, 0 for no row
+    __shared__ alignas(8) float s_lse[2][ROWS];
+    __shared__ alignas(8) int s_sees[2][ROWS];    // tokens that the row sees, 0 for no row
     pdl_launch_dependents();
     pdl_wait();
     const AttnArgs& a = m.a;
