@@ -471,7 +471,7 @@ sqap_status sqap_kv_attention_mass(const sqap_kv_cache* cache, const int32_t* ta
  * kept: device int32 [n rows, ldkept apart], the tokens that stay, ascending, then -1 up to ldkept; n_kept: device int32 [n]. At most
  * ldkept tokens stay. That is the list that sqap_kv_compact takes. dst_rows (may be NULL): the weights of the tokens that stay become
  * the first n_kept[i] of row dst_rows[i] of mass; no row may be the destination of two entries, or of one and the source of another. A source
- * that is no row has no tokens; a destination that is no row gets nothing. `rows` rows of mass and lens exist. max_len only sizes the
+ * that is no row has no tokens; a destination that is no row, or the source itself, gets nothing. `rows` rows of mass and lens exist. max_len only sizes the
  * launch beyond that.
  */
 sqap_status sqap_kv_evict(float* mass, int64_t ldm, int rows, const int32_t* lens, const int32_t* src_rows, const int32_t* dst_rows,

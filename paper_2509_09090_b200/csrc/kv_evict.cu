@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
     }
 
     int32_t* kept = a.kept + i * a.ldkept;
-    float* carry = dst >= 0 && dst < a.rows ? a.mass + dst * a.ldm : nullptr;
+    float* carry = dst >= 0 && dst < a.rows && dst != row ? a.mass + dst * a.ldm : nullptr;
     uint32_t sure_before = 0, ties_before = 0;               // of earlier rounds, and of CTAs in front
     for (int r = 0; r < rounds; ++r) {
         if (rounds > 1) load(r);

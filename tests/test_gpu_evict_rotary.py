@@ -165,3 +165,16 @@ def test_rotary_is_undone_by_the_opposite_positions():
     pair = (size.reshape(50, 8, 2, 32) ** 2).sum(2, keepdim=True).sqrt().expand(-1, -1, 2, -1).reshape(50, 512)
     # two roundings to bf16, the first of which (of either element of the pair, 2^-8 of its value) is turned back
     assert ((z.float() - x.float()).abs() <= pair * (2.0 ** -8 * math.sqrt(2) + 2.0 ** -8 + 2.0 ** -10)).all()
+
+
+@pytest.mark.parametrize("width", [96, 4097, 16384, 40000])
+def test_evict_into_the_source_itself(width):
+    """An entry whose destination is its own source chooses its tokens, and moves no weights."""
+    m = weights(np.random.default_rng(width), 2, width)
+    keep = width // 3
+    d, kept = dev(m.copy()), torch.zeros((2, keep), dtype=torch.int32, device=DEV)
+    count = torch.zeros(2, dtype=torch.int32, device=DEV)
+    B.sqap_kv_evict(d, width, 2, ints([width, width - 5]), ints([0, 1]), ints([0, 1]), 2, ints([keep, keep]), 4, 9, width, kept, keep, count)
+    torch.cuda.synchronize()
+    assert kept.tolist() == C.evict(m, [width, width - 5], [0, 1], [keep, keep], 4, 9, width, keep)
+    assert count.tolist() == [keep, keep] and np.array_equal(d.cpu().numpy(), m)
