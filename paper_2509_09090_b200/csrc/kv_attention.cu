@@ -192,9 +192,9 @@ SharedPlan plan_shared(int kv_heads, int group, int head_dim, int64_t max_q, int
     const int64_t own = max_len > max_prefix ? max_len - max_prefix : 1;
     const int tile = decode_max_rows(head_dim);
     const int64_t met = size_product(own, least(max_group, 8 / rows + 1));      // own tokens of the sequences that a row tile meets
-    p.together = in_row_tiles(head_dim, rows, max_group, max_prefix);
+    p.together = in_row_tiles(head_dim, rows, max_group, max_prefix) && met + max_prefix <= 1 << 30;      // the kernel's 32-bit places
     if (p.together) {
-        p.prefix = p.own = plan_rows(groups, kv_heads, head_dim, together, least(met + max_prefix, 1 << 30), true, EVENLY, 8);
+        p.prefix = p.own = plan_rows(groups, kv_heads, head_dim, together, met + max_prefix, true, EVENLY, 8);
         p.own_view = VIEW_SHARED;
         p.own_units = groups;
         p.prefix_parts = 0;
@@ -208,7 +208,7 @@ SharedPlan plan_shared(int kv_heads, int group, int head_dim, int64_t max_q, int
     p.own_view = rows <= 4 && own <= 512 && size_product(places, kv_heads) > 8ll * sm_count() ? VIEW_OWN_ROWS : VIEW_OWN;
     p.own_units = p.own_view == VIEW_OWN ? places : groups;
     p.own = p.own_view == VIEW_OWN ? plan_rows(places, kv_heads, head_dim, rows, own, rows <= tile, EVENLY)
-                                   : plan_rows(groups, kv_heads, head_dim, together, least(met, 1 << 30), true, EVENLY, 8);
+                                   : plan_rows(groups, kv_heads, head_dim, together, met, true, EVENLY, 8);
     p.prefix = plan_rows(groups, kv_heads, head_dim, together, max_prefix, false, EVENLY);
     p.prefix_parts = max_prefix > 0 ? p.prefix.splits : 0;
     p.join = p.own.decode && p.own.splits == 1 && p.prefix_parts > 0;

@@ -95,3 +95,15 @@ def test_attention_arguments_are_checked_in_one_manner():
         if "window" in change:
             continue
         assert call("sqap_kv_attention", cache(), ATTEND, change) == want, change
+
+
+def test_long_tokens_of_a_group_are_not_taken_together():
+    """Places in the own tokens of all sequences that a tile of rows meets are 32-bit numbers: where they pass 2^30, sequences go one by one, and each
+    takes pieces for its prefix beside its own, unlike tiles of rows."""
+    shared = B.lib().sqap_kv_attention_shared_workspace_bytes
+
+    def workspace(max_len):
+        return shared(cache(), 8, 1, max_len, 1, 8, 1024, 2)
+
+    together, apart = workspace((1 << 27) - 2048), workspace((1 << 27) + 2048)      # eight times the own tokens: just below 2^30, just above
+    assert together != apart == workspace(1 << 30)
