@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
     __shared__ alignas(8) uint8_t bins_or_list[SHARED];
     uint32_t (*bins)[BINS] = reinterpret_cast<uint32_t (*)[BINS]>(bins_or_list);
     uint16_t* list = reinterpret_cast<uint16_t*>(bins_or_list);
-    __shared__ alignas(8) uint32_t of_all[3][CTAS][2];      // of each CTA: smallest and largest order; places and ties, by parity of the round
+    __shared__ alignas(8) uint32_t of_all[3][CTAS][2];      // of each CTA: smallest order - 1 and largest + 1; places and ties, by parity of the round
     __shared__ uint32_t part[WARPS], least[WARPS], most[WARPS];
     __shared__ uint32_t found[3];        // the bin, how many are above it, how many in it
     __shared__ uint32_t front[RUNS];     // of each run of 32 tokens: those in front of it that stay, and (upper half) that are at the border
@@ -115,10 +115,12 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
     // border: orders above it stay, of those equal to it the first `ties` in their places
     uint32_t border = ALWAYS - 1, ties = 0;
     if (wanted > 0) {
+        // The smallest order less 1 and the largest plus 1: 0 then comes out on top of all and ALWAYS at the bottom. They are taken back only
+        // once all CTAs' are known: one without a token to choose from has none to take back, the sequence has `wanted` or more.
         uint32_t lo = 0xFFFFFFFFu, hi = 0;
         each([&](uint32_t k) {
-            lo = min(lo, k - 1);         // 0 comes out on top
-            hi = max(hi, k + 1);         // and ALWAYS at the bottom
+            lo = min(lo, k - 1);
+            hi = max(hi, k + 1);
         });
         lo = __reduce_min_sync(0xffffffffu, lo);
         hi = __reduce_max_sync(0xffffffffu, hi);
@@ -127,8 +129,8 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
             most[warp] = hi;
         }
         __syncthreads();
-        lo = __reduce_min_sync(0xffffffffu, least[lane < WARPS ? lane : 0]) + 1;
-        hi = __reduce_max_sync(0xffffffffu, most[lane < WARPS ? lane : 0]) - 1;
+        lo = __reduce_min_sync(0xffffffffu, least[lane < WARPS ? lane : 0]);
+        hi = __reduce_max_sync(0xffffffffu, most[lane < WARPS ? lane : 0]);
         if (CTAS > 1) {
             if (tid < CTAS) remote_store(remote_address(&of_all[2][rank], tid), lo, hi);
             cluster_sync();
@@ -138,6 +140,8 @@ __global__ void __launch_bounds__(THREADS) kv_evict_kernel(EvictArgs a) {
                 hi = max(hi, of_all[2][q][1]);
             }
         }
+        ++lo;
+        --hi;
         int buffer = 0;
         uint32_t left = wanted;          // of the orders in lo .. hi, the left-th largest is the border
         for (;;) {
