@@ -189,8 +189,11 @@ template <int VIEW, int ALIGN>
 __device__ __forceinline__ Span span_of(const AttnArgs& a, const Where& w, int i0) {
     Span s = {0, 0};
     if constexpr (VIEW == VIEW_WINDOW || VIEW == VIEW_OWN) {
-        const int low = first_seen<VIEW>(a, w, i0);
-        if (VIEW == VIEW_WINDOW) s.stop = (min(a.sinks, low) + ALIGN - 1) / ALIGN * ALIGN;
+        int low = first_seen<VIEW>(a, w, i0);
+        if (VIEW == VIEW_WINDOW) {
+            low = min(low, w.len);                           // a window behind max_len leaves the sinks
+            s.stop = (min(a.sinks, low) + ALIGN - 1) / ALIGN * ALIGN;
+        }
         s.gap = max(0, low / ALIGN * ALIGN - s.stop);
     }
     return s;

@@ -1,13 +1,21 @@
-"""The operators around the cache at their limits: shares of a long sequence of which every token stays. Lists are whole numbers and equal
-the plain statement's."""
+"""The operators around the cache at their limits: shares of a long sequence of which every token stays, more tokens than a launch was sized
+for. Lists are whole numbers and equal the plain statement's; tolerances of outputs are those of the single operators
+(test_gpu_kv_views.py)."""
+import math
+
 import numpy as np
 import pytest
+
+import cache_reference as C
+import lowbit_reference as R
 
 pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 if torch.cuda.is_available():
     from test_gpu_evict_rotary import check_evict, weights
+    from test_gpu_kv import Setup
+    from test_gpu_kv_views import Queries, check_rows, run_window, tokens_of
 
 
 @pytest.mark.parametrize("n,top,share", [(3, 8192, 4096), (5, 16384, 4096), (37, 14000, 4096), (2, 32768, 4096), (40, 33000, 16384), (20, 40000, 16384),
@@ -24,3 +32,23 @@ def test_evict_where_all_of_a_share_stays(n, top, share):
         free = max(top - first - recent, 0)
         for keep in {first + recent + 1, first + recent + free // 3, top - 1}:
             check_evict(m, lens, list(range(n)), [keep] * n, first, recent, dst=[n, n + 1] + [-1] * (n - 3) + [n + 2] if n > 2 else [n, n + 2], max_len=top)
+
+
+@pytest.mark.parametrize("max_len,window,sinks", [(1000, 100, 16), (1000, 100, 0), (1000, 2500, 5), (999, 1, 1200), (64, 7, 64), (1700, 300, 900)])
+@pytest.mark.parametrize("kind,dtype,heads,H,D,P,lens,new", [
+    (R.INT8, "fp16", 2, 2, 64, 16, [2600, 1000, 30, 1120], [1, 1, 1, 1]),
+    (R.E4M3, "bf16", 8, 2, 128, 64, [2600, 1001, 1150], [1, 1, 1]),
+    (R.E4M3, "fp16", 4, 1, 128, 32, [2600, 1040], [4, 3]),
+    (R.INT8, "bf16", 3, 1, 256, 128, [2600, 1090, 999], [1, 2, 1]),
+    (R.INT8, "fp16", 2, 2, 64, 16, [2600, 1030, 0], [300, 100, 30]),
+    (R.E4M3, "bf16", 8, 2, 128, 64, [2600, 1100], [129, 200]),
+    (R.E4M3, "fp16", 2, 2, 256, 128, [2600, 1033], [150, 40])])
+def test_sinks_of_histories_beyond_max_len_stay_visible(kind, dtype, heads, H, D, P, lens, new, max_len, window, sinks):
+    """A window that lies behind max_len holds no token that is looked at; the first tokens are seen all the same."""
+    s = Setup(lens, H, D, P, kind, seed=max_len + D)
+    qs = Queries(s, new, heads, dtype, seed=window)
+    run_window(s, qs, new, window, sinks, lens, max_len=max_len)
+    o, l = qs.results([(qs.cu[0], qs.cu[-1])])
+    for b, n in enumerate(lens):
+        r, held = slice(qs.cu[b], qs.cu[b + 1]), min(n, max_len)
+        check_rows(s, o[r], l[r], qs.qn[r], *tokens_of(s, s.table[b], held), C.in_window(n, new[b], window, sinks)[:, :held], dtype, 1 / math.sqrt(D))
