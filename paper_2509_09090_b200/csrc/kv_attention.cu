@@ -189,10 +189,13 @@ SharedPlan plan_shared(int kv_heads, int group, int head_dim, int64_t max_q, int
                        int64_t max_prefix) {
     SharedPlan p;
     const int64_t rows = max_q * group, together = rows * max_group;
-    const int64_t own = max_len > max_prefix ? max_len - max_prefix : 1;
+    const int64_t own = max_len > max_prefix ? max_len - max_prefix : 1;        // behind the longest prefix
     const int tile = decode_max_rows(head_dim);
-    const int64_t met = size_product(own, least(max_group, 8 / rows + 1));      // own tokens of the sequences that a row tile meets
-    p.together = in_row_tiles(head_dim, rows, max_group, max_prefix) && met + max_prefix <= 1 << 30;      // the kernel's 32-bit places
+    const int64_t sequences = least(max_group, 8 / rows + 1);                   // that a row tile meets
+    const int64_t met = size_product(own, sequences);
+    // The register kernel's places in all that a row tile meets are 32-bit numbers; behind a prefix shorter than the longest, own tokens are up to max_len.
+    const bool places_fit = size_product(sequences, max_len) + max_prefix <= 1 << 30;
+    p.together = places_fit && in_row_tiles(head_dim, rows, max_group, max_prefix);
     if (p.together) {
         p.prefix = p.own = plan_rows(groups, kv_heads, head_dim, together, met + max_prefix, true, EVENLY, 8);
         p.own_view = VIEW_SHARED;
@@ -205,7 +208,7 @@ SharedPlan plan_shared(int kv_heads, int group, int head_dim, int64_t max_q, int
     const int64_t places = size_product(groups, max_group);
     // Short tokens of many sequences: a tile of rows to a CTA (16 x 16 sequences of 4 rows, 8 heads, 64 own tokens: 49 us, a sequence to a CTA 53;
     // 16 x 64 of one row, 32 heads, 40 own tokens: 165 / 311; but 4 x 64 of one row, 8 heads, 1000 own tokens: 157 / 143).
-    p.own_view = rows <= 4 && own <= 512 && size_product(places, kv_heads) > 8ll * sm_count() ? VIEW_OWN_ROWS : VIEW_OWN;
+    p.own_view = places_fit && rows <= 4 && own <= 512 && size_product(places, kv_heads) > 8ll * sm_count() ? VIEW_OWN_ROWS : VIEW_OWN;
     p.own_units = p.own_view == VIEW_OWN ? places : groups;
     p.own = p.own_view == VIEW_OWN ? plan_rows(places, kv_heads, head_dim, rows, own, rows <= tile, EVENLY)
                                    : plan_rows(groups, kv_heads, head_dim, together, met, true, EVENLY, 8);

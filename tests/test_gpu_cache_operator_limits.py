@@ -15,7 +15,7 @@ torch = pytest.importorskip("torch")
 if torch.cuda.is_available():
     from test_gpu_evict_rotary import check_evict, weights
     from test_gpu_kv import Setup
-    from test_gpu_kv_views import Queries, check_rows, run_window, tokens_of
+    from test_gpu_kv_views import Group, Queries, check_rows, check_shared, run_window, tokens_of
 
 
 @pytest.mark.parametrize("n,top,share", [(3, 8192, 4096), (5, 16384, 4096), (37, 14000, 4096), (2, 32768, 4096), (40, 33000, 16384), (20, 40000, 16384),
@@ -52,3 +52,14 @@ def test_sinks_of_histories_beyond_max_len_stay_visible(kind, dtype, heads, H, D
     for b, n in enumerate(lens):
         r, held = slice(qs.cu[b], qs.cu[b + 1]), min(n, max_len)
         check_rows(s, o[r], l[r], qs.qn[r], *tokens_of(s, s.table[b], held), C.in_window(n, new[b], window, sinks)[:, :held], dtype, 1 / math.sqrt(D))
+
+
+@pytest.mark.parametrize("dtype,heads,H,D,P,sizes,prefixes,own", [
+    ("fp16", 2, 2, 64, 16, [8, 8], [2000, 0], [5] * 8 + [2005 - 70 * b for b in range(8)]),                  # one tile of rows to a group
+    ("bf16", 4, 1, 128, 64, [6, 3, 1], [1600, 100, 0], [9, 1, 30, 4, 5, 6, 1500, 7, 800, 1601]),             # three
+    ("fp16", 128, 32, 64, 16, [20, 19], [600, 0], [30] * 20 + [620 - 31 * b for b in range(19)]),            # prefix in a launch of its own, tiles of rows
+    ("bf16", 8, 1, 128, 64, [40, 3], [1500, 0], [7] * 40 + [1507, 900, 1]),                                  # the same, a sequence to a CTA
+    ("fp16", 2, 1, 256, 16, [7, 5], [900, 3], [4] * 7 + [850, 3, 777, 901, 90])])
+def test_prefixes_of_very_uneven_lengths(dtype, heads, H, D, P, sizes, prefixes, own):
+    """Own tokens behind a short prefix are as many as the longest prefix lets no group have."""
+    check_shared(Group(sizes, prefixes, own, H, D, P, R.INT8, seed=sum(own)), [1] * len(own), heads, dtype)
