@@ -191,7 +191,7 @@ SharedPlan plan_shared(int kv_heads, int group, int head_dim, int64_t max_q, int
     const int64_t rows = max_q * group, together = rows * max_group;
     const int64_t own = max_len > max_prefix ? max_len - max_prefix : 1;        // behind the longest prefix
     const int tile = decode_max_rows(head_dim);
-    const int64_t sequences = least(max_group, 8 / rows + 1);                   // that a row tile meets
+    const int64_t sequences = least(max_group, (rows + 6) / rows + 1);          // that a tile of 8 rows meets, if it begins with a sequence's last row
     const int64_t met = size_product(own, sequences);
     // The register kernel's places in all that a row tile meets are 32-bit numbers; behind a prefix shorter than the longest, own tokens are up to max_len.
     const bool places_fit = size_product(sequences, max_len) + max_prefix <= 1 << 30;
