@@ -30,7 +30,7 @@ struct RotaryArgs {
     int turning, per_head;               // units of a head that hold pairs, and with those that are only copied
     int by_row, by_head;                 // at_once, in rows and heads
     uint32_t by_per_head, by_half;       // 2^16 / per_head and 2^16 / half, rounded up: quotients of numbers below THREADS without a division
-    int table_pairs;                     // of a block's rows, rounded up to even
+    int touched, table_pairs;            // rows that a block's units can lie in (times the heads 31 bits), and the pairs of these
     int rows_at_once;                    // rows whose pairs the CTA's threads take at once
     int at_once, slots;                  // heads that the CTA's threads take at once, and how often
     const int32_t* positions;
@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) rotary_kernel(const __grid_cons
         const int64_t left = a.units - first;
         const int last = head0 + static_cast<int>(left < per_block ? left : per_block);
         if (turn_row < a.rows_at_once)
-            for (int r = turn_row; r * a.heads < last; r += a.rows_at_once) {
+            for (int r = turn_row; r < a.touched && r * a.heads < last; r += a.rows_at_once) {
                 const uint64_t at = part * static_cast<uint64_t>(static_cast<int64_t>(__ldg(position + row0 + r)));
                 float s, c;
                 sincospif(static_cast<float>(static_cast<int32_t>(at >> 32)) * 4.656612873077393e-10f, &s, &c);     // half turns
@@ -219,7 +219,8 @@ extern "C" sqap_status sqap_rotary(const void* x, int64_t ldx, int rows, int hea
         return static_cast<int>(n < rows ? n : rows);
     };
     while (a.slots > 1 && static_cast<int64_t>(touched(a.slots)) * a.half * 8 > TABLE_BYTES) --a.slots;
-    a.table_pairs = touched(a.slots) * a.half;
+    a.touched = touched(a.slots);
+    a.table_pairs = a.touched * a.half;
     const int64_t per_block = static_cast<int64_t>(a.at_once) * a.slots, blocks = (a.units + per_block - 1) / per_block;
     const int64_t at_once = static_cast<int64_t>(sm_count()) * CTAS, grid = blocks < at_once ? blocks : at_once;
     const size_t table = static_cast<size_t>(a.table_pairs) * 8 * (blocks > grid ? 2 : 1);

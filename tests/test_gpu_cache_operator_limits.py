@@ -13,8 +13,9 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 if torch.cuda.is_available():
+    from paper_2509_09090_b200 import binding as B
     from test_gpu_evict_rotary import check_evict, weights
-    from test_gpu_kv import Setup
+    from test_gpu_kv import DEV, Setup
     from test_gpu_kv_views import Group, Queries, check_rows, check_shared, run_window, tokens_of
 
 
@@ -63,3 +64,26 @@ def test_sinks_of_histories_beyond_max_len_stay_visible(kind, dtype, heads, H, D
 def test_prefixes_of_very_uneven_lengths(dtype, heads, H, D, P, sizes, prefixes, own):
     """Own tokens behind a short prefix are as many as the longest prefix lets no group have."""
     check_shared(Group(sizes, prefixes, own, H, D, P, R.INT8, seed=sum(own)), [1] * len(own), heads, dtype)
+
+
+@pytest.mark.parametrize("rows,heads,D,rot", [(2, 70_000_000, 8, 8), (1, 70_000_000, 24, 8)])
+def test_rotary_of_very_many_heads(rows, heads, D, rot):
+    """31 times the heads pass 31 bits. Tolerance: that of the other rotary tests (test_gpu_evict_rotary.py)."""
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB")
+    x = torch.randn((rows, heads * D), device=DEV, dtype=torch.float16)
+    out = torch.full_like(x, 3.0)
+    freq = torch.tensor([1.0, 0.1, 0.01, 0.001], device=DEV)
+    at = torch.tensor([[5, 77]], device=DEV, dtype=torch.int32)
+    B.sqap_rotary(x, heads * D, rows, heads, D, rot, at, 2, 1, None, freq, 0, out, heads * D, 0)
+    torch.cuda.synchronize()
+    for row in range(rows):
+        angle = at[0, row].double() * freq.double()
+        c, s = angle.cos(), angle.sin()
+        for h in range(0, heads, 8_000_000):
+            a, y = (t[row].view(heads, D)[h:h + 8_000_000] for t in (x, out))
+            p, q = a[:, :4].double(), a[:, 4:8].double()
+            size = 2.0 ** -20 * (p.abs() + q.abs()) + 2.0 ** -24
+            for ref, got in ((p * c - q * s, y[:, :4]), (q * c + p * s, y[:, 4:8])):
+                assert ((got.double() - ref).abs() <= ref.abs() * 2.0 ** -11 + size).all()
+            assert torch.equal(a[:, 8:], y[:, 8:])
