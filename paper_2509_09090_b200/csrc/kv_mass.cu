@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(WARPS * 32, D <= 128 ? 5 : 2) kv_mass_kernel(M
             for (int x = threadIdx.x; x < ROWS * PIECES; x += WARPS * 32) {
                 const int k = x / PIECES, piece = x % PIECES, r = stage * ROWS + k, i = r / G;
                 const bool real = r < rows;
-                const T* src = static_cast<const T*>(a.q) + (static_cast<int64_t>(w.row0) + i0 + i) * a.ldq + (h * G + r - i * G) * D + 8 * piece;
+                const T* src = static_cast<const T*>(a.q) + (static_cast<int64_t>(w.row0) + i0 + i) * a.ldq + static_cast<int64_t>(h * G + r - i * G) * D + 8 * piece;
                 copy_async_16(&s_q[buffer][k][8 * piece], real ? src : a.q, real);
             }
             if (threadIdx.x < ROWS) {

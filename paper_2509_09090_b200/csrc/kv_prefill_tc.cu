@@ -532,7 +532,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prefill_tc_kernel(AttnArgs a, u
                 const int by = RPI % G;
                 const int64_t step = (RPI / G) * a.ldq + by * D, carry = a.ldq - static_cast<int64_t>(G) * D;
                 int g = first % G;
-                const T* p = q + (first / G) * a.ldq + g * D;
+                const T* p = q + (first / G) * a.ldq + static_cast<int64_t>(g) * D;
 #pragma unroll
                 for (int i = 0; i < Q_STEPS; ++i) {
                     const bool there = first + i * RPI < t.rows;

@@ -15,8 +15,8 @@ torch = pytest.importorskip("torch")
 if torch.cuda.is_available():
     from paper_2509_09090_b200 import binding as B
     from test_gpu_evict_rotary import check_evict, weights
-    from test_gpu_kv import DEV, Setup
-    from test_gpu_kv_views import Group, Queries, check_rows, check_shared, run_window, tokens_of
+    from test_gpu_kv import DEV, Setup, ints
+    from test_gpu_kv_views import GUARD, Group, Queries, check_rows, check_shared, run_window, scratch, tokens_of
 
 
 @pytest.mark.parametrize("n,top,share", [(3, 8192, 4096), (5, 16384, 4096), (37, 14000, 4096), (2, 32768, 4096), (40, 33000, 16384), (20, 40000, 16384),
@@ -87,3 +87,41 @@ def test_rotary_of_very_many_heads(rows, heads, D, rot):
             for ref, got in ((p * c - q * s, y[:, :4]), (q * c + p * s, y[:, 4:8])):
                 assert ((got.double() - ref).abs() <= ref.abs() * 2.0 ** -11 + size).all()
             assert torch.equal(a[:, 8:], y[:, 8:])
+
+
+def test_rows_of_queries_beyond_32_bit_offsets():
+    """2^24 + 16 heads of 128 on one key/value head: all but the last 16, which lie beyond 2^31 elements, see token 69 alone (the others' weights are
+    below 2^-300). Its received weight is 2^24 and a sum of 16 weights: an addition at 2^22, where each of four lanes is by then, is off by 2^-2 at
+    most, one of the three that join the lanes by 1."""
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB")
+    D, n, heads, more = 128, 70, (1 << 24) + 16, 16
+    s = Setup([n], 1, D, 128, R.INT8, seed=7)
+    page = s.table[0, 0]
+    s.raw["k"][page, 0, :, :64] = np.int8(-100).view(np.uint8)
+    s.raw["k"][page, 0, n - 1, :64] = 100
+    s.scale["k"][:] = 1 / 40
+    s.to_device()
+    g = np.random.default_rng(1)
+    last = np.concatenate([np.zeros((more, 64)), g.standard_normal((more, 64))], 1)
+    q = torch.zeros((heads, D), device=DEV, dtype=torch.float16)
+    q[:, :64] = 8.0
+    q[-more:] = torch.from_numpy(last).to(DEV).half()
+    out, lse = torch.full_like(q, GUARD), torch.full((heads,), GUARD, device=DEV)
+    mass = torch.full((n,), GUARD, device=DEV)
+    ld, scale = heads * D, 1 / math.sqrt(D)
+    size = B.sqap_kv_attention_mass_workspace_bytes(s.cache, 1, 1, n, heads, 1)
+    B.sqap_kv_attention_mass(s.cache, s.dtable, s.width, 1, ints([n]), ints([0, 1]), 1, n, q, ld, heads, scale, 1, 1, out, ld, lse, None, mass, n, 0,
+                             scratch(size), size)
+    torch.cuda.synchronize()
+    assert B.sqap_device_status() == B.SQAP_OK
+    k, (v, vs), there = tokens_of(s, s.table[0], n)
+    seen = np.ones((1, n), bool)
+    for at in (0, 12345678, heads - more - 40, heads - more):
+        rows = slice(at, at + more)
+        o, l, x = (t[rows].double().cpu().numpy() for t in (out, lse, q))
+        p, need = check_rows(s, o[None], l[None], x[None], k, (v, vs), there, seen, "fp16", scale)
+    m = mass.double().cpu().numpy()
+    p, need = p[0], (p * need[..., None])[0]
+    assert (np.abs(m - p.sum(0)) <= need.sum(0) + more * 2.0 ** -24 * p.sum(0) + 2.0 ** -126)[:-1].all()
+    assert abs(m[-1] - (1 << 24) - p[:, -1].sum()) <= need[:, -1].sum() + more / 4 + 3
