@@ -523,7 +523,8 @@ cudaError_t launch_rows(const AttnArgs& a, unsigned grid, cudaStream_t s) {
     // flight count for more. Measured, one / two groups, us: D = 128, 16 x 290 tokens x 32 heads 11.6 / 13.5, 16 x 2048 51.6 / 53.4,
     // 32 sequences of up to 16384 x 8 heads 126 / 137; D = 64, the same, 9.1 / 8.7, 35.0 / 32.7, 83 / 76.
     constexpr int GROUPS = D == 64 ? 2 : 1;
-    if constexpr (D != 256)                         // 8 rows at most: decode_max_rows()
+    // D = 256: 8 rows at most (decode_max_rows()); the rows of a group are always taken in tiles of 8
+    if constexpr (D != 256 && !of_several<VIEW>)
         // 9 to 16 rows: one / two groups, 32 x 8192 tokens x 8 heads of 128, 12 rows, 134 / 115; 16 x 2048, 16 rows, 35 / 31.
         if (a.row_tile > 8)
             return launch_dependent(kv_decode_kernel<T, TYPE, D, 2, 2, VIEW>, dim3(grid), dim3(WARPS * 32), 0, s, a);
