@@ -1,6 +1,6 @@
-// Attention with the weight that each token received. Few rows (decoding): the register kernel keeps its scores, 4 bytes for each
-// row beside the 2 D bytes of the keys and values that it reads, and a second kernel turns them into weights once the
-// log-sum-exps are there. Many rows: their scores would be more than the keys; those of the rows that count are computed once more.
+// Attention with the weight that each token received. Few rows (decoding, see keeps_scores): the register kernel keeps its scores, 4 bytes for
+// each row beside the 2 D bytes of the keys and values that it reads, and a second kernel turns them into weights once the
+// log-sum-exps are there. More rows: their scores would be more than the keys; those of the rows that count are computed once more.
 //
 // A warp holds 16 tokens' keys of a head as the A operand (from codes in registers, as in kv_decode.cu) and goes over the
 // query rows, eight at a time, as the B operand: S[token][row], p = 2^(s scale log2 e - lse log2 e), summed over the row in the lane that
@@ -314,9 +314,20 @@ struct MassPlan {
     size_t attention, bytes;       // of the workspace: the attention's part in front, and all
     bool fits;
 };
+// Scores are kept where the register kernel has at most 8 rows of a head, or at most 15 and either no more heads than the second kernel has
+// warps, or long histories: 4 bytes a row and token, written and read, against 2 D of codes. Kept / computed again, us, D = 128: 1 row, 16 x 290
+// tokens of 32 heads 14 / 23; 4 rows, 32 x 16384 of 8 heads 149 / 230; 8 rows, 16 x 290 of 32 23 / 22, 16 x 1000 42 / 52, 32 x 12000 of 8
+// 117 / 168; 12 rows, 16 x 290 of 32 43 / 30, 16 x 1000 75 / 66, 16 x 4000 156 / 179, of 8 heads 32 x 290 26 / 27, 32 x 1000 41 / 48, 32 x 12000
+// 185 / 217; 16 rows, 16 x 290 of 32 51 / 30, 16 x 4000 200 / 182, of 8 heads 32 x 290 29 / 27, 32 x 1000 44 / 49, 32 x 12000 220 / 221.
+bool keeps_scores(const sqap_kv_cache* c, int max_q, int max_len, int heads) {
+    const int group = heads / c->kv_heads;
+    if (!few_rows(max_q, group, c->head_dim)) return false;
+    const int rows = max_q * group;
+    return rows <= 8 || (rows < 16 && (c->kv_heads <= FOLD_WARPS || max_len > 2048));
+}
 MassPlan plan_mass(const sqap_kv_cache* c, int batch, int max_q, int max_len, int heads) {
     MassPlan p;
-    p.keep = few_rows(max_q, heads / c->kv_heads, c->head_dim);
+    p.keep = keeps_scores(c, max_q, max_len, heads);
     p.attention = (sqap_kv_attention_workspace_bytes(c, batch, max_q, max_len, heads) + 15) / 16 * 16;
     if (p.keep) {
         const int64_t runs = max_len > 0 ? (max_len - 1) / 32 + 1 : 0;

@@ -16,7 +16,7 @@ if torch.cuda.is_available():
     from paper_2509_09090_b200 import binding as B
     from test_gpu_evict_rotary import check_evict, weights
     from test_gpu_kv import DEV, Setup, ints
-    from test_gpu_kv_views import GUARD, Group, Queries, check_rows, check_shared, run_window, scratch, tokens_of
+    from test_gpu_kv_views import GUARD, Group, Queries, check_mass, check_rows, check_shared, run_window, scratch, tokens_of
 
 
 @pytest.mark.parametrize("n,top,share", [(3, 8192, 4096), (5, 16384, 4096), (37, 14000, 4096), (2, 32768, 4096), (40, 33000, 16384), (20, 40000, 16384),
@@ -125,3 +125,19 @@ def test_rows_of_queries_beyond_32_bit_offsets():
     p, need = p[0], (p * need[..., None])[0]
     assert (np.abs(m - p.sum(0)) <= need.sum(0) + more * 2.0 ** -24 * p.sum(0) + 2.0 ** -126)[:-1].all()
     assert abs(m[-1] - (1 << 24) - p[:, -1].sum()) <= need[:, -1].sum() + more / 4 + 3
+
+
+@pytest.mark.parametrize("dtype,heads,H,D,P,lens,new", [
+    ("fp16", 9, 9, 64, 16, [60, 9, 290], [9, 9, 9]),                   # more than eight heads, 9 to 16 rows of each
+    ("bf16", 20, 10, 128, 64, [33, 300], [5, 4]), ("fp16", 48, 12, 64, 16, [100, 3], [3, 2]), ("bf16", 126, 9, 64, 32, [70], [2]),
+    ("fp16", 9, 9, 64, 32, [2049, 700], [9, 1]),                       # long histories
+    ("bf16", 15, 1, 64, 16, [400, 30], [1, 1]), ("fp16", 12, 4, 128, 64, [290, 31], [4, 5]),      # eight heads or fewer
+    ("fp16", 16, 1, 128, 16, [500, 40], [1, 1]), ("bf16", 4, 1, 64, 64, [2300, 100], [4, 3])])    # 16 rows
+def test_received_weights_of_up_to_16_rows(dtype, heads, H, D, P, lens, new):
+    """Either side of the rule by which scores are kept or computed again."""
+    for kind in (R.INT8, R.E4M3):
+        s = Setup(lens, H, D, P, kind, seed=heads + D)
+        for last_q, past in ((max(new), "given"), (1, "same"), (2, "none")):
+            check_mass(s, new, heads, dtype, last_q, past=past)
+        check_mass(s, new, heads, dtype, max(new), causal=False, max_len=max(lens) - 7, ldm=max(lens) - 3)
+        check_mass(s, new, heads, dtype, max(new), spoil=0)
