@@ -454,7 +454,7 @@ sqap_status sqap_kv_attention_shared(const sqap_kv_cache* cache, const int32_t* 
  * The same attention, and what each token received of it:
  *   mass[b*ldm + t] = (t < lens[b] - n_q and past given ? past[b*ldm + t] : 0) + sum over i, h of p_t(i, h)
  * for t < lens[b] (and < ldm, max_len), p_t the softmax weight of token t, i the last last_q of the sequence's n_q query rows, h all
- * heads. Tokens that are new in the call have no past. past: device fp32 [batch rows, ldm apart], NULL for zeros; may be the same array
+ * heads. lse has to be given. Tokens that are new in the call have no past. past: device fp32 [batch rows, ldm apart], NULL for zeros; may be the same array
  * as mass, and overlaps it in no other way. Query rows without a finite log-sum-exp add nothing. Sums in fp32 in an order that depends
  * on the sizes alone. Other places of mass stay as they are.
  */

@@ -6,8 +6,8 @@
 // warp owns runs of 32 consecutive tokens, a lane one of each: its votes give a token's place within the run, one sum over
 // the runs in front of it the rest, and the lanes that write the list write side by side.
 // Bounded by latency: 4 bytes a token are read once (up to 16384 tokens a CTA are kept in registers, longer ones read again each
-// round), and some seven steps of the whole CTA follow one another, four of them with a cluster's barrier: 16 x 288 tokens 4.5 us,
-// 32 uneven sequences of up to 16384 11.4 us, one of 131072 17.6 us.
+// round), and some seven steps of the whole CTA follow one another, four of them with a cluster's barrier: 16 x 288 tokens 4.2 us,
+// 32 uneven sequences of up to 16384 12.2 us, one of 131072 18.9 us (weights from HBM; from L2 4.5, 11.4 and 17.6).
 #include "kv.cuh"
 
 namespace sqap {
@@ -338,7 +338,7 @@ extern "C" sqap_status sqap_kv_evict(float* mass, int64_t ldm, int rows, const i
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (max_len <= 1024) return finish_launch(launch_evict<256, 4, 1>(a, n, s));
     if (max_len <= 4096) return finish_launch(launch_evict<1024, 4, 1>(a, n, s));
-    // As many CTAs to a sequence as the device has SMs for, as long as each has 4096 tokens or more, and two only where they save a round (us,
+    // As many CTAs to a sequence as the device has SMs for, as long as each has 4096 tokens or more, and two only where they save a round (us, weights in L2,
     // one CTA / as many as here: 32 x 16384 13.0 / 11.4; one / two: 64 x 16384 13.5 / 16.7). Up to 16 tokens a thread rather than
     // a second round (131072 tokens in eight CTAs, 4 / 16: 31.9 / 17.6).
     const int64_t ctas = sm_count() / (n < sm_count() ? n : sm_count());

@@ -6,8 +6,8 @@
 // query rows, eight at a time, as the B operand: S[token][row], p = 2^(s scale log2 e - lse log2 e), summed over the row in the lane that
 // holds it. Codes are exact in fp16 and in bf16, so the queries enter in the type that they have. A CTA's four warps
 // take neighbouring tokens and share the query rows, staged 32 at a time in shared memory; heads are shared out over CTAs where tokens are few,
-// and their sums added by a second kernel, in the order of the heads. Measured, calls in a graph: 16 x 290 single tokens 13 us, 32 uneven
-// histories of up to 16384 148 us (few rows: the attention's reads bound it); 16 prompts of 288, the last 32 queries, 77 us, most of it attention;
+// and their sums added by a second kernel, in the order of the heads. Measured, calls in a graph: 16 x 290 single tokens 15 us, 32 uneven
+// histories of up to 16384 148 us (few rows: the attention's reads bound it); 16 prompts of 288, the last 32 queries, 76.5 us, most of it attention;
 // this kernel alone 16 us with cold caches, bound by instruction latency (issue 48 %, tensor pipe 18 %).
 #include "kv_attention.cuh"
 
