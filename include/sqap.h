@@ -440,7 +440,8 @@ sqap_status sqap_kv_attention_window(const sqap_kv_cache* cache, const int32_t* 
  * of the sums. cu_group: device int32 [groups + 1], not decreasing; prefix: device int32 [groups], < 0 counts as 0; a prefix need not
  * end with a page and may be longer than a sequence. max_group, max_prefix: no group has more sequences, no prefix is longer (the rest of a
  * group's sequences is not computed; tokens beyond max_prefix are read for each sequence). They size the launch, like max_q and
- * max_len. Rows of sequences that are in no group are left as they are.
+ * max_len. Rows of sequences that are in no group are left as they are. Value codes that a sequence sees are numbers, as sqap_kv_append
+ * writes them: an e4m3 code that is none may reach the rows of its whole group.
  */
 size_t sqap_kv_attention_shared_workspace_bytes(const sqap_kv_cache* cache, int batch, int max_q, int max_len, int groups, int max_group,
                                                 int max_prefix, int heads);
